@@ -335,6 +335,101 @@ int hs_decode_step(hs_model *m, hs_kv *kv, const int32_t *tokens_in, int32_t *to
 int hs_decode_step_static(hs_model *m, hs_kv *kv, const int32_t *tokens_in, int32_t *tokens_out, float *logits,
                           float *hidden_out, hs_stream_t stream);
 
+/* ---- the KV cache held in 4 bits ----
+ *
+ * Decode over long contexts streams the cache; held in 4 bits it is 17/64 of
+ * its 16-bit size.  A row of head_dim elements (one position, head, K or V) is
+ * cut into groups of 32.  With a the largest |x| of a group, its elements are
+ * the nearest (ties to even) of 0, 1/2, 1, 3/2, 2, 3, 4, 6 with a sign, times
+ * 2^e for the least integer e with a < 7 * 2^e, so that none is off by more than
+ * 2^e; e is kept in -23..13 for HS_F16 rows and -125..125 for HS_F32 and HS_BF16
+ * (larger elements saturate at 6 * 2^e), where every value is a number of the
+ * row type.  A group that holds a NaN or an infinity becomes 32 NaNs.
+ *
+ * The cache is caller-owned device memory cut into blocks of block_tokens
+ * positions (a power of two in 16..16384), and a table of their numbers.  A
+ * block is, for each layer, then K and V, then KV head, block_tokens / 16 spans
+ * of 16 positions; a span is
+ *   16 rows of head_dim / 2 bytes, element 2 i of a row in the low half of its
+ *   byte i: bit 3 the sign, bits 0..2 the index of the size in the list above;
+ *   head_dim / 32 times 16 bytes: for each group of 32 elements the 16
+ *   positions' e + 127 (255: NaN).
+ * hs_kvq_block_bytes: 2 * n_layers * n_kv_heads * block_tokens * head_dim * 17/32.
+ * Position p of sequence s lives in block table[s * table_ld + p / block_tokens];
+ * a number that is negative or not below bytes / block_bytes means that there is
+ * no block: nothing is stored there, nothing read, and attention masks it.
+ * blocks: 16-byte aligned; head_dim 64 or 128. */
+typedef struct hs_kvq_cache {
+  void *blocks;         /* device */
+  uint64_t bytes;       /* of blocks; at least one block */
+  const int64_t *table; /* device [n_seqs][table_ld] */
+  int32_t n_seqs, table_ld;
+  int32_t n_layers, n_kv_heads, head_dim, block_tokens;
+} hs_kvq_cache;
+
+int hs_kvq_block_bytes(int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, int32_t block_tokens, uint64_t *bytes);
+
+/* Stores n rows of K and V of one layer.  Element (row r, head j, channel c) of
+ * K is k[r * ld + j * ld_head + c] in `dtype` (v alike; device, 16-byte aligned;
+ * ld and ld_head multiples of 8, HS_F32 4, and rows and heads do not overlap).
+ * Row r goes to position positions[r] (device int32) of sequence seqs[r] (device
+ * int32; NULL: sequence r).  A row whose position is negative, whose sequence is
+ * outside the table or whose place has no block is not stored, which is how a
+ * padded batch is passed.  No two stored rows of a call may name the same place
+ * (the bytes of either may remain).  k_values / v_values, if not NULL (both or
+ * neither), receive what the 4 bits stand for, of every row, stored or not, in
+ * the layout of k and v; they may be k and v. */
+int hs_kvq_append(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, int32_t n, const void *k, const void *v,
+                  int64_t ld, int64_t ld_head, const int32_t *seqs, const int32_t *positions, void *k_values,
+                  void *v_values, hs_stream_t stream);
+
+/* The reverse: fetches the rows at the given places as `dtype` into k and v,
+ * laid out as above; a place without a block, or none, gives zeros. */
+int hs_kvq_read(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, int32_t n, void *k, void *v, int64_t ld,
+                int64_t ld_head, const int32_t *seqs, const int32_t *positions, hs_stream_t stream);
+
+/* Decode attention: row r of q ([n_heads][head_dim] in `dtype`, rows ld_q
+ * elements apart) attends over the first lengths[r] positions (device int32) of
+ * sequence seqs[r] (NULL: r), query head i reading KV head
+ * i / (n_heads / n_kv_heads), at most 16 heads to a KV head:
+ *   out[r][i] = sum_p softmax_p(scale * q_i . k_p) v_p
+ * over the positions that have a block, in fp32, rounded once to `dtype`; a row
+ * without one (length 0 or negative) gives zeros.  max_len (host, > 0) bounds
+ * the lengths and shapes the launch; positions from it on are not attended.
+ * q, out, ld_q and ld_out are aligned as in hs_kvq_append.  workspace is device
+ * memory of hs_kvq_attention_workspace bytes (which may be 0: then it may be
+ * NULL), 16-byte aligned, that calls which may run at the same time do not share;
+ * nothing in it is kept from call to call.  Rows of a call may share sequences.
+ * Like hs_decode_step, this and the two calls above only enqueue kernels and can
+ * be captured. */
+int hs_kvq_attention_workspace(const hs_kvq_cache *cache, int32_t dtype, int32_t n, int32_t n_heads, int32_t max_len,
+                               uint64_t *bytes);
+int hs_kvq_attention(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, int32_t n, int32_t n_heads,
+                     const void *q, int64_t ld_q, const int32_t *seqs, const int32_t *lengths, int32_t max_len,
+                     float scale, void *out, int64_t ld_out, void *workspace, uint64_t workspace_bytes,
+                     hs_stream_t stream);
+
+/* ---- log probabilities of tokens ----
+ *
+ * For each of `rows` rows of logits (device, `dtype`, vocab elements, rows ld
+ * elements apart, aligned to their elements), with M = max x, Z = sum e^(x - M):
+ *   logprob[r]  = x[tokens[r]] - M - log Z, the log probability of the given
+ *                 token (device int32 [rows]); 0 for a negative token (none is
+ *                 asked for: a padded batch), NaN for one from vocab on;
+ *   entropy[r]  = log Z - sum (x - M) e^(x - M) / Z, in nats;
+ *   top_ids, top_logprobs [rows][top]: the `top` (0..64, at most vocab) largest
+ *                 logits' tokens and log probabilities, largest first, the
+ *                 lowest index first among equals.
+ * Each output may be NULL; logprob needs tokens.  Logits of -inf have
+ * probability 0.  A row that holds a NaN or +inf, or nothing but -inf, has no
+ * distribution: its values are NaN (a negative token's 0 stays) and its ids -1.
+ * Everything is computed in fp32 from the exact logits.  workspace: device
+ * memory of hs_token_logprobs_workspace bytes, as in hs_kvq_attention. */
+int hs_token_logprobs_workspace(int64_t rows, int32_t vocab, int32_t top, uint64_t *bytes);
+int hs_token_logprobs(int32_t dtype, const void *logits, int64_t rows, int32_t vocab, int64_t ld,
+                      const int32_t *tokens, int32_t top, float *logprob, float *entropy, int32_t *top_ids,
+                      float *top_logprobs, void *workspace, uint64_t workspace_bytes, hs_stream_t stream);
+
 /* Reads and clears the device-side flags.  Synchronises the device.
  *   bit 0 (1): a token id outside [0, vocab) was replaced by 0;
  *   bit 2 (4): a pooled cache ran out of free blocks inside a replayed decode

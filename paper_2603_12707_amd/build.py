@@ -13,6 +13,7 @@ SOURCES = [os.path.join(CSRC, f) for f in ("hs_api.cpp", "hs_gemm.hip", "hs_attn
 DEPS = SOURCES + [os.path.join(CSRC, "hs_internal.h"), os.path.join(CSRC, "hs_device.h"),
                   os.path.join(CSRC, "hs_gemm_epi.h"), os.path.join(CSRC, "hs_gemm_dma.h"),
                   os.path.join(CSRC, "hs_gemm_plan.h"),
+                  os.path.join(CSRC, "hs_kvq.h"), os.path.join(CSRC, "hs_logprobs.h"),
                   os.path.join(ROOT, "include", "hs.h")]
 
 FLAGS = [

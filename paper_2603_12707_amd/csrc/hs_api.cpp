@@ -1222,4 +1222,203 @@ int hs_kv_set_length(hs_kv *kv, int32_t req, int32_t len, int32_t rope_pos) {
   return HS_OK;
 }
 
+// ---- the cache held in 4 bits ----
+
+int hs_kvq_block_bytes(int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, int32_t block_tokens, uint64_t *bytes) {
+  static const char *fn = "hs_kvq_block_bytes";
+  if (!bytes) return fail(HS_E_INVALID, "%s: bytes is NULL", fn);
+  if (n_layers <= 0 || n_kv_heads <= 0) return fail(HS_E_INVALID, "%s: non-positive size", fn);
+  if (head_dim != 64 && head_dim != 128) return fail(HS_E_INVALID, "%s: head_dim %d is not 64 or 128", fn, head_dim);
+  if (block_tokens < 16 || block_tokens > 16384 || (block_tokens & (block_tokens - 1)))
+    return fail(HS_E_INVALID, "%s: block_tokens must be a power of two in 16..16384", fn);
+  uint64_t b = 2ull * kvq_slab_bytes(block_tokens, head_dim);
+  if (__builtin_mul_overflow(b, (uint64_t)n_layers * (uint64_t)n_kv_heads, &b) || b > (uint64_t)INT64_MAX)
+    return fail(HS_E_INVALID, "%s: size overflows 63 bits", fn);
+  *bytes = b;
+  return HS_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+int kvq_ref(const hs_kvq_cache *c, int layer, const char *fn, KvqRef *out) {
+  if (!c || !c->blocks || !c->table) return fail(HS_E_INVALID, "%s: NULL argument", fn);
+  uint64_t bb;
+  const int rc = hs_kvq_block_bytes(c->n_layers, c->n_kv_heads, c->head_dim, c->block_tokens, &bb);
+  if (rc) return rc;
+  if (((uintptr_t)c->blocks) % 16 || ((uintptr_t)c->table) % 8)
+    return fail(HS_E_INVALID, "%s: blocks must be 16-byte aligned, the table 8-byte", fn);
+  if (c->n_seqs <= 0 || c->table_ld <= 0) return fail(HS_E_INVALID, "%s: non-positive table size", fn);
+  if (layer < 0 || layer >= c->n_layers) return fail(HS_E_INVALID, "%s: layer %d out of range", fn, layer);
+  if (c->bytes / bb < 1) return fail(HS_E_BUFFER, "%s: the buffer holds no block of %llu bytes", fn, (unsigned long long)bb);
+  *out = KvqRef{(uint8_t *)c->blocks, (int64_t)(c->bytes / bb), (int64_t)bb,        c->table,      c->n_seqs,
+                c->table_ld,          __builtin_ctz(c->block_tokens), c->n_kv_heads, layer};
+  return HS_OK;
+}
+
+// rows of n_heads heads of head_dim elements: the strides keep them apart and
+// aligned to 16 bytes (one row needs no row stride)
+int kvq_strides(const char *fn, int dtype, int64_t n, int64_t ld, int64_t ld_head, int heads, int hd) {
+  const int ce = 16 / dtype_bytes(dtype);
+  if (ld % ce || ld_head % ce) return fail(HS_E_INVALID, "%s: strides must be multiples of %d elements", fn, ce);
+  // far below 64 bits in bytes, so that no offset wraps
+  if (ld < 0 || ld_head < 0 || ld > (1ll << 40) || ld_head > (1ll << 40)) return fail(HS_E_INVALID, "%s: stride out of range", fn);
+  if (heads > 1 && ld_head < hd) return fail(HS_E_INVALID, "%s: heads overlap", fn);
+  // rows of heads side by side, or heads of rows side by side
+  const int64_t per_head = n > 1 ? (n - 1) * ld + hd : hd, per_row = (int64_t)(heads - 1) * ld_head + hd;
+  if (n > 1 && (ld < hd || (ld < per_row && heads > 1 && ld_head < per_head)))
+    return fail(HS_E_INVALID, "%s: rows overlap", fn);
+  return HS_OK;
+}
+
+int kvq_rows_args(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, int32_t n, const void *k, const void *v,
+                  int64_t ld, int64_t ld_head, const int32_t *positions, const char *fn, KvqRef *ref) {
+  const int rc = kvq_ref(cache, layer, fn, ref);
+  if (rc) return rc;
+  if (dtype < HS_F32 || dtype > HS_BF16) return fail(HS_E_INVALID, "%s: unknown dtype", fn);
+  if (n < 0) return fail(HS_E_INVALID, "%s: negative row count", fn);
+  if (n == 0) return HS_OK;
+  if (!k || !v || !positions) return fail(HS_E_INVALID, "%s: NULL argument", fn);
+  if (((uintptr_t)k | (uintptr_t)v) % 16) return fail(HS_E_INVALID, "%s: rows must be 16-byte aligned", fn);
+  if ((int64_t)n * cache->n_kv_heads > (1ll << 31)) return fail(HS_E_INVALID, "%s: too many rows", fn);
+  return kvq_strides(fn, dtype, n, ld, ld_head, cache->n_kv_heads, cache->head_dim);
+}
+
+}  // namespace
+
+extern "C" {
+
+int hs_kvq_append(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, int32_t n, const void *k, const void *v,
+                  int64_t ld, int64_t ld_head, const int32_t *seqs, const int32_t *positions, void *k_values,
+                  void *v_values, hs_stream_t stream) {
+  static const char *fn = "hs_kvq_append";
+  KvqRows a{};
+  const int rc = kvq_rows_args(cache, layer, dtype, n, k, v, ld, ld_head, positions, fn, &a.c);
+  if (rc || n == 0) return rc;
+  if (!k_values != !v_values) return fail(HS_E_INVALID, "%s: k_values and v_values are given together", fn);
+  if (((uintptr_t)k_values | (uintptr_t)v_values) % 16) return fail(HS_E_INVALID, "%s: rows must be 16-byte aligned", fn);
+  a.n = n;
+  a.k = k;
+  a.v = v;
+  a.k_out = k_values;
+  a.v_out = v_values;
+  a.ld = ld;
+  a.ld_head = ld_head;
+  a.seqs = seqs;
+  a.pos = positions;
+  HIP_TRY(launch_kvq_append(dtype, cache->head_dim, a, (hipStream_t)stream));
+  return HS_OK;
+}
+
+int hs_kvq_read(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, int32_t n, void *k, void *v, int64_t ld,
+                int64_t ld_head, const int32_t *seqs, const int32_t *positions, hs_stream_t stream) {
+  static const char *fn = "hs_kvq_read";
+  KvqRows a{};
+  const int rc = kvq_rows_args(cache, layer, dtype, n, k, v, ld, ld_head, positions, fn, &a.c);
+  if (rc || n == 0) return rc;
+  a.n = n;
+  a.k_out = k;
+  a.v_out = v;
+  a.ld = ld;
+  a.ld_head = ld_head;
+  a.seqs = seqs;
+  a.pos = positions;
+  HIP_TRY(launch_kvq_read(dtype, cache->head_dim, a, (hipStream_t)stream));
+  return HS_OK;
+}
+
+int hs_kvq_attention_workspace(const hs_kvq_cache *cache, int32_t dtype, int32_t n, int32_t n_heads, int32_t max_len,
+                               uint64_t *bytes) {
+  static const char *fn = "hs_kvq_attention_workspace";
+  if (!cache || !bytes) return fail(HS_E_INVALID, "%s: NULL argument", fn);
+  uint64_t bb;
+  const int rc = hs_kvq_block_bytes(cache->n_layers, cache->n_kv_heads, cache->head_dim, cache->block_tokens, &bb);
+  if (rc) return rc;
+  if (dtype < HS_F32 || dtype > HS_BF16) return fail(HS_E_INVALID, "%s: unknown dtype", fn);
+  if (n < 0 || max_len <= 0) return fail(HS_E_INVALID, "%s: negative row count or max_len not positive", fn);
+  if (n_heads <= 0 || n_heads % cache->n_kv_heads || n_heads / cache->n_kv_heads > 16)
+    return fail(HS_E_INVALID, "%s: n_heads %d is not 1..16 times n_kv_heads %d", fn, n_heads, cache->n_kv_heads);
+  if ((int64_t)n * n_heads > (1 << 30)) return fail(HS_E_INVALID, "%s: too many rows", fn);
+  *bytes = 0;
+  return HS_OK;
+}
+
+int hs_kvq_attention(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, int32_t n, int32_t n_heads,
+                     const void *q, int64_t ld_q, const int32_t *seqs, const int32_t *lengths, int32_t max_len,
+                     float scale, void *out, int64_t ld_out, void *workspace, uint64_t workspace_bytes,
+                     hs_stream_t stream) {
+  static const char *fn = "hs_kvq_attention";
+  KvqAttn a{};
+  int rc = kvq_ref(cache, layer, fn, &a.c);
+  if (rc) return rc;
+  uint64_t need;
+  rc = hs_kvq_attention_workspace(cache, dtype, n, n_heads, max_len, &need);
+  if (rc || n == 0) return rc;
+  if (!q || !out || !lengths) return fail(HS_E_INVALID, "%s: NULL argument", fn);
+  if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)workspace) % 16)
+    return fail(HS_E_INVALID, "%s: q, out and workspace must be 16-byte aligned", fn);
+  rc = kvq_strides(fn, dtype, n, ld_q, cache->head_dim, n_heads, cache->head_dim);
+  if (!rc) rc = kvq_strides(fn, dtype, n, ld_out, cache->head_dim, n_heads, cache->head_dim);
+  if (rc) return rc;
+  if (need && (!workspace || workspace_bytes < need))
+    return fail(HS_E_BUFFER, "%s: the workspace holds %llu bytes, %llu are needed", fn,
+                (unsigned long long)(workspace ? workspace_bytes : 0), (unsigned long long)need);
+  a.q = q;
+  a.ld_q = ld_q;
+  a.n = n;
+  a.n_heads = n_heads;
+  a.seqs = seqs;
+  a.lens = lengths;
+  a.max_len = max_len;
+  a.scale = scale;
+  a.out = out;
+  a.ld_out = ld_out;
+  HIP_TRY(launch_kvq_attention(dtype, cache->head_dim, a, (hipStream_t)stream));
+  return HS_OK;
+}
+
+// ---- log probabilities of tokens ----
+
+int hs_token_logprobs_workspace(int64_t rows, int32_t vocab, int32_t top, uint64_t *bytes) {
+  static const char *fn = "hs_token_logprobs_workspace";
+  if (!bytes) return fail(HS_E_INVALID, "%s: bytes is NULL", fn);
+  if (rows < 0 || rows > INT32_MAX / 64 || vocab <= 0) return fail(HS_E_INVALID, "%s: rows or vocab out of range", fn);
+  if (top < 0 || top > 64 || top > vocab) return fail(HS_E_INVALID, "%s: top %d is not in 0..64 or exceeds vocab", fn, top);
+  *bytes = 0;
+  return HS_OK;
+}
+
+int hs_token_logprobs(int32_t dtype, const void *logits, int64_t rows, int32_t vocab, int64_t ld,
+                      const int32_t *tokens, int32_t top, float *logprob, float *entropy, int32_t *top_ids,
+                      float *top_logprobs, void *workspace, uint64_t workspace_bytes, hs_stream_t stream) {
+  static const char *fn = "hs_token_logprobs";
+  uint64_t need;
+  const int rc = hs_token_logprobs_workspace(rows, vocab, top, &need);
+  if (rc) return rc;
+  if (dtype < HS_F32 || dtype > HS_BF16) return fail(HS_E_INVALID, "%s: unknown dtype", fn);
+  if (rows == 0) return HS_OK;
+  if (!logits) return fail(HS_E_INVALID, "%s: logits is NULL", fn);
+  if (((uintptr_t)logits) % dtype_bytes(dtype)) return fail(HS_E_INVALID, "%s: logits are not aligned to their type", fn);
+  if (rows > 1 && (ld < vocab || ld > (1ll << 40))) return fail(HS_E_INVALID, "%s: rows overlap, or ld out of range", fn);
+  if (logprob && !tokens) return fail(HS_E_INVALID, "%s: logprob needs tokens", fn);
+  if (need && (!workspace || workspace_bytes < need))
+    return fail(HS_E_BUFFER, "%s: the workspace holds %llu bytes, %llu are needed", fn,
+                (unsigned long long)(workspace ? workspace_bytes : 0), (unsigned long long)need);
+  if (((uintptr_t)workspace) % 16) return fail(HS_E_INVALID, "%s: workspace must be 16-byte aligned", fn);
+  LogprobArgs a{};
+  a.logits = logits;
+  a.rows = rows;
+  a.ld = rows > 1 ? ld : 0;
+  a.vocab = vocab;
+  a.top = top;
+  a.tokens = tokens;
+  a.logprob = logprob;
+  a.entropy = entropy;
+  a.top_ids = top_ids;
+  a.top_logprobs = top_logprobs;
+  HIP_TRY(launch_logprobs(dtype, a, (hipStream_t)stream));
+  return HS_OK;
+}
+
 }  // extern "C"

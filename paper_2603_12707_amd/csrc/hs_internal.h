@@ -304,6 +304,60 @@ hipError_t launch_gather_last(const float *x, int d, const PackedRows &pk, float
 
 bool attn_supported(int dtype, int head_dim, int group);
 
+// ---- the cache held in 4 bits (layout: hs_kvq_cache in hs.h) ----
+struct KvqRef {
+  uint8_t *blocks;
+  int64_t n_blocks, block_bytes;
+  const int64_t *table;  // [n_seqs][table_ld] block numbers
+  int n_seqs, table_ld;
+  int bt_log2;           // log2 of the positions of a block
+  int n_kv, layer;
+};
+// bytes of one layer's K or V of one head in a block of bt positions
+inline int64_t kvq_slab_bytes(int bt, int hd) { return (int64_t)bt * hd / 32 * 17; }
+// Rows to store or fetch: element (row, head, e) of K sits at k + row * ld +
+// head * ld_head + e, V alike.  Row r goes to sequence seqs[r] (NULL: r) and
+// position pos[r] (pos_by_seq: pos[sequence]); past cap[sequence], if given, it
+// is not stored.
+struct KvqRows {
+  KvqRef c;
+  int n;
+  const void *k, *v;     // append
+  void *k_out, *v_out;   // append: the values stored, or NULL; read: the rows
+  int64_t ld, ld_head;
+  const int *seqs, *pos, *cap;
+  int pos_by_seq;
+};
+// Row r of q attends over the first len positions of sequence seqs[r] (NULL:
+// r); len = lens[r] or (len_by_seq) lens[sequence], plus len_add, at most max_len
+// and, if given, cap[sequence].
+struct KvqAttn {
+  KvqRef c;
+  const void *q;
+  int64_t ld_q;
+  int n, n_heads;
+  const int *seqs, *lens, *cap;
+  int len_by_seq, len_add, max_len;
+  float scale;
+  void *out;
+  int64_t ld_out;
+};
+hipError_t launch_kvq_append(int dtype, int head_dim, const KvqRows &a, hipStream_t st);
+hipError_t launch_kvq_read(int dtype, int head_dim, const KvqRows &a, hipStream_t st);
+hipError_t launch_kvq_attention(int dtype, int head_dim, const KvqAttn &a, hipStream_t st);
+
+// log probabilities of rows of logits (hs_token_logprobs)
+struct LogprobArgs {
+  const void *logits;
+  int64_t rows, ld;
+  int vocab, top;
+  const int *tokens;
+  float *logprob, *entropy;
+  int *top_ids;
+  float *top_logprobs;
+};
+hipError_t launch_logprobs(int dtype, const LogprobArgs &a, hipStream_t st);
+
 // records the thread's error message (hs_last_error) and returns code
 int fail(int code, const char *fmt, ...);
 

@@ -1,6 +1,9 @@
 // hs_misc.hip — embedding gather, prefill input rows, greedy selection and
-// length bookkeeping kernels of the decode engine (gfx950).
+// length bookkeeping kernels of the decode engine (gfx950); the 4-bit cache's
+// kernels and the token log probabilities come in by their headers.
 #include "hs_device.h"
+#include "hs_kvq.h"
+#include "hs_logprobs.h"
 
 namespace hs {
 namespace {

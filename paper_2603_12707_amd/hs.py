@@ -25,7 +25,9 @@ EXPORTS = ("hs_last_error", "hs_kv_bytes", "hs_model_create", "hs_model_free", "
            "hs_kv_read", "hs_kv_set_length", "hs_replay_kernels", "hs_packed_bytes", "hs_pack_matrix", "hs_pack_matrix_heads", "hs_kv_sync",
            "hs_prefill_batch", "hs_model_reserve_rows", "hs_kv_pool_create", "hs_kv_admit", "hs_kv_release",
            "hs_kv_pool_blocks", "hs_handoff_create", "hs_handoff_free", "hs_handoff_push", "hs_handoff_pop",
-           "hs_handoff_pending", "hs_stream_read", "hs_decode_step_static")
+           "hs_handoff_pending", "hs_stream_read", "hs_decode_step_static", "hs_kvq_block_bytes", "hs_kvq_append",
+           "hs_kvq_read", "hs_kvq_attention_workspace", "hs_kvq_attention", "hs_token_logprobs_workspace",
+           "hs_token_logprobs")
 
 # projection matrices the library reads in its packed layout
 PACKED = ("wq", "wk", "wv", "wo", "w_gate", "w_up", "w_down", "lm_head")
@@ -55,6 +57,12 @@ class hs_layer_weights(ctypes.Structure):
 class hs_weights(ctypes.Structure):
     _fields_ = [("embed", ctypes.c_void_p), ("final_norm", ctypes.c_void_p), ("lm_head", ctypes.c_void_p),
                 ("layers", ctypes.POINTER(hs_layer_weights))]
+
+
+class hs_kvq_cache(ctypes.Structure):
+    _fields_ = [("blocks", ctypes.c_void_p), ("bytes", ctypes.c_uint64), ("table", ctypes.c_void_p),
+                ("n_seqs", ctypes.c_int32), ("table_ld", ctypes.c_int32), ("n_layers", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("block_tokens", ctypes.c_int32)]
 
 
 _lib = None
@@ -108,6 +116,13 @@ def lib() -> ctypes.CDLL:
         "hs_packed_bytes": [I32, I64, I64, ctypes.POINTER(U64)],
         "hs_pack_matrix": [I32, P, I64, I64, P, P],
         "hs_pack_matrix_heads": [I32, P, I64, I64, I32, P, P],
+        "hs_kvq_block_bytes": [I32, I32, I32, I32, ctypes.POINTER(U64)],
+        "hs_kvq_append": [P, I32, I32, I32, P, P, I64, I64, P, P, P, P, P],
+        "hs_kvq_read": [P, I32, I32, I32, P, P, I64, I64, P, P, P],
+        "hs_kvq_attention_workspace": [P, I32, I32, I32, I32, ctypes.POINTER(U64)],
+        "hs_kvq_attention": [P, I32, I32, I32, I32, P, I64, P, P, I32, ctypes.c_float, P, I64, P, U64, P],
+        "hs_token_logprobs_workspace": [I64, I32, I32, ctypes.POINTER(U64)],
+        "hs_token_logprobs": [I32, P, I64, I32, I64, P, I32, P, P, P, P, P, U64, P],
     }
     for name, args in sig.items():
         fn = getattr(L, name)
@@ -385,6 +400,198 @@ class KVPool(KVCache):
         f, n = ctypes.c_int32(), ctypes.c_int32()
         _call("hs_kv_pool_blocks", self.handle, ctypes.byref(f), ctypes.byref(n))
         return f.value, n.value
+
+
+def _dtype_code(func: str, t) -> int:
+    import torch
+    if t.dtype is torch.bfloat16:
+        return HS_BF16
+    if t.dtype is torch.float16:
+        return HS_F16
+    if t.dtype is torch.float32:
+        return HS_F32
+    raise ValueError(f"{func}: {t.dtype} is none of float32, float16, bfloat16")
+
+
+def _int32(func: str, name: str, t, n: int, device):
+    """Address of a contiguous int32 tensor of n values on the device (None: NULL)."""
+    import torch
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{func}: {name} must be {n} contiguous int32 values on {device}")
+    return t.data_ptr()
+
+
+def _on_device(func: str, device, call):
+    """call(stream), with the tensors' device current."""
+    import torch
+    if device.type != "cuda":
+        raise ValueError(f"{func}: tensors must be on the GPU")
+    if device.index == torch.cuda.current_device():
+        return call(torch.cuda.current_stream().cuda_stream)
+    with torch.cuda.device(device):
+        return call(torch.cuda.current_stream().cuda_stream)
+
+
+def kvq_block_bytes(n_layers: int, n_kv_heads: int, head_dim: int, block_tokens: int) -> int:
+    """Bytes of one block of a cache held in 4 bits."""
+    out = ctypes.c_uint64()
+    _call("hs_kvq_block_bytes", n_layers, n_kv_heads, head_dim, block_tokens, ctypes.byref(out))
+    return out.value
+
+
+class QuantCache:
+    """A KV cache held in 4 bits (hs_kvq_cache) over caller-owned tensors:
+    blocks, a contiguous uint8 tensor of whole blocks (kvq_block_bytes each),
+    and table, a contiguous int64 tensor [sequences][blocks per sequence] of
+    block numbers, negative where there is none.  The table may be rewritten
+    between calls."""
+
+    def __init__(self, blocks, table, n_layers: int, n_kv_heads: int, head_dim: int, block_tokens: int):
+        import torch
+        if blocks.dtype is not torch.uint8 or not blocks.is_contiguous():
+            raise ValueError("QuantCache: blocks must be a contiguous uint8 tensor")
+        if table.dtype is not torch.int64 or table.dim() != 2 or not table.is_contiguous() or \
+                table.device != blocks.device:
+            raise ValueError("QuantCache: table must be a contiguous int64 matrix on the blocks' device")
+        kvq_block_bytes(n_layers, n_kv_heads, head_dim, block_tokens)  # checks the sizes
+        self.blocks, self.table = blocks, table  # keeps the tensors alive
+        self.n_layers, self.n_kv_heads, self.head_dim, self.block_tokens = n_layers, n_kv_heads, head_dim, block_tokens
+        self._c = hs_kvq_cache(blocks.data_ptr(), blocks.numel(), table.data_ptr(), table.shape[0], table.shape[1],
+                               n_layers, n_kv_heads, head_dim, block_tokens)
+        self._ref = ctypes.addressof(self._c)
+        self._lib = lib()
+
+    def _check_rows(self, func: str, k, v):
+        """k, v: [n][n_kv_heads][head_dim], equal strides, channels contiguous."""
+        if k.dim() != 3 or k.shape[1] != self.n_kv_heads or k.shape[2] != self.head_dim or v.shape != k.shape or \
+                v.dtype != k.dtype or k.stride(2) != 1 or v.stride() != k.stride() or \
+                k.device != self.blocks.device or v.device != k.device:
+            raise ValueError(f"{func}: k and v must be [n][{self.n_kv_heads}][{self.head_dim}] on {self.blocks.device}, "
+                             "of one type and equal strides, channels contiguous")
+
+    def append(self, layer: int, k, v, positions, seqs=None, k_values=None, v_values=None) -> None:
+        """Stores rows of K and V ([n][n_kv_heads][head_dim]) at positions (int32 [n]) of sequences seqs (int32 [n];
+        None: row i is sequence i).  k_values / v_values (of k's strides; may be k and v) receive the stored values."""
+        func = "QuantCache.append"
+        self._check_rows(func, k, v)
+        if k_values is not None or v_values is not None:
+            if k_values is None or v_values is None:
+                raise ValueError(f"{func}: k_values and v_values are given together")
+            self._check_rows(func, k_values, v_values)
+            if k_values.dtype != k.dtype or k_values.shape != k.shape or k_values.stride() != k.stride():
+                raise ValueError(f"{func}: k_values and v_values must be laid out as k")
+        n, dt, device = k.shape[0], _dtype_code(func, k), k.device
+        pos, sq = _int32(func, "positions", positions, n, device), _int32(func, "seqs", seqs, n, device)
+        kv, vv = (None, None) if k_values is None else (k_values.data_ptr(), v_values.data_ptr())
+        rc = _on_device(func, device, lambda st: self._lib.hs_kvq_append(
+            self._ref, layer, dt, n, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), sq, pos, kv, vv, st))
+        check("hs_kvq_append", rc)
+
+    def read(self, layer: int, positions, dtype, seqs=None, k=None, v=None):
+        """The rows at positions of sequences seqs, as (k, v) of a torch dtype (or into k and v)."""
+        import torch
+        func = "QuantCache.read"
+        n, device = positions.numel(), self.blocks.device
+        if k is None:
+            k = torch.empty(n, self.n_kv_heads, self.head_dim, dtype=dtype, device=device)
+        if v is None:
+            v = torch.empty_strided(k.shape, k.stride(), dtype=k.dtype, device=device)
+        self._check_rows(func, k, v)
+        if k.shape[0] != n or k.dtype != dtype:
+            raise ValueError(f"{func}: k and v must hold {n} rows of {dtype}")
+        dt = _dtype_code(func, k)
+        pos, sq = _int32(func, "positions", positions, n, device), _int32(func, "seqs", seqs, n, device)
+        rc = _on_device(func, device, lambda st: self._lib.hs_kvq_read(
+            self._ref, layer, dt, n, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), sq, pos, st))
+        check("hs_kvq_read", rc)
+        return k, v
+
+    def _workspace_bytes(self, dt: int, n: int, n_heads: int, max_len: int) -> int:
+        out = ctypes.c_uint64()
+        check("hs_kvq_attention_workspace", self._lib.hs_kvq_attention_workspace(self._ref, dt, n, n_heads, max_len,
+                                                                                ctypes.byref(out)))
+        return out.value
+
+    def attention_workspace(self, n: int, n_heads: int, max_len: int, dtype=None):
+        """A workspace for attention over n rows of n_heads heads and max_len positions (dtype None: of any type)."""
+        import torch
+        codes = range(HS_F32, HS_BF16 + 1) if dtype is None else (_dtype_code("QuantCache.attention_workspace",
+                                                                              torch.empty(0, dtype=dtype)),)
+        most = max(self._workspace_bytes(dt, n, n_heads, max_len) for dt in codes)
+        return torch.empty(most, dtype=torch.uint8, device=self.blocks.device)
+
+    def attention(self, layer: int, q, lengths, seqs=None, max_len=None, scale=None, out=None, workspace=None):
+        """Decode attention of q ([n][n_heads][head_dim]) over the first lengths (int32 [n]) positions of sequences
+        seqs; max_len bounds the lengths (None: what the table holds), scale None: head_dim ** -0.5.  A workspace may
+        be kept from call to call (attention_workspace), not shared by calls on several streams."""
+        import torch
+        func = "QuantCache.attention"
+        device, hd = self.blocks.device, self.head_dim
+        if q.dim() != 3 or q.shape[2] != hd or q.stride(2) != 1 or (q.shape[1] > 1 and q.stride(1) != hd) or \
+                q.device != device:
+            raise ValueError(f"{func}: q must be [n][n_heads][{hd}] on {device}, each row contiguous")
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=device)
+        elif out.shape != q.shape or out.dtype != q.dtype or out.device != device or out.stride(2) != 1 or \
+                (q.shape[1] > 1 and out.stride(1) != hd):
+            raise ValueError(f"{func}: out must be of q's shape and type, each row contiguous")
+        n, heads, dt = q.shape[0], q.shape[1], _dtype_code(func, q)
+        if max_len is None:
+            max_len = min(self.table.shape[1] * self.block_tokens, 2**31 - 1)
+        if scale is None:
+            scale = hd ** -0.5
+        ln, sq = _int32(func, "lengths", lengths, n, device), _int32(func, "seqs", seqs, n, device)
+        if workspace is None:
+            workspace = torch.empty(self._workspace_bytes(dt, n, heads, max_len), dtype=torch.uint8, device=device)
+        elif workspace.device != device or not workspace.is_contiguous():
+            raise ValueError(f"{func}: workspace must be contiguous on {device}")
+        rc = _on_device(func, device, lambda st: self._lib.hs_kvq_attention(
+            self._ref, layer, dt, n, heads, q.data_ptr(), q.stride(0), sq, ln, max_len, scale, out.data_ptr(),
+            out.stride(0), workspace.data_ptr() or None, workspace.numel() * workspace.element_size(), st))
+        check("hs_kvq_attention", rc)
+        return out
+
+
+def _logprobs_bytes(rows: int, vocab: int, top: int) -> int:
+    out = ctypes.c_uint64()
+    _call("hs_token_logprobs_workspace", rows, vocab, top, ctypes.byref(out))
+    return out.value
+
+
+def token_logprobs_workspace(rows: int, vocab: int, top: int = 0, device="cuda"):
+    """A workspace for token_logprobs over rows of vocab logits."""
+    import torch
+    return torch.empty(_logprobs_bytes(rows, vocab, top), dtype=torch.uint8, device=device)
+
+
+def token_logprobs(logits, tokens=None, top: int = 0, workspace=None):
+    """(logprob, entropy, top_ids, top_logprobs) of rows of logits ([rows][vocab]; float32, float16 or bfloat16):
+    the log probability of each row's given token (int32 [rows]; a negative one asks for none and gives 0; None: no
+    logprob), the row's entropy in nats, and its `top` most probable tokens with their log probabilities
+    ([rows][top]; None without)."""
+    import torch
+    func = "token_logprobs"
+    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError(f"{func}: logits must be [rows][vocab], each row contiguous")
+    rows, vocab = logits.shape
+    device, dt = logits.device, _dtype_code(func, logits)
+    tk = _int32(func, "tokens", tokens, rows, device)
+    lp = None if tokens is None else torch.empty(rows, dtype=torch.float32, device=device)
+    entropy = torch.empty(rows, dtype=torch.float32, device=device)
+    ids = torch.empty(rows, top, dtype=torch.int32, device=device) if top > 0 else None
+    tops = torch.empty(rows, top, dtype=torch.float32, device=device) if top > 0 else None
+    if workspace is None:
+        workspace = torch.empty(_logprobs_bytes(rows, vocab, top), dtype=torch.uint8, device=device)
+    elif workspace.device != device or not workspace.is_contiguous():
+        raise ValueError(f"{func}: workspace must be contiguous on {device}")
+    rc = _on_device(func, device, lambda st: lib().hs_token_logprobs(
+        dt, logits.data_ptr(), rows, vocab, logits.stride(0), tk, top, None if lp is None else lp.data_ptr(),
+        entropy.data_ptr(), None if ids is None else ids.data_ptr(), None if tops is None else tops.data_ptr(),
+        workspace.data_ptr() or None, workspace.numel() * workspace.element_size(), st))
+    check("hs_token_logprobs", rc)
+    return lp, entropy, ids, tops
 
 
 class Handoff:

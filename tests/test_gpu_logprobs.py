@@ -1,0 +1,172 @@
+"""Token log probabilities, entropies and alternatives on the GPU against a plain 64-bit form."""
+from __future__ import annotations
+
+import math
+
+import pytest
+import torch
+
+import kvq_ref as R
+
+pytestmark = pytest.mark.gpu
+
+
+def check(hs, x, tokens, top, workspace=None):
+    tk = tokens.to(torch.int32).cuda()
+    lp, ent, ids, tops = hs.token_logprobs(x, tk, top=top, workspace=workspace)
+    want = R.logprobs(x.float().cpu(), tokens, top)
+    for got, ref in ((lp, want[0]), (ent, want[1])) + (((tops, want[3]),) if top else ()):
+        got = got.double().cpu()
+        assert torch.equal(torch.isnan(got), torch.isnan(ref))
+        inf = torch.isinf(ref)
+        assert torch.equal(got[inf], ref[inf])
+        fine = torch.isfinite(ref)
+        err = (got[fine] - ref[fine]).abs()
+        assert (err <= R.logprob_tolerance(ref[fine])).all(), float(err.max())
+    if top:
+        assert torch.equal(ids.long().cpu(), want[2])
+    return lp, ent, ids, tops
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(1, 1), (3, 2), (2, 63), (2, 64), (2, 65), (5, 997), (1, 4096), (2, 8191),
+                                        (2, 8192), (2, 8193), (3, 16385), (3, 32000), (2, 152064), (1, 200001)])
+def test_logprobs_of_every_size(dtype, rows, vocab):
+    import paper_2603_12707_amd as hs
+    g = torch.Generator().manual_seed(vocab)
+    x = (torch.randn(rows, vocab, generator=g) * 3).to(R.DT[dtype]).cuda()
+    tokens = torch.randint(0, vocab, (rows,), generator=g)
+    for top in sorted({0, 1, min(5, vocab), min(20, vocab), min(64, vocab)}):
+        check(hs, x, tokens, top)
+
+
+@pytest.mark.parametrize("vocab", [3, 100, 4099, 40000])
+def test_equal_logits_come_by_index(vocab):
+    """Ties everywhere: rows of one value, of two values, of zeros of both signs."""
+    import paper_2603_12707_amd as hs
+    x = torch.zeros(5, vocab)
+    x[1] = -2.5
+    x[2, 1::2] = 1.0
+    x[3, ::2] = -0.0
+    x[4] = torch.arange(vocab) // 7
+    top = min(vocab, 64)
+    for dtype in ("f32", "bf16"):
+        check(hs, x.to(R.DT[dtype]).cuda(), torch.tensor([0, vocab - 1, 1, 2, vocab // 2]), top)
+
+
+@pytest.mark.parametrize("vocab", [4097, 40000])
+def test_sorted_rows(vocab):
+    """The largest logits side by side at the start, at the end, and a stride apart."""
+    import paper_2603_12707_amd as hs
+    up = torch.linspace(-8, 8, vocab)
+    x = torch.stack([up, up.flip(0), up.reshape(-1)[torch.arange(vocab) * 64 % vocab] if vocab % 2 else up])
+    check(hs, x.cuda(), torch.tensor([0, 1, 2]), 64)
+
+
+@pytest.mark.parametrize("vocab", [5, 9001, 33000])
+def test_banned_words_and_rows_without_a_distribution(vocab):
+    import paper_2603_12707_amd as hs
+    g = torch.Generator().manual_seed(1)
+    x = torch.randn(12, vocab, generator=g)
+    x[0, torch.rand(vocab, generator=g) < 0.9] = -math.inf
+    x[0, 2] = 0.0
+    x[1] = -math.inf
+    x[1, vocab - 1] = -300.0  # one word left
+    x[2] = -math.inf          # none
+    x[3, 1] = math.nan
+    x[4, vocab - 1] = math.inf
+    x[5] = torch.finfo(torch.float32).min  # the lowest number, everywhere: an even distribution
+    x[6] = torch.finfo(torch.float32).min
+    x[6, 3] = 0.0
+    x[7, vocab // 2] = -math.nan
+    x[8] = math.inf
+    x[9] = -math.inf
+    x[9, :2] = torch.tensor([1.0, 1.0])
+    x[10, 0] = 80.0
+    x[11] *= 1e30
+    tokens = torch.tensor([2, vocab - 1, 0, 0, 0, 1, 0, -1, 4, 3, 0, 0])
+    check(hs, x.cuda(), tokens, 5)
+    check(hs, x.cuda(), torch.full((12,), -1), 3)
+    check(hs, x.cuda(), torch.tensor([vocab, vocab + 5, 2 ** 31 - 1, -2 ** 31] * 3), 1)
+
+
+def test_nearly_certain_tokens_keep_their_digits():
+    """log Z of a row with one likely word: as small as e^-40, and within a few 2^-22 of itself."""
+    import paper_2603_12707_amd as hs
+    x = torch.zeros(3, 20000)
+    for r, gap in enumerate((20.0, 30.0, 50.0)):
+        x[r, 12345] = gap
+    lp, ent, ids, tops = hs.token_logprobs(x.cuda(), torch.full((3,), 12345, dtype=torch.int32).cuda(), top=1)
+    want = R.logprobs(x, torch.full((3,), 12345), 1)
+    assert ids.flatten().tolist() == [12345] * 3
+    assert ((lp.double().cpu() - want[0]).abs() <= 2.0 ** -18 * want[0].abs()).all()
+    assert ((ent.double().cpu() - want[1]).abs() <= 2.0 ** -18 * want[1].abs()).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_strides_and_unaligned_rows(dtype):
+    """Rows inside a wider matrix, from every offset of a 16-byte chunk."""
+    import paper_2603_12707_amd as hs
+    g = torch.Generator().manual_seed(2)
+    base = (torch.randn(4, 9100, generator=g) * 2).to(R.DT[dtype])
+    for off in range(0, 9):
+        for vocab in (8192, 9000 + off, 3 + off):
+            x = base.cuda()[:, off : off + vocab]
+            check(hs, x, torch.tensor([0, vocab - 1, 1, -1]), min(vocab, 7))
+
+
+def test_many_rows():
+    import paper_2603_12707_amd as hs
+    g = torch.Generator().manual_seed(3)
+    x = (torch.randn(70000, 17, generator=g) * 2).cuda()  # more rows than a grid's second dimension takes
+    tokens = torch.randint(-1, 17, (70000,), generator=g)
+    lp, ent, ids, tops = hs.token_logprobs(x, tokens.int().cuda(), top=2)
+    ref = torch.log_softmax(x.double(), -1).cpu()
+    want = torch.where(tokens >= 0, ref.gather(1, tokens.clamp(min=0)[:, None])[:, 0], 0.0)
+    assert ((lp.double().cpu() - want).abs() <= R.logprob_tolerance(want)).all()
+    assert ((ent.double().cpu() + (ref.exp() * ref).sum(-1)).abs() <= 2.0 ** -16).all()
+    order = torch.sort(x.cpu(), descending=True, stable=True)
+    assert torch.equal(ids.long().cpu(), order.indices[:, :2])
+
+
+def test_outputs_are_optional():
+    import paper_2603_12707_amd as hs
+    x = torch.randn(3, 5000, device="cuda")
+    tk = torch.tensor([1, 2, 3], dtype=torch.int32, device="cuda")
+    lp, ent, ids, tops = hs.token_logprobs(x, tk, top=4)
+    a = hs.token_logprobs(x)
+    assert a[0] is None and a[2] is None and a[3] is None and torch.equal(a[1], ent)
+    b = hs.token_logprobs(x, top=4)
+    assert b[0] is None and torch.equal(b[2], ids) and torch.equal(b[3], tops)
+    empty = hs.token_logprobs(x[:0], tk[:0], top=4)
+    assert empty[0].shape == (0,) and empty[2].shape == (0, 4)
+    L = hs.lib()
+    need = hs.token_logprobs_workspace(3, 5000, 4)
+    lp2 = torch.empty_like(lp)
+    P = lambda t: t.data_ptr() or None  # noqa: E731
+    st = torch.cuda.current_stream().cuda_stream
+    rc = L.hs_token_logprobs(0, P(x), 3, 5000, 5000, P(tk), 4, P(lp2), None, None, None, P(need), need.numel(), st)
+    assert rc == hs.HS_OK and torch.equal(lp2, lp)
+    rc = L.hs_token_logprobs(0, P(x), 3, 5000, 5000, None, 4, None, None, None, None, P(need), need.numel(), st)
+    assert rc == hs.HS_OK
+
+
+def test_deterministic_and_replayed_in_a_graph():
+    import paper_2603_12707_amd as hs
+    x = torch.randn(6, 40001, device="cuda")
+    tk = torch.arange(6, dtype=torch.int32, device="cuda")
+    ws = hs.token_logprobs_workspace(6, 40001, 20).fill_(0xFF)
+    first = [t.clone() for t in hs.token_logprobs(x, tk, top=20, workspace=ws)]
+    again = hs.token_logprobs(x, tk, top=20, workspace=ws)
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        outs = hs.token_logprobs(x, tk, top=20, workspace=ws)
+    for i in range(4):
+        x.copy_(torch.randn(x.shape, device="cuda"))
+        want = [t.clone() for t in hs.token_logprobs(x, tk, top=20)]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)), i
