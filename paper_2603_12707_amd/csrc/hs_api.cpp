@@ -1340,7 +1340,9 @@ int hs_kvq_attention_workspace(const hs_kvq_cache *cache, int32_t dtype, int32_t
   if (n_heads <= 0 || n_heads % cache->n_kv_heads || n_heads / cache->n_kv_heads > 16)
     return fail(HS_E_INVALID, "%s: n_heads %d is not 1..16 times n_kv_heads %d", fn, n_heads, cache->n_kv_heads);
   if ((int64_t)n * n_heads > (1 << 30)) return fail(HS_E_INVALID, "%s: too many rows", fn);
-  *bytes = 0;
+  int S, ns;
+  kvq_split_policy(n, cache->n_kv_heads, max_len, &S, &ns);
+  *bytes = ns > 1 ? (uint64_t)n * n_heads * ns * (cache->head_dim + 2) * 4 : 0;
   return HS_OK;
 }
 
@@ -1371,6 +1373,9 @@ int hs_kvq_attention(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, in
   a.seqs = seqs;
   a.lens = lengths;
   a.max_len = max_len;
+  kvq_split_policy(n, cache->n_kv_heads, max_len, &a.S, &a.n_split);
+  a.part_o = (float *)workspace;
+  a.part_ml = need ? a.part_o + (int64_t)n * n_heads * a.n_split * cache->head_dim : nullptr;
   a.scale = scale;
   a.out = out;
   a.ld_out = ld_out;

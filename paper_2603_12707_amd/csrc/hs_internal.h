@@ -341,7 +341,14 @@ struct KvqAttn {
   float scale;
   void *out;
   int64_t ld_out;
+  const int *order;  // the z-th row to be started is order[z]; NULL: z
+  int S, n_split;    // positions per split (a multiple of 256), splits
+  float *part_o;     // [n][n_heads][n_split][head_dim]
+  float *part_ml;    // [n][n_heads][n_split][2]: maximum (base-2 units; -inf: no position), sum
 };
+constexpr int KVQ_MAX_SPLITS = 256;
+// positions per split and splits for n rows of at most max_len positions
+void kvq_split_policy(int64_t n, int n_kv, int max_len, int *S, int *n_split);
 hipError_t launch_kvq_append(int dtype, int head_dim, const KvqRows &a, hipStream_t st);
 hipError_t launch_kvq_read(int dtype, int head_dim, const KvqRows &a, hipStream_t st);
 hipError_t launch_kvq_attention(int dtype, int head_dim, const KvqAttn &a, hipStream_t st);

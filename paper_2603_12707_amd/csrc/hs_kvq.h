@@ -14,6 +14,9 @@
 
 #include "hs_device.h"
 
+#include <algorithm>
+#include <cfloat>
+
 namespace hs {
 namespace {
 
@@ -86,9 +89,9 @@ __device__ __forceinline__ void st8(void *p, const float *f) {
   }
 }
 
-// weight of a part with maximum m_part in a softmax with maximum m_all
-__device__ __forceinline__ float kvq_weight(float m_part, float m_all) {
-  return m_part == -INFINITY ? 0.f : expf(m_part - m_all);
+// element c of row's output
+__device__ __forceinline__ int64_t kvq_out_at(const KvqAttn &a, int64_t row, int c, int hd) {
+  return row * a.ld_out + c;
 }
 
 // row's positions
@@ -177,59 +180,375 @@ __global__ __launch_bounds__(256) void k_kvq_read(KvqRows a) {
   st8<DT>((char *)(sel ? a.v_out : a.k_out) + ((int64_t)row * a.ld + (int64_t)head * a.ld_head + c * 8) * SB, f);
 }
 
-// Decode attention: one work group takes one query head of one row; each of its
-// 4 waves walks positions, HD / 8 lanes to a position, with an online softmax per
-// group of lanes that is merged at the end.
-template <int DT, int HD>
-__global__ __launch_bounds__(256) void k_kvq_attn(KvqAttn a) {
-  constexpr int CPR = HD / 8, TPW = 64 / CPR;
-  const int h = blockIdx.x % a.n_heads;
-  const int64_t row = blockIdx.x / a.n_heads;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int c = lane % CPR, tg = lane / CPR, head = h / (a.n_heads / a.c.n_kv);
-  const int seq = a.seqs ? a.seqs[row] : (int)row;
-  const int len = kvq_length(a, row, seq);
+// Decode attention over the 4-bit cache.  One work group = (split of the row's
+// positions, row, KV head j); each of its NW waves takes tiles of 64 positions
+// and keeps an online softmax for the G query heads of the head in the 16
+// columns of the matrix products.
+//
+// Scores: S^T = K Q^T, MFMA 16x16x32 with 16 positions as rows.  Lane (li, lg) =
+// (lane % 16, lane / 16) converts HD / 4 consecutive elements of its position,
+// one load and one group's scale, straight into A operands; the order of the
+// elements inside the contraction is the same for Q.  Row r of the tile's
+// product t is position 16 (r / 4) + 4 t + r % 4, so that a lane ends up with
+// the scores of the 16 consecutive positions 16 lg .. for head li, which is the
+// B operand of O^T += V^T P^T: positions 8 m .. 8 m + 7 of each lane group are
+// the k range of MFMA m.  For V^T a lane reads its HD / 16 channels of those 16
+// positions, converts pairs of channels and pairs the positions with v_perm; no
+// value goes through LDS.  The 4-bit values are exact in the 16-bit type, P
+// enters as the sum of parts in that type (two: 16 bits and more; fp32: three,
+// 24 bits, and Q alike), every sum is fp32.
+//
+// Blocks of 64 positions and more (WIDE) hold a tile whole: it is read through a
+// buffer range that ends at its last span, past which nothing is fetched.
+// Smaller blocks are found span by span, per lane.
+template <int DT>
+constexpr int KVQ_MMA = DT == HS_F16 ? HS_F16 : HS_BF16;
+template <int DT>
+constexpr int KVQ_P_PARTS = DT == HS_F32 ? 3 : 2;
+template <int DT>
+constexpr int KVQ_Q_PARTS = DT == HS_F32 ? 3 : 1;
+constexpr int KVQ_TILE = 64;
+// In units of the base-2 exponent: a column's probabilities are 2^(s - m) for a
+// reference m that is put KVQ_BIAS below the largest score when a score passes it
+// by more than KVQ_BIAS + KVQ_SLACK, and o and l are rescaled then.  f16 parts
+// reach from 2^16 down to 2^-24 only: the bias puts the largest probability at
+// 2^11 at least, so that what is dropped is below 2^-36 of it.  The other types
+// have fp32's range.
+template <int DT>
+constexpr float KVQ_BIAS = DT == HS_F16 ? 11.f : 0.f;
+template <int DT>
+constexpr float KVQ_SLACK = DT == HS_F16 ? 4.f : 11.5f;
+// From this reference on, scores are rounded before it is subtracted (as in
+// prefill attention: below it one fma leaves s - m off by at most half an ulp of
+// m, 2^-5, the same factor in o and l).
+constexpr float KVQ_ROUND_FROM = 0x1p20f;
+
+// word x of a matrix operand of parts: R(f0) | R(f1) << 16, and what is left
+template <int MT>
+__device__ __forceinline__ uint32_t take_part(float &f0, float &f1) {
+  const uint32_t w = pack2<MT>(f0, f1);
+  f0 -= lo_f32<MT>(w);
+  f1 -= hi_f32<MT>(w);
+  return w;
+}
+
+template <int DT, int HD, int NW, bool WIDE>
+__global__ __launch_bounds__(64 * NW) void k_kvq_attn(KvqAttn a) {
+  constexpr int MT = KVQ_MMA<DT>, PP = KVQ_P_PARTS<DT>, QP = KVQ_Q_PARTS<DT>;
+  constexpr int NC = HD / 32;             // words of a lane's K elements: k steps of the scores
+  constexpr int VB = HD / 32;             // bytes of a lane's V elements of one position
+  constexpr int ND = HD / 16;             // 16-channel tiles of the output
+  constexpr int SPAN = kvq_span_bytes(HD);
   constexpr int SB = DT == HS_F32 ? 4 : 2;
-  float q[8], o[8] = {};
-  ld8<DT>((const char *)a.q + (row * a.ld_q + h * HD + c * 8) * SB, q);
-  float m = -INFINITY, l = 0.f;
-  for (int p0 = 0; p0 < len; p0 += 4 * TPW) {
-    const int pos = p0 + wave * TPW + tg;
-    const int64_t id = pos < len ? kvq_block(a.c, seq, pos) : -1;
-    float k[8] = {}, v[8] = {};
-    if (id >= 0) {
-      const uint8_t *ks = kvq_span(a.c, HD, id, 0, head, pos), *vs = kvq_span(a.c, HD, id, 1, head, pos);
-      const int at = (pos & 15) * CPR + c, mark = HD * 8 + (c >> 2) * 16 + (pos & 15);
-      kvq_decode(((const uint32_t *)ks)[at], kvq_scale(ks[mark]), k);
-      kvq_decode(((const uint32_t *)vs)[at], kvq_scale(vs[mark]), v);
+  const int G = a.n_heads / a.c.n_kv;
+  // every row's first split comes before any row's second: the empty ones are last
+  const int64_t bid = blockIdx.x, per = (int64_t)a.n * a.c.n_kv;
+  const int split = (int)(bid / per), j = (int)(bid % a.c.n_kv);
+  const int z = (int)(bid % per / a.c.n_kv);
+  const int row = a.order ? a.order[z] : z;
+  const int lane = threadIdx.x & 63, li = lane & 15, lg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int seq = a.seqs ? a.seqs[row] : row;
+  const int len = kvq_length(a, row, seq);
+  const int t0 = split * a.S;
+  const int64_t rh = (int64_t)row * a.n_heads + j * G;  // first (row, head) of the group
+  if (t0 >= len) {
+    for (int i = threadIdx.x; i < G * HD; i += 64 * NW) {
+      const int h = i / HD, e = i - h * HD;
+      if (a.n_split == 1) {
+        st_elem<DT>(a.out, kvq_out_at(a, row, (j * G + h) * HD + e, HD), 0.f);
+      } else {
+        a.part_o[((rh + h) * a.n_split + split) * HD + e] = 0.f;
+        if (e == 0) {
+          a.part_ml[((rh + h) * a.n_split + split) * 2] = -INFINITY;
+          a.part_ml[((rh + h) * a.n_split + split) * 2 + 1] = 0.f;
+        }
+      }
     }
-    float d = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) d += q[e] * k[e];
-    d = group_sum<CPR>(d);
-    if (id < 0) continue;
-    const float s = d * a.scale, mn = fmaxf(m, s), corr = kvq_weight(m, mn), p = expf(s - mn);
-    l = l * corr + p;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = o[e] * corr + p * v[e];
-    m = mn;
+    return;
   }
-  __shared__ float s_m[4 * TPW], s_l[4 * TPW], s_o[4 * TPW][HD];
-  const int slot = wave * TPW + tg;
-  if (c == 0) s_m[slot] = m, s_l[slot] = l;
+  const int end = min(t0 + a.S, len);  // the split's positions: t0 .. end - 1
+  const int n_tiles = (end - t0 + KVQ_TILE - 1) / KVQ_TILE;
+  const int64_t *tab = a.c.table + (int64_t)seq * a.c.table_ld;
+  const int64_t kin = ((int64_t)(a.c.layer * 2) * a.c.n_kv + j) << (a.c.bt_log2 - 4);  // spans before the head's
+  const int64_t vin = kin + ((int64_t)a.c.n_kv << (a.c.bt_log2 - 4));
+  const int in_mask = (1 << a.c.bt_log2) - 1;
+
+  // Q^T operand: head li of the group (zeros past it)
+  u32x4 qb[QP][NC];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) s_o[slot][c * 8 + e] = o[e];
+  for (int c = 0; c < NC; ++c) {
+    float f[8] = {};
+    if (li < G) ld8<DT>((const char *)a.q + ((int64_t)row * a.ld_q + (j * G + li) * HD + lg * (HD / 4) + c * 8) * SB, f);
+    // (a negative scale's sign goes to Q, so that the scores' order is that of the products)
+    if (a.scale < 0.f)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = -f[e];
+#pragma unroll
+    for (int p = 0; p < QP; ++p)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) qb[p][c][x] = take_part<MT>(f[2 * x], f[2 * x + 1]);
+  }
+  const float c2 = fabsf(a.scale) * 1.44269504088896341f;
+
+  // a tile's data in flight: K words and scale bytes, V words and scale bytes
+  uint32_t kc[4][NC], vc[16];
+  u32x4 ks, vs;
+  struct At {           // where a tile is
+    int64_t kid, vid;   // WIDE: the tile's block, twice; else the blocks of the lane's K and V spans
+  };
+  const int kspan = li >> 2, kgrp = HD == 128 ? lg : lg >> 1, vgrp = HD == 128 ? li >> 2 : li >> 3;
+  auto find = [&](int t) {
+    At w{-1, -1};
+    if (t >= n_tiles) return w;
+    const int p0 = t0 + t * KVQ_TILE;
+    if constexpr (WIDE) {
+      w.kid = tab[p0 >> a.c.bt_log2];
+    } else {
+      // past the last span: that span again
+      const int last = (end - 1) & ~15;
+      w.kid = tab[min(p0 + kspan * 16, last) >> a.c.bt_log2];
+      w.vid = tab[min(p0 + lg * 16, last) >> a.c.bt_log2];
+      if ((uint64_t)w.vid >= (uint64_t)a.c.n_blocks) w.vid = -1;
+    }
+    if ((uint64_t)w.kid >= (uint64_t)a.c.n_blocks) w.kid = -1;
+    if constexpr (WIDE) w.vid = w.kid;
+    return w;
+  };
+  auto range = [&](int t, int64_t id, int64_t in) {  // WIDE: the tile's spans
+    const int p0 = t0 + t * KVQ_TILE, spans = (min(end - p0, KVQ_TILE) + 15) / 16;
+    return make_rsrc(a.c.blocks + max(id, (int64_t)0) * a.c.block_bytes + (in + ((p0 & in_mask) >> 4)) * SPAN,
+                     id < 0 || t >= n_tiles ? 0u : (uint32_t)(spans * SPAN));
+  };
+  auto load_k = [&](int t, const At &w) {
+    if constexpr (WIDE) {
+      const rsrc_t r = range(t, w.kid, kin);
+      const uint32_t o = kspan * SPAN + (li & 3) * (HD / 2) + lg * (HD / 8);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        if constexpr (HD == 128) *(u32x4 *)kc[x] = bld16_stream(r, o + x * 4 * (HD / 2));
+        else *(u32x2 *)kc[x] = bld8(r, o + x * 4 * (HD / 2));
+      }
+      ks = bld16_stream(r, kspan * SPAN + HD * 8 + kgrp * 16);
+    } else if (t < n_tiles) {
+      const int p = min(t0 + t * KVQ_TILE + kspan * 16, (end - 1) & ~15);
+      const uint8_t *s = a.c.blocks + max(w.kid, (int64_t)0) * a.c.block_bytes + (kin + ((p & in_mask) >> 4)) * SPAN;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const uint8_t *at = s + (4 * x + (li & 3)) * (HD / 2) + lg * (HD / 8);
+        if constexpr (HD == 128) *(u32x4 *)kc[x] = *(const u32x4 *)at;
+        else *(u32x2 *)kc[x] = *(const u32x2 *)at;
+      }
+      ks = *(const u32x4 *)(s + HD * 8 + kgrp * 16);
+    }
+  };
+  auto load_v = [&](int t, const At &w) {
+    if constexpr (WIDE) {
+      const rsrc_t r = range(t, w.vid, vin);
+      const uint32_t o = lg * SPAN + li * VB;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        if constexpr (HD == 128) vc[i] = bld4(r, o + i * (HD / 2));
+        else vc[i] = (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, o + i * (HD / 2), 0, 0);
+      }
+      vs = bld16_stream(r, lg * SPAN + HD * 8 + vgrp * 16);
+    } else if (t < n_tiles) {
+      const int p = min(t0 + t * KVQ_TILE + lg * 16, (end - 1) & ~15);
+      const uint8_t *s = a.c.blocks + max(w.vid, (int64_t)0) * a.c.block_bytes + (vin + ((p & in_mask) >> 4)) * SPAN;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        if constexpr (HD == 128) vc[i] = *(const uint32_t *)(s + i * (HD / 2) + li * VB);
+        else vc[i] = *(const uint16_t *)(s + i * (HD / 2) + li * VB);
+      }
+      vs = *(const u32x4 *)(s + HD * 8 + vgrp * 16);
+    }
+  };
+
+  // the reference (base-2 units) and this lane's share of the sum; the reference
+  // starts at the lowest finite number, so that s - m is a number for s = -inf
+  float m = -FLT_MAX, l = 0.f;
+  bool big = true;  // some column's |m| >= KVQ_ROUND_FROM (wave-uniform)
+  f32x4 o[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  At cur = find(wave), nxt = find(wave + NW);
+  load_k(wave, cur);
+  load_v(wave, cur);
+  for (int t = wave; t < n_tiles; t += NW) {
+    const int p0 = t0 + t * KVQ_TILE;
+    f32x4 sc[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const float s = kvq_scale((ks[x] >> (8 * (li & 3))) & 255u);
+      sc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const u32x4 kv{kvq_pair<MT, 0>(kc[x][c], s), kvq_pair<MT, 1>(kc[x][c], s), kvq_pair<MT, 2>(kc[x][c], s),
+                       kvq_pair<MT, 3>(kc[x][c], s)};
+#pragma unroll
+        for (int p = 0; p < QP; ++p) sc[x] = mma<MT>(kv, qb[p][c], sc[x]);
+      }
+    }
+    load_k(t + NW, nxt);
+    // which of the lane's 16 positions count: all of them in a whole tile
+    const bool held = cur.vid >= 0;
+    const int left = end - p0 - 16 * lg;
+    const bool whole = p0 + KVQ_TILE <= end && __ballot(!held) == 0;
+    if (!whole) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!held || 4 * x + i >= left) {
+            sc[x][i] = -INFINITY;
+            vc[4 * x + i] = 0u;                       // what lies there may be NaN
+            vs[x] &= ~(255u << (8 * i));
+          }
+    }
+    float tmax = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) tmax = fmaxf(tmax, sc[x][i]);
+    tmax *= c2;
+    if (__ballot(tmax > m + (KVQ_BIAS<DT> + KVQ_SLACK<DT>))) {
+      tmax = fmaxf(tmax, __shfl_xor(tmax, 16));
+      tmax = fmaxf(tmax, __shfl_xor(tmax, 32));
+      const float mn = fmaxf(m, tmax - KVQ_BIAS<DT>);
+      const float corr = __builtin_amdgcn_exp2f(m - mn);
+      l *= corr;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[d] *= corr;
+      m = mn;
+      big = __ballot(fabsf(mn) >= KVQ_ROUND_FROM) != 0;
+    }
+    const float mul = big ? 1.f : c2, sub = big ? 0.f : m;
+    if (big) {
+#pragma clang fp contract(off)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[x][i] = sc[x][i] * c2 - m;
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sc[x][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x][i], mul, -sub));
+    if (!whole) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[x][i] = !held || 4 * x + i >= left ? 0.f : sc[x][i];
+    }
+    float vf[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) vf[i] = kvq_scale((vs[i >> 2] >> (8 * (i & 3))) & 255u);
+    u32x4 pb[2][PP];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        float f0 = sc[2 * h + (x >> 1)][2 * (x & 1)], f1 = sc[2 * h + (x >> 1)][2 * (x & 1) + 1];
+        l += f0 + f1;
+#pragma unroll
+        for (int p = 0; p < PP; ++p) pb[h][p][x] = take_part<MT>(f0, f1);
+      }
+    auto pv = [&](auto bc) {
+      constexpr int B = decltype(bc)::value;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        u32x4 lo, hi;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const uint32_t w0 = kvq_pair<MT, B>(vc[8 * h + 2 * x], vf[8 * h + 2 * x]);
+          const uint32_t w1 = kvq_pair<MT, B>(vc[8 * h + 2 * x + 1], vf[8 * h + 2 * x + 1]);
+          lo[x] = __builtin_amdgcn_perm(w1, w0, 0x05040100u);
+          hi[x] = __builtin_amdgcn_perm(w1, w0, 0x07060302u);
+        }
+#pragma unroll
+        for (int p = 0; p < PP; ++p) {
+          o[2 * B] = mma<MT>(lo, pb[h][p], o[2 * B]);
+          o[2 * B + 1] = mma<MT>(hi, pb[h][p], o[2 * B + 1]);
+        }
+      }
+    };
+    pv(std::integral_constant<int, 0>{});
+    pv(std::integral_constant<int, 1>{});
+    if constexpr (HD == 128) {
+      pv(std::integral_constant<int, 2>{});
+      pv(std::integral_constant<int, 3>{});
+    }
+    load_v(t + NW, nxt);
+    cur = nxt;
+    nxt = find(t + 2 * NW);
+  }
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+
+  // merge the waves: lane (li, lg) holds channels d = (4 lg + i) (HD / 16) + dt of head li
+  __shared__ float s_m[NW][16], s_l[NW][16];
+  __shared__ float s_o[NW][16][HD + 1];
+  if (lg == 0) {
+    s_m[wave][li] = m;
+    s_l[wave][li] = l;
+  }
+  if (li < G)
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s_o[wave][li][(4 * lg + i) * ND + dt] = o[dt][i];
   __syncthreads();
-  for (int e = threadIdx.x; e < HD; e += 256) {
-    float M = -INFINITY, num = 0.f, den = 0.f;
-    for (int s = 0; s < 4 * TPW; ++s) M = fmaxf(M, s_m[s]);
-    for (int s = 0; s < 4 * TPW; ++s) {
-      const float w = kvq_weight(s_m[s], M);
-      num += w * s_o[s][e];
-      den += w * s_l[s];
+  for (int i = threadIdx.x; i < G * HD; i += 64 * NW) {
+    const int h = i / HD, e = i - h * HD;
+    float M = s_m[0][h];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) M = fmaxf(M, s_m[w][h]);
+    float num = 0.f, den = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float wt = __builtin_amdgcn_exp2f(s_m[w][h] - M);
+      num += wt * s_o[w][h][e];
+      den += wt * s_l[w][h];
     }
-    st_elem<DT>(a.out, row * a.ld_out + h * HD + e, M == -INFINITY ? 0.f : num / den);
+    if (a.n_split == 1) {
+      // no position held: zeros
+      st_elem<DT>(a.out, kvq_out_at(a, row, (j * G + h) * HD + e, HD), den == 0.f ? 0.f : num / den);
+    } else {
+      a.part_o[((rh + h) * a.n_split + split) * HD + e] = num;
+      if (e == 0) {
+        a.part_ml[((rh + h) * a.n_split + split) * 2] = den == 0.f ? -INFINITY : M;
+        a.part_ml[((rh + h) * a.n_split + split) * 2 + 1] = den;
+      }
+    }
   }
+}
+
+// o = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s over the splits of a (row,
+// head), in split order; zeros where none holds a position
+template <int DT, int HD>
+__global__ __launch_bounds__(256) void k_kvq_combine(KvqAttn a) {
+  constexpr int PARTS = 256 / HD;
+  __shared__ float s_w[KVQ_MAX_SPLITS], s_l[KVQ_MAX_SPLITS], s_n[PARTS][HD];
+  const int h = blockIdx.x % a.n_heads, ns = a.n_split;
+  const int64_t row = blockIdx.x / a.n_heads, base = (row * a.n_heads + h) * ns;
+  const int e = threadIdx.x % HD, part = threadIdx.x / HD;
+  for (int s = threadIdx.x; s < ns; s += 256) {
+    s_w[s] = a.part_ml[(base + s) * 2];
+    s_l[s] = a.part_ml[(base + s) * 2 + 1];
+  }
+  __syncthreads();
+  float M = -FLT_MAX;
+  for (int s = 0; s < ns; ++s) M = fmaxf(M, s_w[s]);
+  float num = 0.f, den = 0.f;
+  for (int s = 0; s < ns; ++s) den += __builtin_amdgcn_exp2f(s_w[s] - M) * s_l[s];
+  for (int s = part; s < ns; s += PARTS) num += __builtin_amdgcn_exp2f(s_w[s] - M) * a.part_o[(base + s) * HD + e];
+  s_n[part][e] = num;
+  __syncthreads();
+  if (part) return;
+#pragma unroll
+  for (int p = 1; p < PARTS; ++p) num += s_n[p][e];
+  st_elem<DT>(a.out, kvq_out_at(a, row, h * HD + e, HD), den == 0.f ? 0.f : num / den);
 }
 
 template <int DT, int HD>
@@ -256,17 +575,33 @@ hipError_t kvq_rows_any(int dtype, int hd, const KvqRows &a, bool read, hipStrea
   return hipErrorInvalidValue;
 }
 
+template <int DT, int HD>
+hipError_t kvq_attn_hd(const KvqAttn &a, hipStream_t st) {
+  const int64_t grid = (int64_t)a.n * a.c.n_kv * a.n_split, rows = (int64_t)a.n * a.n_heads;
+  if (grid > INT32_MAX || rows > INT32_MAX || a.n_split > KVQ_MAX_SPLITS) return hipErrorInvalidValue;
+  if ((1 << a.c.bt_log2) >= KVQ_TILE) HS_LAUNCH((k_kvq_attn<DT, HD, 4, true>), dim3((uint32_t)grid), dim3(256), 0, st, a);
+  else HS_LAUNCH((k_kvq_attn<DT, HD, 4, false>), dim3((uint32_t)grid), dim3(256), 0, st, a);
+  if (a.n_split > 1) HS_LAUNCH((k_kvq_combine<DT, HD>), dim3((uint32_t)rows), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
 template <int DT>
 hipError_t kvq_attn_dt(int hd, const KvqAttn &a, hipStream_t st) {
-  const int64_t grid = (int64_t)a.n * a.n_heads;
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
-  if (hd == 64) HS_LAUNCH((k_kvq_attn<DT, 64>), dim3((uint32_t)grid), dim3(256), 0, st, a);
-  else if (hd == 128) HS_LAUNCH((k_kvq_attn<DT, 128>), dim3((uint32_t)grid), dim3(256), 0, st, a);
-  else return hipErrorInvalidValue;
-  return hipGetLastError();
+  if (hd == 64) return kvq_attn_hd<DT, 64>(a, st);
+  if (hd == 128) return kvq_attn_hd<DT, 128>(a, st);
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
+
+void kvq_split_policy(int64_t n, int n_kv, int max_len, int *S, int *n_split) {
+  constexpr int ROUND = 4 * KVQ_TILE;  // one tile for each wave
+  const int64_t pairs = std::max<int64_t>(1, n * n_kv), want = (2048 + pairs - 1) / pairs;
+  const int64_t most = ((int64_t)max_len + ROUND - 1) / ROUND;
+  const int64_t ns = std::max<int64_t>(1, std::min(std::min(want, most), (int64_t)KVQ_MAX_SPLITS));
+  const int64_t s = ((max_len + ns - 1) / ns + ROUND - 1) / ROUND * ROUND;
+  *S = (int)std::min<int64_t>(s, 1 << 30);
+  *n_split = (int)((max_len + s - 1) / s);
+}
 
 hipError_t launch_kvq_append(int dtype, int head_dim, const KvqRows &a, hipStream_t st) {
   return kvq_rows_any(dtype, head_dim, a, false, st);
