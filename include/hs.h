@@ -411,8 +411,8 @@ int hs_kvq_attention(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, in
 
 /* ---- log probabilities of tokens ----
  *
- * For each of `rows` rows of logits (device, `dtype`, vocab elements, rows ld
- * elements apart, aligned to their elements), with M = max x, Z = sum e^(x - M):
+ * For each of `rows` rows of logits (device, `dtype`, vocab elements, 1..2^30, rows
+ * ld elements apart, aligned to their elements), with M = max x, Z = sum e^(x - M):
  *   logprob[r]  = x[tokens[r]] - M - log Z, the log probability of the given
  *                 token (device int32 [rows]); 0 for a negative token (none is
  *                 asked for: a padded batch), NaN for one from vocab on;

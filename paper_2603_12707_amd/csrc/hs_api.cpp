@@ -1388,9 +1388,10 @@ int hs_kvq_attention(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, in
 int hs_token_logprobs_workspace(int64_t rows, int32_t vocab, int32_t top, uint64_t *bytes) {
   static const char *fn = "hs_token_logprobs_workspace";
   if (!bytes) return fail(HS_E_INVALID, "%s: bytes is NULL", fn);
-  if (rows < 0 || rows > INT32_MAX / 64 || vocab <= 0) return fail(HS_E_INVALID, "%s: rows or vocab out of range", fn);
+  if (rows < 0 || rows > INT32_MAX || vocab <= 0 || vocab > (1 << 30)) return fail(HS_E_INVALID, "%s: rows or vocab out of range", fn);
   if (top < 0 || top > 64 || top > vocab) return fail(HS_E_INVALID, "%s: top %d is not in 0..64 or exceeds vocab", fn, top);
-  *bytes = 0;
+  if (rows * logprob_parts(vocab) > INT32_MAX) return fail(HS_E_INVALID, "%s: too many rows", fn);
+  *bytes = logprob_workspace(rows, vocab, top);
   return HS_OK;
 }
 
@@ -1422,6 +1423,8 @@ int hs_token_logprobs(int32_t dtype, const void *logits, int64_t rows, int32_t v
   a.entropy = entropy;
   a.top_ids = top_ids;
   a.top_logprobs = top_logprobs;
+  a.parts = logprob_parts(vocab);
+  a.ws = workspace;
   HIP_TRY(launch_logprobs(dtype, a, (hipStream_t)stream));
   return HS_OK;
 }

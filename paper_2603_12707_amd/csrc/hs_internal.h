@@ -362,7 +362,13 @@ struct LogprobArgs {
   float *logprob, *entropy;
   int *top_ids;
   float *top_logprobs;
+  int parts;  // logprob_parts(vocab)
+  void *ws;   // logprob_workspace bytes
 };
+// a row is cut into parts of this many elements
+constexpr int LOGPROB_PART = 8192;
+inline int logprob_parts(int vocab) { return (int)(((int64_t)vocab + LOGPROB_PART - 1) / LOGPROB_PART); }
+uint64_t logprob_workspace(int64_t rows, int vocab, int top);
 hipError_t launch_logprobs(int dtype, const LogprobArgs &a, hipStream_t st);
 
 // records the thread's error message (hs_last_error) and returns code
