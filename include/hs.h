@@ -409,6 +409,19 @@ int hs_kvq_attention(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, in
                      float scale, void *out, int64_t ld_out, void *workspace, uint64_t workspace_bytes,
                      hs_stream_t stream);
 
+/* A pooled cache (hs_kv_pool_create) held in 4 bits: the same handle, calls and
+ * rules, over blocks of hs_kvq_block_bytes(n_layers, n_kv_heads, head_dim,
+ * block_tokens) bytes in the layout above.  What a step or a prefill pass stores
+ * is rounded as hs_kvq_append does, and every attention, a prompt's own rows
+ * among themselves too, sees the stored values.  hs_kv_write rounds its rows,
+ * hs_kv_read gives the stored values.  The handle owns, besides its metadata,
+ * room for one layer's new rows of a prefill pass in the model dtype,
+ * 2 * n_kv_heads * head_dim elements for each of max(max_batch, max_ctx, slots)
+ * rows (or what hs_model_reserve_rows had set when the handle was created, which
+ * then bounds its passes). */
+int hs_kvq_pool_create(hs_model *m, int32_t slots, int32_t block_tokens, void *dev_buf, uint64_t buf_bytes,
+                       hs_kv **out);
+
 /* ---- log probabilities of tokens ----
  *
  * For each of `rows` rows of logits (device, `dtype`, vocab elements, 1..2^30, rows
@@ -429,6 +442,16 @@ int hs_token_logprobs_workspace(int64_t rows, int32_t vocab, int32_t top, uint64
 int hs_token_logprobs(int32_t dtype, const void *logits, int64_t rows, int32_t vocab, int64_t ld,
                       const int32_t *tokens, int32_t top, float *logprob, float *entropy, int32_t *top_ids,
                       float *top_logprobs, void *workspace, uint64_t workspace_bytes, hs_stream_t stream);
+
+/* hs_decode_step with the log probabilities of its logits, as hs_token_logprobs
+ * gives them: of the tokens in targets (device int32, indexed like tokens_in;
+ * NULL: of the tokens that the step chooses), the entropy and the `top`
+ * alternatives.  logprob, entropy, top_ids and top_logprobs have a row for each
+ * decoded request, in the order of the logits' rows; each may be NULL.  Feeding a
+ * given text's tokens and asking for each next one scores the text. */
+int hs_decode_step_logprobs(hs_model *m, hs_kv *kv, const int32_t *tokens_in, int32_t *tokens_out,
+                            const int32_t *targets, int32_t top, float *logits, float *hidden_out, float *logprob,
+                            float *entropy, int32_t *top_ids, float *top_logprobs, hs_stream_t stream);
 
 /* Reads and clears the device-side flags.  Synchronises the device.
  *   bit 0 (1): a token id outside [0, vocab) was replaced by 0;

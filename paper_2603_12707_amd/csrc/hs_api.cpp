@@ -110,6 +110,19 @@ KvRef kv_ref(const hs_kv *kv) {
                kv->d_len, kv->d_act,  kv->batch,  kv->ntab, kv->pool ? 1 : 0};
 }
 
+// where the q/k/v projection puts new rows of a pool held in 4 bits: decode,
+// slot r's one row; prefill, the pass's rows (launch_kvq_stage)
+KvRef stage_ref(const hs_kv *kv, bool prefill) {
+  const int *bt = prefill ? kv->d_pstage.bt : kv->d_one;
+  return KvRef{kv->stage, prefill ? kv->d_pstage.start : kv->d_sbase, kv->d_ident, bt, bt, kv->d_zero, kv->d_act,
+               kv->batch, kv->batch, 1};
+}
+
+KvqRef kvq_ref(const hs_kv *kv, int layer) {
+  return KvqRef{(uint8_t *)kv->buf, kv->n_blocks,  kv->block_bytes, kv->d_base, kv->batch, kv->max_blocks,
+                __builtin_ctz(kv->block_tokens), kv->m->cfg.n_kv_heads, layer};
+}
+
 KvPool kv_pool(const hs_kv *kv) {
   return KvPool{kv->d_base, kv->d_toff,  kv->d_cap, kv->d_len,   kv->d_rope,       kv->d_ready,
                 kv->d_nblk, kv->d_stack, kv->d_top, kv->m->status, kv->d_act, kv->block_tokens,
@@ -150,7 +163,7 @@ hipError_t rebuild_active(hs_kv *kv, hipStream_t st) {
 void free_model(hs_model *m) {
   if (!m) return;
   void *ptrs[] = {m->x,      m->q,      m->attn,    m->act,      m->hnorm,  m->splitk, m->xlast,
-                  m->pk_dev, m->pk_order, m->logits, m->part_o, m->part_ml, m->rope_tab, m->status};
+                  m->pk_dev, m->pk_order, m->lp_ws, m->logits, m->part_o, m->part_ml, m->rope_tab, m->status};
   for (void *p : ptrs)
     if (p) (void)hipFree(p);
   delete m;
@@ -231,8 +244,8 @@ struct Step {
     g.head_dim = c.head_dim;
     g.n_heads = c.n_heads;
     g.n_kv = c.n_kv_heads;
-    g.kv = kv_ref(kv);
-    g.layer = l;
+    g.kv = kv->quant ? stage_ref(kv, prefill) : kv_ref(kv);
+    g.layer = kv->quant ? 0 : l;
     g.prefill = prefill;
     g.pk = m->pk_dev;
     g.rope_pos = rope_pos;
@@ -245,7 +258,69 @@ struct Step {
     g.status = m->status;
     g.splitk_ws = ws.splitk;
     g.splitk_cap = ws.splitk_floats;
-    return launch_gemm(c.dtype, PRO_NORM, kv->pool ? EPI_QKV_PAGED : EPI_QKV, g, st);
+    const hipError_t e = launch_gemm(c.dtype, PRO_NORM, kv->pool ? EPI_QKV_PAGED : EPI_QKV, g, st);
+    return e == hipSuccess && kv->quant ? store_quant(l) : e;
+  }
+
+  // A pool held in 4 bits: the staged rows of the layer go to their places.  In
+  // prefill the staged rows become what the cache holds, so that every
+  // attention, a prompt's own too, sees the same keys and values.
+  hipError_t store_quant(int l) const {
+    const hs_config &c = m->cfg;
+    const int64_t hd = c.head_dim, plane = (prefill ? ncols : 1) * hd * c.n_kv_heads;  // from K to V
+    KvqRows a{};
+    a.c = kvq_ref(kv, l);
+    a.n = ncols;
+    a.heads = c.n_kv_heads;
+    a.sel = a.seq = -1;
+    a.k = kv->stage;
+    a.v = (const uint16_t *)kv->stage + plane;
+    if (prefill) {
+      a.ld = hd;
+      a.ld_head = ncols * hd;
+      a.seqs = kv->d_pstage.seqs;
+      a.pos = kv->d_pstage.pos;
+      a.k_out = kv->stage;
+      a.v_out = (uint16_t *)kv->stage + plane;
+    } else {
+      // slot act[column]'s row, at its length
+      a.ld = 2 * plane;
+      a.ld_head = hd;
+      a.seqs = kv->d_act;
+      a.row_by_seq = 1;
+      a.pos = kv->d_len;
+      a.pos_by_seq = 1;
+      a.cap = kv->d_cap;
+    }
+    return launch_kvq_append(c.dtype, c.head_dim, a, st);
+  }
+
+  // decode attention over a pool held in 4 bits
+  KvqAttn kvq_attn_args(int l) const {
+    const AttnArgs b = attn_args(l);
+    KvqAttn a{};
+    a.c = kvq_ref(kv, l);
+    a.q = b.q;
+    a.ld_q = b.ld_q;
+    a.n = ncols;
+    a.n_heads = b.n_heads;
+    a.seqs = kv->d_act;
+    a.lens = kv->d_len;
+    a.cap = kv->d_cap;
+    a.len_by_seq = 1;
+    a.len_add = 1;
+    a.max_len = kv->max_cap;
+    a.scale = b.scale;
+    a.out = b.out;
+    a.ld_out = b.ld_q;
+    a.out_packed = b.out_packed;
+    a.order = b.order;
+    a.S = S;
+    a.n_split = n_split;
+    a.part_o = b.part_o;
+    a.part_ml = b.part_ml;
+    a.nat = 1;
+    return a;
   }
 
   AttnArgs attn_args(int l) const {
@@ -253,8 +328,8 @@ struct Step {
     AttnArgs a{};
     a.q = ws.q;
     a.ld_q = c.n_heads * c.head_dim;
-    a.kv = kv_ref(kv);
-    a.layer = l;
+    a.kv = kv->quant ? stage_ref(kv, prefill) : kv_ref(kv);
+    a.layer = kv->quant ? 0 : l;
     a.n_heads = c.n_heads;
     a.n_kv = c.n_kv_heads;
     a.prefill = prefill;
@@ -280,6 +355,7 @@ struct Step {
     const hs_config &c = m->cfg;
     if (prefill && attn_prefill_on_mma(c.dtype))
       return launch_attention_prefill(c.dtype, c.head_dim, c.n_heads / c.n_kv_heads, ncols, attn_args(l), st);
+    if (kv->quant) return launch_kvq_attention(c.dtype, c.head_dim, kvq_attn_args(l), st);
     return launch_attention(c.dtype, c.head_dim, c.n_heads / c.n_kv_heads, ncols, attn_args(l), st);
   }
 
@@ -466,13 +542,14 @@ int prefill_requests(hs_model *m, hs_kv *kv, int n, const int32_t *reqs, const v
   const int b = dtype_bytes(c.dtype);
   // without a caller logits buffer, a pass's logits go to the [max_batch][V] workspace
   const int max_np = last_logits ? PACK_MAX : std::min(PACK_MAX, m->max_batch);
+  const int64_t room = kv->quant ? std::min(m->rows, kv->stage_rows) : m->rows;
   int64_t voff = 0, toff = 0, roff = 0;
   for (int i0 = 0; i0 < n;) {
     PackedRows pk{};
     int rows = 0;
     while (i0 + pk.n < n && pk.n < max_np) {
       const int k = i0 + pk.n, s_ctx = kv->n_v[reqs[k]] + s_text[k];
-      if (pk.n > 0 && rows + s_ctx > m->rows) break;  // one request always fits (s_ctx <= max_ctx <= rows)
+      if (pk.n > 0 && rows + s_ctx > room) break;  // one request always fits (s_ctx <= max_ctx <= rows)
       pk.req[pk.n] = reqs[k];
       pk.cu[pk.n] = rows;
       rows += s_ctx;
@@ -483,6 +560,7 @@ int prefill_requests(hs_model *m, hs_kv *kv, int n, const int32_t *reqs, const v
     for (int k = 0; k < pk.n; ++k) pk.vis[k + 1] = pk.vis[k] + kv->n_v[pk.req[k]];
     const KvPool pool = kv_pool(kv);  // takes the blocks for the pass's contexts
     HIP_TRY(launch_prefill_begin(pk, m->pk_dev, m->pk_order, kv->pool ? &pool : nullptr, st));
+    if (kv->quant) HIP_TRY(launch_kvq_stage(pk, c.head_dim, kv->d_pstage, st));
     HIP_TRY(launch_prefill_rows(c.dtype, (const char *)emb + voff * c.d_model * b, m->w.embed, c.vocab, c.d_model,
                                 text_ids + toff, m->pk_dev, rows, m->x, m->status, st));
     voff += pk.vis[pk.n];
@@ -636,6 +714,7 @@ int hs_model_create(const hs_config *cfg, const hs_weights *w, int32_t max_batch
       {(void **)&m->xlast, (size_t)PACK_MAX * c.d_model * 4},
       {(void **)&m->pk_dev, sizeof(PackedRows)},
       {(void **)&m->pk_order, (size_t)prefill_groups_max(rows) * sizeof(PrefillGroup)},
+      {&m->lp_ws, w->lm_head ? (size_t)logprob_workspace(max_batch, c.vocab, LOGPROB_TOP) : 0},
       {(void **)&m->logits, w->lm_head ? (size_t)max_batch * c.vocab * 4 : 0},
       {(void **)&m->part_o, (size_t)std::max<int64_t>(entries, 1) * hd * 4},
       {(void **)&m->part_ml, (size_t)std::max<int64_t>(entries, 1) * 2 * 4},
@@ -754,29 +833,37 @@ int hs_kv_alloc(hs_model *m, int32_t batch, const int32_t *n_v, const int32_t *c
 int hs_kv_free(hs_kv *kv) {
   if (!kv) return fail(HS_E_INVALID, "hs_kv_free: NULL");
   void *ptrs[] = {kv->d_base,  kv->d_cap,   kv->d_len,  kv->d_rope, kv->d_toff, kv->d_act, kv->d_order,
-                  kv->d_ready, kv->d_stack, kv->d_top, kv->d_nblk, kv->d_bt == kv->d_cap ? nullptr : kv->d_bt};
+                  kv->d_ready, kv->d_stack, kv->d_top, kv->d_nblk, kv->d_bt == kv->d_cap ? nullptr : kv->d_bt,
+                  kv->stage,   kv->d_sbase, kv->d_pstage.start, kv->d_pstage.bt, kv->d_pstage.seqs, kv->d_pstage.pos,
+                  kv->d_ident, kv->d_one,   kv->d_zero};
   for (void *p : ptrs)
     if (p) (void)hipFree(p);
   delete kv;
   return HS_OK;
 }
 
-int hs_kv_pool_create(hs_model *m, int32_t slots, int32_t block_tokens, void *dev_buf, uint64_t buf_bytes,
-                      hs_kv **out) {
-  if (!out) return fail(HS_E_INVALID, "hs_kv_pool_create: out is NULL");
+// a pool in the model dtype, or held in 4 bits (quant)
+static int pool_create(hs_model *m, int32_t slots, int32_t block_tokens, void *dev_buf, uint64_t buf_bytes, bool quant,
+                       hs_kv **out, const char *fn) {
+  if (!out) return fail(HS_E_INVALID, "%s: out is NULL", fn);
   *out = nullptr;
-  if (!m || !dev_buf) return fail(HS_E_INVALID, "hs_kv_pool_create: NULL argument");
+  if (!m || !dev_buf) return fail(HS_E_INVALID, "%s: NULL argument", fn);
   const hs_config &c = m->cfg;
-  if (c.dtype == HS_F32) return fail(HS_E_INVALID, "hs_kv_pool_create: pooled caches take 16-bit storage");
-  if (slots <= 0 || slots > 4096) return fail(HS_E_INVALID, "hs_kv_pool_create: slots must be in 1..4096");
+  if (c.dtype == HS_F32) return fail(HS_E_INVALID, "%s: pooled caches take 16-bit storage", fn);
+  if (slots <= 0 || slots > 4096) return fail(HS_E_INVALID, "%s: slots must be in 1..4096", fn);
   if (block_tokens < POOL_SPAN || block_tokens > 16384 || (block_tokens & (block_tokens - 1)))
-    return fail(HS_E_INVALID, "hs_kv_pool_create: block_tokens must be a power of two in 256..16384");
-  if (((uintptr_t)dev_buf) % 16) return fail(HS_E_INVALID, "hs_kv_pool_create: buffer must be 16-byte aligned");
-  const int64_t block_elems = kv_request_elems(c, block_tokens);
-  const uint64_t block_bytes = (uint64_t)block_elems * dtype_bytes(c.dtype);
+    return fail(HS_E_INVALID, "%s: block_tokens must be a power of two in 256..16384", fn);
+  if (((uintptr_t)dev_buf) % 16) return fail(HS_E_INVALID, "%s: buffer must be 16-byte aligned", fn);
+  // the table holds the blocks' first elements, or (4 bits) their numbers
+  const int64_t block_elems = quant ? 1 : kv_request_elems(c, block_tokens);
+  uint64_t block_bytes = (uint64_t)block_elems * dtype_bytes(c.dtype);
+  if (quant) {
+    const int rc = hs_kvq_block_bytes(c.n_layers, c.n_kv_heads, c.head_dim, block_tokens, &block_bytes);
+    if (rc) return rc;
+  }
   const uint64_t n_blocks = buf_bytes / block_bytes;
   if (n_blocks < 1 || n_blocks > (1u << 30))
-    return fail(HS_E_BUFFER, "hs_kv_pool_create: buffer holds %llu blocks of %llu bytes",
+    return fail(HS_E_BUFFER, "%s: buffer holds %llu blocks of %llu bytes", fn,
                 (unsigned long long)n_blocks, (unsigned long long)block_bytes);
   // attention partials for the block-aligned splits: a pooled split is the
   // unpooled one rounded up to whole POOL_SPANs, so it never needs more
@@ -786,11 +873,11 @@ int hs_kv_pool_create(hs_model *m, int32_t slots, int32_t block_tokens, void *de
     int S, ns;
     kv_split_policy(c, true, nq, m->max_ctx, &S, &ns);
     if (ns > 1 && (int64_t)nq * c.n_heads * ns > m->part_entries)
-      return fail(HS_E_INVALID, "hs_kv_pool_create: %d queries x %d splits exceed the model's attention workspace",
+      return fail(HS_E_INVALID, "%s: %d queries x %d splits exceed the model's attention workspace", fn,
                   nq, ns);
   }
   hs_kv *kv = new (std::nothrow) hs_kv();
-  if (!kv) return fail(HS_E_DEVICE, "hs_kv_pool_create: out of host memory");
+  if (!kv) return fail(HS_E_DEVICE, "%s: out of host memory", fn);
   kv->m = m;
   kv->batch = slots;
   kv->buf = dev_buf;
@@ -809,6 +896,8 @@ int hs_kv_pool_create(hs_model *m, int32_t slots, int32_t block_tokens, void *de
   kv->ready.assign(slots, 0);
   kv->nblk.assign(slots, 0);
   kv->n_active = 0;
+  kv->quant = quant;
+  kv->block_bytes = (int64_t)block_bytes;
   std::vector<int64_t> tab(kv->ntab, -1);
   std::vector<int> toff(slots), bt(slots, block_tokens), stack(n_blocks);
   for (int i = 0; i < slots; ++i) toff[i] = i * kv->max_blocks;
@@ -831,12 +920,44 @@ int hs_kv_pool_create(hs_model *m, int32_t slots, int32_t block_tokens, void *de
        hipMemset(kv->d_rope, 0, sb) == hipSuccess && hipMemset(kv->d_act, 0, sb) == hipSuccess &&
        hipMemset(kv->d_order, 0, sb) == hipSuccess &&
        hipMemset(kv->d_ready, 0, sb) == hipSuccess && hipMemset(kv->d_nblk, 0, sb) == hipSuccess;
+  if (ok && quant) {
+    const int64_t row = 2ll * c.n_kv_heads * c.head_dim;  // elements staged for a row
+    kv->stage_rows = std::max<int64_t>(m->rows, slots);
+    std::vector<int64_t> base(slots);
+    std::vector<int> ident(slots), one(slots, 1);
+    for (int i = 0; i < slots; ++i) {
+      base[i] = i * row;
+      ident[i] = i;
+    }
+    ok = hipMalloc(&kv->stage, (size_t)(kv->stage_rows * row) * dtype_bytes(c.dtype)) == hipSuccess &&
+         hipMalloc(&kv->d_sbase, (size_t)slots * 8) == hipSuccess &&
+         hipMalloc(&kv->d_pstage.start, (size_t)slots * 8) == hipSuccess &&
+         hipMalloc(&kv->d_pstage.bt, sb) == hipSuccess &&
+         hipMalloc(&kv->d_pstage.seqs, (size_t)kv->stage_rows * 4) == hipSuccess &&
+         hipMalloc(&kv->d_pstage.pos, (size_t)kv->stage_rows * 4) == hipSuccess &&
+         hipMalloc(&kv->d_ident, sb) == hipSuccess && hipMalloc(&kv->d_one, sb) == hipSuccess &&
+         hipMalloc(&kv->d_zero, sb) == hipSuccess;
+    ok = ok && hipMemcpy(kv->d_sbase, base.data(), (size_t)slots * 8, hipMemcpyHostToDevice) == hipSuccess &&
+         hipMemcpy(kv->d_ident, ident.data(), sb, hipMemcpyHostToDevice) == hipSuccess &&
+         hipMemcpy(kv->d_one, one.data(), sb, hipMemcpyHostToDevice) == hipSuccess &&
+         hipMemset(kv->d_zero, 0, sb) == hipSuccess;
+  }
   if (!ok) {
     hs_kv_free(kv);
-    return fail(HS_E_DEVICE, "hs_kv_pool_create: metadata allocation failed");
+    return fail(HS_E_DEVICE, "%s: metadata allocation failed", fn);
   }
   *out = kv;
   return HS_OK;
+}
+
+int hs_kv_pool_create(hs_model *m, int32_t slots, int32_t block_tokens, void *dev_buf, uint64_t buf_bytes,
+                      hs_kv **out) {
+  return pool_create(m, slots, block_tokens, dev_buf, buf_bytes, false, out, "hs_kv_pool_create");
+}
+
+int hs_kvq_pool_create(hs_model *m, int32_t slots, int32_t block_tokens, void *dev_buf, uint64_t buf_bytes,
+                       hs_kv **out) {
+  return pool_create(m, slots, block_tokens, dev_buf, buf_bytes, true, out, "hs_kvq_pool_create");
 }
 
 int hs_kv_admit(hs_kv *kv, int32_t slot, int32_t n_v, int32_t capacity, hs_stream_t stream) {
@@ -938,9 +1059,11 @@ int hs_model_reserve_rows(hs_model *m, int64_t rows) {
 }
 
 // One decode step (hs_decode_step); ovr, when given, replaces the model's
-// workspaces as the step's scratch.
+// workspaces as the step's scratch; lp, when given, asks for log probabilities
+// (its outputs, top and given tokens; tokens NULL: the chosen ones).
 static int decode_impl(hs_model *m, hs_kv *kv, const int32_t *tokens_in, int32_t *tokens_out, float *logits,
-                       float *hidden_out, hs_stream_t stream, const StepWs *ovr, const char *fn) {
+                       float *hidden_out, hs_stream_t stream, const StepWs *ovr, const char *fn,
+                       const LogprobArgs *lp = nullptr) {
   if (!kv_matches(kv, m)) return fail(HS_E_INVALID, "%s: model/handle mismatch", fn);
   if (!tokens_in) return fail(HS_E_INVALID, "%s: tokens_in is NULL", fn);
   const hs_config &c = m->cfg;
@@ -970,6 +1093,18 @@ static int decode_impl(hs_model *m, hs_kv *kv, const int32_t *tokens_in, int32_t
     float *lg = logits ? logits : step.ws.logits;
     HIP_TRY(step.head(step.ws.x, lg, pend));
     HIP_TRY(launch_argmax(lg, c.vocab, c.vocab, B, tokens_out, act, kv->d_len, kv->d_rope, 1, st));
+    if (lp) {
+      LogprobArgs a = *lp;
+      a.logits = lg;
+      a.rows = B;
+      a.ld = c.vocab;
+      a.vocab = c.vocab;
+      if (!a.tokens) a.tokens = tokens_out;
+      a.act = act;
+      a.parts = logprob_parts(c.vocab);
+      a.ws = m->lp_ws;
+      HIP_TRY(launch_logprobs(HS_F32, a, st));
+    }
   } else {
     if (pend) HIP_TRY(launch_resid_pending((const double *)step.ws.splitk, pend, B, c.d_model, step.ws.x, st));
     HIP_TRY(launch_advance(kv->d_len, kv->d_rope, act, B, st));
@@ -990,6 +1125,24 @@ static int decode_impl(hs_model *m, hs_kv *kv, const int32_t *tokens_in, int32_t
 int hs_decode_step(hs_model *m, hs_kv *kv, const int32_t *tokens_in, int32_t *tokens_out, float *logits,
                    float *hidden_out, hs_stream_t stream) {
   return decode_impl(m, kv, tokens_in, tokens_out, logits, hidden_out, stream, nullptr, "hs_decode_step");
+}
+
+int hs_decode_step_logprobs(hs_model *m, hs_kv *kv, const int32_t *tokens_in, int32_t *tokens_out,
+                            const int32_t *targets, int32_t top, float *logits, float *hidden_out, float *logprob,
+                            float *entropy, int32_t *top_ids, float *top_logprobs, hs_stream_t stream) {
+  static const char *fn = "hs_decode_step_logprobs";
+  if (!kv_matches(kv, m)) return fail(HS_E_INVALID, "%s: model/handle mismatch", fn);
+  if (!m->w.lm_head) return fail(HS_E_STATE, "%s: model has no LM head", fn);
+  if (top < 0 || top > LOGPROB_TOP || top > m->cfg.vocab)
+    return fail(HS_E_INVALID, "%s: top %d is not in 0..%d or exceeds vocab", fn, top, LOGPROB_TOP);
+  LogprobArgs lp{};
+  lp.top = top;
+  lp.tokens = targets;
+  lp.logprob = logprob;
+  lp.entropy = entropy;
+  lp.top_ids = top_ids;
+  lp.top_logprobs = top_logprobs;
+  return decode_impl(m, kv, tokens_in, tokens_out, logits, hidden_out, stream, nullptr, fn, &lp);
 }
 
 // ---- the decode step with its scratch in a static device array ----
@@ -1160,12 +1313,47 @@ static int kv_slabs(const hs_kv *kv, int32_t req, int32_t layer, int32_t kv_sel,
   return HS_OK;
 }
 
+// hs_kv_write / hs_kv_read of a pool held in 4 bits, whose places kv_slabs has
+// checked: through a buffer of rows, as the kernels take aligned ones
+static int kvq_copy(const hs_kv *kv, int32_t req, int32_t layer, int32_t kv_sel, int32_t head, int32_t pos0, int32_t n,
+                    void *rows, int32_t is_device, bool write) {
+  if (n == 0) return HS_OK;
+  const hs_config &c = kv->m->cfg;
+  const size_t bytes = (size_t)n * c.head_dim * dtype_bytes(c.dtype);
+  void *tmp = nullptr;
+  if (hipMalloc(&tmp, bytes) != hipSuccess) return fail(HS_E_DEVICE, "kv copy: hipMalloc of %zu bytes failed", bytes);
+  KvqRows a{};
+  a.c = kvq_ref(kv, layer);
+  a.n = n;
+  a.head0 = head;
+  a.heads = 1;
+  a.sel = kv_sel;
+  a.seq = req;
+  a.pos0 = pos0;
+  a.ld = a.ld_head = c.head_dim;
+  hipError_t e;
+  if (write) {
+    a.k = a.v = tmp;
+    e = hipMemcpy(tmp, rows, bytes, is_device ? hipMemcpyDeviceToDevice : hipMemcpyHostToDevice);
+    if (e == hipSuccess) e = launch_kvq_append(c.dtype, c.head_dim, a, nullptr);
+  } else {
+    a.k_out = a.v_out = tmp;
+    e = launch_kvq_read(c.dtype, c.head_dim, a, nullptr);
+    if (e == hipSuccess) e = hipMemcpy(rows, tmp, bytes, is_device ? hipMemcpyDeviceToDevice : hipMemcpyDeviceToHost);
+  }
+  if (e == hipSuccess) e = hipDeviceSynchronize();
+  (void)hipFree(tmp);
+  if (e != hipSuccess) return fail(HS_E_DEVICE, "kv copy: %s", hipGetErrorString(e));
+  return HS_OK;
+}
+
 int hs_kv_write(hs_kv *kv, int32_t req, int32_t layer, int32_t kv_sel, int32_t head, int32_t pos0, int32_t n,
                 const void *src, int32_t src_is_device) {
   std::vector<std::pair<int64_t, size_t>> slabs;
   int rc = kv_slabs(kv, req, layer, kv_sel, head, pos0, n, src, &slabs);
   if (rc) return rc;
   HIP_TRY(hipDeviceSynchronize());
+  if (kv->quant) return kvq_copy(kv, req, layer, kv_sel, head, pos0, n, const_cast<void *>(src), src_is_device, true);
   size_t done = 0;
   for (auto &sl : slabs) {
     HIP_TRY(hipMemcpy((char *)kv->buf + sl.first, (const char *)src + done, sl.second,
@@ -1182,6 +1370,7 @@ int hs_kv_read(const hs_kv *kv, int32_t req, int32_t layer, int32_t kv_sel, int3
   int rc = kv_slabs(kv, req, layer, kv_sel, head, pos0, n, dst, &slabs);
   if (rc) return rc;
   HIP_TRY(hipDeviceSynchronize());
+  if (kv->quant) return kvq_copy(kv, req, layer, kv_sel, head, pos0, n, dst, dst_is_device, false);
   size_t done = 0;
   for (auto &sl : slabs) {
     HIP_TRY(hipMemcpy((char *)dst + done, (const char *)kv->buf + sl.first, sl.second,
@@ -1299,6 +1488,8 @@ int hs_kvq_append(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, int32
   if (!k_values != !v_values) return fail(HS_E_INVALID, "%s: k_values and v_values are given together", fn);
   if (((uintptr_t)k_values | (uintptr_t)v_values) % 16) return fail(HS_E_INVALID, "%s: rows must be 16-byte aligned", fn);
   a.n = n;
+  a.heads = cache->n_kv_heads;
+  a.sel = a.seq = -1;
   a.k = k;
   a.v = v;
   a.k_out = k_values;
@@ -1318,6 +1509,8 @@ int hs_kvq_read(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, int32_t
   const int rc = kvq_rows_args(cache, layer, dtype, n, k, v, ld, ld_head, positions, fn, &a.c);
   if (rc || n == 0) return rc;
   a.n = n;
+  a.heads = cache->n_kv_heads;
+  a.sel = a.seq = -1;
   a.k_out = k;
   a.v_out = v;
   a.ld = ld;
@@ -1380,6 +1573,7 @@ int hs_kvq_attention(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, in
   a.out = out;
   a.ld_out = ld_out;
   HIP_TRY(launch_kvq_attention(dtype, cache->head_dim, a, (hipStream_t)stream));
+  HIP_TRY(launch_kvq_combine(dtype, cache->head_dim, a, (hipStream_t)stream));
   return HS_OK;
 }
 
@@ -1389,7 +1583,8 @@ int hs_token_logprobs_workspace(int64_t rows, int32_t vocab, int32_t top, uint64
   static const char *fn = "hs_token_logprobs_workspace";
   if (!bytes) return fail(HS_E_INVALID, "%s: bytes is NULL", fn);
   if (rows < 0 || rows > INT32_MAX || vocab <= 0 || vocab > (1 << 30)) return fail(HS_E_INVALID, "%s: rows or vocab out of range", fn);
-  if (top < 0 || top > 64 || top > vocab) return fail(HS_E_INVALID, "%s: top %d is not in 0..64 or exceeds vocab", fn, top);
+  if (top < 0 || top > LOGPROB_TOP || top > vocab)
+    return fail(HS_E_INVALID, "%s: top %d is not in 0..%d or exceeds vocab", fn, top, LOGPROB_TOP);
   if (rows * logprob_parts(vocab) > INT32_MAX) return fail(HS_E_INVALID, "%s: too many rows", fn);
   *bytes = logprob_workspace(rows, vocab, top);
   return HS_OK;

@@ -316,17 +316,20 @@ struct KvqRef {
 // bytes of one layer's K or V of one head in a block of bt positions
 inline int64_t kvq_slab_bytes(int bt, int hd) { return (int64_t)bt * hd / 32 * 17; }
 // Rows to store or fetch: element (row, head, e) of K sits at k + row * ld +
-// head * ld_head + e, V alike.  Row r goes to sequence seqs[r] (NULL: r) and
-// position pos[r] (pos_by_seq: pos[sequence]); past cap[sequence], if given, it
-// is not stored.
+// head * ld_head + e, V alike, for the heads head0 .. head0 + heads - 1 and both
+// K and V (sel < 0) or one of them.  Row r goes to sequence seqs[r] (NULL: r, or
+// seq if that is not negative) and position pos[r] (pos_by_seq: pos[sequence];
+// NULL: pos0 + r); from cap[sequence] on, if given, it is not stored.
 struct KvqRows {
   KvqRef c;
   int n;
+  int head0, heads, sel, seq, pos0;
   const void *k, *v;     // append
   void *k_out, *v_out;   // append: the values stored, or NULL; read: the rows
   int64_t ld, ld_head;
   const int *seqs, *pos, *cap;
   int pos_by_seq;
+  int row_by_seq;        // row r's elements are those of row seqs[r] of k and v
 };
 // Row r of q attends over the first len positions of sequence seqs[r] (NULL:
 // r); len = lens[r] or (len_by_seq) lens[sequence], plus len_add, at most max_len
@@ -344,7 +347,9 @@ struct KvqAttn {
   const int *order;  // the z-th row to be started is order[z]; NULL: z
   int S, n_split;    // positions per split (a multiple of 256), splits
   float *part_o;     // [n][n_heads][n_split][head_dim]
-  float *part_ml;    // [n][n_heads][n_split][2]: maximum (base-2 units; -inf: no position), sum
+  float *part_ml;    // [n][n_heads][n_split][2]: maximum (-inf: no position), sum
+  int nat;           // maxima in units of the natural exponent, as AttnArgs has them, not of the base-2 one
+  int out_packed;    // out in the packed activation layout
 };
 constexpr int KVQ_MAX_SPLITS = 256;
 // positions per split and splits for n rows of at most max_len positions
@@ -352,13 +357,24 @@ void kvq_split_policy(int64_t n, int n_kv, int max_len, int *S, int *n_split);
 hipError_t launch_kvq_append(int dtype, int head_dim, const KvqRows &a, hipStream_t st);
 hipError_t launch_kvq_read(int dtype, int head_dim, const KvqRows &a, hipStream_t st);
 hipError_t launch_kvq_attention(int dtype, int head_dim, const KvqAttn &a, hipStream_t st);
+// joins the splits (base-2 maxima); nothing with a single one
+hipError_t launch_kvq_combine(int dtype, int head_dim, const KvqAttn &a, hipStream_t st);
+// The places of a prefill pass's rows (seqs, pos [rows]), and the start and
+// the block size of its requests in a buffer [K|V][n_kv][rows][head_dim] that
+// holds them back to back.
+struct KvqStage {
+  int64_t *start;
+  int *bt;
+  int *seqs, *pos;
+};
+hipError_t launch_kvq_stage(const PackedRows &pk, int head_dim, const KvqStage &s, hipStream_t st);
 
 // log probabilities of rows of logits (hs_token_logprobs)
 struct LogprobArgs {
   const void *logits;
   int64_t rows, ld;
   int vocab, top;
-  const int *tokens;
+  const int *tokens, *act;  // row r's given token: tokens[act[r]] (act NULL: [r])
   float *logprob, *entropy;
   int *top_ids;
   float *top_logprobs;
@@ -367,6 +383,7 @@ struct LogprobArgs {
 };
 // a row is cut into parts of this many elements
 constexpr int LOGPROB_PART = 8192;
+constexpr int LOGPROB_TOP = 64;  // most alternatives
 inline int logprob_parts(int vocab) { return (int)(((int64_t)vocab + LOGPROB_PART - 1) / LOGPROB_PART); }
 uint64_t logprob_workspace(int64_t rows, int vocab, int top);
 hipError_t launch_logprobs(int dtype, const LogprobArgs &a, hipStream_t st);
@@ -395,6 +412,7 @@ struct hs_model {
   float *xlast = nullptr;   // [PACK_MAX][d] last rows of the requests of a prefill pass
   hs::PackedRows *pk_dev = nullptr;  // the rows of the current prefill pass
   hs::PrefillGroup *pk_order = nullptr;  // [prefill_groups_max(max_rows)] its attention groups, longest first
+  void *lp_ws = nullptr;    // logprob_workspace(max_batch, V, LOGPROB_TOP)
   float *logits = nullptr;  // [max_batch][V] (used when the caller passes no logits buffer)
   float *part_o = nullptr;
   float *part_ml = nullptr;
@@ -424,4 +442,14 @@ struct hs_kv {
   int *d_stack = nullptr, *d_top = nullptr, *d_nblk = nullptr;
   std::vector<int> nblk;     // blocks held per request (host mirror)
   std::vector<int> act_host; // decode columns' requests (host mirror of d_act)
+  // a pool held in 4 bits (handles from hs_kvq_pool_create): block numbers in
+  // the table.  The q/k/v projection writes one layer's new rows to `stage`, in
+  // the model dtype: in a decode step slot r's [K|V][n_kv][head_dim] at start
+  // d_sbase[r]; in a prefill pass [K|V][n_kv][rows][head_dim] (d_pstage)
+  bool quant = false;
+  int64_t block_bytes = 0, stage_rows = 0;
+  void *stage = nullptr;
+  int64_t *d_sbase = nullptr;
+  int *d_ident = nullptr, *d_one = nullptr, *d_zero = nullptr;  // [slots]: r, 1, 0
+  hs::KvqStage d_pstage{};
 };

@@ -91,7 +91,7 @@ __device__ __forceinline__ void st8(void *p, const float *f) {
 
 // element c of row's output
 __device__ __forceinline__ int64_t kvq_out_at(const KvqAttn &a, int64_t row, int c, int hd) {
-  return row * a.ld_out + c;
+  return a.out_packed ? packed_x_index((int)row, c, (a.n_heads * hd / 8 + 15) / 16) : row * a.ld_out + c;
 }
 
 // row's positions
@@ -121,6 +121,12 @@ __device__ __forceinline__ uint8_t *kvq_span(const KvqRef &c, int hd, int64_t id
          ((((int64_t)(c.layer * 2 + sel) * c.n_kv + head) << (c.bt_log2 - 4)) + (in >> 4)) * kvq_span_bytes(hd);
 }
 
+// row's sequence and position
+__device__ __forceinline__ void kvq_place(const KvqRows &a, int row, int &seq, int &pos) {
+  seq = a.seqs ? a.seqs[row] : a.seq >= 0 ? a.seq : row;
+  pos = !a.pos ? a.pos0 + row : !a.pos_by_seq ? a.pos[row] : (uint32_t)seq < (uint32_t)a.c.n_seqs ? a.pos[seq] : -1;
+}
+
 // One thread takes eight elements of a row of K or V.
 template <int DT, int HD>
 __global__ __launch_bounds__(256) void k_kvq_append(KvqRows a) {
@@ -128,20 +134,21 @@ __global__ __launch_bounds__(256) void k_kvq_append(KvqRows a) {
   const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int c = (int)(t % CPR);
   const int64_t line = t / CPR;
-  const int head = (int)(line % a.c.n_kv);
-  const int64_t rs = line / a.c.n_kv;
-  const int sel = (int)(rs & 1);
-  const int row = (int)(rs >> 1);
+  const int hi = (int)(line % a.heads), head = a.head0 + hi;
+  const int64_t rs = line / a.heads;
+  const int sel = a.sel < 0 ? (int)(rs & 1) : a.sel;
+  const int row = (int)(a.sel < 0 ? rs >> 1 : rs);
   if (row >= a.n) return;
   constexpr int SB = DT == HS_F32 ? 4 : 2;
-  const int64_t at = ((int64_t)row * a.ld + (int64_t)head * a.ld_head + c * 8) * SB;
+  int seq, pos;
+  kvq_place(a, row, seq, pos);
+  const int64_t at = ((int64_t)(a.row_by_seq ? seq : row) * a.ld + (int64_t)hi * a.ld_head + c * 8) * SB;
   float f[8];
   ld8<DT>((const char *)(sel ? a.v : a.k) + at, f);
   uint32_t byte;
   const uint32_t w = kvq_encode<DT>(f, byte);
-  const int seq = a.seqs ? a.seqs[row] : row;
-  const int pos = !a.pos_by_seq ? a.pos[row] : (uint32_t)seq < (uint32_t)a.c.n_seqs ? a.pos[seq] : -1;
-  const int64_t id = a.cap && pos >= 0 && pos >= a.cap[seq] ? -1 : kvq_block(a.c, seq, pos);
+  int64_t id = kvq_block(a.c, seq, pos);
+  if (id >= 0 && a.cap && pos >= a.cap[seq]) id = -1;
   if (id >= 0) {
     uint8_t *span = kvq_span(a.c, HD, id, sel, head, pos);
     ((uint32_t *)span)[(pos & 15) * CPR + c] = w;
@@ -161,13 +168,14 @@ __global__ __launch_bounds__(256) void k_kvq_read(KvqRows a) {
   const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int c = (int)(t % CPR);
   const int64_t line = t / CPR;
-  const int head = (int)(line % a.c.n_kv);
-  const int64_t rs = line / a.c.n_kv;
-  const int sel = (int)(rs & 1);
-  const int row = (int)(rs >> 1);
+  const int hi = (int)(line % a.heads), head = a.head0 + hi;
+  const int64_t rs = line / a.heads;
+  const int sel = a.sel < 0 ? (int)(rs & 1) : a.sel;
+  const int row = (int)(a.sel < 0 ? rs >> 1 : rs);
   if (row >= a.n) return;
   constexpr int SB = DT == HS_F32 ? 4 : 2;
-  const int seq = a.seqs ? a.seqs[row] : row, pos = a.pos[row];
+  int seq, pos;
+  kvq_place(a, row, seq, pos);
   const int64_t id = kvq_block(a.c, seq, pos);
   uint32_t w = 0, byte = KvqByte<DT>::lo;
   if (id >= 0) {
@@ -177,7 +185,7 @@ __global__ __launch_bounds__(256) void k_kvq_read(KvqRows a) {
   }
   float f[8];
   kvq_decode(w, kvq_scale(byte), f);
-  st8<DT>((char *)(sel ? a.v_out : a.k_out) + ((int64_t)row * a.ld + (int64_t)head * a.ld_head + c * 8) * SB, f);
+  st8<DT>((char *)(sel ? a.v_out : a.k_out) + ((int64_t)row * a.ld + (int64_t)hi * a.ld_head + c * 8) * SB, f);
 }
 
 // Decode attention over the 4-bit cache.  One work group = (split of the row's
@@ -517,7 +525,7 @@ __global__ __launch_bounds__(64 * NW) void k_kvq_attn(KvqAttn a) {
     } else {
       a.part_o[((rh + h) * a.n_split + split) * HD + e] = num;
       if (e == 0) {
-        a.part_ml[((rh + h) * a.n_split + split) * 2] = den == 0.f ? -INFINITY : M;
+        a.part_ml[((rh + h) * a.n_split + split) * 2] = den == 0.f ? -INFINITY : a.nat ? M * 0.693147180559945309f : M;
         a.part_ml[((rh + h) * a.n_split + split) * 2 + 1] = den;
       }
     }
@@ -553,7 +561,7 @@ __global__ __launch_bounds__(256) void k_kvq_combine(KvqAttn a) {
 
 template <int DT, int HD>
 hipError_t kvq_rows(const KvqRows &a, bool read, hipStream_t st) {
-  const int64_t threads = (int64_t)a.n * 2 * a.c.n_kv * (HD / 8), grid = (threads + 255) / 256;
+  const int64_t threads = (int64_t)a.n * (a.sel < 0 ? 2 : 1) * a.heads * (HD / 8), grid = (threads + 255) / 256;
   if (grid > INT32_MAX) return hipErrorInvalidValue;
   if (read) HS_LAUNCH((k_kvq_read<DT, HD>), dim3((uint32_t)grid), dim3(256), 0, st, a);
   else HS_LAUNCH((k_kvq_append<DT, HD>), dim3((uint32_t)grid), dim3(256), 0, st, a);
@@ -581,14 +589,41 @@ hipError_t kvq_attn_hd(const KvqAttn &a, hipStream_t st) {
   if (grid > INT32_MAX || rows > INT32_MAX || a.n_split > KVQ_MAX_SPLITS) return hipErrorInvalidValue;
   if ((1 << a.c.bt_log2) >= KVQ_TILE) HS_LAUNCH((k_kvq_attn<DT, HD, 4, true>), dim3((uint32_t)grid), dim3(256), 0, st, a);
   else HS_LAUNCH((k_kvq_attn<DT, HD, 4, false>), dim3((uint32_t)grid), dim3(256), 0, st, a);
-  if (a.n_split > 1) HS_LAUNCH((k_kvq_combine<DT, HD>), dim3((uint32_t)rows), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+template <int DT, int HD>
+hipError_t kvq_combine_hd(const KvqAttn &a, hipStream_t st) {
+  const int64_t rows = (int64_t)a.n * a.n_heads;
+  if (rows > INT32_MAX || a.n_split > KVQ_MAX_SPLITS || a.nat) return hipErrorInvalidValue;
+  HS_LAUNCH((k_kvq_combine<DT, HD>), dim3((uint32_t)rows), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 template <int DT>
-hipError_t kvq_attn_dt(int hd, const KvqAttn &a, hipStream_t st) {
-  if (hd == 64) return kvq_attn_hd<DT, 64>(a, st);
-  if (hd == 128) return kvq_attn_hd<DT, 128>(a, st);
+hipError_t kvq_attn_dt(int hd, bool combine, const KvqAttn &a, hipStream_t st) {
+  if (hd == 64) return combine ? kvq_combine_hd<DT, 64>(a, st) : kvq_attn_hd<DT, 64>(a, st);
+  if (hd == 128) return combine ? kvq_combine_hd<DT, 128>(a, st) : kvq_attn_hd<DT, 128>(a, st);
   return hipErrorInvalidValue;
+}
+hipError_t kvq_attn_any(int dtype, int hd, bool combine, const KvqAttn &a, hipStream_t st) {
+  if (a.n <= 0) return hipSuccess;
+  switch (dtype) {
+    case HS_F32: return kvq_attn_dt<HS_F32>(hd, combine, a, st);
+    case HS_F16: return kvq_attn_dt<HS_F16>(hd, combine, a, st);
+    case HS_BF16: return kvq_attn_dt<HS_BF16>(hd, combine, a, st);
+  }
+  return hipErrorInvalidValue;
+}
+
+__global__ __launch_bounds__(256) void k_kvq_stage(PackedRows pk, int hd, KvqStage s) {
+  const int r = (int)blockIdx.x * 256 + threadIdx.x, rows = pk.cu[pk.n];
+  if (r < pk.n) {
+    s.start[pk.req[r]] = (int64_t)pk.cu[r] * hd;
+    s.bt[pk.req[r]] = rows;
+  }
+  if (r >= rows) return;
+  const int i = packed_request(&pk, r);
+  s.seqs[r] = pk.req[i];
+  s.pos[r] = r - pk.cu[i];
 }
 
 }  // namespace
@@ -610,13 +645,16 @@ hipError_t launch_kvq_read(int dtype, int head_dim, const KvqRows &a, hipStream_
   return kvq_rows_any(dtype, head_dim, a, true, st);
 }
 hipError_t launch_kvq_attention(int dtype, int head_dim, const KvqAttn &a, hipStream_t st) {
-  if (a.n <= 0) return hipSuccess;
-  switch (dtype) {
-    case HS_F32: return kvq_attn_dt<HS_F32>(head_dim, a, st);
-    case HS_F16: return kvq_attn_dt<HS_F16>(head_dim, a, st);
-    case HS_BF16: return kvq_attn_dt<HS_BF16>(head_dim, a, st);
-  }
-  return hipErrorInvalidValue;
+  return kvq_attn_any(dtype, head_dim, false, a, st);
+}
+hipError_t launch_kvq_combine(int dtype, int head_dim, const KvqAttn &a, hipStream_t st) {
+  return a.n_split > 1 ? kvq_attn_any(dtype, head_dim, true, a, st) : hipSuccess;
+}
+hipError_t launch_kvq_stage(const PackedRows &pk, int head_dim, const KvqStage &s, hipStream_t st) {
+  const int rows = std::max(pk.cu[pk.n], pk.n);
+  if (rows <= 0) return hipSuccess;
+  HS_LAUNCH(k_kvq_stage, dim3((rows + 255) / 256), dim3(256), 0, st, pk, head_dim, s);
+  return hipGetLastError();
 }
 
 }  // namespace hs

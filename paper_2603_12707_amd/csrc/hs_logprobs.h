@@ -120,7 +120,7 @@ __device__ __forceinline__ void put_row(const LogprobArgs &a, int64_t row, bool 
   const float lz = log1pf(r);
   if (a.entropy) a.entropy[row] = none ? NAN : lz - s1 / (1.f + r);
   if (a.logprob) {
-    const int t = a.tokens[row];
+    const int t = a.tokens[a.act ? a.act[row] : row];
     float v = NAN;
     if (t >= 0 && t < a.vocab) v = ld_elem<DT>(a.logits, row * a.ld + t) - M - lz;
     a.logprob[row] = t < 0 ? 0.f : none ? NAN : v;

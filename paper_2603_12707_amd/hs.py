@@ -27,7 +27,7 @@ EXPORTS = ("hs_last_error", "hs_kv_bytes", "hs_model_create", "hs_model_free", "
            "hs_kv_pool_blocks", "hs_handoff_create", "hs_handoff_free", "hs_handoff_push", "hs_handoff_pop",
            "hs_handoff_pending", "hs_stream_read", "hs_decode_step_static", "hs_kvq_block_bytes", "hs_kvq_append",
            "hs_kvq_read", "hs_kvq_attention_workspace", "hs_kvq_attention", "hs_token_logprobs_workspace",
-           "hs_token_logprobs")
+           "hs_token_logprobs", "hs_kvq_pool_create", "hs_decode_step_logprobs")
 
 # projection matrices the library reads in its packed layout
 PACKED = ("wq", "wk", "wv", "wo", "w_gate", "w_up", "w_down", "lm_head")
@@ -122,6 +122,8 @@ def lib() -> ctypes.CDLL:
         "hs_kvq_attention_workspace": [P, I32, I32, I32, I32, ctypes.POINTER(U64)],
         "hs_kvq_attention": [P, I32, I32, I32, I32, P, I64, P, P, I32, ctypes.c_float, P, I64, P, U64, P],
         "hs_token_logprobs_workspace": [I64, I32, I32, ctypes.POINTER(U64)],
+        "hs_kvq_pool_create": [P, I32, I32, P, U64, ctypes.POINTER(P)],
+        "hs_decode_step_logprobs": [P, P, P, P, P, I32, P, P, P, P, P, P, P],
         "hs_token_logprobs": [I32, P, I64, I32, I64, P, I32, P, P, P, P, P, U64, P],
     }
     for name, args in sig.items():
@@ -334,6 +336,23 @@ class KVCache:
         _call("hs_decode_step_static", (model or self.model).handle, self.handle, _ptr(tokens_in), _ptr(tokens_out),
               _ptr(logits), _ptr(hidden_out), _stream())
 
+    def decode_logprobs(self, tokens_in, tokens_out, targets=None, top: int = 0, logits=None, hidden_out=None,
+                        model=None):
+        """The same step, and of its logits (logprob, entropy, top_ids, top_logprobs) as token_logprobs gives them,
+        a row for each decoded request: of the tokens in targets (int32, indexed like tokens_in; None: the chosen
+        ones), with `top` alternatives (None without)."""
+        import torch
+        m = model or self.model
+        device = tokens_in.device
+        # as many rows as requests can be decoded; a pool that decodes fewer leaves the last ones unwritten
+        rows = min(self.batch, m.max_batch)
+        lp, entropy = (torch.empty(rows, dtype=torch.float32, device=device) for _ in range(2))
+        ids = torch.empty(rows, top, dtype=torch.int32, device=device) if top > 0 else None
+        tops = torch.empty(rows, top, dtype=torch.float32, device=device) if top > 0 else None
+        _call("hs_decode_step_logprobs", m.handle, self.handle, _ptr(tokens_in), _ptr(tokens_out), _ptr(targets), top,
+              _ptr(logits), _ptr(hidden_out), _ptr(lp), _ptr(entropy), _ptr(ids), _ptr(tops), _stream())
+        return lp, entropy, ids, tops
+
     def sync(self) -> None:
         """Host mirrors of the lengths from the device (after graph replays)."""
         _call("hs_kv_sync", self.handle)
@@ -375,19 +394,23 @@ class KVPool(KVCache):
     Requests are admitted into empty slots, prefilled and decoded like
     KVCache requests (slot = request number) and released when done."""
 
+    _create = "hs_kv_pool_create"
+
     def __init__(self, model: Model, slots: int, block_tokens: int, n_blocks: int, buf=None):
         import torch
         self.model = model
         self.batch = slots
         self.block_tokens = block_tokens
-        block_bytes = hs_kv_bytes(model.cfg, 0, block_tokens)[0]
         if buf is None:
-            buf = torch.empty(n_blocks * block_bytes, dtype=torch.uint8, device="cuda")
+            buf = torch.empty(n_blocks * self._block_bytes(), dtype=torch.uint8, device="cuda")
         self.buf = buf
         h = ctypes.c_void_p()
-        _call("hs_kv_pool_create", model.handle, slots, block_tokens, _ptr(buf), buf.numel() * buf.element_size(),
+        _call(self._create, model.handle, slots, block_tokens, _ptr(buf), buf.numel() * buf.element_size(),
               ctypes.byref(h))
         self.handle = h
+
+    def _block_bytes(self) -> int:
+        return hs_kv_bytes(self.model.cfg, 0, self.block_tokens)[0]
 
     def admit(self, slot: int, n_v: int, capacity: int) -> None:
         _call("hs_kv_admit", self.handle, slot, n_v, capacity, _stream())
@@ -400,6 +423,17 @@ class KVPool(KVCache):
         f, n = ctypes.c_int32(), ctypes.c_int32()
         _call("hs_kv_pool_blocks", self.handle, ctypes.byref(f), ctypes.byref(n))
         return f.value, n.value
+
+
+class QuantKVPool(KVPool):
+    """A KVPool held in 4 bits (hs_kvq_pool_create): 17/64 of its bytes, the
+    rows rounded as they are stored, read and written through the same calls."""
+
+    _create = "hs_kvq_pool_create"
+
+    def _block_bytes(self) -> int:
+        cfg = self.model.cfg
+        return kvq_block_bytes(cfg["n_layers"], cfg["n_kv_heads"], cfg["head_dim"], self.block_tokens)
 
 
 def _dtype_code(func: str, t) -> int:
