@@ -16,6 +16,7 @@
 
 #include <algorithm>
 #include <cfloat>
+#include <utility>
 
 namespace hs {
 namespace {
@@ -193,29 +194,49 @@ __global__ __launch_bounds__(256) void k_kvq_read(KvqRows a) {
 // and keeps an online softmax for the G query heads of the head in the 16
 // columns of the matrix products.
 //
-// Scores: S^T = K Q^T, MFMA 16x16x32 with 16 positions as rows.  Lane (li, lg) =
-// (lane % 16, lane / 16) converts HD / 4 consecutive elements of its position,
-// one load and one group's scale, straight into A operands; the order of the
-// elements inside the contraction is the same for Q.  Row r of the tile's
-// product t is position 16 (r / 4) + 4 t + r % 4, so that a lane ends up with
-// the scores of the 16 consecutive positions 16 lg .. for head li, which is the
-// B operand of O^T += V^T P^T: positions 8 m .. 8 m + 7 of each lane group are
+// Scores: S^T = K Q^T, the scaled MFMA 16x16x128 with 16 positions as rows.  It
+// takes K as it lies in memory: lane (li, lg) = (lane % 16, lane / 16) supplies
+// group lg of its position and the group's exponent byte.  Q enters as the sum of
+// e4m3 parts, each with what the parts before left, times 16 (two hold a bf16
+// number, three an f16, six an fp32), scaled by a power of two of the head's
+// largest element: every product is exact, an element below 2^-13 of the largest
+// is off by at most 2^-17 of 16^-parts of it.  Row r of the tile's product t is
+// position 16 (r / 4) + 4 t + r % 4, so that a lane ends up with the scores of
+// the 16 consecutive positions 16 lg .. for head li, which is the B operand of
+// O^T += V^T P^T (MFMA 16x16x32): positions 8 m .. 8 m + 7 of each lane group are
 // the k range of MFMA m.  For V^T a lane reads its HD / 16 channels of those 16
-// positions, converts pairs of channels and pairs the positions with v_perm; no
-// value goes through LDS.  The 4-bit values are exact in the 16-bit type, P
-// enters as the sum of parts in that type (two: 16 bits and more; fp32: three,
-// 24 bits, and Q alike), every sum is fp32.
+// positions, converts pairs of channels (exact in the 16-bit type) and pairs the
+// positions with v_perm.  P enters as the sum of parts in that type (two: 16 bits
+// and more; fp32: three, 24 bits), every sum is fp32.
 //
-// Blocks of 64 positions and more (WIDE) hold a tile whole: it is read through a
-// buffer range that ends at its last span, past which nothing is fetched.
-// Smaller blocks are found span by span, per lane.
+// Each wave copies its tiles straight into LDS, K and V alike as they lie in
+// memory, a tile and a half ahead, through buffer ranges that end at the last span with a
+// position (past it LDS gets zeros and nothing is fetched).  The waits count the
+// wave's own copies, so that the waves never meet before the end.  Blocks of 64
+// positions and more (WIDE) hold a tile whole; smaller ones are copied span by
+// span.
 template <int DT>
 constexpr int KVQ_MMA = DT == HS_F16 ? HS_F16 : HS_BF16;
 template <int DT>
 constexpr int KVQ_P_PARTS = DT == HS_F32 ? 3 : 2;
 template <int DT>
-constexpr int KVQ_Q_PARTS = DT == HS_F32 ? 3 : 1;
-constexpr int KVQ_TILE = 64;
+constexpr int KVQ_Q_PARTS = DT == HS_F32 ? 6 : DT == HS_F16 ? 3 : 2;
+constexpr int KVQ_TILE = 64, KVQ_PLANES = 3;
+typedef const __attribute__((address_space(4))) int64_t ConstI64;
+
+// as dma_1k_stream, four bytes a lane
+__device__ __forceinline__ void dma_dwords_stream(u32x4 rsrc, uint32_t voff, uint32_t soff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen nt lds" ::"s"(lds), "v"(voff),
+               "s"(rsrc), "s"(soff)
+               : "memory");
+}
+// at most N of this wave's copies still in flight
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// this wave's LDS reads done
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 // In units of the base-2 exponent: a column's probabilities are 2^(s - m) for a
 // reference m that is put KVQ_BIAS below the largest score when a score passes it
 // by more than KVQ_BIAS + KVQ_SLACK, and o and l are rescaled then.  f16 parts
@@ -231,6 +252,15 @@ constexpr float KVQ_SLACK = DT == HS_F16 ? 4.f : 11.5f;
 // m, 2^-5, the same factor in o and l).
 constexpr float KVQ_ROUND_FROM = 0x1p20f;
 
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+// sc += K Q^T over the parts P of Q: K fp4 with its group's exponent byte, Q e4m3 with byte P % 4 of qs
+template <int QP, int... P>
+__device__ __forceinline__ void score_parts(f32x4 &sc, u32x4 k, int byte, const i32x8 (&qb)[QP],
+                                            const int (&qs)[(QP + 3) / 4], std::integer_sequence<int, P...>) {
+  const i32x8 kv{(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
+  ((sc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kv, qb[P], sc, 4, 0, 0, byte, P % 4, qs[P / 4])), ...);
+}
+
 // word x of a matrix operand of parts: R(f0) | R(f1) << 16, and what is left
 template <int MT>
 __device__ __forceinline__ uint32_t take_part(float &f0, float &f1) {
@@ -241,9 +271,8 @@ __device__ __forceinline__ uint32_t take_part(float &f0, float &f1) {
 }
 
 template <int DT, int HD, int NW, bool WIDE>
-__global__ __launch_bounds__(64 * NW) void k_kvq_attn(KvqAttn a) {
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == HS_F32 ? 2 : 3))) void k_kvq_attn(KvqAttn a) {
   constexpr int MT = KVQ_MMA<DT>, PP = KVQ_P_PARTS<DT>, QP = KVQ_Q_PARTS<DT>;
-  constexpr int NC = HD / 32;             // words of a lane's K elements: k steps of the scores
   constexpr int VB = HD / 32;             // bytes of a lane's V elements of one position
   constexpr int ND = HD / 16;             // 16-channel tiles of the output
   constexpr int SPAN = kvq_span_bytes(HD);
@@ -277,98 +306,55 @@ __global__ __launch_bounds__(64 * NW) void k_kvq_attn(KvqAttn a) {
   }
   const int end = min(t0 + a.S, len);  // the split's positions: t0 .. end - 1
   const int n_tiles = (end - t0 + KVQ_TILE - 1) / KVQ_TILE;
-  const int64_t *tab = a.c.table + (int64_t)seq * a.c.table_ld;
+  // read through the scalar cache: the copies below clobber memory for all that the compiler knows
+  const ConstI64 *tab = (const ConstI64 *)(uintptr_t)(a.c.table + (int64_t)seq * a.c.table_ld);
   const int64_t kin = ((int64_t)(a.c.layer * 2) * a.c.n_kv + j) << (a.c.bt_log2 - 4);  // spans before the head's
   const int64_t vin = kin + ((int64_t)a.c.n_kv << (a.c.bt_log2 - 4));
   const int in_mask = (1 << a.c.bt_log2) - 1;
 
-  // Q^T operand: head li of the group (zeros past it)
-  u32x4 qb[QP][NC];
-#pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    float f[8] = {};
-    if (li < G) ld8<DT>((const char *)a.q + ((int64_t)row * a.ld_q + (j * G + li) * HD + lg * (HD / 4) + c * 8) * SB, f);
-    // (a negative scale's sign goes to Q, so that the scores' order is that of the products)
-    if (a.scale < 0.f)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = -f[e];
-#pragma unroll
-    for (int p = 0; p < QP; ++p)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) qb[p][c][x] = take_part<MT>(f[2 * x], f[2 * x + 1]);
-  }
-  const float c2 = fabsf(a.scale) * 1.44269504088896341f;
-
-  // a tile's data in flight: K words and scale bytes, V words and scale bytes
-  uint32_t kc[4][NC], vc[16];
-  u32x4 ks, vs;
-  struct At {           // where a tile is
-    int64_t kid, vid;   // WIDE: the tile's block, twice; else the blocks of the lane's K and V spans
+  // the wave's ring of planes, a plane being a tile's four K or V spans
+  constexpr int PLANE = 4 * SPAN;
+  __shared__ __align__(1024) unsigned char s_mem[NW * KVQ_PLANES * PLANE];
+  constexpr int COPIES = WIDE ? PLANE / 1024 + 1 : 8;  // of a plane
+  unsigned char *ring = s_mem + wave * (KVQ_PLANES * PLANE);
+  const uint32_t ring0 = __builtin_amdgcn_readfirstlane(lds_addr(ring));
+  const int kspan = li >> 2, kgrp = HD == 128 ? lg : lg & 1, vgrp = HD == 128 ? li >> 2 : li >> 3;
+  // block numbers of a tile: of its spans, or (WIDE) of the tile
+  constexpr int NB = WIDE ? 1 : 4;
+  struct Ids {
+    int64_t id[NB];
   };
-  const int kspan = li >> 2, kgrp = HD == 128 ? lg : lg >> 1, vgrp = HD == 128 ? li >> 2 : li >> 3;
   auto find = [&](int t) {
-    At w{-1, -1};
-    if (t >= n_tiles) return w;
-    const int p0 = t0 + t * KVQ_TILE;
-    if constexpr (WIDE) {
-      w.kid = tab[p0 >> a.c.bt_log2];
-    } else {
-      // past the last span: that span again
-      const int last = (end - 1) & ~15;
-      w.kid = tab[min(p0 + kspan * 16, last) >> a.c.bt_log2];
-      w.vid = tab[min(p0 + lg * 16, last) >> a.c.bt_log2];
-      if ((uint64_t)w.vid >= (uint64_t)a.c.n_blocks) w.vid = -1;
+    Ids w;
+#pragma unroll
+    for (int s = 0; s < NB; ++s) {
+      const int p = t0 + t * KVQ_TILE + s * 16;
+      w.id[s] = p < end ? tab[p >> a.c.bt_log2] : -1;
+      if ((uint64_t)w.id[s] >= (uint64_t)a.c.n_blocks) w.id[s] = -1;
     }
-    if ((uint64_t)w.kid >= (uint64_t)a.c.n_blocks) w.kid = -1;
-    if constexpr (WIDE) w.vid = w.kid;
     return w;
   };
-  auto range = [&](int t, int64_t id, int64_t in) {  // WIDE: the tile's spans
-    const int p0 = t0 + t * KVQ_TILE, spans = (min(end - p0, KVQ_TILE) + 15) / 16;
-    return make_rsrc(a.c.blocks + max(id, (int64_t)0) * a.c.block_bytes + (in + ((p0 & in_mask) >> 4)) * SPAN,
-                     id < 0 || t >= n_tiles ? 0u : (uint32_t)(spans * SPAN));
-  };
-  auto load_k = [&](int t, const At &w) {
+  // K (v = 0) or V of tile t into plane `slot` of the ring
+  auto copy = [&](int t, const Ids &w, int v, int slot) {
+    const int p0 = t0 + t * KVQ_TILE;
+    const uint32_t lds = ring0 + slot * PLANE;
     if constexpr (WIDE) {
-      const rsrc_t r = range(t, w.kid, kin);
-      const uint32_t o = kspan * SPAN + (li & 3) * (HD / 2) + lg * (HD / 8);
+      const uint64_t at = (uint64_t)(uintptr_t)a.c.blocks + (uint64_t)max(w.id[0], (int64_t)0) * a.c.block_bytes +
+                          (uint64_t)((v ? vin : kin) + ((p0 & in_mask) >> 4)) * SPAN;
+      const uint32_t bytes = w.id[0] < 0 ? 0u : (uint32_t)((min(end - p0, KVQ_TILE) + 15) / 16 * SPAN);
+      const u32x4 r{(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, bytes, (uint32_t)BUF_WORD3};
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        if constexpr (HD == 128) *(u32x4 *)kc[x] = bld16_stream(r, o + x * 4 * (HD / 2));
-        else *(u32x2 *)kc[x] = bld8(r, o + x * 4 * (HD / 2));
-      }
-      ks = bld16_stream(r, kspan * SPAN + HD * 8 + kgrp * 16);
-    } else if (t < n_tiles) {
-      const int p = min(t0 + t * KVQ_TILE + kspan * 16, (end - 1) & ~15);
-      const uint8_t *s = a.c.blocks + max(w.kid, (int64_t)0) * a.c.block_bytes + (kin + ((p & in_mask) >> 4)) * SPAN;
+      for (int x = 0; x < PLANE / 1024; ++x) dma_1k_stream(r, lane * 16, x * 1024, lds + x * 1024);
+      if (lane < PLANE % 1024 / 4) dma_dwords_stream(r, lane * 4, PLANE / 1024 * 1024, lds + PLANE / 1024 * 1024);
+    } else {
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const uint8_t *at = s + (4 * x + (li & 3)) * (HD / 2) + lg * (HD / 8);
-        if constexpr (HD == 128) *(u32x4 *)kc[x] = *(const u32x4 *)at;
-        else *(u32x2 *)kc[x] = *(const u32x2 *)at;
+      for (int s = 0; s < 4; ++s) {
+        const uint64_t at = (uint64_t)(uintptr_t)a.c.blocks + (uint64_t)max(w.id[s], (int64_t)0) * a.c.block_bytes +
+                            (uint64_t)((v ? vin : kin) + (((p0 + s * 16) & in_mask) >> 4)) * SPAN;
+        const u32x4 r{(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, w.id[s] < 0 ? 0u : (uint32_t)SPAN, (uint32_t)BUF_WORD3};
+        if (lane < HD / 2) dma_1k_stream(r, lane * 16, 0, lds + s * SPAN);
+        if (lane < HD / 8) dma_dwords_stream(r, lane * 4, HD * 8, lds + s * SPAN + HD * 8);
       }
-      ks = *(const u32x4 *)(s + HD * 8 + kgrp * 16);
-    }
-  };
-  auto load_v = [&](int t, const At &w) {
-    if constexpr (WIDE) {
-      const rsrc_t r = range(t, w.vid, vin);
-      const uint32_t o = lg * SPAN + li * VB;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        if constexpr (HD == 128) vc[i] = bld4(r, o + i * (HD / 2));
-        else vc[i] = (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, o + i * (HD / 2), 0, 0);
-      }
-      vs = bld16_stream(r, lg * SPAN + HD * 8 + vgrp * 16);
-    } else if (t < n_tiles) {
-      const int p = min(t0 + t * KVQ_TILE + lg * 16, (end - 1) & ~15);
-      const uint8_t *s = a.c.blocks + max(w.vid, (int64_t)0) * a.c.block_bytes + (vin + ((p & in_mask) >> 4)) * SPAN;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        if constexpr (HD == 128) vc[i] = *(const uint32_t *)(s + i * (HD / 2) + li * VB);
-        else vc[i] = *(const uint16_t *)(s + i * (HD / 2) + li * VB);
-      }
-      vs = *(const u32x4 *)(s + HD * 8 + vgrp * 16);
     }
   };
 
@@ -380,29 +366,117 @@ __global__ __launch_bounds__(64 * NW) void k_kvq_attn(KvqAttn a) {
 #pragma unroll
   for (int d = 0; d < ND; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  At cur = find(wave), nxt = find(wave + NW);
-  load_k(wave, cur);
-  load_v(wave, cur);
+  // The first planes' copies go out before the query is read; plane x + 3 (K and
+  // V of the wave's tiles in turn) follows as soon as plane x is read.  After the
+  // wait for a plane at most two that were asked for later are in flight.
+  static_assert(KVQ_PLANES == 3, "the order of the copies below");
+  Ids nxt = find(wave + NW);
+  auto held_of = [&](const Ids &w) {  // bit s: span s has a block
+    if constexpr (WIDE) return w.id[0] >= 0 ? 15u : 0u;
+    else return (w.id[0] >= 0 ? 1u : 0u) | (w.id[1] >= 0 ? 2u : 0u) | (w.id[2] >= 0 ? 4u : 0u) | (w.id[3] >= 0 ? 8u : 0u);
+  };
+  uint32_t held_cur;
+  {
+    const Ids cur = find(wave);
+    held_cur = held_of(cur);
+    if (wave < n_tiles) {
+      copy(wave, cur, 0, 0);
+      copy(wave, cur, 1, 1);
+    }
+  }
+  if (wave + NW < n_tiles) copy(wave + NW, nxt, 0, 2);
+  int slot = 0;  // of the tile's K
+  auto next_slot = [](int x) { return x == KVQ_PLANES - 1 ? 0 : x + 1; };
+  // Q^T operand: head li of the group (zeros past it); the MFMA's byte e of lane
+  // group lg is channel 16 lg + e, from byte 16 on 64 further
+  i32x8 qb[QP];
+  int qs[(QP + 3) / 4];  // the parts' scale bytes
+  {
+    float f[32];
+#pragma unroll
+    for (int e = 0; e < 32; ++e) f[e] = 0.f;
+    if (li < G) {
+      const char *at = (const char *)a.q + ((int64_t)row * a.ld_q + (j * G + li) * HD + lg * 16) * SB;
+#pragma unroll
+      for (int x = 0; x < HD / 32; ++x) ld8<DT>(at + ((x >> 1) * 64 + (x & 1) * 8) * SB, f + 8 * x);
+    }
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) top = max(top, __float_as_uint(f[e]) & 0x7FFFFFFFu);
+    top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+    // 2^s puts the largest into 128 .. 256 (e4m3 ends at 448); a NaN or an infinity makes the head's scores NaN
+    const int s = min(max((int)(top >> 23) - 127 - 7, -100), 120);
+    // (a negative scale's sign goes to Q, so that the scores' order is that of the products)
+    const float mul = __uint_as_float((uint32_t)(127 - s) << 23) * (a.scale < 0.f ? -1.f : 1.f);
+#pragma unroll
+    for (int e = 0; e < 32; ++e) f[e] *= mul;
+#pragma unroll
+    for (int p = 0; p < QP; ++p) {
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * x], f[4 * x + 1], 0, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * x + 2], f[4 * x + 3], w, true);
+        qb[p][x] = w;
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+        f[4 * x] = (f[4 * x] - lo[0]) * 16.f;
+        f[4 * x + 1] = (f[4 * x + 1] - lo[1]) * 16.f;
+        f[4 * x + 2] = (f[4 * x + 2] - hi[0]) * 16.f;
+        f[4 * x + 3] = (f[4 * x + 3] - hi[1]) * 16.f;
+      }
+      const int byte = top >= 0x7F800000u ? 255 : 127 + s - 4 * p;
+      if (p % 4 == 0) qs[p / 4] = 0;
+      qs[p / 4] |= byte << (8 * (p % 4));
+    }
+  }
+  const float c2 = fabsf(a.scale) * 1.44269504088896341f;
+
   for (int t = wave; t < n_tiles; t += NW) {
     const int p0 = t0 + t * KVQ_TILE;
+    const bool one = t + NW < n_tiles, two = t + 2 * NW < n_tiles;  // tiles that follow
+    const int vslot = next_slot(slot);
+    const unsigned char *kp = ring + slot * PLANE, *vp = ring + vslot * PLANE;
+    const Ids far = find(t + 2 * NW);
+    if (one) wait_copies<2 * COPIES>();  // V, and the next tile's K
+    else wait_copies<COPIES>();
+    u32x4 kc[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      kc[x] = *(const u32x4 *)(kp + kspan * SPAN + (4 * x + (li & 3)) * (HD / 2) + kgrp * 16);
+    u32x4 ks = *(const u32x4 *)(kp + kspan * SPAN + HD * 8 + kgrp * 16);
+    if constexpr (HD == 64) {  // the upper half of the contraction: zeros, times 1
+      if (lg >= 2) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) kc[x] = u32x4{0u, 0u, 0u, 0u};
+        ks = u32x4{0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu};
+      }
+    }
     f32x4 sc[4];
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-      const float s = kvq_scale((ks[x] >> (8 * (li & 3))) & 255u);
+      const int byte = (int)(ks[x] >> (8 * (li & 3)));  // the MFMA reads the lowest byte
       sc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const u32x4 kv{kvq_pair<MT, 0>(kc[x][c], s), kvq_pair<MT, 1>(kc[x][c], s), kvq_pair<MT, 2>(kc[x][c], s),
-                       kvq_pair<MT, 3>(kc[x][c], s)};
-#pragma unroll
-        for (int p = 0; p < QP; ++p) sc[x] = mma<MT>(kv, qb[p][c], sc[x]);
-      }
+      score_parts<QP>(sc[x], kc[x], byte, qb, qs, std::make_integer_sequence<int, QP>{});
     }
-    load_k(t + NW, nxt);
+    if (one) {
+      wait_lds();
+      copy(t + NW, nxt, 1, slot);
+      wait_copies<2 * COPIES>();  // the next tile's K and V
+    } else {
+      wait_copies<0>();
+    }
+    uint32_t vc[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const unsigned char *at = vp + lg * SPAN + i * (HD / 2) + li * VB;
+      if constexpr (HD == 128) vc[i] = *(const uint32_t *)at;
+      else vc[i] = *(const uint16_t *)at;
+    }
+    u32x4 vs = *(const u32x4 *)(vp + lg * SPAN + HD * 8 + vgrp * 16);
     // which of the lane's 16 positions count: all of them in a whole tile
-    const bool held = cur.vid >= 0;
+    const bool held = (held_cur >> lg) & 1;
     const int left = end - p0 - 16 * lg;
-    const bool whole = p0 + KVQ_TILE <= end && __ballot(!held) == 0;
+    const bool whole = p0 + KVQ_TILE <= end && held_cur == 15u;
     if (!whole) {
 #pragma unroll
       for (int x = 0; x < 4; ++x)
@@ -449,9 +523,15 @@ __global__ __launch_bounds__(64 * NW) void k_kvq_attn(KvqAttn a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) sc[x][i] = !held || 4 * x + i >= left ? 0.f : sc[x][i];
     }
+    // the conversion reads bits 23 .. 30 of its scale, the exponent, alone
     float vf[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) vf[i] = kvq_scale((vs[i >> 2] >> (8 * (i & 3))) & 255u);
+    for (int x = 0; x < 4; ++x) {
+      vf[4 * x] = __uint_as_float(vs[x] << 23);
+      vf[4 * x + 1] = __uint_as_float(vs[x] << 15);
+      vf[4 * x + 2] = __uint_as_float(vs[x] << 7);
+      vf[4 * x + 3] = __uint_as_float(vs[x] >> 1);
+    }
     u32x4 pb[2][PP];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -487,20 +567,26 @@ __global__ __launch_bounds__(64 * NW) void k_kvq_attn(KvqAttn a) {
       pv(std::integral_constant<int, 2>{});
       pv(std::integral_constant<int, 3>{});
     }
-    load_v(t + NW, nxt);
-    cur = nxt;
-    nxt = find(t + 2 * NW);
+    if (two) {
+      wait_lds();
+      copy(t + 2 * NW, far, 0, vslot);
+    }
+    held_cur = held_of(nxt);
+    nxt = far;
+    slot = next_slot(vslot);
   }
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
 
   // merge the waves: lane (li, lg) holds channels d = (4 lg + i) (HD / 16) + dt of head li
   __shared__ float s_m[NW][16], s_l[NW][16];
-  __shared__ float s_o[NW][16][HD + 1];
+  float(*s_o)[16][HD + 1] = (float(*)[16][HD + 1]) s_mem;  // over the rings
+  static_assert(16 * (HD + 1) * 4 <= KVQ_PLANES * PLANE, "the merge fits the rings");
   if (lg == 0) {
     s_m[wave][li] = m;
     s_l[wave][li] = l;
   }
+  __syncthreads();
   if (li < G)
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt)
@@ -533,30 +619,52 @@ __global__ __launch_bounds__(64 * NW) void k_kvq_attn(KvqAttn a) {
 }
 
 // o = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s over the splits of a (row,
-// head), in split order; zeros where none holds a position
+// head); zeros where none holds a position.  HD / 4 threads take a split's
+// partial, 1024 / HD splits at a time, several of them in flight.
 template <int DT, int HD>
 __global__ __launch_bounds__(256) void k_kvq_combine(KvqAttn a) {
-  constexpr int PARTS = 256 / HD;
-  __shared__ float s_w[KVQ_MAX_SPLITS], s_l[KVQ_MAX_SPLITS], s_n[PARTS][HD];
+  constexpr int TPS = HD / 4, PARTS = 256 / TPS, AHEAD = 4;
+  __shared__ float s_w[KVQ_MAX_SPLITS];
+  __shared__ float s_m[4], s_d[4];
+  __shared__ __align__(16) float s_n[PARTS][HD];
   const int h = blockIdx.x % a.n_heads, ns = a.n_split;
   const int64_t row = blockIdx.x / a.n_heads, base = (row * a.n_heads + h) * ns;
-  const int e = threadIdx.x % HD, part = threadIdx.x / HD;
-  for (int s = threadIdx.x; s < ns; s += 256) {
-    s_w[s] = a.part_ml[(base + s) * 2];
-    s_l[s] = a.part_ml[(base + s) * 2 + 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int c = threadIdx.x % TPS, part = threadIdx.x / TPS;
+  static_assert(KVQ_MAX_SPLITS <= 256, "one split's maximum and sum per thread");
+  float m = -FLT_MAX, l = 0.f;
+  if ((int)threadIdx.x < ns) {
+    m = fmaxf(a.part_ml[(base + threadIdx.x) * 2], -FLT_MAX);
+    l = a.part_ml[(base + threadIdx.x) * 2 + 1];
   }
+  const float wm = wave_max(m);
+  if (lane == 0) s_m[wave] = wm;
   __syncthreads();
-  float M = -FLT_MAX;
-  for (int s = 0; s < ns; ++s) M = fmaxf(M, s_w[s]);
-  float num = 0.f, den = 0.f;
-  for (int s = 0; s < ns; ++s) den += __builtin_amdgcn_exp2f(s_w[s] - M) * s_l[s];
-  for (int s = part; s < ns; s += PARTS) num += __builtin_amdgcn_exp2f(s_w[s] - M) * a.part_o[(base + s) * HD + e];
-  s_n[part][e] = num;
+  const float M = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+  const float w = __builtin_amdgcn_exp2f(m - M), wd = wave_sum(w * l);
+  s_w[threadIdx.x] = w;
+  if (lane == 0) s_d[wave] = wd;
   __syncthreads();
-  if (part) return;
+  const float den = (s_d[0] + s_d[1]) + (s_d[2] + s_d[3]);
+  const f32x4 *po = (const f32x4 *)(a.part_o + base * HD) + c;
+  f32x4 num{0.f, 0.f, 0.f, 0.f};
+  int s = part;
+  for (; s + (AHEAD - 1) * PARTS < ns; s += AHEAD * PARTS) {
+    f32x4 v[AHEAD];
 #pragma unroll
-  for (int p = 1; p < PARTS; ++p) num += s_n[p][e];
-  st_elem<DT>(a.out, kvq_out_at(a, row, h * HD + e, HD), den == 0.f ? 0.f : num / den);
+    for (int u = 0; u < AHEAD; ++u) v[u] = po[(int64_t)(s + u * PARTS) * TPS];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) num += s_w[s + u * PARTS] * v[u];
+  }
+  for (; s < ns; s += PARTS) num += s_w[s] * po[(int64_t)s * TPS];
+  *(f32x4 *)&s_n[part][c * 4] = num;
+  __syncthreads();
+  const int e = threadIdx.x;
+  if (e >= HD) return;
+  float v = 0.f;
+#pragma unroll
+  for (int p = 0; p < PARTS; ++p) v += s_n[p][e];
+  st_elem<DT>(a.out, kvq_out_at(a, row, h * HD + e, HD), den == 0.f ? 0.f : v / den);
 }
 
 template <int DT, int HD>
