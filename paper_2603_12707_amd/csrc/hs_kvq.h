@@ -222,6 +222,10 @@ constexpr int KVQ_P_PARTS = DT == HS_F32 ? 3 : 2;
 template <int DT>
 constexpr int KVQ_Q_PARTS = DT == HS_F32 ? 6 : DT == HS_F16 ? 3 : 2;
 constexpr int KVQ_TILE = 64, KVQ_PLANES = 3;
+// work groups of four waves that the GPU holds at once, and rows up to which a
+// work group ranks them
+constexpr int KVQ_RESIDENT = 3 * 256, KVQ_RANK_MOST = 512;
+inline int kvq_waves(int64_t groups) { return groups <= 256 ? 8 : 4; }  // waves of a work group: eight where there is one for a CU at most
 typedef const __attribute__((address_space(4))) int64_t ConstI64;
 
 // as dma_1k_stream, four bytes a lane
@@ -270,19 +274,45 @@ __device__ __forceinline__ uint32_t take_part(float &f0, float &f1) {
   return w;
 }
 
+// The z-th longest row (the lower number first among equals), found by the work
+// group itself: every thread ranks a few rows against all.
+__device__ __forceinline__ int kvq_ranked_row(const KvqAttn &a, int z, int *s_len /* [KVQ_RANK_MOST + 1] */) {
+  int &s_row = s_len[KVQ_RANK_MOST];
+  const int n4 = (a.n + 3) & ~3;
+  for (int r = threadIdx.x; r < n4; r += blockDim.x) s_len[r] = r < a.n ? kvq_length(a, r, a.seqs ? a.seqs[r] : r) : -1;
+  __syncthreads();
+  for (int r = threadIdx.x; r < a.n; r += blockDim.x) {
+    const int mine = s_len[r];
+    int rank = 0;
+    for (int o = 0; o < n4; o += 4) {
+      const u32x4 w = *(const u32x4 *)&s_len[o];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) rank += (int)w[e] > mine || ((int)w[e] == mine && o + e < r);
+    }
+    if (rank == z) s_row = r;
+  }
+  __syncthreads();
+  const int row = __builtin_amdgcn_readfirstlane(s_row);
+  __syncthreads();
+  return row;
+}
+
 template <int DT, int HD, int NW, bool WIDE>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == HS_F32 ? 2 : 3))) void k_kvq_attn(KvqAttn a) {
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == HS_F32 || NW == 8 ? 2 : 3))) void k_kvq_attn(KvqAttn a) {
   constexpr int MT = KVQ_MMA<DT>, PP = KVQ_P_PARTS<DT>, QP = KVQ_Q_PARTS<DT>;
   constexpr int VB = HD / 32;             // bytes of a lane's V elements of one position
   constexpr int ND = HD / 16;             // 16-channel tiles of the output
   constexpr int SPAN = kvq_span_bytes(HD);
   constexpr int SB = DT == HS_F32 ? 4 : 2;
+  constexpr int PLANE = 4 * SPAN;
+  __shared__ __align__(1024) unsigned char s_mem[NW * KVQ_PLANES * PLANE];
+  static_assert(sizeof(s_mem) >= (KVQ_RANK_MOST + 1) * 4, "the lengths fit");
   const int G = a.n_heads / a.c.n_kv;
   // every row's first split comes before any row's second: the empty ones are last
   const int64_t bid = blockIdx.x, per = (int64_t)a.n * a.c.n_kv;
   const int split = (int)(bid / per), j = (int)(bid % a.c.n_kv);
   const int z = (int)(bid % per / a.c.n_kv);
-  const int row = a.order ? a.order[z] : z;
+  const int row = a.order ? a.order[z] : a.rank ? kvq_ranked_row(a, z, (int *)s_mem) : z;
   const int lane = threadIdx.x & 63, li = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int seq = a.seqs ? a.seqs[row] : row;
@@ -313,8 +343,6 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
   const int in_mask = (1 << a.c.bt_log2) - 1;
 
   // the wave's ring of planes, a plane being a tile's four K or V spans
-  constexpr int PLANE = 4 * SPAN;
-  __shared__ __align__(1024) unsigned char s_mem[NW * KVQ_PLANES * PLANE];
   constexpr int COPIES = WIDE ? PLANE / 1024 + 1 : 8;  // of a plane
   unsigned char *ring = s_mem + wave * (KVQ_PLANES * PLANE);
   const uint32_t ring0 = __builtin_amdgcn_readfirstlane(lds_addr(ring));
@@ -691,12 +719,18 @@ hipError_t kvq_rows_any(int dtype, int hd, const KvqRows &a, bool read, hipStrea
   return hipErrorInvalidValue;
 }
 
+template <int DT, int HD, int NW>
+void kvq_attn_start(const KvqAttn &a, uint32_t grid, hipStream_t st) {
+  if ((1 << a.c.bt_log2) >= KVQ_TILE) HS_LAUNCH((k_kvq_attn<DT, HD, NW, true>), dim3(grid), dim3(64 * NW), 0, st, a);
+  else HS_LAUNCH((k_kvq_attn<DT, HD, NW, false>), dim3(grid), dim3(64 * NW), 0, st, a);
+}
 template <int DT, int HD>
-hipError_t kvq_attn_hd(const KvqAttn &a, hipStream_t st) {
-  const int64_t grid = (int64_t)a.n * a.c.n_kv * a.n_split, rows = (int64_t)a.n * a.n_heads;
-  if (grid > INT32_MAX || rows > INT32_MAX || a.n_split > KVQ_MAX_SPLITS) return hipErrorInvalidValue;
-  if ((1 << a.c.bt_log2) >= KVQ_TILE) HS_LAUNCH((k_kvq_attn<DT, HD, 4, true>), dim3((uint32_t)grid), dim3(256), 0, st, a);
-  else HS_LAUNCH((k_kvq_attn<DT, HD, 4, false>), dim3((uint32_t)grid), dim3(256), 0, st, a);
+hipError_t kvq_attn_hd(KvqAttn a, hipStream_t st) {
+  const int64_t grid = (int64_t)a.n * a.c.n_kv * a.n_split;
+  if (grid > INT32_MAX || a.n_split > KVQ_MAX_SPLITS) return hipErrorInvalidValue;
+  a.rank = !a.order && a.n_split == 1 && a.n > 1 && a.n <= KVQ_RANK_MOST && grid > KVQ_RESIDENT;
+  if (kvq_waves((int64_t)a.n * a.c.n_kv * a.n_split) == 8) kvq_attn_start<DT, HD, 8>(a, (uint32_t)grid, st);
+  else kvq_attn_start<DT, HD, 4>(a, (uint32_t)grid, st);
   return hipGetLastError();
 }
 template <int DT, int HD>
@@ -736,12 +770,17 @@ __global__ __launch_bounds__(256) void k_kvq_stage(PackedRows pk, int hd, KvqSta
 
 }  // namespace
 
+
+// Splits: as many as bring two waves to each of the 1024 SIMDs, but none shorter
+// than four tiles for each wave of the work group: joining splits takes a second
+// kernel.
 void kvq_split_policy(int64_t n, int n_kv, int max_len, int *S, int *n_split) {
-  constexpr int ROUND = 4 * KVQ_TILE;  // one tile for each wave
-  const int64_t pairs = std::max<int64_t>(1, n * n_kv), want = (2048 + pairs - 1) / pairs;
-  const int64_t most = ((int64_t)max_len + ROUND - 1) / ROUND;
+  const int64_t pairs = std::max<int64_t>(1, n * n_kv);
+  const int nw = kvq_waves(pairs);
+  const int64_t want = (2048 + pairs * nw - 1) / (pairs * nw), least = 4 * nw * KVQ_TILE;
+  const int64_t most = ((int64_t)max_len + least - 1) / least;
   const int64_t ns = std::max<int64_t>(1, std::min(std::min(want, most), (int64_t)KVQ_MAX_SPLITS));
-  const int64_t s = ((max_len + ns - 1) / ns + ROUND - 1) / ROUND * ROUND;
+  const int64_t s = ((max_len + ns - 1) / ns + 255) / 256 * 256;
   *S = (int)std::min<int64_t>(s, 1 << 30);
   *n_split = (int)((max_len + s - 1) / s);
 }
