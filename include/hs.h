@@ -398,8 +398,10 @@ int hs_kvq_read(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, int32_t
  * the lengths and shapes the launch; positions from it on are not attended.
  * q, out, ld_q and ld_out are aligned as in hs_kvq_append.  workspace is device
  * memory of hs_kvq_attention_workspace bytes (which may be 0: then it may be
- * NULL), 16-byte aligned, that calls which may run at the same time do not share;
- * nothing in it is kept from call to call.  Rows of a call may share sequences.
+ * NULL), 16-byte aligned, whose first 2048 bytes are zero before its first use;
+ * every call leaves them so, and nothing else in it is kept from call to call, so
+ * that it serves calls of any shape it is large enough for.  Calls that may run at
+ * the same time (on several streams, or two graphs) do not share one.  Rows of a call may share sequences.
  * Like hs_decode_step, this and the two calls above only enqueue kernels and can
  * be captured. */
 int hs_kvq_attention_workspace(const hs_kvq_cache *cache, int32_t dtype, int32_t n, int32_t n_heads, int32_t max_len,

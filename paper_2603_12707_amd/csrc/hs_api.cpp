@@ -135,7 +135,9 @@ int blocks_for(const hs_kv *kv, int len) { return (len + kv->block_tokens - 1) /
 // POOL_SPAN positions, the longest batch of loads of any attention kernel, so
 // that no batch crosses a block (blocks are multiples of it too).
 constexpr int POOL_SPAN = 256;
-void kv_split_policy(const hs_config &c, bool pool, int nq, int max_len, int *S, int *ns) {
+// (One held in 4 bits has a policy of its own, with no more splits.)
+void kv_split_policy(const hs_config &c, bool pool, bool quant, int nq, int max_len, int *S, int *ns) {
+  if (quant) return kvq_split_policy(nq, c.n_kv_heads, max_len, S, ns);
   split_policy(nq, c.n_kv_heads, c.n_heads / c.n_kv_heads, c.head_dim, c.dtype, max_len, S, ns);
   if (!pool) return;
   *S = (*S + POOL_SPAN - 1) / POOL_SPAN * POOL_SPAN;
@@ -490,7 +492,7 @@ int decode_step_args(hs_model *m, hs_kv *kv, hipStream_t st, Step *out, int *blo
     return fail(HS_E_CAPACITY, "decode: the pool has %d free blocks, the step needs %d", kv->free_blocks, need);
   if (blocks_needed) *blocks_needed = need;
   int S, ns;
-  kv_split_policy(c, kv->pool, B, kv->max_cap, &S, &ns);
+  kv_split_policy(c, kv->pool, kv->quant, B, kv->max_cap, &S, &ns);
   if (ns > 1 && (int64_t)B * c.n_heads * ns > m->part_entries)
     return fail(HS_E_INVALID, "decode: attention workspace too small");
   *out = Step{m, kv, B, 0, PackedRows{}, kv->d_rope, B, S, ns, st, model_ws(m)};
@@ -871,7 +873,7 @@ static int pool_create(hs_model *m, int32_t slots, int32_t block_tokens, void *d
   // workspace that a captured decode graph may hold)
   for (int nq = 1; nq <= std::min(slots, m->max_batch); ++nq) {
     int S, ns;
-    kv_split_policy(c, true, nq, m->max_ctx, &S, &ns);
+    kv_split_policy(c, true, quant, nq, m->max_ctx, &S, &ns);
     if (ns > 1 && (int64_t)nq * c.n_heads * ns > m->part_entries)
       return fail(HS_E_INVALID, "%s: %d queries x %d splits exceed the model's attention workspace", fn,
                   nq, ns);
@@ -1186,7 +1188,7 @@ extern "C" int hs_decode_step_static(hs_model *m, hs_kv *kv, const int32_t *toke
   const int B = kv->n_active;
   if (B <= 0) return fail(HS_E_STATE, "%s: no prefilled request", fn);
   int S, ns;
-  kv_split_policy(c, kv->pool, B, kv->max_cap, &S, &ns);
+  kv_split_policy(c, kv->pool, kv->quant, B, kv->max_cap, &S, &ns);
   const StepScratch sz = step_scratch(c, B, ns);
   const uint64_t own_logits = m->w.lm_head && !logits ? sz.logits : 0;
   const uint64_t least = sz.layers() + own_logits + whole256(SPLITK_MAX * B * splitk_rows(c) * 4);
@@ -1535,7 +1537,7 @@ int hs_kvq_attention_workspace(const hs_kvq_cache *cache, int32_t dtype, int32_t
   if ((int64_t)n * n_heads > (1 << 30)) return fail(HS_E_INVALID, "%s: too many rows", fn);
   int S, ns;
   kvq_split_policy(n, cache->n_kv_heads, max_len, &S, &ns);
-  *bytes = ns > 1 ? (uint64_t)n * n_heads * ns * (cache->head_dim + 2) * 4 : 0;
+  *bytes = ns > 1 ? KVQ_COUNTERS * 4 + (uint64_t)n * n_heads * ns * (cache->head_dim + 2) * 4 : 0;
   return HS_OK;
 }
 
@@ -1567,13 +1569,16 @@ int hs_kvq_attention(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, in
   a.lens = lengths;
   a.max_len = max_len;
   kvq_split_policy(n, cache->n_kv_heads, max_len, &a.S, &a.n_split);
-  a.part_o = (float *)workspace;
-  a.part_ml = need ? a.part_o + (int64_t)n * n_heads * a.n_split * cache->head_dim : nullptr;
+  if (need) {
+    a.part_o = (float *)workspace + KVQ_COUNTERS;
+    a.part_ml = a.part_o + (int64_t)n * n_heads * a.n_split * cache->head_dim;
+    if (a.n_split <= KVQ_JOIN_SPLITS && (int64_t)n * cache->n_kv_heads <= KVQ_COUNTERS) a.count = (uint32_t *)workspace;
+  }
   a.scale = scale;
   a.out = out;
   a.ld_out = ld_out;
   HIP_TRY(launch_kvq_attention(dtype, cache->head_dim, a, (hipStream_t)stream));
-  HIP_TRY(launch_kvq_combine(dtype, cache->head_dim, a, (hipStream_t)stream));
+  if (!a.count) HIP_TRY(launch_kvq_combine(dtype, cache->head_dim, a, (hipStream_t)stream));
   return HS_OK;
 }
 

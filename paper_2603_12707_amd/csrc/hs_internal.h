@@ -349,10 +349,16 @@ struct KvqAttn {
   int S, n_split;    // positions per split (a multiple of 256), splits
   float *part_o;     // [n][n_heads][n_split][head_dim]
   float *part_ml;    // [n][n_heads][n_split][2]: maximum (-inf: no position), sum
+  uint32_t *count;
   int nat;           // maxima in units of the natural exponent, as AttnArgs has them, not of the base-2 one
   int out_packed;    // out in the packed activation layout
 };
 constexpr int KVQ_MAX_SPLITS = 256;
+// up to this many splits are joined by the last work group to arrive, which
+// counts in `count` (one word per row and KV head, zero between calls); more, or
+// without `count`, by launch_kvq_combine
+constexpr int KVQ_JOIN_SPLITS = 32;
+constexpr int KVQ_COUNTERS = 512;  // rows of one KV head up to which there are splits
 // positions per split and splits for n rows of at most max_len positions
 void kvq_split_policy(int64_t n, int n_kv, int max_len, int *S, int *n_split);
 hipError_t launch_kvq_append(int dtype, int head_dim, const KvqRows &a, hipStream_t st);

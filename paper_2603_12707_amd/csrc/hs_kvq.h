@@ -222,10 +222,10 @@ constexpr int KVQ_P_PARTS = DT == HS_F32 ? 3 : 2;
 template <int DT>
 constexpr int KVQ_Q_PARTS = DT == HS_F32 ? 6 : DT == HS_F16 ? 3 : 2;
 constexpr int KVQ_TILE = 64, KVQ_PLANES = 3;
-// work groups of four waves that the GPU holds at once, and rows up to which a
-// work group ranks them
-constexpr int KVQ_RESIDENT = 3 * 256, KVQ_RANK_MOST = 512;
-inline int kvq_waves(int64_t groups) { return groups <= 256 ? 8 : 4; }  // waves of a work group: eight where there is one for a CU at most
+// Rows are started longest first where the GPU does not hold all work groups at
+// once and the longest rows take a while: up to this many rows, and from so many
+// positions on.
+constexpr int KVQ_RESIDENT = 3 * 256, KVQ_RANK_MOST = 256, KVQ_RANK_FROM = 2048;
 typedef const __attribute__((address_space(4))) int64_t ConstI64;
 
 // as dma_1k_stream, four bytes a lane
@@ -274,27 +274,46 @@ __device__ __forceinline__ uint32_t take_part(float &f0, float &f1) {
   return w;
 }
 
-// The z-th longest row (the lower number first among equals), found by the work
-// group itself: every thread ranks a few rows against all.
-__device__ __forceinline__ int kvq_ranked_row(const KvqAttn &a, int z, int *s_len /* [KVQ_RANK_MOST + 1] */) {
-  int &s_row = s_len[KVQ_RANK_MOST];
-  const int n4 = (a.n + 3) & ~3;
-  for (int r = threadIdx.x; r < n4; r += blockDim.x) s_len[r] = r < a.n ? kvq_length(a, r, a.seqs ? a.seqs[r] : r) : -1;
-  __syncthreads();
-  for (int r = threadIdx.x; r < a.n; r += blockDim.x) {
-    const int mine = s_len[r];
-    int rank = 0;
-    for (int o = 0; o < n4; o += 4) {
-      const u32x4 w = *(const u32x4 *)&s_len[o];
+// past the caches of one XCD
+__device__ __forceinline__ void st_agent(float *p, float v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float ld_agent(const float *p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// The z-th longest row (the lower number first among equals) of at most 256, which
+// every wave finds by itself: the largest length that more than z rows reach, bit by
+// bit, then the row among those of that length.
+__device__ __forceinline__ int kvq_ranked_row(const KvqAttn &a, int z) {
+  constexpr int PER = KVQ_RANK_MOST / 64;
+  const int lane = threadIdx.x & 63;
+  int len[PER];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) rank += (int)w[e] > mine || ((int)w[e] == mine && o + e < r);
-    }
-    if (rank == z) s_row = r;
+  for (int k = 0; k < PER; ++k) {
+    const int r = k * 64 + lane;
+    len[k] = r < a.n ? max(kvq_length(a, r, a.seqs ? a.seqs[r] : r), 0) : -1;
   }
-  __syncthreads();
-  const int row = __builtin_amdgcn_readfirstlane(s_row);
-  __syncthreads();
-  return row;
+  auto reach = [&](int v) {
+    int n = 0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) n += (int)__popcll(__ballot(len[k] >= v));
+    return n;
+  };
+  int t = 0;
+  for (int b = 31 - __builtin_clz(a.max_len); b >= 0; --b)
+    if (reach(t | 1 << b) > z) t |= 1 << b;
+  int left = z - reach(t + 1), row = 0;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const uint64_t same = __ballot(len[k] == t);
+    const int n = (int)__popcll(same);
+    if (left >= 0 && left < n)
+      row = k * 64 + (int)__builtin_ctzll(__ballot(((same >> lane) & 1) &&
+                                                   (int)__popcll(same & ((1ull << lane) - 1)) == left));
+    left -= n;
+  }
+  return __builtin_amdgcn_readfirstlane(row);
 }
 
 template <int DT, int HD, int NW, bool WIDE>
@@ -306,23 +325,51 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
   constexpr int SB = DT == HS_F32 ? 4 : 2;
   constexpr int PLANE = 4 * SPAN;
   __shared__ __align__(1024) unsigned char s_mem[NW * KVQ_PLANES * PLANE];
-  static_assert(sizeof(s_mem) >= (KVQ_RANK_MOST + 1) * 4, "the lengths fit");
   const int G = a.n_heads / a.c.n_kv;
   // every row's first split comes before any row's second: the empty ones are last
   const int64_t bid = blockIdx.x, per = (int64_t)a.n * a.c.n_kv;
   const int split = (int)(bid / per), j = (int)(bid % a.c.n_kv);
   const int z = (int)(bid % per / a.c.n_kv);
-  const int row = a.order ? a.order[z] : a.rank ? kvq_ranked_row(a, z, (int *)s_mem) : z;
+  const int row = a.order ? a.order[z] : a.rank ? kvq_ranked_row(a, z) : z;
   const int lane = threadIdx.x & 63, li = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int seq = a.seqs ? a.seqs[row] : row;
-  const int len = kvq_length(a, row, seq);
   const int t0 = split * a.S;
+  // the first tiles' block numbers are asked for beside the length
+  // (through the scalar cache: the copies below clobber memory for all that the compiler knows)
+  constexpr int NB = WIDE ? 1 : 4;  // of a tile: its block, or its spans' blocks
+  struct Ids {
+    int64_t id[NB];
+  };
+  const bool known = (uint32_t)seq < (uint32_t)a.c.n_seqs;
+  const ConstI64 *tab = (const ConstI64 *)(uintptr_t)(a.c.table + (known ? (int64_t)seq * a.c.table_ld : 0));
+  const int room = (int)min((int64_t)a.c.table_ld << a.c.bt_log2, (int64_t)INT32_MAX);
+  auto lookup = [&](int t, int before) {  // places from `before` on have none
+    Ids w;
+#pragma unroll
+    for (int s = 0; s < NB; ++s) {
+      const int p = t0 + t * KVQ_TILE + s * 16;
+      w.id[s] = p < before ? tab[p >> a.c.bt_log2] : -1;
+    }
+    return w;
+  };
+  auto settle = [&](Ids w, int t, int end) {
+#pragma unroll
+    for (int s = 0; s < NB; ++s)
+      if (t0 + t * KVQ_TILE + s * 16 >= end || (uint64_t)w.id[s] >= (uint64_t)a.c.n_blocks) w.id[s] = -1;
+    return w;
+  };
+  const Ids first = lookup(wave, room), second = lookup(wave + NW, room);
+  const int len = kvq_length(a, row, seq);
   const int64_t rh = (int64_t)row * a.n_heads + j * G;  // first (row, head) of the group
+  // the row's splits that have a position; a single one writes the output itself,
+  // unless every split's partial is wanted (a.nat)
+  const int live = a.nat ? a.n_split : max(1, (len + a.S - 1) / a.S);
+  if (split >= live) return;
   if (t0 >= len) {
     for (int i = threadIdx.x; i < G * HD; i += 64 * NW) {
       const int h = i / HD, e = i - h * HD;
-      if (a.n_split == 1) {
+      if (live == 1) {
         st_elem<DT>(a.out, kvq_out_at(a, row, (j * G + h) * HD + e, HD), 0.f);
       } else {
         a.part_o[((rh + h) * a.n_split + split) * HD + e] = 0.f;
@@ -336,8 +383,6 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
   }
   const int end = min(t0 + a.S, len);  // the split's positions: t0 .. end - 1
   const int n_tiles = (end - t0 + KVQ_TILE - 1) / KVQ_TILE;
-  // read through the scalar cache: the copies below clobber memory for all that the compiler knows
-  const ConstI64 *tab = (const ConstI64 *)(uintptr_t)(a.c.table + (int64_t)seq * a.c.table_ld);
   const int64_t kin = ((int64_t)(a.c.layer * 2) * a.c.n_kv + j) << (a.c.bt_log2 - 4);  // spans before the head's
   const int64_t vin = kin + ((int64_t)a.c.n_kv << (a.c.bt_log2 - 4));
   const int in_mask = (1 << a.c.bt_log2) - 1;
@@ -347,21 +392,6 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
   unsigned char *ring = s_mem + wave * (KVQ_PLANES * PLANE);
   const uint32_t ring0 = __builtin_amdgcn_readfirstlane(lds_addr(ring));
   const int kspan = li >> 2, kgrp = HD == 128 ? lg : lg & 1, vgrp = HD == 128 ? li >> 2 : li >> 3;
-  // block numbers of a tile: of its spans, or (WIDE) of the tile
-  constexpr int NB = WIDE ? 1 : 4;
-  struct Ids {
-    int64_t id[NB];
-  };
-  auto find = [&](int t) {
-    Ids w;
-#pragma unroll
-    for (int s = 0; s < NB; ++s) {
-      const int p = t0 + t * KVQ_TILE + s * 16;
-      w.id[s] = p < end ? tab[p >> a.c.bt_log2] : -1;
-      if ((uint64_t)w.id[s] >= (uint64_t)a.c.n_blocks) w.id[s] = -1;
-    }
-    return w;
-  };
   // K (v = 0) or V of tile t into plane `slot` of the ring
   auto copy = [&](int t, const Ids &w, int v, int slot) {
     const int p0 = t0 + t * KVQ_TILE;
@@ -398,14 +428,14 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
   // V of the wave's tiles in turn) follows as soon as plane x is read.  After the
   // wait for a plane at most two that were asked for later are in flight.
   static_assert(KVQ_PLANES == 3, "the order of the copies below");
-  Ids nxt = find(wave + NW);
+  Ids nxt = settle(second, wave + NW, end);
   auto held_of = [&](const Ids &w) {  // bit s: span s has a block
     if constexpr (WIDE) return w.id[0] >= 0 ? 15u : 0u;
     else return (w.id[0] >= 0 ? 1u : 0u) | (w.id[1] >= 0 ? 2u : 0u) | (w.id[2] >= 0 ? 4u : 0u) | (w.id[3] >= 0 ? 8u : 0u);
   };
   uint32_t held_cur;
   {
-    const Ids cur = find(wave);
+    const Ids cur = settle(first, wave, end);
     held_cur = held_of(cur);
     if (wave < n_tiles) {
       copy(wave, cur, 0, 0);
@@ -464,7 +494,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
     const bool one = t + NW < n_tiles, two = t + 2 * NW < n_tiles;  // tiles that follow
     const int vslot = next_slot(slot);
     const unsigned char *kp = ring + slot * PLANE, *vp = ring + vslot * PLANE;
-    const Ids far = find(t + 2 * NW);
+    const Ids far = settle(lookup(t + 2 * NW, end), t + 2 * NW, end);
     if (one) wait_copies<2 * COPIES>();  // V, and the next tile's K
     else wait_copies<COPIES>();
     u32x4 kc[4];
@@ -633,16 +663,66 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
       num += wt * s_o[w][h][e];
       den += wt * s_l[w][h];
     }
-    if (a.n_split == 1) {
-      // no position held: zeros
+    const float mp = den == 0.f ? -INFINITY : a.nat ? M * 0.693147180559945309f : M;  // -inf: no position held
+    const int64_t at = (rh + h) * a.n_split + split;
+    if (live == 1) {
       st_elem<DT>(a.out, kvq_out_at(a, row, (j * G + h) * HD + e, HD), den == 0.f ? 0.f : num / den);
-    } else {
-      a.part_o[((rh + h) * a.n_split + split) * HD + e] = num;
+    } else if (a.count) {
+      st_agent(&a.part_o[at * HD + e], num);
       if (e == 0) {
-        a.part_ml[((rh + h) * a.n_split + split) * 2] = den == 0.f ? -INFINITY : a.nat ? M * 0.693147180559945309f : M;
-        a.part_ml[((rh + h) * a.n_split + split) * 2 + 1] = den;
+        st_agent(&a.part_ml[at * 2], mp);
+        st_agent(&a.part_ml[at * 2 + 1], den);
+      }
+    } else {
+      a.part_o[at * HD + e] = num;
+      if (e == 0) {
+        a.part_ml[at * 2] = mp;
+        a.part_ml[at * 2 + 1] = den;
       }
     }
+  }
+  if (!a.count || live == 1) return;
+  // The row's last work group to arrive joins the splits.  Partials are stored and
+  // read at agent scope, past the caches of one XCD; each wave's are done before
+  // the barrier, behind which one thread counts the work group in.
+  int &s_last = *(int *)&s_m[0][0];
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    uint32_t *c = a.count + (int64_t)row * a.c.n_kv + j;
+    const bool last = __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(live - 1);
+    if (last) __hip_atomic_store(c, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next call
+    s_last = last;
+  }
+  __syncthreads();
+  if (!s_last) return;
+  float *jm = (float *)s_mem, *jl = jm + 16 * KVQ_JOIN_SPLITS;
+  static_assert(sizeof(s_mem) >= 2 * 16 * KVQ_JOIN_SPLITS * 4, "maxima and sums of the splits");
+  for (int i = threadIdx.x; i < G * live; i += 64 * NW) {
+    const int h = i / live, s = i - h * live;
+    jm[h * KVQ_JOIN_SPLITS + s] = ld_agent(&a.part_ml[((rh + h) * a.n_split + s) * 2]);
+    jl[h * KVQ_JOIN_SPLITS + s] = ld_agent(&a.part_ml[((rh + h) * a.n_split + s) * 2 + 1]);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < G * HD; i += 64 * NW) {
+    const int h = i / HD, e = i - h * HD;
+    const float *hm = jm + h * KVQ_JOIN_SPLITS, *hl = jl + h * KVQ_JOIN_SPLITS;
+    float M = -FLT_MAX;
+    for (int s = 0; s < live; ++s) M = fmaxf(M, hm[s]);
+    float num = 0.f, den = 0.f;
+    constexpr int AHEAD = 8;
+    for (int s0 = 0; s0 < live; s0 += AHEAD) {
+      float v[AHEAD];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) v[u] = ld_agent(&a.part_o[((rh + h) * a.n_split + min(s0 + u, live - 1)) * HD + e]);
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const float w = s0 + u < live ? __builtin_amdgcn_exp2f(hm[min(s0 + u, live - 1)] - M) : 0.f;
+        num += w * v[u];
+        den += w * hl[min(s0 + u, live - 1)];
+      }
+    }
+    st_elem<DT>(a.out, kvq_out_at(a, row, (j * G + h) * HD + e, HD), den == 0.f ? 0.f : num / den);
   }
 }
 
@@ -655,8 +735,10 @@ __global__ __launch_bounds__(256) void k_kvq_combine(KvqAttn a) {
   __shared__ float s_w[KVQ_MAX_SPLITS];
   __shared__ float s_m[4], s_d[4];
   __shared__ __align__(16) float s_n[PARTS][HD];
-  const int h = blockIdx.x % a.n_heads, ns = a.n_split;
-  const int64_t row = blockIdx.x / a.n_heads, base = (row * a.n_heads + h) * ns;
+  const int h = blockIdx.x % a.n_heads;
+  const int64_t row = blockIdx.x / a.n_heads, base = (row * a.n_heads + h) * a.n_split;
+  const int ns = (kvq_length(a, row, a.seqs ? a.seqs[row] : (int)row) + a.S - 1) / a.S;
+  if (ns <= 1) return;  // written already
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c = threadIdx.x % TPS, part = threadIdx.x / TPS;
   static_assert(KVQ_MAX_SPLITS <= 256, "one split's maximum and sum per thread");
@@ -719,6 +801,10 @@ hipError_t kvq_rows_any(int dtype, int hd, const KvqRows &a, bool read, hipStrea
   return hipErrorInvalidValue;
 }
 
+// Waves of a work group: eight while there are no more pairs than CUs, four where
+// several work groups share a CU (their LDS holds three).
+int kvq_waves(int64_t pairs) { return pairs <= 256 ? 8 : 4; }
+
 template <int DT, int HD, int NW>
 void kvq_attn_start(const KvqAttn &a, uint32_t grid, hipStream_t st) {
   if ((1 << a.c.bt_log2) >= KVQ_TILE) HS_LAUNCH((k_kvq_attn<DT, HD, NW, true>), dim3(grid), dim3(64 * NW), 0, st, a);
@@ -728,8 +814,9 @@ template <int DT, int HD>
 hipError_t kvq_attn_hd(KvqAttn a, hipStream_t st) {
   const int64_t grid = (int64_t)a.n * a.c.n_kv * a.n_split;
   if (grid > INT32_MAX || a.n_split > KVQ_MAX_SPLITS) return hipErrorInvalidValue;
-  a.rank = !a.order && a.n_split == 1 && a.n > 1 && a.n <= KVQ_RANK_MOST && grid > KVQ_RESIDENT;
-  if (kvq_waves((int64_t)a.n * a.c.n_kv * a.n_split) == 8) kvq_attn_start<DT, HD, 8>(a, (uint32_t)grid, st);
+  a.rank = !a.order && a.n_split == 1 && a.n > 1 && a.n <= KVQ_RANK_MOST && a.max_len >= KVQ_RANK_FROM &&
+           grid > KVQ_RESIDENT;
+  if (kvq_waves((int64_t)a.n * a.c.n_kv) == 8) kvq_attn_start<DT, HD, 8>(a, (uint32_t)grid, st);
   else kvq_attn_start<DT, HD, 4>(a, (uint32_t)grid, st);
   return hipGetLastError();
 }
@@ -771,15 +858,16 @@ __global__ __launch_bounds__(256) void k_kvq_stage(PackedRows pk, int hd, KvqSta
 }  // namespace
 
 
-// Splits: as many as bring two waves to each of the 1024 SIMDs, but none shorter
-// than four tiles for each wave of the work group: joining splits takes a second
-// kernel.
+// Splits where there are at most half as many (row, KV head) pairs as CUs: as many
+// as the CUs hold at once (a work group of eight waves takes one), but none without
+// a tile for each of its waves, and none up to 1024 positions, where joining takes
+// the time of the two tiles a wave that it would save (one row of 768, 32/32 heads:
+// 9.2 us whole, 10.1 in two).
 void kvq_split_policy(int64_t n, int n_kv, int max_len, int *S, int *n_split) {
   const int64_t pairs = std::max<int64_t>(1, n * n_kv);
-  const int nw = kvq_waves(pairs);
-  const int64_t want = (2048 + pairs * nw - 1) / (pairs * nw), least = 4 * nw * KVQ_TILE;
-  const int64_t most = ((int64_t)max_len + least - 1) / least;
-  const int64_t ns = std::max<int64_t>(1, std::min(std::min(want, most), (int64_t)KVQ_MAX_SPLITS));
+  constexpr int LEAST = 8 * KVQ_TILE;
+  const int64_t most = max_len <= 2 * LEAST ? 1 : ((int64_t)max_len + LEAST - 1) / LEAST;
+  const int64_t ns = std::max<int64_t>(1, std::min(std::min(256 / pairs, most), (int64_t)KVQ_MAX_SPLITS));
   const int64_t s = ((max_len + ns - 1) / ns + 255) / 256 * 256;
   *S = (int)std::min<int64_t>(s, 1 << 30);
   *n_split = (int)((max_len + s - 1) / s);

@@ -554,12 +554,13 @@ class QuantCache:
         codes = range(HS_F32, HS_BF16 + 1) if dtype is None else (_dtype_code("QuantCache.attention_workspace",
                                                                               torch.empty(0, dtype=dtype)),)
         most = max(self._workspace_bytes(dt, n, n_heads, max_len) for dt in codes)
-        return torch.empty(most, dtype=torch.uint8, device=self.blocks.device)
+        return torch.zeros(most, dtype=torch.uint8, device=self.blocks.device)
 
     def attention(self, layer: int, q, lengths, seqs=None, max_len=None, scale=None, out=None, workspace=None):
         """Decode attention of q ([n][n_heads][head_dim]) over the first lengths (int32 [n]) positions of sequences
-        seqs; max_len bounds the lengths (None: what the table holds), scale None: head_dim ** -0.5.  A workspace may
-        be kept from call to call (attention_workspace), not shared by calls on several streams."""
+        seqs; max_len bounds the lengths (None: what the table holds), scale None: head_dim ** -0.5.  A workspace
+        (attention_workspace) may be kept from call to call, which saves clearing a new one; calls on several streams
+        do not share one."""
         import torch
         func = "QuantCache.attention"
         device, hd = self.blocks.device, self.head_dim
@@ -579,6 +580,7 @@ class QuantCache:
         ln, sq = _int32(func, "lengths", lengths, n, device), _int32(func, "seqs", seqs, n, device)
         if workspace is None:
             workspace = torch.empty(self._workspace_bytes(dt, n, heads, max_len), dtype=torch.uint8, device=device)
+            workspace[:2048].zero_()
         elif workspace.device != device or not workspace.is_contiguous():
             raise ValueError(f"{func}: workspace must be contiguous on {device}")
         rc = _on_device(func, device, lambda st: self._lib.hs_kvq_attention(

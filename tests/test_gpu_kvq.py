@@ -336,10 +336,14 @@ def test_calls_are_deterministic_and_run_on_the_current_stream():
         b = cache.attention(0, q, lens)
     torch.cuda.current_stream().wait_stream(side)
     assert torch.equal(a, want) and torch.equal(b, want)
-    ws = cache.attention_workspace(3, 28, 3000, torch.bfloat16).fill_(0xFF)
+    ws = cache.attention_workspace(3, 28, 3000, torch.bfloat16)
+    ws[2048:].fill_(0xFF)  # only the first 2048 bytes are kept between calls
     c = cache.attention(0, q, lens, max_len=3000, workspace=ws)
     d = cache.attention(0, q, lens, max_len=3000, workspace=ws)
-    assert torch.equal(c, d)
+    assert torch.equal(c, d) and not ws[:2048].any()
+    # the same workspace serves another shape, and the first one again
+    fill_and_check(hs, "f16", [1200, 5, 700, 900], 4, 4, 64, 16, seed=16, workspace=ws)
+    assert torch.equal(cache.attention(0, q, lens, max_len=3000, workspace=ws), c)
 
 
 def test_append_and_attention_in_a_replayed_graph():
