@@ -447,25 +447,29 @@ def _dtype_code(func: str, t) -> int:
     raise ValueError(f"{func}: {t.dtype} is none of float32, float16, bfloat16")
 
 
-def _int32(func: str, name: str, t, n: int, device):
-    """Address of a contiguous int32 tensor of n values on the device (None: NULL)."""
+def _int32(func: str, name: str, t, n: int, index: int):
+    """Address of a contiguous int32 tensor of n values on GPU `index` (None: NULL)."""
     import torch
     if t is None:
         return None
-    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous() or t.device != device:
-        raise ValueError(f"{func}: {name} must be {n} contiguous int32 values on {device}")
+    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous() or t.get_device() != index:
+        raise ValueError(f"{func}: {name} must be {n} contiguous int32 values on GPU {index}")
     return t.data_ptr()
 
 
-def _on_device(func: str, device, call):
-    """call(stream), with the tensors' device current."""
+def _on_device(func: str, name: str, index: int, *args) -> None:
+    """Calls the library's function `name` with args and the current stream of GPU `index`, that GPU current."""
     import torch
-    if device.type != "cuda":
+    if index < 0:
         raise ValueError(f"{func}: tensors must be on the GPU")
-    if device.index == torch.cuda.current_device():
-        return call(torch.cuda.current_stream().cuda_stream)
-    with torch.cuda.device(device):
-        return call(torch.cuda.current_stream().cuda_stream)
+    stream = torch._C._cuda_getCurrentRawStream(index)
+    if index == torch.cuda.current_device():
+        rc = getattr(_lib, name)(*args, stream)
+    else:
+        with torch.cuda.device(index):
+            rc = getattr(_lib, name)(*args, stream)
+    if rc != HS_OK:
+        check(name, rc)
 
 
 def kvq_block_bytes(n_layers: int, n_kv_heads: int, head_dim: int, block_tokens: int) -> int:
@@ -492,60 +496,59 @@ class QuantCache:
         kvq_block_bytes(n_layers, n_kv_heads, head_dim, block_tokens)  # checks the sizes
         self.blocks, self.table = blocks, table  # keeps the tensors alive
         self.n_layers, self.n_kv_heads, self.head_dim, self.block_tokens = n_layers, n_kv_heads, head_dim, block_tokens
+        self._index = blocks.get_device()
         self._c = hs_kvq_cache(blocks.data_ptr(), blocks.numel(), table.data_ptr(), table.shape[0], table.shape[1],
                                n_layers, n_kv_heads, head_dim, block_tokens)
         self._ref = ctypes.addressof(self._c)
-        self._lib = lib()
 
     def _check_rows(self, func: str, k, v):
-        """k, v: [n][n_kv_heads][head_dim], equal strides, channels contiguous."""
-        if k.dim() != 3 or k.shape[1] != self.n_kv_heads or k.shape[2] != self.head_dim or v.shape != k.shape or \
-                v.dtype != k.dtype or k.stride(2) != 1 or v.stride() != k.stride() or \
-                k.device != self.blocks.device or v.device != k.device:
+        """k, v: [n][n_kv_heads][head_dim], equal strides, channels contiguous; returns (n, strides)."""
+        shape, stride = k.shape, k.stride()
+        if len(shape) != 3 or shape[1] != self.n_kv_heads or shape[2] != self.head_dim or v.shape != shape or \
+                v.dtype != k.dtype or stride[2] != 1 or v.stride() != stride or \
+                k.get_device() != self._index or v.get_device() != self._index:
             raise ValueError(f"{func}: k and v must be [n][{self.n_kv_heads}][{self.head_dim}] on {self.blocks.device}, "
                              "of one type and equal strides, channels contiguous")
+        return shape[0], stride
 
     def append(self, layer: int, k, v, positions, seqs=None, k_values=None, v_values=None) -> None:
         """Stores rows of K and V ([n][n_kv_heads][head_dim]) at positions (int32 [n]) of sequences seqs (int32 [n];
         None: row i is sequence i).  k_values / v_values (of k's strides; may be k and v) receive the stored values."""
         func = "QuantCache.append"
-        self._check_rows(func, k, v)
+        n, stride = self._check_rows(func, k, v)
+        kv = vv = None
         if k_values is not None or v_values is not None:
             if k_values is None or v_values is None:
                 raise ValueError(f"{func}: k_values and v_values are given together")
-            self._check_rows(func, k_values, v_values)
-            if k_values.dtype != k.dtype or k_values.shape != k.shape or k_values.stride() != k.stride():
+            if self._check_rows(func, k_values, v_values) != (n, stride) or k_values.dtype != k.dtype:
                 raise ValueError(f"{func}: k_values and v_values must be laid out as k")
-        n, dt, device = k.shape[0], _dtype_code(func, k), k.device
-        pos, sq = _int32(func, "positions", positions, n, device), _int32(func, "seqs", seqs, n, device)
-        kv, vv = (None, None) if k_values is None else (k_values.data_ptr(), v_values.data_ptr())
-        rc = _on_device(func, device, lambda st: self._lib.hs_kvq_append(
-            self._ref, layer, dt, n, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), sq, pos, kv, vv, st))
-        check("hs_kvq_append", rc)
+            kv, vv = k_values.data_ptr(), v_values.data_ptr()
+        index = self._index
+        _on_device(func, "hs_kvq_append", index, self._ref, layer, _dtype_code(func, k), n, k.data_ptr(), v.data_ptr(),
+                   stride[0], stride[1], _int32(func, "seqs", seqs, n, index),
+                   _int32(func, "positions", positions, n, index), kv, vv)
 
     def read(self, layer: int, positions, dtype, seqs=None, k=None, v=None):
         """The rows at positions of sequences seqs, as (k, v) of a torch dtype (or into k and v)."""
         import torch
         func = "QuantCache.read"
-        n, device = positions.numel(), self.blocks.device
+        n, index = positions.numel(), self._index
         if k is None:
-            k = torch.empty(n, self.n_kv_heads, self.head_dim, dtype=dtype, device=device)
+            k = torch.empty((n, self.n_kv_heads, self.head_dim), dtype=dtype, device=self.blocks.device)
         if v is None:
-            v = torch.empty_strided(k.shape, k.stride(), dtype=k.dtype, device=device)
-        self._check_rows(func, k, v)
-        if k.shape[0] != n or k.dtype != dtype:
+            v = torch.empty_like(k) if k.is_contiguous() else torch.empty_strided(k.shape, k.stride(), dtype=k.dtype,
+                                                                                 device=k.device)
+        rows, stride = self._check_rows(func, k, v)
+        if rows != n or k.dtype != dtype:
             raise ValueError(f"{func}: k and v must hold {n} rows of {dtype}")
-        dt = _dtype_code(func, k)
-        pos, sq = _int32(func, "positions", positions, n, device), _int32(func, "seqs", seqs, n, device)
-        rc = _on_device(func, device, lambda st: self._lib.hs_kvq_read(
-            self._ref, layer, dt, n, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), sq, pos, st))
-        check("hs_kvq_read", rc)
+        _on_device(func, "hs_kvq_read", index, self._ref, layer, _dtype_code(func, k), n, k.data_ptr(), v.data_ptr(),
+                   stride[0], stride[1], _int32(func, "seqs", seqs, n, index),
+                   _int32(func, "positions", positions, n, index))
         return k, v
 
     def _workspace_bytes(self, dt: int, n: int, n_heads: int, max_len: int) -> int:
         out = ctypes.c_uint64()
-        check("hs_kvq_attention_workspace", self._lib.hs_kvq_attention_workspace(self._ref, dt, n, n_heads, max_len,
-                                                                                ctypes.byref(out)))
+        _call("hs_kvq_attention_workspace", self._ref, dt, n, n_heads, max_len, ctypes.byref(out))
         return out.value
 
     def attention_workspace(self, n: int, n_heads: int, max_len: int, dtype=None):
@@ -563,30 +566,28 @@ class QuantCache:
         do not share one."""
         import torch
         func = "QuantCache.attention"
-        device, hd = self.blocks.device, self.head_dim
-        if q.dim() != 3 or q.shape[2] != hd or q.stride(2) != 1 or (q.shape[1] > 1 and q.stride(1) != hd) or \
-                q.device != device:
-            raise ValueError(f"{func}: q must be [n][n_heads][{hd}] on {device}, each row contiguous")
+        index, hd, shape, stride = self._index, self.head_dim, q.shape, q.stride()
+        if len(shape) != 3 or shape[2] != hd or stride[2] != 1 or (shape[1] > 1 and stride[1] != hd) or \
+                q.get_device() != index:
+            raise ValueError(f"{func}: q must be [n][n_heads][{hd}] on {self.blocks.device}, each row contiguous")
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=device)
-        elif out.shape != q.shape or out.dtype != q.dtype or out.device != device or out.stride(2) != 1 or \
-                (q.shape[1] > 1 and out.stride(1) != hd):
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        elif out.shape != shape or out.dtype != q.dtype or out.get_device() != index or out.stride(2) != 1 or \
+                (shape[1] > 1 and out.stride(1) != hd):
             raise ValueError(f"{func}: out must be of q's shape and type, each row contiguous")
-        n, heads, dt = q.shape[0], q.shape[1], _dtype_code(func, q)
+        n, heads, dt = shape[0], shape[1], _dtype_code(func, q)
         if max_len is None:
             max_len = min(self.table.shape[1] * self.block_tokens, 2**31 - 1)
-        if scale is None:
-            scale = hd ** -0.5
-        ln, sq = _int32(func, "lengths", lengths, n, device), _int32(func, "seqs", seqs, n, device)
         if workspace is None:
-            workspace = torch.empty(self._workspace_bytes(dt, n, heads, max_len), dtype=torch.uint8, device=device)
+            workspace = torch.empty(self._workspace_bytes(dt, n, heads, max_len), dtype=torch.uint8,
+                                    device=self.blocks.device)
             workspace[:2048].zero_()
-        elif workspace.device != device or not workspace.is_contiguous():
-            raise ValueError(f"{func}: workspace must be contiguous on {device}")
-        rc = _on_device(func, device, lambda st: self._lib.hs_kvq_attention(
-            self._ref, layer, dt, n, heads, q.data_ptr(), q.stride(0), sq, ln, max_len, scale, out.data_ptr(),
-            out.stride(0), workspace.data_ptr() or None, workspace.numel() * workspace.element_size(), st))
-        check("hs_kvq_attention", rc)
+        elif workspace.get_device() != index or not workspace.is_contiguous():
+            raise ValueError(f"{func}: workspace must be contiguous on {self.blocks.device}")
+        _on_device(func, "hs_kvq_attention", index, self._ref, layer, dt, n, heads, q.data_ptr(), stride[0],
+                   _int32(func, "seqs", seqs, n, index), _int32(func, "lengths", lengths, n, index), max_len,
+                   hd ** -0.5 if scale is None else scale, out.data_ptr(), out.stride(0), workspace.data_ptr(),
+                   workspace.nbytes)
         return out
 
 
@@ -612,21 +613,21 @@ def token_logprobs(logits, tokens=None, top: int = 0, workspace=None):
     if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError(f"{func}: logits must be [rows][vocab], each row contiguous")
     rows, vocab = logits.shape
-    device, dt = logits.device, _dtype_code(func, logits)
-    tk = _int32(func, "tokens", tokens, rows, device)
-    lp = None if tokens is None else torch.empty(rows, dtype=torch.float32, device=device)
-    entropy = torch.empty(rows, dtype=torch.float32, device=device)
-    ids = torch.empty(rows, top, dtype=torch.int32, device=device) if top > 0 else None
-    tops = torch.empty(rows, top, dtype=torch.float32, device=device) if top > 0 else None
+    index, dt = logits.get_device(), _dtype_code(func, logits)
+    tk = _int32(func, "tokens", tokens, rows, index)
+    lp = None if tokens is None else torch.empty_like(tokens, dtype=torch.float32)
+    entropy = logits.new_empty((rows,), dtype=torch.float32) if lp is None else torch.empty_like(lp)
+    ids = tops = None
+    if top > 0:
+        tops = logits.new_empty((rows, top), dtype=torch.float32)
+        ids = torch.empty_like(tops, dtype=torch.int32)
     if workspace is None:
-        workspace = torch.empty(_logprobs_bytes(rows, vocab, top), dtype=torch.uint8, device=device)
-    elif workspace.device != device or not workspace.is_contiguous():
-        raise ValueError(f"{func}: workspace must be contiguous on {device}")
-    rc = _on_device(func, device, lambda st: lib().hs_token_logprobs(
-        dt, logits.data_ptr(), rows, vocab, logits.stride(0), tk, top, None if lp is None else lp.data_ptr(),
-        entropy.data_ptr(), None if ids is None else ids.data_ptr(), None if tops is None else tops.data_ptr(),
-        workspace.data_ptr() or None, workspace.numel() * workspace.element_size(), st))
-    check("hs_token_logprobs", rc)
+        workspace = logits.new_empty((_logprobs_bytes(rows, vocab, top),), dtype=torch.uint8)
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError(f"{func}: workspace must be contiguous on the logits' device")
+    _on_device(func, "hs_token_logprobs", index, dt, logits.data_ptr(), rows, vocab, logits.stride(0), tk, top,
+               None if lp is None else lp.data_ptr(), entropy.data_ptr(), None if ids is None else ids.data_ptr(),
+               None if tops is None else tops.data_ptr(), workspace.data_ptr(), workspace.nbytes)
     return lp, entropy, ids, tops
 
 
