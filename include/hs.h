@@ -439,7 +439,8 @@ int hs_kvq_pool_create(hs_model *m, int32_t slots, int32_t block_tokens, void *d
  * probability 0.  A row that holds a NaN or +inf, or nothing but -inf, has no
  * distribution: its values are NaN (a negative token's 0 stays) and its ids -1.
  * Everything is computed in fp32 from the exact logits.  workspace: device
- * memory of hs_token_logprobs_workspace bytes, as in hs_kvq_attention. */
+ * memory of hs_token_logprobs_workspace bytes under the rules of
+ * hs_kvq_attention's, its first 2048 bytes zero before its first use. */
 int hs_token_logprobs_workspace(int64_t rows, int32_t vocab, int32_t top, uint64_t *bytes);
 int hs_token_logprobs(int32_t dtype, const void *logits, int64_t rows, int32_t vocab, int64_t ld,
                       const int32_t *tokens, int32_t top, float *logprob, float *entropy, int32_t *top_ids,

@@ -744,7 +744,8 @@ int hs_model_create(const hs_config *cfg, const hs_weights *w, int32_t max_batch
   // past K against zero weight rows: those elements must hold finite values
   // (they are never written, so cleared once here)
   if (hipMemcpy(m->rope_tab, tab.data(), tab.size() * 4, hipMemcpyHostToDevice) != hipSuccess ||
-      hipMemset(m->status, 0, 4) != hipSuccess || hipMemset(m->attn, 0, (size_t)act_elems(rows, nh * hd) * b) ||
+      hipMemset(m->status, 0, 4) != hipSuccess ||
+      (m->lp_ws && hipMemset(m->lp_ws, 0, LOGPROB_COUNTERS * 4) != hipSuccess) || hipMemset(m->attn, 0, (size_t)act_elems(rows, nh * hd) * b) ||
       hipMemset(m->act, 0, (size_t)act_elems(rows, c.ffn_dim) * b) ||
       hipMemset(m->hnorm, 0, (size_t)act_elems(rows, c.d_model) * b)) {
     free_model(m);
@@ -1103,7 +1104,6 @@ static int decode_impl(hs_model *m, hs_kv *kv, const int32_t *tokens_in, int32_t
       a.vocab = c.vocab;
       if (!a.tokens) a.tokens = tokens_out;
       a.act = act;
-      a.parts = logprob_parts(c.vocab);
       a.ws = m->lp_ws;
       HIP_TRY(launch_logprobs(HS_F32, a, st));
     }
@@ -1623,7 +1623,6 @@ int hs_token_logprobs(int32_t dtype, const void *logits, int64_t rows, int32_t v
   a.entropy = entropy;
   a.top_ids = top_ids;
   a.top_logprobs = top_logprobs;
-  a.parts = logprob_parts(vocab);
   a.ws = workspace;
   HIP_TRY(launch_logprobs(dtype, a, (hipStream_t)stream));
   return HS_OK;

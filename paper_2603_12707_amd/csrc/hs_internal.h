@@ -385,12 +385,14 @@ struct LogprobArgs {
   float *logprob, *entropy;
   int *top_ids;
   float *top_logprobs;
-  int parts;  // logprob_parts(vocab)
-  void *ws;   // logprob_workspace bytes
+  int parts;  // (set by the launcher) parts of a row, at most logprob_parts(vocab)
+  void *ws;   // logprob_workspace bytes, its counters zero between calls
+  int count;  // (set by the launcher) the last work group of a row joins its parts
 };
-// a row is cut into parts of this many elements
+// a row is cut into parts of this many elements at least
 constexpr int LOGPROB_PART = 8192;
 constexpr int LOGPROB_TOP = 64;  // most alternatives
+constexpr int LOGPROB_COUNTERS = 512;  // rows up to which they are joined in one launch
 inline int logprob_parts(int vocab) { return (int)(((int64_t)vocab + LOGPROB_PART - 1) / LOGPROB_PART); }
 uint64_t logprob_workspace(int64_t rows, int vocab, int top);
 hipError_t launch_logprobs(int dtype, const LogprobArgs &a, hipStream_t st);

@@ -59,47 +59,54 @@ __device__ __forceinline__ uint64_t block_max(uint64_t v, uint64_t *s_tmp) {
   return v;
 }
 
-// The k-th largest of the wave's 64 values (k in 1..64), bit by bit.
-__device__ __forceinline__ uint32_t wave_kth(uint32_t v, int k) {
-  uint32_t t = 0;
-  for (int b = 31; b >= 0; --b) {
+// The k-th largest of PER * 64 values, PER to a lane, bit by bit: bits `from` down
+// to `to` of it, those above given.
+template <int PER>
+__device__ __forceinline__ uint32_t wave_kth(const uint32_t (&v)[PER], int k, int from, int to, uint32_t t = 0) {
+  for (int b = from; b >= to; --b) {
     const uint32_t c = t | 1u << b;
-    if ((int)__popcll(__ballot(v >= c)) >= k) t = c;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) n += (int)__popcll(__ballot(v[i] >= c));
+    if (n >= k) t = c;
   }
   return t;
 }
 
 // Hands the `top` largest of the work group's keys to put(rank, key), each once.
-// for_each(f) calls f(key) for the thread's own keys; floor_key is a key that at
-// least `top` of all keys reach.  Keys are distinct.  The keys that reach the
-// floor are gathered in LDS and ranked by counting; where they are more than fit,
-// the largest is taken `top` times.
+// for_each(floor, f) calls f(key) for those of the thread's own keys whose value
+// reaches the floor (or for all of them); at least `top` keys reach floor_key.
+// Keys are distinct.  The keys that reach the floor are gathered in LDS and
+// ranked by counting; where they are more than fit, the largest is taken `top`
+// times.  lds.n is 0 and that is seen by all threads.
+struct SelectLds {
+  __align__(16) uint64_t key[LP_CAND + 8];
+  uint64_t tmp[LP_WAVES];
+  int n;
+};
 template <class ForEach, class Put>
-__device__ __forceinline__ void select_top(int top, uint64_t floor_key, ForEach for_each, Put put) {
-  __shared__ __align__(16) uint64_t s_key[LP_CAND + 2];
-  __shared__ uint64_t s_tmp[LP_WAVES];
-  __shared__ int s_n;
-  __syncthreads();
-  if (threadIdx.x == 0) s_n = 0;
-  __syncthreads();
-  for_each([&](uint64_t key) {
+__device__ __forceinline__ void select_top(SelectLds &lds, int top, uint64_t floor_key, ForEach for_each, Put put) {
+  for_each(key_value(floor_key), [&](uint64_t key) {
     if (key >= floor_key) {
-      const int at = atomicAdd(&s_n, 1);
-      if (at < LP_CAND) s_key[at] = key;
+      const int at = atomicAdd(&lds.n, 1);
+      if (at < LP_CAND) lds.key[at] = key;
     }
   });
   __syncthreads();
-  const int n = s_n;
+  const int n = lds.n;
   if (n <= LP_CAND) {
-    if (threadIdx.x < 2) s_key[n + threadIdx.x] = 0;  // pads the pairs below
-    __syncthreads();
     for (int i = threadIdx.x; i < n; i += LP_THREADS) {
-      const uint64_t mine = s_key[i];
+      const uint64_t mine = lds.key[i];
       int rank = 0;
-      for (int o = 0; o < n; o += 2) {
-        const u32x4 two = *(const u32x4 *)&s_key[o];
-        rank += ((uint64_t)two[1] << 32 | two[0]) > mine;
-        rank += ((uint64_t)two[3] << 32 | two[2]) > mine;
+      for (int o = 0; o < n; o += 8) {
+        u32x4 two[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) two[u] = *(const u32x4 *)&lds.key[o + 2 * u];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          rank += o + 2 * u < n && ((uint64_t)two[u][1] << 32 | two[u][0]) > mine;
+          rank += o + 2 * u + 1 < n && ((uint64_t)two[u][3] << 32 | two[u][2]) > mine;
+        }
       }
       if (rank < top) put(rank, mine);
     }
@@ -108,8 +115,8 @@ __device__ __forceinline__ void select_top(int top, uint64_t floor_key, ForEach 
   uint64_t last = ~0ull;
   for (int k = 0; k < top; ++k) {
     uint64_t best = 0;
-    for_each([&](uint64_t key) { best = key < last ? max(best, key) : best; });
-    last = block_max(best, s_tmp);
+    for_each(key_value(floor_key), [&](uint64_t key) { best = key < last ? max(best, key) : best; });
+    last = block_max(best, lds.tmp);
     if (threadIdx.x == 0) put(k, last);
   }
 }
@@ -132,201 +139,333 @@ __device__ __forceinline__ void put_top(const LogprobArgs &a, int64_t row, bool 
   if (a.top_logprobs) a.top_logprobs[row * a.top + rank] = none ? NAN : key_value(key) - M - lz;
 }
 
-// One work group takes one part of a row, VPT elements a thread, which stay in
-// registers: read once, all loads in flight together.  First the maximum, then
-// the sums, then the alternatives: a wave's top-th largest lane maximum is a
-// value that at least `top` of its elements reach (bit by bit with ballots), so
-// the largest of the waves' is a floor that few elements pass.  A row of one part
-// is finished here.
-template <int DT, int VPT>
-__global__ __launch_bounds__(LP_THREADS) void k_logprobs(LogprobArgs a) {
-  constexpr int VEC = DT == HS_F32 ? 4 : 8, NV = VPT / VEC;
+// a row without a distribution has no alternatives
+__device__ __forceinline__ void put_no_top(const LogprobArgs &a, int64_t row) {
+  for (int k = threadIdx.x; k < a.top; k += LP_THREADS) put_top(a, row, true, 0.f, 0.f, k, 0);
+}
+
+// past the caches of one XCD
+template <class T>
+__device__ __forceinline__ void st_part(T *p, T v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <class T>
+__device__ __forceinline__ T ld_part(const T *p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// the workspace: a counter for each row, the parts' sums, the parts' keys
+__device__ __forceinline__ LogprobPart *row_parts(const LogprobArgs &a, int64_t row) {
+  return (LogprobPart *)((char *)a.ws + LOGPROB_COUNTERS * 4) + row * a.parts;
+}
+__device__ __forceinline__ uint64_t *row_keys(const LogprobArgs &a, int64_t row) {
+  return (uint64_t *)(row_parts(a, a.rows)) + row * a.parts * a.top;
+}
+
+// A work group joins a row's parts.  Every part gave its `top` largest keys in
+// order (elements past the row's end among them: they have the lowest keys).
+// The k-th keys of all parts, k = ceil(top / parts): at least `top` keys reach the
+// least of them.  Every wave joins the sums by itself, the keys are asked for
+// beside them.
+template <int DT>
+__device__ __forceinline__ void join_parts(const LogprobArgs &a, int64_t row, SelectLds &lds) {
+  constexpr int HOLD = 4;  // keys of a thread that stay in registers
+  const int lane = threadIdx.x & 63;
+  const LogprobPart *p = row_parts(a, row);
+  const uint64_t *keys = row_keys(a, row);
+  const int64_t n_keys = (int64_t)a.parts * a.top;
+  uint64_t hold[HOLD];
+#pragma unroll
+  for (int u = 0; u < HOLD; ++u) {
+    const int64_t i = u * LP_THREADS + threadIdx.x;
+    hold[u] = i < n_keys ? ld_part(&keys[i]) : 0;
+  }
+  const int kth = a.top > 0 ? (a.top + a.parts - 1) / a.parts - 1 : 0;
+  // parts lane, lane + 64, ..; the first of them kept
+  auto part = [&](int c) { return LogprobPart{ld_part(&p[c].m), ld_part(&p[c].r), ld_part(&p[c].s1), ld_part(&p[c].bad)}; };
+  const LogprobPart mine = lane < a.parts ? part(lane) : LogprobPart{-INFINITY, 0.f, 0.f, 0.f};
+  uint64_t low = a.top > 0 && lane < a.parts ? ld_part(&keys[(int64_t)lane * a.top + kth]) : ~0ull;
+  float m = mine.m;
+  bool bad = mine.bad != 0.f;
+  for (int c = lane + 64; c < a.parts; c += 64) {
+    m = fmaxf(m, ld_part(&p[c].m));
+    bad |= ld_part(&p[c].bad) != 0.f;
+    if (a.top > 0) low = min(low, ld_part(&keys[(int64_t)c * a.top + kth]));
+  }
+  const float M = wave_max(m);
+  if (__ballot(bad) || M == -INFINITY) {
+    if (threadIdx.x == 0) put_row<DT>(a, row, true, 0.f, 0.f, 0.f);
+    put_no_top(a, row);
+    return;
+  }
+  for (int off = 32; off >= 1; off >>= 1) low = min(low, (uint64_t)__shfl_xor((unsigned long long)low, off));
+  // the first part that holds the maximum leads
+  int lead = mine.m == M ? lane : 0x7FFFFFFF;
+  for (int c = lane + 64; c < a.parts && lead == 0x7FFFFFFF; c += 64)
+    if (ld_part(&p[c].m) == M) lead = c;
+  for (int off = 32; off >= 1; off >>= 1) lead = min(lead, __shfl_xor(lead, off));
+  float r = 0.f, s1 = 0.f;
+  if (lane < a.parts) add_part(mine, M, lane == lead, r, s1);
+  for (int c = lane + 64; c < a.parts; c += 64) add_part(part(c), M, c == lead, r, s1);
+  r = wave_sum(r);
+  s1 = wave_sum(s1);
+  if (threadIdx.x == 0) {
+    put_row<DT>(a, row, false, M, r, s1);
+    lds.n = 0;
+  }
+  if (a.top <= 0) return;
+  __syncthreads();
+  const float lz = log1pf(r);
+  select_top(
+      lds, a.top, low,
+      [&](float floor, auto f) {
+#pragma unroll
+        for (int u = 0; u < HOLD; ++u)
+          if (hold[u]) f(hold[u]);
+        for (int64_t i = HOLD * LP_THREADS + threadIdx.x; i < n_keys; i += LP_THREADS) f(ld_part(&keys[i]));
+      },
+      [&](int rank, uint64_t key) { put_top(a, row, false, M, lz, rank, key); });
+}
+
+// element i of a thread's raw words: as fp32
+template <int DT, int NW>
+__device__ __forceinline__ float raw_elem(const uint32_t (&w)[NW], int i) {
+  if constexpr (DT == HS_F32) return __uint_as_float(w[i]);
+  else return i & 1 ? hi_f32<DT>(w[i >> 1]) : lo_f32<DT>(w[i >> 1]);
+}
+
+// One work group takes one part of a row, NW words a thread, which stay in
+// registers as they are: read once, all loads in flight together.  First the
+// maximum, then the sums, then the alternatives: the top-th largest of the 256
+// threads' own maxima is a value that at least `top` elements reach, and few more
+// (every wave finds it, bit by bit with ballots).  A single alternative is the
+// maximum's first place.  A NaN makes the sum NaN.  A row of one part is finished here; of several, by the last
+// of its work groups to arrive, or by k_logprobs_join.
+template <int DT, int NW>
+__global__ __launch_bounds__(LP_THREADS, 5) void k_logprobs(LogprobArgs a) {
+  constexpr int VEC = DT == HS_F32 ? 4 : 8, VPT = NW * VEC / 4, NV = NW / 4, PART = LP_THREADS * VPT;
   using S = typename Ty<DT>::S;
+  __shared__ SelectLds s_sel;
   __shared__ float s_m[LP_WAVES], s_r[LP_WAVES], s_1[LP_WAVES];
-  __shared__ int s_bad[LP_WAVES], s_lead[LP_WAVES];
-  __shared__ uint64_t s_t[LP_WAVES];
+  __shared__ int s_lead[LP_WAVES], s_last;
+  __shared__ uint32_t s_ord[LP_THREADS];
+  __shared__ int s_first[LP_WAVES];
   const int64_t row = blockIdx.x / (uint32_t)a.parts;
   const int part = (int)(blockIdx.x % (uint32_t)a.parts), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int i0 = part * (LP_THREADS * VPT), n = min(a.vocab - i0, LP_THREADS * VPT);
+  // the last of several parts is read from further ahead, so that it is whole; what
+  // the part before it has counts as lying past the row's end
+  const int i0 = min(part * PART, max(0, a.vocab - PART)), n = min(a.vocab - i0, PART), skip0 = part * PART - i0;
   const S *x = (const S *)a.logits + row * a.ld + i0;
   // element e of vector u: VEC consecutive ones to a thread; rows start anywhere
   auto index = [&](int u, int e) { return (u * LP_THREADS + (int)threadIdx.x) * VEC + e; };
-  float v[VPT];
-  if (n == LP_THREADS * VPT) {
-    struct __attribute__((packed, aligned(sizeof(S)))) Loose {
-      u32x4 w;
-    };
-    u32x4 w[NV];
+  struct __attribute__((packed, aligned(sizeof(S)))) Loose {
+    u32x4 w;
+  };
+  constexpr uint32_t NEG = DT == HS_F32 ? 0xFF800000u : DT == HS_F16 ? 0xFC00FC00u : 0xFF80FF80u;  // -inf
+  uint32_t w[NW];
 #pragma unroll
-    for (int u = 0; u < NV; ++u) w[u] = ((const Loose *)(x + index(u, 0)))->w;
+  for (int u = 0; u < NV; ++u) {
+    if (n == PART || index(u, VEC - 1) < n) {
+      *(u32x4 *)&w[4 * u] = ((const Loose *)(x + index(u, 0)))->w;
+    } else {
 #pragma unroll
-    for (int u = 0; u < NV; ++u) unpack<DT>(w[u], v + u * VEC);
-  } else {
+      for (int k = 0; k < 4; ++k) {
+        w[4 * u + k] = NEG;
+        constexpr int PER = VEC / 4;
+        uint32_t bits = NEG;
 #pragma unroll
-    for (int u = 0; u < NV; ++u)
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) v[u * VEC + e] = index(u, e) < n ? ld_elem<DT>(x, index(u, e)) : -INFINITY;
-  }
-  float tm = -INFINITY;
-  bool bad = false;
-#pragma unroll
-  for (int i = 0; i < VPT; ++i) {
-    tm = fmaxf(tm, v[i]);
-    bad |= !(v[i] < INFINITY);
-  }
-  // the floor of the alternatives
-  if (a.top > 0) {
-    const uint32_t u = __float_as_uint(tm + 0.f), ord = u >> 31 ? ~u : u | 0x80000000u;
-    const uint32_t kth = wave_kth(ord, a.top);
-    uint64_t floor_key = (uint64_t)kth << 32;
-    // lanes that share it: the lowest indices among them come first
-    const int above = (int)__popcll(__ballot(ord > kth)), share = (int)__popcll(__ballot(ord == kth));
-    if (above + share > a.top) {
-      int first = 0x7FFFFFFF;
-      if (ord == kth)
-#pragma unroll
-        for (int i = VPT - 1; i >= 0; --i)
-          if (v[i] == tm) first = index(i / VEC, i % VEC);
-      // the largest complement is the lowest index
-      floor_key |= wave_kth(ord == kth ? (uint32_t)~(i0 + first) : 0u, a.top - above);
+        for (int e = 0; e < PER; ++e)
+          if (index(u, k * PER + e) < n) {
+            const S v = x[index(u, k * PER + e)];
+            if constexpr (DT == HS_F32) bits = __float_as_uint(v);
+            else bits = (bits & ~(0xFFFFu << (16 * e))) | (uint32_t)v << (16 * e);
+          }
+        w[4 * u + k] = bits;
+      }
     }
-    if (lane == 0) s_t[wave] = floor_key;
   }
+  if (skip0) {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+      if (index(i / VEC, i % VEC) < skip0) {
+        if constexpr (DT == HS_F32) w[i] = NEG;
+        else w[i >> 1] = i & 1 ? (w[i >> 1] & 0xFFFFu) | (NEG & 0xFFFF0000u) : (w[i >> 1] & 0xFFFF0000u) | (NEG & 0xFFFFu);
+      }
+  }
+  // an element's index in the row, or past its end
+  auto place = [&](int i) {
+    const int k = index(i / VEC, i % VEC);
+    return k < skip0 ? a.vocab + k : i0 + k;
+  };
+  // the words are opaque from one use to the next: 16-bit elements are unpacked again
+  auto keep = [&] {
+    if constexpr (DT != HS_F32)
+#pragma unroll
+      for (int k = 0; k < NW; ++k) asm volatile("" : "+v"(w[k]));
+  };
+  float tm = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) tm = fmaxf(tm, raw_elem<DT, NW>(w, i));
+  keep();
   const float wm = wave_max(tm);
-  const bool wbad = __ballot(bad) != 0;
-  if (lane == 0) s_m[wave] = wm, s_bad[wave] = wbad;
+  if (lane == 0) s_m[wave] = wm;
+  if (threadIdx.x == 0) s_sel.n = 0;
+  const uint32_t bits = __float_as_uint(tm + 0.f), ord = bits >> 31 ? ~bits : bits | 0x80000000u;
+  if (a.top > 1) s_ord[threadIdx.x] = ord;
   __syncthreads();
   float M = s_m[0];
-  uint64_t floor_key = a.top > 0 ? s_t[0] : 0;
-  bool any_bad = s_bad[0];
 #pragma unroll
-  for (int w = 1; w < LP_WAVES; ++w) {
-    M = fmaxf(M, s_m[w]);
-    any_bad |= s_bad[w] != 0;
-    if (a.top > 0) floor_key = max(floor_key, s_t[w]);
+  for (int w2 = 1; w2 < LP_WAVES; ++w2) M = fmaxf(M, s_m[w2]);
+  // the lowest place of value v among the thread's elements
+  auto first_of = [&](float v) {
+    int first = 0x7FFFFFFF;
+#pragma unroll
+    for (int i = VPT - 1; i >= 0; --i)
+      if (raw_elem<DT, NW>(w, i) == v) first = min(first, place(i));
+    keep();
+    return first;
+  };
+  uint64_t floor_key = 0;
+  if (a.top > 1) {
+    uint32_t all[LP_WAVES];
+#pragma unroll
+    for (int i = 0; i < LP_WAVES; ++i) all[i] = s_ord[i * 64 + lane];
+    auto count = [&](uint32_t c, bool equal) {
+      int n2 = 0;
+#pragma unroll
+      for (int i = 0; i < LP_WAVES; ++i) n2 += (int)__popcll(__ballot(equal ? all[i] == c : all[i] >= c));
+      return n2;
+    };
+    // the upper half of the bits does, unless many threads share it
+    // (no number orders below -inf, whose lower bits are set)
+    constexpr uint32_t LEAST = 0x007FFFFFu;
+    uint32_t kth = max(wave_kth(all, a.top, 31, 16), LEAST);
+    if (count(kth, false) > a.top + 16) kth = max(wave_kth(all, a.top, 15, 0, kth & 0xFFFF0000u), LEAST);
+    floor_key = (uint64_t)kth << 32;
+    const int reach = count(kth, false), share = count(kth, true);
+    if (reach > a.top + 16) {
+      // threads that share all of it: the lowest places among them come first
+      __syncthreads();
+      s_ord[threadIdx.x] = ord == kth ? (uint32_t)~first_of(tm) : 0u;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < LP_WAVES; ++i) all[i] = s_ord[i * 64 + lane];
+      floor_key |= wave_kth(all, a.top - (reach - share), 31, 0);  // the largest complement is the lowest place
+    }
   }
   float r = 0.f, s1 = 0.f;
-  int lead = 0;  // threads that leave out one instance of the maximum
+  bool lead = false;  // leaves one instance of the maximum out of its sum
   if (M > -INFINITY) {
-    int skip = -1;
-    if (tm == M) {
+    if (__ballot(tm == M)) {
+      // a wave that holds the maximum: a thread's first instance of it is left out
 #pragma unroll
-      for (int i = VPT - 1; i >= 0; --i) skip = v[i] == M ? i : skip;
-      lead = 1;
-    }
+      for (int i = 0; i < VPT; ++i) {
+        const float v = raw_elem<DT, NW>(w, i), d = v - M, e = __expf(d);
+        const bool out = v == M && !lead;
+        lead |= out;
+        r += out ? 0.f : e;
+        s1 = __builtin_fmaf(fmaxf(d, LOGPROB_FAR), e, s1);
+      }
+    } else {
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      const float d = fmaxf(v[i] - M, LOGPROB_FAR), e = __expf(d);
-      r += e;
-      s1 = __builtin_fmaf(d, e, s1);
+      for (int i = 0; i < VPT; ++i) {
+        const float d = raw_elem<DT, NW>(w, i) - M, e = __expf(d);
+        r += e;
+        s1 = __builtin_fmaf(fmaxf(d, LOGPROB_FAR), e, s1);
+      }
     }
-    // the instance itself added exactly e^0 = 1: the sum is made again without it
-    if (skip >= 0) {
-      r = 0.f;
-#pragma unroll
-      for (int i = 0; i < VPT; ++i) r += i == skip ? 0.f : __expf(fmaxf(v[i] - M, LOGPROB_FAR));
-    }
+    keep();
   }
   r = wave_sum(r);
   s1 = wave_sum(s1);
   const int wlead = (int)__popcll(__ballot(lead));
-  if (lane == 0) s_r[wave] = r, s_1[wave] = s1, s_lead[wave] = wlead;
+  int first = 0x7FFFFFFF;
+  if (a.top == 1 && wm == M) {
+    first = first_of(M);
+    for (int off = 32; off >= 1; off >>= 1) first = min(first, __shfl_xor(first, off));
+  }
+  if (lane == 0) s_r[wave] = r, s_1[wave] = s1, s_lead[wave] = wlead, s_first[wave] = first;
   __syncthreads();
   r = s1 = 0.f;
-  lead = 0;
+  int leads = 0;
 #pragma unroll
-  for (int w = 0; w < LP_WAVES; ++w) r += s_r[w], s1 += s_1[w], lead += s_lead[w];
-  r += (float)max(lead - 1, 0);
-  const bool whole = a.parts == 1, none = any_bad || M == -INFINITY;
+  for (int w2 = 0; w2 < LP_WAVES; ++w2) r += s_r[w2], s1 += s_1[w2], leads += s_lead[w2];
+  r += (float)max(leads - 1, 0);
+  const bool bad = !(r < INFINITY) || M == INFINITY;
+  const bool whole = a.parts == 1, none = bad || M == -INFINITY;
+  LogprobPart *mine = row_parts(a, row) + part;
   if (threadIdx.x == 0) {
-    if (whole) put_row<DT>(a, row, none, M, r, s1);
-    else ((LogprobPart *)a.ws)[blockIdx.x] = LogprobPart{M, r, s1, any_bad ? 1.f : 0.f};
+    if (whole) {
+      put_row<DT>(a, row, none, M, r, s1);
+    } else {
+      st_part(&mine->m, M);
+      st_part(&mine->r, r);
+      st_part(&mine->s1, s1);
+      st_part(&mine->bad, bad ? 1.f : 0.f);
+    }
   }
-  if (a.top <= 0) return;
-  const float lz = log1pf(r);
-  uint64_t *keys = (uint64_t *)((LogprobPart *)a.ws + a.rows * a.parts) + (int64_t)blockIdx.x * a.top;
-  select_top(
-      a.top, floor_key,
-      [&](auto f) {
+  if (whole && none) {
+    put_no_top(a, row);
+  } else if (a.top > 0 && !bad) {  // (the keys of a part with a NaN are not looked at)
+    const float lz = log1pf(r);
+    uint64_t *keys = row_keys(a, row) + (int64_t)part * a.top;
+    if (a.top == 1) {
+      if (threadIdx.x == 0) {
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) f(logit_key(v[i], i0 + index(i / VEC, i % VEC)));
-      },
-      [&](int rank, uint64_t key) {
-        if (whole) put_top(a, row, none, M, lz, rank, key);
-        else keys[rank] = key;
-      });
+        for (int w2 = 0; w2 < LP_WAVES; ++w2) first = min(first, s_first[w2]);
+        const uint64_t key = logit_key(M, first);
+        if (whole) put_top(a, row, false, M, lz, 0, key);
+        else st_part(keys, key);
+      }
+    } else select_top(
+        s_sel, a.top, floor_key,
+        [&](float floor, auto f) {
+#pragma unroll
+          for (int i = 0; i < VPT; ++i) {
+            const float v = raw_elem<DT, NW>(w, i);
+            if (v >= floor) f(logit_key(v, place(i)));
+          }
+          keep();
+        },
+        [&](int rank, uint64_t key) {
+          if (whole) put_top(a, row, false, M, lz, rank, key);
+          else st_part(&keys[rank], key);
+        });
+  }
+  if (whole || !a.count) return;
+  // Parts are stored and read past the caches of one XCD; every wave's stores are
+  // done before the barrier, behind which one thread counts the work group in.
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    uint32_t *c = (uint32_t *)a.ws + row;
+    const bool last = __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(a.parts - 1);
+    if (last) st_part(c, 0u);  // for the next call
+    s_last = last;
+  }
+  __syncthreads();
+  if (s_last) join_parts<DT>(a, row, s_sel);
 }
 
-// One work group joins a row's parts.  Every part gave its `top` largest keys in
-// order (elements past the row's end among them: they have the lowest keys).
-// The k-th keys of all parts, k = ceil(top / parts): at least `top` keys reach the
-// least of them.
 template <int DT>
 __global__ __launch_bounds__(LP_THREADS) void k_logprobs_join(LogprobArgs a) {
-  __shared__ float s_m[LP_WAVES], s_r[LP_WAVES], s_1[LP_WAVES];
-  __shared__ int s_bad[LP_WAVES];
-  __shared__ uint64_t s_t[LP_WAVES], s_lead[LP_WAVES];
-  const int64_t row = blockIdx.x;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const LogprobPart *p = (const LogprobPart *)a.ws + row * a.parts;
-  const uint64_t *keys = (const uint64_t *)((const LogprobPart *)a.ws + a.rows * a.parts) + row * a.parts * a.top;
-  const int kth = a.top > 0 ? (a.top + a.parts - 1) / a.parts - 1 : 0;
-  float m = -INFINITY;
-  bool bad = false;
-  uint64_t low = ~0ull;
-  for (int c = threadIdx.x; c < a.parts; c += LP_THREADS) {
-    m = fmaxf(m, p[c].m);
-    bad |= p[c].bad != 0.f;
-    if (a.top > 0) low = min(low, keys[(int64_t)c * a.top + kth]);
-  }
-  m = wave_max(m);
-  for (int off = 32; off >= 1; off >>= 1) low = min(low, (uint64_t)__shfl_xor((unsigned long long)low, off));
-  const bool wbad = __ballot(bad) != 0;
-  if (lane == 0) s_m[wave] = m, s_bad[wave] = wbad, s_t[wave] = low;
-  __syncthreads();
-  float M = s_m[0];
-  bool any_bad = s_bad[0];
-  uint64_t floor_key = s_t[0];
-#pragma unroll
-  for (int w = 1; w < LP_WAVES; ++w) {
-    M = fmaxf(M, s_m[w]);
-    any_bad |= s_bad[w] != 0;
-    floor_key = min(floor_key, s_t[w]);
-  }
-  // the first part that holds the maximum leads
-  uint64_t first = ~0ull;
-  for (int c = threadIdx.x; c < a.parts; c += LP_THREADS)
-    if (p[c].m == M) first = min(first, (uint64_t)c);
-  for (int off = 32; off >= 1; off >>= 1) first = min(first, (uint64_t)__shfl_xor((unsigned long long)first, off));
-  if (lane == 0) s_lead[wave] = first;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < LP_WAVES; ++w) first = min(first, s_lead[w]);
-  float r = 0.f, s1 = 0.f;
-  for (int c = threadIdx.x; c < a.parts; c += LP_THREADS) add_part(p[c], M, (uint64_t)c == first, r, s1);
-  r = wave_sum(r);
-  s1 = wave_sum(s1);
-  if (lane == 0) s_r[wave] = r, s_1[wave] = s1;
-  __syncthreads();
-  r = s1 = 0.f;
-#pragma unroll
-  for (int w = 0; w < LP_WAVES; ++w) r += s_r[w], s1 += s_1[w];
-  const bool none = any_bad || M == -INFINITY;
-  if (threadIdx.x == 0) put_row<DT>(a, row, none, M, r, s1);
-  if (a.top <= 0) return;
-  const float lz = log1pf(r);
-  select_top(
-      a.top, floor_key,
-      [&](auto f) {
-        for (int64_t i = threadIdx.x; i < (int64_t)a.parts * a.top; i += LP_THREADS) f(keys[i]);
-      },
-      [&](int rank, uint64_t key) { put_top(a, row, none, M, lz, rank, key); });
+  __shared__ SelectLds s_sel;
+  join_parts<DT>(a, blockIdx.x, s_sel);
 }
 
 template <int DT>
-hipError_t logprobs_dt(const LogprobArgs &a, hipStream_t st) {
-  HS_LAUNCH((k_logprobs<DT, LOGPROB_PART / LP_THREADS>), dim3((uint32_t)(a.rows * a.parts)), dim3(LP_THREADS), 0, st, a);
-  if (a.parts > 1) HS_LAUNCH((k_logprobs_join<DT>), dim3((uint32_t)a.rows), dim3(LP_THREADS), 0, st, a);
+hipError_t logprobs_dt(LogprobArgs a, hipStream_t st) {
+  constexpr int CE = Ty<DT>::CE / 4;  // elements of a word
+  // rows that eight words a thread hold: fewer registers, and no thread without an element
+  const bool small = a.vocab <= LP_THREADS * 8 * CE;
+  a.parts = small ? 1 : (int)(((int64_t)a.vocab + LP_THREADS * 32 * CE - 1) / (LP_THREADS * 32 * CE));
+  const int64_t groups = a.rows * a.parts;
+  if (groups > INT32_MAX) return hipErrorInvalidValue;
+  // One launch while the GPU holds all work groups at once: where more wait, joining
+  // at the end of a work group keeps its place for longer than a second launch takes.
+  a.count = a.parts > 1 && groups <= 1024 && a.rows <= LOGPROB_COUNTERS;
+  if (small) HS_LAUNCH((k_logprobs<DT, 8>), dim3((uint32_t)groups), dim3(LP_THREADS), 0, st, a);
+  else HS_LAUNCH((k_logprobs<DT, 32>), dim3((uint32_t)groups), dim3(LP_THREADS), 0, st, a);
+  if (a.parts > 1 && !a.count) HS_LAUNCH((k_logprobs_join<DT>), dim3((uint32_t)a.rows), dim3(LP_THREADS), 0, st, a);
   return hipGetLastError();
 }
 
@@ -334,12 +473,11 @@ hipError_t logprobs_dt(const LogprobArgs &a, hipStream_t st) {
 
 uint64_t logprob_workspace(int64_t rows, int vocab, int top) {
   const int64_t parts = logprob_parts(vocab);
-  return parts > 1 ? (uint64_t)rows * parts * (sizeof(LogprobPart) + top * 8) : 0;
+  return parts > 1 ? LOGPROB_COUNTERS * 4 + (uint64_t)rows * parts * (sizeof(LogprobPart) + top * 8) : 0;
 }
 
 hipError_t launch_logprobs(int dtype, const LogprobArgs &a, hipStream_t st) {
   if (a.rows <= 0) return hipSuccess;
-  if (a.rows * a.parts > INT32_MAX) return hipErrorInvalidValue;
   switch (dtype) {
     case HS_F32: return logprobs_dt<HS_F32>(a, st);
     case HS_F16: return logprobs_dt<HS_F16>(a, st);

@@ -581,7 +581,8 @@ class QuantCache:
         if workspace is None:
             workspace = torch.empty(self._workspace_bytes(dt, n, heads, max_len), dtype=torch.uint8,
                                     device=self.blocks.device)
-            workspace[:2048].zero_()
+            if workspace.numel():
+                workspace[:2048].zero_()
         elif workspace.get_device() != index or not workspace.is_contiguous():
             raise ValueError(f"{func}: workspace must be contiguous on {self.blocks.device}")
         _on_device(func, "hs_kvq_attention", index, self._ref, layer, dt, n, heads, q.data_ptr(), stride[0],
@@ -598,9 +599,9 @@ def _logprobs_bytes(rows: int, vocab: int, top: int) -> int:
 
 
 def token_logprobs_workspace(rows: int, vocab: int, top: int = 0, device="cuda"):
-    """A workspace for token_logprobs over rows of vocab logits."""
+    """A workspace for token_logprobs over rows of vocab logits, which may be kept from call to call."""
     import torch
-    return torch.empty(_logprobs_bytes(rows, vocab, top), dtype=torch.uint8, device=device)
+    return torch.zeros(_logprobs_bytes(rows, vocab, top), dtype=torch.uint8, device=device)
 
 
 def token_logprobs(logits, tokens=None, top: int = 0, workspace=None):
@@ -623,6 +624,8 @@ def token_logprobs(logits, tokens=None, top: int = 0, workspace=None):
         ids = torch.empty_like(tops, dtype=torch.int32)
     if workspace is None:
         workspace = logits.new_empty((_logprobs_bytes(rows, vocab, top),), dtype=torch.uint8)
+        if workspace.numel():
+            workspace[:2048].zero_()
     elif workspace.get_device() != index or not workspace.is_contiguous():
         raise ValueError(f"{func}: workspace must be contiguous on the logits' device")
     _on_device(func, "hs_token_logprobs", index, dt, logits.data_ptr(), rows, vocab, logits.stride(0), tk, top,

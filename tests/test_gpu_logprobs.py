@@ -115,6 +115,26 @@ def test_strides_and_unaligned_rows(dtype):
             check(hs, x, torch.tensor([0, vocab - 1, 1, -1]), min(vocab, 7))
 
 
+@pytest.mark.parametrize("rows", [511, 513])
+def test_rows_of_several_parts_on_both_sides_of_the_one_launch_limit(rows):
+    import paper_2603_12707_amd as hs
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x = (torch.randn(rows, 8200, device="cuda", generator=g) * 2).bfloat16()
+    x[::3, 8192:] = 30.0  # the largest, and equal, in the short part
+    x[1::7, :8192] = -math.inf
+    tokens = torch.randint(-1, 8200, (rows,), device="cuda", generator=g)
+    lp, ent, ids, tops = hs.token_logprobs(x, tokens.int(), top=3)
+    ref = torch.log_softmax(x.double(), -1)
+    want = torch.where(tokens >= 0, ref.gather(1, tokens.clamp(min=0)[:, None])[:, 0], 0.0)
+    fine = torch.isfinite(want)
+    assert torch.equal(torch.isneginf(lp), torch.isneginf(want))
+    assert ((lp.double() - want).abs()[fine] <= R.logprob_tolerance(want)[fine]).all()
+    assert ((ent.double() + torch.where(ref > -math.inf, ref.exp() * ref, 0.0).sum(-1)).abs() <= 2.0 ** -16).all()
+    order = torch.sort(x.float(), descending=True, stable=True)
+    assert torch.equal(ids.long(), order.indices[:, :3])
+    assert ((tops.double() - ref.gather(1, order.indices[:, :3])).abs() <= 2.0 ** -16).all()
+
+
 def test_many_rows():
     import paper_2603_12707_amd as hs
     g = torch.Generator().manual_seed(3)
@@ -155,8 +175,14 @@ def test_deterministic_and_replayed_in_a_graph():
     import paper_2603_12707_amd as hs
     x = torch.randn(6, 40001, device="cuda")
     tk = torch.arange(6, dtype=torch.int32, device="cuda")
-    ws = hs.token_logprobs_workspace(6, 40001, 20).fill_(0xFF)
+    ws = hs.token_logprobs_workspace(6, 40001, 20)
+    ws[2048:].fill_(0xFF)  # only the first 2048 bytes are kept between calls
     first = [t.clone() for t in hs.token_logprobs(x, tk, top=20, workspace=ws)]
+    again = hs.token_logprobs(x, tk, top=20, workspace=ws)
+    assert all(torch.equal(a, b) for a, b in zip(first, again)) and not ws[:2048].any()
+    # the same workspace serves another shape, and the first one again
+    g = torch.Generator().manual_seed(5)
+    check(hs, torch.randn(3, 70000, generator=g).half().cuda(), torch.tensor([1, 2, 69999]), 7, workspace=ws)
     again = hs.token_logprobs(x, tk, top=20, workspace=ws)
     assert all(torch.equal(a, b) for a, b in zip(first, again))
     graph = torch.cuda.CUDAGraph()
