@@ -358,7 +358,7 @@ int hs_decode_step_static(hs_model *m, hs_kv *kv, const int32_t *tokens_in, int3
  * Position p of sequence s lives in block table[s * table_ld + p / block_tokens];
  * a number that is negative or not below bytes / block_bytes means that there is
  * no block: nothing is stored there, nothing read, and attention masks it.
- * blocks: 16-byte aligned; head_dim 64 or 128. */
+ * blocks: 16-byte aligned; head_dim 64 or 128, n_kv_heads 1..4096. */
 typedef struct hs_kvq_cache {
   void *blocks;         /* device */
   uint64_t bytes;       /* of blocks; at least one block */

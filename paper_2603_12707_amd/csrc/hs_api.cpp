@@ -1418,7 +1418,8 @@ int hs_kv_set_length(hs_kv *kv, int32_t req, int32_t len, int32_t rope_pos) {
 int hs_kvq_block_bytes(int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, int32_t block_tokens, uint64_t *bytes) {
   static const char *fn = "hs_kvq_block_bytes";
   if (!bytes) return fail(HS_E_INVALID, "%s: bytes is NULL", fn);
-  if (n_layers <= 0 || n_kv_heads <= 0) return fail(HS_E_INVALID, "%s: non-positive size", fn);
+  if (n_layers <= 0 || n_kv_heads <= 0 || n_kv_heads > 4096)
+    return fail(HS_E_INVALID, "%s: n_layers must be positive, n_kv_heads in 1..4096", fn);
   if (head_dim != 64 && head_dim != 128) return fail(HS_E_INVALID, "%s: head_dim %d is not 64 or 128", fn, head_dim);
   if (block_tokens < 16 || block_tokens > 16384 || (block_tokens & (block_tokens - 1)))
     return fail(HS_E_INVALID, "%s: block_tokens must be a power of two in 16..16384", fn);

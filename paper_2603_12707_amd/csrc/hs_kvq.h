@@ -128,34 +128,45 @@ __device__ __forceinline__ void kvq_place(const KvqRows &a, int row, int &seq, i
   pos = !a.pos ? a.pos0 + row : !a.pos_by_seq ? a.pos[row] : (uint32_t)seq < (uint32_t)a.c.n_seqs ? a.pos[seq] : -1;
 }
 
-// One thread takes eight elements of a row of K or V.
+// One thread takes eight elements; a work group takes one head of K or V of
+// 2048 / HD consecutive rows, so that a prefill pass's rows fill whole spans of 16
+// positions in one place.
+template <int DT, int HD>
+struct KvqLine {
+  static constexpr int CPR = HD / 8, ROWS = 256 / CPR, SB = DT == HS_F32 ? 4 : 2;
+  int row, c, hi, head, sel;
+  __device__ __forceinline__ explicit KvqLine(const KvqRows &a) {
+    row = (int)blockIdx.x * ROWS + (int)threadIdx.x / CPR;
+    c = (int)threadIdx.x % CPR;
+    hi = (int)blockIdx.y;
+    sel = a.sel;
+    if (sel < 0) sel = hi >= a.heads, hi -= sel * a.heads;
+    head = a.head0 + hi;
+  }
+  __device__ __forceinline__ int64_t at(const KvqRows &a, int r) const {
+    return ((int64_t)r * a.ld + (int64_t)hi * a.ld_head + c * 8) * SB;
+  }
+};
+
 template <int DT, int HD>
 __global__ __launch_bounds__(256) void k_kvq_append(KvqRows a) {
-  constexpr int CPR = HD / 8;
-  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int c = (int)(t % CPR);
-  const int64_t line = t / CPR;
-  const int hi = (int)(line % a.heads), head = a.head0 + hi;
-  const int64_t rs = line / a.heads;
-  const int sel = a.sel < 0 ? (int)(rs & 1) : a.sel;
-  const int row = (int)(a.sel < 0 ? rs >> 1 : rs);
-  if (row >= a.n) return;
-  constexpr int SB = DT == HS_F32 ? 4 : 2;
+  const KvqLine<DT, HD> t(a);
+  if (t.row >= a.n) return;
   int seq, pos;
-  kvq_place(a, row, seq, pos);
-  const int64_t at = ((int64_t)(a.row_by_seq ? seq : row) * a.ld + (int64_t)hi * a.ld_head + c * 8) * SB;
+  kvq_place(a, t.row, seq, pos);
+  const int64_t at = t.at(a, a.row_by_seq ? seq : t.row);
   float f[8];
-  ld8<DT>((const char *)(sel ? a.v : a.k) + at, f);
+  ld8<DT>((const char *)(t.sel ? a.v : a.k) + at, f);
   uint32_t byte;
   const uint32_t w = kvq_encode<DT>(f, byte);
   int64_t id = kvq_block(a.c, seq, pos);
   if (id >= 0 && a.cap && pos >= a.cap[seq]) id = -1;
   if (id >= 0) {
-    uint8_t *span = kvq_span(a.c, HD, id, sel, head, pos);
-    ((uint32_t *)span)[(pos & 15) * CPR + c] = w;
-    if ((c & 3) == 0) span[HD * 8 + (c >> 2) * 16 + (pos & 15)] = (uint8_t)byte;
+    uint8_t *span = kvq_span(a.c, HD, id, t.sel, t.head, pos);
+    ((uint32_t *)span)[(pos & 15) * t.CPR + t.c] = w;
+    if ((t.c & 3) == 0) span[HD * 8 + (t.c >> 2) * 16 + (pos & 15)] = (uint8_t)byte;
   }
-  char *val = (char *)(sel ? a.v_out : a.k_out);
+  char *val = (char *)(t.sel ? a.v_out : a.k_out);
   if (val) {
     kvq_decode(w, kvq_scale(byte), f);
     st8<DT>(val + at, f);
@@ -165,28 +176,20 @@ __global__ __launch_bounds__(256) void k_kvq_append(KvqRows a) {
 // The reverse: rows of K and V in the row type; a place without a block gives zeros.
 template <int DT, int HD>
 __global__ __launch_bounds__(256) void k_kvq_read(KvqRows a) {
-  constexpr int CPR = HD / 8;
-  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int c = (int)(t % CPR);
-  const int64_t line = t / CPR;
-  const int hi = (int)(line % a.heads), head = a.head0 + hi;
-  const int64_t rs = line / a.heads;
-  const int sel = a.sel < 0 ? (int)(rs & 1) : a.sel;
-  const int row = (int)(a.sel < 0 ? rs >> 1 : rs);
-  if (row >= a.n) return;
-  constexpr int SB = DT == HS_F32 ? 4 : 2;
+  const KvqLine<DT, HD> t(a);
+  if (t.row >= a.n) return;
   int seq, pos;
-  kvq_place(a, row, seq, pos);
+  kvq_place(a, t.row, seq, pos);
   const int64_t id = kvq_block(a.c, seq, pos);
   uint32_t w = 0, byte = KvqByte<DT>::lo;
   if (id >= 0) {
-    const uint8_t *span = kvq_span(a.c, HD, id, sel, head, pos);
-    w = ((const uint32_t *)span)[(pos & 15) * CPR + c];
-    byte = span[HD * 8 + (c >> 2) * 16 + (pos & 15)];
+    const uint8_t *span = kvq_span(a.c, HD, id, t.sel, t.head, pos);
+    w = ((const uint32_t *)span)[(pos & 15) * t.CPR + t.c];
+    byte = span[HD * 8 + (t.c >> 2) * 16 + (pos & 15)];
   }
   float f[8];
   kvq_decode(w, kvq_scale(byte), f);
-  st8<DT>((char *)(sel ? a.v_out : a.k_out) + ((int64_t)row * a.ld + (int64_t)hi * a.ld_head + c * 8) * SB, f);
+  st8<DT>((char *)(t.sel ? a.v_out : a.k_out) + t.at(a, t.row), f);
 }
 
 // Decode attention over the 4-bit cache.  One work group = (split of the row's
@@ -779,10 +782,11 @@ __global__ __launch_bounds__(256) void k_kvq_combine(KvqAttn a) {
 
 template <int DT, int HD>
 hipError_t kvq_rows(const KvqRows &a, bool read, hipStream_t st) {
-  const int64_t threads = (int64_t)a.n * (a.sel < 0 ? 2 : 1) * a.heads * (HD / 8), grid = (threads + 255) / 256;
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
-  if (read) HS_LAUNCH((k_kvq_read<DT, HD>), dim3((uint32_t)grid), dim3(256), 0, st, a);
-  else HS_LAUNCH((k_kvq_append<DT, HD>), dim3((uint32_t)grid), dim3(256), 0, st, a);
+  const int rows = KvqLine<DT, HD>::ROWS, lines = (a.sel < 0 ? 2 : 1) * a.heads;
+  if (lines > 65535) return hipErrorInvalidValue;
+  const dim3 grid((a.n + (int64_t)rows - 1) / rows, lines);
+  if (read) HS_LAUNCH((k_kvq_read<DT, HD>), grid, dim3(256), 0, st, a);
+  else HS_LAUNCH((k_kvq_append<DT, HD>), grid, dim3(256), 0, st, a);
   return hipGetLastError();
 }
 template <int DT>

@@ -15,7 +15,8 @@ namespace {
 
 using namespace dev;
 
-// d = x - M is cut here: e^-200 is 0 in fp32, and d e^d then 0 and not NaN
+// d = x - M is cut here as the factor of d e^d: e^-200 is 0 in fp32, and the
+// product then 0 and not NaN
 constexpr float LOGPROB_FAR = -200.f;
 
 // Orders logits by value, the lowest index first among equals: larger keys
@@ -256,7 +257,8 @@ __global__ __launch_bounds__(LP_THREADS, 5) void k_logprobs(LogprobArgs a) {
   const int i0 = min(part * PART, max(0, a.vocab - PART)), n = min(a.vocab - i0, PART), skip0 = part * PART - i0;
   const S *x = (const S *)a.logits + row * a.ld + i0;
   // element e of vector u: VEC consecutive ones to a thread; rows start anywhere
-  auto index = [&](int u, int e) { return (u * LP_THREADS + (int)threadIdx.x) * VEC + e; };
+  int tid = (int)threadIdx.x;
+  auto index = [&](int u, int e) { return (u * LP_THREADS + tid) * VEC + e; };
   struct __attribute__((packed, aligned(sizeof(S)))) Loose {
     u32x4 w;
   };
@@ -296,8 +298,10 @@ __global__ __launch_bounds__(LP_THREADS, 5) void k_logprobs(LogprobArgs a) {
     const int k = index(i / VEC, i % VEC);
     return k < skip0 ? a.vocab + k : i0 + k;
   };
-  // the words are opaque from one use to the next: 16-bit elements are unpacked again
+  // the words and places are opaque from one use to the next: 16-bit elements are
+  // unpacked and places made again, not kept in registers
   auto keep = [&] {
+    asm volatile("" : "+v"(tid));
     if constexpr (DT != HS_F32)
 #pragma unroll
       for (int k = 0; k < NW; ++k) asm volatile("" : "+v"(w[k]));
@@ -359,10 +363,11 @@ __global__ __launch_bounds__(LP_THREADS, 5) void k_logprobs(LogprobArgs a) {
       // a wave that holds the maximum: a thread's first instance of it is left out
 #pragma unroll
       for (int i = 0; i < VPT; ++i) {
-        const float v = raw_elem<DT, NW>(w, i), d = v - M, e = __expf(d);
+        const float v = raw_elem<DT, NW>(w, i), d = v - M;
         const bool out = v == M && !lead;
+        const float e = out ? 0.f : __expf(d);
         lead |= out;
-        r += out ? 0.f : e;
+        r += e;
         s1 = __builtin_fmaf(fmaxf(d, LOGPROB_FAR), e, s1);
       }
     } else {
