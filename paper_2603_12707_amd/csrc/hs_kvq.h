@@ -201,9 +201,11 @@ __global__ __launch_bounds__(256) void k_kvq_read(KvqRows a) {
 // takes K as it lies in memory: lane (li, lg) = (lane % 16, lane / 16) supplies
 // group lg of its position and the group's exponent byte.  Q enters as the sum of
 // e4m3 parts, each with what the parts before left, times 16 (two hold a bf16
-// number, three an f16, six an fp32), scaled by a power of two of the head's
-// largest element: every product is exact, an element below 2^-13 of the largest
-// is off by at most 2^-17 of 16^-parts of it.  Row r of the tile's product t is
+// number, three an f16), scaled by a power of two of the head's largest element:
+// every product is exact, an element below 2^-13 of the largest is off by at most
+// 2^-17 of 16^-parts of it.  The instruction's sums are good to about 2^-20 of the
+// largest product (measured), which is short of fp32: fp32 rows convert K to bf16
+// and take Q as three bf16 parts through the MFMA 16x16x32.  Row r of the tile's product t is
 // position 16 (r / 4) + 4 t + r % 4, so that a lane ends up with the scores of
 // the 16 consecutive positions 16 lg .. for head li, which is the B operand of
 // O^T += V^T P^T (MFMA 16x16x32): positions 8 m .. 8 m + 7 of each lane group are
@@ -223,7 +225,7 @@ constexpr int KVQ_MMA = DT == HS_F16 ? HS_F16 : HS_BF16;
 template <int DT>
 constexpr int KVQ_P_PARTS = DT == HS_F32 ? 3 : 2;
 template <int DT>
-constexpr int KVQ_Q_PARTS = DT == HS_F32 ? 6 : DT == HS_F16 ? 3 : 2;
+constexpr int KVQ_Q_PARTS = DT == HS_BF16 ? 2 : 3;
 constexpr int KVQ_TILE = 64, KVQ_PLANES = 3;
 // Rows are started longest first where the GPU does not hold all work groups at
 // once and the longest rows take a while: up to this many rows, and from so many
@@ -260,12 +262,12 @@ constexpr float KVQ_SLACK = DT == HS_F16 ? 4.f : 11.5f;
 constexpr float KVQ_ROUND_FROM = 0x1p20f;
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-// sc += K Q^T over the parts P of Q: K fp4 with its group's exponent byte, Q e4m3 with byte P % 4 of qs
+// sc += K Q^T over the parts P of Q: K fp4 with its group's exponent byte, Q e4m3 with byte P of qs
 template <int QP, int... P>
-__device__ __forceinline__ void score_parts(f32x4 &sc, u32x4 k, int byte, const i32x8 (&qb)[QP],
-                                            const int (&qs)[(QP + 3) / 4], std::integer_sequence<int, P...>) {
+__device__ __forceinline__ void score_parts(f32x4 &sc, u32x4 k, int byte, const i32x8 (&qb)[QP], int qs,
+                                            std::integer_sequence<int, P...>) {
   const i32x8 kv{(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
-  ((sc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kv, qb[P], sc, 4, 0, 0, byte, P % 4, qs[P / 4])), ...);
+  ((sc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kv, qb[P], sc, 4, 0, 0, byte, P, qs)), ...);
 }
 
 // word x of a matrix operand of parts: R(f0) | R(f1) << 16, and what is left
@@ -448,11 +450,26 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
   if (wave + NW < n_tiles) copy(wave + NW, nxt, 0, 2);
   int slot = 0;  // of the tile's K
   auto next_slot = [](int x) { return x == KVQ_PLANES - 1 ? 0 : x + 1; };
-  // Q^T operand: head li of the group (zeros past it); the MFMA's byte e of lane
-  // group lg is channel 16 lg + e, from byte 16 on 64 further
-  i32x8 qb[QP];
-  int qs[(QP + 3) / 4];  // the parts' scale bytes
-  {
+  // Q^T operand: head li of the group (zeros past it)
+  // (a negative scale's sign goes to Q, so that the scores' order is that of the products)
+  const float sign = a.scale < 0.f ? -1.f : 1.f;
+  [[maybe_unused]] i32x8 qb[QP];               // scaled MFMA: e4m3 parts
+  [[maybe_unused]] int qs = 0;                 // and their scale bytes
+  [[maybe_unused]] u32x4 qh[QP][HD / 32];      // fp32 rows: bf16 parts
+  if constexpr (DT == HS_F32) {
+#pragma unroll
+    for (int c = 0; c < HD / 32; ++c) {
+      float f[8] = {};
+      if (li < G) ld8<DT>((const char *)a.q + ((int64_t)row * a.ld_q + (j * G + li) * HD + lg * (HD / 4) + c * 8) * SB, f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] *= sign;
+#pragma unroll
+      for (int p = 0; p < QP; ++p)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) qh[p][c][x] = take_part<MT>(f[2 * x], f[2 * x + 1]);
+    }
+  } else {
+    // the MFMA's byte e of lane group lg is channel 16 lg + e, from byte 16 on 64 further
     float f[32];
 #pragma unroll
     for (int e = 0; e < 32; ++e) f[e] = 0.f;
@@ -468,8 +485,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
     top = max(top, (uint32_t)__shfl_xor((int)top, 32));
     // 2^s puts the largest into 128 .. 256 (e4m3 ends at 448); a NaN or an infinity makes the head's scores NaN
     const int s = min(max((int)(top >> 23) - 127 - 7, -100), 120);
-    // (a negative scale's sign goes to Q, so that the scores' order is that of the products)
-    const float mul = __uint_as_float((uint32_t)(127 - s) << 23) * (a.scale < 0.f ? -1.f : 1.f);
+    const float mul = __uint_as_float((uint32_t)(127 - s) << 23) * sign;
 #pragma unroll
     for (int e = 0; e < 32; ++e) f[e] *= mul;
 #pragma unroll
@@ -485,9 +501,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
         f[4 * x + 2] = (f[4 * x + 2] - hi[0]) * 16.f;
         f[4 * x + 3] = (f[4 * x + 3] - hi[1]) * 16.f;
       }
-      const int byte = top >= 0x7F800000u ? 255 : 127 + s - 4 * p;
-      if (p % 4 == 0) qs[p / 4] = 0;
-      qs[p / 4] |= byte << (8 * (p % 4));
+      qs |= (top >= 0x7F800000u ? 255 : 127 + s - 4 * p) << (8 * p);
     }
   }
   const float c2 = fabsf(a.scale) * 1.44269504088896341f;
@@ -500,24 +514,42 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
     const Ids far = settle(lookup(t + 2 * NW, end), t + 2 * NW, end);
     if (one) wait_copies<2 * COPIES>();  // V, and the next tile's K
     else wait_copies<COPIES>();
-    u32x4 kc[4];
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-      kc[x] = *(const u32x4 *)(kp + kspan * SPAN + (4 * x + (li & 3)) * (HD / 2) + kgrp * 16);
-    u32x4 ks = *(const u32x4 *)(kp + kspan * SPAN + HD * 8 + kgrp * 16);
-    if constexpr (HD == 64) {  // the upper half of the contraction: zeros, times 1
-      if (lg >= 2) {
-#pragma unroll
-        for (int x = 0; x < 4; ++x) kc[x] = u32x4{0u, 0u, 0u, 0u};
-        ks = u32x4{0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu};
-      }
-    }
     f32x4 sc[4];
+    if constexpr (DT == HS_F32) {
+      constexpr int FGRP = HD == 128 ? 0 : 1;  // lane groups to a group of 32, as a shift
+      const u32x4 ks = *(const u32x4 *)(kp + kspan * SPAN + HD * 8 + (lg >> FGRP) * 16);
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const int byte = (int)(ks[x] >> (8 * (li & 3)));  // the MFMA reads the lowest byte
-      sc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-      score_parts<QP>(sc[x], kc[x], byte, qb, qs, std::make_integer_sequence<int, QP>{});
+      for (int x = 0; x < 4; ++x) {
+        const uint32_t *at = (const uint32_t *)(kp + kspan * SPAN + (4 * x + (li & 3)) * (HD / 2) + lg * (HD / 8));
+        const float s = kvq_scale((ks[x] >> (8 * (li & 3))) & 255u);
+        sc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < HD / 32; ++c) {
+          const uint32_t w = at[c];
+          const u32x4 kv{kvq_pair<MT, 0>(w, s), kvq_pair<MT, 1>(w, s), kvq_pair<MT, 2>(w, s), kvq_pair<MT, 3>(w, s)};
+#pragma unroll
+          for (int p = QP - 1; p >= 0; --p) sc[x] = mma<MT>(kv, qh[p][c], sc[x]);
+        }
+      }
+    } else {
+      u32x4 kc[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        kc[x] = *(const u32x4 *)(kp + kspan * SPAN + (4 * x + (li & 3)) * (HD / 2) + kgrp * 16);
+      u32x4 ks = *(const u32x4 *)(kp + kspan * SPAN + HD * 8 + kgrp * 16);
+      if constexpr (HD == 64) {  // the upper half of the contraction: zeros, times 1
+        if (lg >= 2) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) kc[x] = u32x4{0u, 0u, 0u, 0u};
+          ks = u32x4{0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu};
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int byte = (int)(ks[x] >> (8 * (li & 3)));  // the MFMA reads the lowest byte
+        sc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+        score_parts<QP>(sc[x], kc[x], byte, qb, qs, std::make_integer_sequence<int, QP>{});
+      }
     }
     if (one) {
       wait_lds();

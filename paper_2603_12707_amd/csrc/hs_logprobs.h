@@ -145,14 +145,17 @@ __device__ __forceinline__ void put_no_top(const LogprobArgs &a, int64_t row) {
   for (int k = threadIdx.x; k < a.top; k += LP_THREADS) put_top(a, row, true, 0.f, 0.f, k, 0);
 }
 
-// past the caches of one XCD
-template <class T>
-__device__ __forceinline__ void st_part(T *p, T v) {
-  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+// parts that another work group of the same launch reads (past the caches of one
+// XCD), or another launch
+template <bool SAME, class T>
+__device__ __forceinline__ T ld_part(const T *p) {
+  if constexpr (SAME) return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  else return *p;
 }
 template <class T>
-__device__ __forceinline__ T ld_part(const T *p) {
-  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+__device__ __forceinline__ void st_part(bool same, T *p, T v) {
+  if (same) __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  else *p = v;
 }
 // the workspace: a counter for each row, the parts' sums, the parts' keys
 __device__ __forceinline__ LogprobPart *row_parts(const LogprobArgs &a, int64_t row) {
@@ -167,7 +170,7 @@ __device__ __forceinline__ uint64_t *row_keys(const LogprobArgs &a, int64_t row)
 // The k-th keys of all parts, k = ceil(top / parts): at least `top` keys reach the
 // least of them.  Every wave joins the sums by itself, the keys are asked for
 // beside them.
-template <int DT>
+template <int DT, bool SAME>
 __device__ __forceinline__ void join_parts(const LogprobArgs &a, int64_t row, SelectLds &lds) {
   constexpr int HOLD = 4;  // keys of a thread that stay in registers
   const int lane = threadIdx.x & 63;
@@ -178,19 +181,19 @@ __device__ __forceinline__ void join_parts(const LogprobArgs &a, int64_t row, Se
 #pragma unroll
   for (int u = 0; u < HOLD; ++u) {
     const int64_t i = u * LP_THREADS + threadIdx.x;
-    hold[u] = i < n_keys ? ld_part(&keys[i]) : 0;
+    hold[u] = i < n_keys ? ld_part<SAME>(&keys[i]) : 0;
   }
   const int kth = a.top > 0 ? (a.top + a.parts - 1) / a.parts - 1 : 0;
   // parts lane, lane + 64, ..; the first of them kept
-  auto part = [&](int c) { return LogprobPart{ld_part(&p[c].m), ld_part(&p[c].r), ld_part(&p[c].s1), ld_part(&p[c].bad)}; };
+  auto part = [&](int c) { return LogprobPart{ld_part<SAME>(&p[c].m), ld_part<SAME>(&p[c].r), ld_part<SAME>(&p[c].s1), ld_part<SAME>(&p[c].bad)}; };
   const LogprobPart mine = lane < a.parts ? part(lane) : LogprobPart{-INFINITY, 0.f, 0.f, 0.f};
-  uint64_t low = a.top > 0 && lane < a.parts ? ld_part(&keys[(int64_t)lane * a.top + kth]) : ~0ull;
+  uint64_t low = a.top > 0 && lane < a.parts ? ld_part<SAME>(&keys[(int64_t)lane * a.top + kth]) : ~0ull;
   float m = mine.m;
   bool bad = mine.bad != 0.f;
   for (int c = lane + 64; c < a.parts; c += 64) {
-    m = fmaxf(m, ld_part(&p[c].m));
-    bad |= ld_part(&p[c].bad) != 0.f;
-    if (a.top > 0) low = min(low, ld_part(&keys[(int64_t)c * a.top + kth]));
+    m = fmaxf(m, ld_part<SAME>(&p[c].m));
+    bad |= ld_part<SAME>(&p[c].bad) != 0.f;
+    if (a.top > 0) low = min(low, ld_part<SAME>(&keys[(int64_t)c * a.top + kth]));
   }
   const float M = wave_max(m);
   if (__ballot(bad) || M == -INFINITY) {
@@ -202,7 +205,7 @@ __device__ __forceinline__ void join_parts(const LogprobArgs &a, int64_t row, Se
   // the first part that holds the maximum leads
   int lead = mine.m == M ? lane : 0x7FFFFFFF;
   for (int c = lane + 64; c < a.parts && lead == 0x7FFFFFFF; c += 64)
-    if (ld_part(&p[c].m) == M) lead = c;
+    if (ld_part<SAME>(&p[c].m) == M) lead = c;
   for (int off = 32; off >= 1; off >>= 1) lead = min(lead, __shfl_xor(lead, off));
   float r = 0.f, s1 = 0.f;
   if (lane < a.parts) add_part(mine, M, lane == lead, r, s1);
@@ -222,7 +225,7 @@ __device__ __forceinline__ void join_parts(const LogprobArgs &a, int64_t row, Se
 #pragma unroll
         for (int u = 0; u < HOLD; ++u)
           if (hold[u]) f(hold[u]);
-        for (int64_t i = HOLD * LP_THREADS + threadIdx.x; i < n_keys; i += LP_THREADS) f(ld_part(&keys[i]));
+        for (int64_t i = HOLD * LP_THREADS + threadIdx.x; i < n_keys; i += LP_THREADS) f(ld_part<SAME>(&keys[i]));
       },
       [&](int rank, uint64_t key) { put_top(a, row, false, M, lz, rank, key); });
 }
@@ -402,10 +405,10 @@ __global__ __launch_bounds__(LP_THREADS, 5) void k_logprobs(LogprobArgs a) {
     if (whole) {
       put_row<DT>(a, row, none, M, r, s1);
     } else {
-      st_part(&mine->m, M);
-      st_part(&mine->r, r);
-      st_part(&mine->s1, s1);
-      st_part(&mine->bad, bad ? 1.f : 0.f);
+      st_part(a.count, &mine->m, M);
+      st_part(a.count, &mine->r, r);
+      st_part(a.count, &mine->s1, s1);
+      st_part(a.count, &mine->bad, bad ? 1.f : 0.f);
     }
   }
   if (whole && none) {
@@ -419,7 +422,7 @@ __global__ __launch_bounds__(LP_THREADS, 5) void k_logprobs(LogprobArgs a) {
         for (int w2 = 0; w2 < LP_WAVES; ++w2) first = min(first, s_first[w2]);
         const uint64_t key = logit_key(M, first);
         if (whole) put_top(a, row, false, M, lz, 0, key);
-        else st_part(keys, key);
+        else st_part(a.count, keys, key);
       }
     } else select_top(
         s_sel, a.top, floor_key,
@@ -433,7 +436,7 @@ __global__ __launch_bounds__(LP_THREADS, 5) void k_logprobs(LogprobArgs a) {
         },
         [&](int rank, uint64_t key) {
           if (whole) put_top(a, row, false, M, lz, rank, key);
-          else st_part(&keys[rank], key);
+          else st_part(a.count, &keys[rank], key);
         });
   }
   if (whole || !a.count) return;
@@ -444,17 +447,17 @@ __global__ __launch_bounds__(LP_THREADS, 5) void k_logprobs(LogprobArgs a) {
   if (threadIdx.x == 0) {
     uint32_t *c = (uint32_t *)a.ws + row;
     const bool last = __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(a.parts - 1);
-    if (last) st_part(c, 0u);  // for the next call
+    if (last) st_part(true, c, 0u);  // for the next call
     s_last = last;
   }
   __syncthreads();
-  if (s_last) join_parts<DT>(a, row, s_sel);
+  if (s_last) join_parts<DT, true>(a, row, s_sel);
 }
 
 template <int DT>
 __global__ __launch_bounds__(LP_THREADS) void k_logprobs_join(LogprobArgs a) {
   __shared__ SelectLds s_sel;
-  join_parts<DT>(a, blockIdx.x, s_sel);
+  join_parts<DT, false>(a, blockIdx.x, s_sel);
 }
 
 template <int DT>
