@@ -122,17 +122,27 @@ __device__ __forceinline__ void select_top(SelectLds &lds, int top, uint64_t flo
   }
 }
 
-// what a row's sums give
+// a row's given token and its logit (0 outside the row), asked for early by the
+// thread that puts the row
+struct Given {
+  int t;
+  float x;
+};
 template <int DT>
-__device__ __forceinline__ void put_row(const LogprobArgs &a, int64_t row, bool none, float M, float r, float s1) {
+__device__ __forceinline__ Given given_token(const LogprobArgs &a, int64_t row) {
+  Given g{-1, 0.f};
+  if (threadIdx.x == 0 && a.logprob) {
+    g.t = a.tokens[a.act ? a.act[row] : row];
+    if (g.t >= 0 && g.t < a.vocab) g.x = ld_elem<DT>(a.logits, row * a.ld + g.t);
+  }
+  return g;
+}
+// what a row's sums give
+__device__ __forceinline__ void put_row(const LogprobArgs &a, int64_t row, const Given &g, bool none, float M, float r,
+                                        float s1) {
   const float lz = log1pf(r);
   if (a.entropy) a.entropy[row] = none ? NAN : lz - s1 / (1.f + r);
-  if (a.logprob) {
-    const int t = a.tokens[a.act ? a.act[row] : row];
-    float v = NAN;
-    if (t >= 0 && t < a.vocab) v = ld_elem<DT>(a.logits, row * a.ld + t) - M - lz;
-    a.logprob[row] = t < 0 ? 0.f : none ? NAN : v;
-  }
+  if (a.logprob) a.logprob[row] = g.t < 0 ? 0.f : none || g.t >= a.vocab ? NAN : g.x - M - lz;
 }
 __device__ __forceinline__ void put_top(const LogprobArgs &a, int64_t row, bool none, float M, float lz, int rank,
                                         uint64_t key) {
@@ -170,8 +180,8 @@ __device__ __forceinline__ uint64_t *row_keys(const LogprobArgs &a, int64_t row)
 // The k-th keys of all parts, k = ceil(top / parts): at least `top` keys reach the
 // least of them.  Every wave joins the sums by itself, the keys are asked for
 // beside them.
-template <int DT, bool SAME>
-__device__ __forceinline__ void join_parts(const LogprobArgs &a, int64_t row, SelectLds &lds) {
+template <bool SAME>
+__device__ __forceinline__ void join_parts(const LogprobArgs &a, int64_t row, const Given &given, SelectLds &lds) {
   constexpr int HOLD = 4;  // keys of a thread that stay in registers
   const int lane = threadIdx.x & 63;
   const LogprobPart *p = row_parts(a, row);
@@ -197,7 +207,7 @@ __device__ __forceinline__ void join_parts(const LogprobArgs &a, int64_t row, Se
   }
   const float M = wave_max(m);
   if (__ballot(bad) || M == -INFINITY) {
-    if (threadIdx.x == 0) put_row<DT>(a, row, true, 0.f, 0.f, 0.f);
+    if (threadIdx.x == 0) put_row(a, row, given, true, 0.f, 0.f, 0.f);
     put_no_top(a, row);
     return;
   }
@@ -213,7 +223,7 @@ __device__ __forceinline__ void join_parts(const LogprobArgs &a, int64_t row, Se
   r = wave_sum(r);
   s1 = wave_sum(s1);
   if (threadIdx.x == 0) {
-    put_row<DT>(a, row, false, M, r, s1);
+    put_row(a, row, given, false, M, r, s1);
     lds.n = 0;
   }
   if (a.top <= 0) return;
@@ -288,6 +298,7 @@ __global__ __launch_bounds__(LP_THREADS, 5) void k_logprobs(LogprobArgs a) {
       }
     }
   }
+  const Given given = given_token<DT>(a, row);
   if (skip0) {
 #pragma unroll
     for (int i = 0; i < VPT; ++i)
@@ -403,7 +414,7 @@ __global__ __launch_bounds__(LP_THREADS, 5) void k_logprobs(LogprobArgs a) {
   LogprobPart *mine = row_parts(a, row) + part;
   if (threadIdx.x == 0) {
     if (whole) {
-      put_row<DT>(a, row, none, M, r, s1);
+      put_row(a, row, given, none, M, r, s1);
     } else {
       st_part(a.count, &mine->m, M);
       st_part(a.count, &mine->r, r);
@@ -451,13 +462,13 @@ __global__ __launch_bounds__(LP_THREADS, 5) void k_logprobs(LogprobArgs a) {
     s_last = last;
   }
   __syncthreads();
-  if (s_last) join_parts<DT, true>(a, row, s_sel);
+  if (s_last) join_parts<true>(a, row, given, s_sel);
 }
 
 template <int DT>
 __global__ __launch_bounds__(LP_THREADS) void k_logprobs_join(LogprobArgs a) {
   __shared__ SelectLds s_sel;
-  join_parts<DT, false>(a, blockIdx.x, s_sel);
+  join_parts<false>(a, blockIdx.x, given_token<DT>(a, blockIdx.x), s_sel);
 }
 
 template <int DT>

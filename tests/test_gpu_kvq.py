@@ -221,6 +221,16 @@ def test_attention_over_long_rows(dtype, lengths):
     fill_and_check(hs, dtype, lengths, 2, 2, 64, 512, seed=4)
 
 
+@pytest.mark.parametrize("heads,n_kv,hd", [(4, 4, 64), (28, 4, 128)])
+def test_fp32_rows_keep_fp32_precision(heads, n_kv, hd):
+    """As a whole: the roundings of fp32 sums (2^-24 of each of a few terms, of either sign) are below 2^-20 of the
+    result in the 2-norm; a product of fewer bits than fp32 anywhere on the way is not."""
+    import paper_2603_12707_amd as hs
+    cache, q, lens, got = fill_and_check(hs, "f32", [620, 90, 1500], heads, n_kv, hd, 32, seed=17)
+    want = R.attention(R.Layout(cache.blocks, cache.table, 1, n_kv, hd, 32), 0, q.cpu(), lens.cpu())[0]
+    assert float((got.double().cpu() - want).norm() / want.norm()) < 2.0 ** -20
+
+
 def test_attention_over_very_long_rows():
     import paper_2603_12707_amd as hs
     fill_and_check(hs, "bf16", [70001, 3], 7, 1, 128, 1024, seed=6)
