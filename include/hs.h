@@ -357,7 +357,8 @@ int hs_decode_step_static(hs_model *m, hs_kv *kv, const int32_t *tokens_in, int3
  * hs_kvq_block_bytes: 2 * n_layers * n_kv_heads * block_tokens * head_dim * 17/32.
  * Position p of sequence s lives in block table[s * table_ld + p / block_tokens];
  * a number that is negative or not below bytes / block_bytes means that there is
- * no block: nothing is stored there, nothing read, and attention masks it.
+ * no block: nothing is stored there, nothing read, and attention masks it.  A
+ * cache is written and read in one row type.
  * blocks: 16-byte aligned; head_dim 64 or 128, n_kv_heads 1..4096. */
 typedef struct hs_kvq_cache {
   void *blocks;         /* device */
@@ -394,7 +395,7 @@ int hs_kvq_read(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, int32_t
  * i / (n_heads / n_kv_heads), at most 16 heads to a KV head:
  *   out[r][i] = sum_p softmax_p(scale * q_i . k_p) v_p
  * over the positions that have a block, in fp32, rounded once to `dtype`; a row
- * without one (length 0 or negative) gives zeros.  max_len (host, > 0) bounds
+ * without one (length 0 or negative) gives zeros.  max_len (host, 1..2^30) bounds
  * the lengths and shapes the launch; positions from it on are not attended.
  * q, out, ld_q and ld_out are aligned as in hs_kvq_append.  workspace is device
  * memory of hs_kvq_attention_workspace bytes (which may be 0: then it may be

@@ -1473,7 +1473,7 @@ int kvq_rows_args(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, int32
   if (n == 0) return HS_OK;
   if (!k || !v || !positions) return fail(HS_E_INVALID, "%s: NULL argument", fn);
   if (((uintptr_t)k | (uintptr_t)v) % 16) return fail(HS_E_INVALID, "%s: rows must be 16-byte aligned", fn);
-  if ((int64_t)n * cache->n_kv_heads > (1ll << 31)) return fail(HS_E_INVALID, "%s: too many rows", fn);
+  if ((int64_t)n * cache->n_kv_heads > (1ll << 30)) return fail(HS_E_INVALID, "%s: too many rows", fn);
   return kvq_strides(fn, dtype, n, ld, ld_head, cache->n_kv_heads, cache->head_dim);
 }
 
@@ -1532,7 +1532,8 @@ int hs_kvq_attention_workspace(const hs_kvq_cache *cache, int32_t dtype, int32_t
   const int rc = hs_kvq_block_bytes(cache->n_layers, cache->n_kv_heads, cache->head_dim, cache->block_tokens, &bb);
   if (rc) return rc;
   if (dtype < HS_F32 || dtype > HS_BF16) return fail(HS_E_INVALID, "%s: unknown dtype", fn);
-  if (n < 0 || max_len <= 0) return fail(HS_E_INVALID, "%s: negative row count or max_len not positive", fn);
+  if (n < 0 || max_len <= 0 || max_len > (1 << 30))
+    return fail(HS_E_INVALID, "%s: negative row count, or max_len not in 1..2^30", fn);
   if (n_heads <= 0 || n_heads % cache->n_kv_heads || n_heads / cache->n_kv_heads > 16)
     return fail(HS_E_INVALID, "%s: n_heads %d is not 1..16 times n_kv_heads %d", fn, n_heads, cache->n_kv_heads);
   if ((int64_t)n * n_heads > (1 << 30)) return fail(HS_E_INVALID, "%s: too many rows", fn);

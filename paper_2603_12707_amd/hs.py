@@ -577,7 +577,7 @@ class QuantCache:
             raise ValueError(f"{func}: out must be of q's shape and type, each row contiguous")
         n, heads, dt = shape[0], shape[1], _dtype_code(func, q)
         if max_len is None:
-            max_len = min(self.table.shape[1] * self.block_tokens, 2**31 - 1)
+            max_len = min(self.table.shape[1] * self.block_tokens, 1 << 30)
         if workspace is None:
             workspace = torch.empty(self._workspace_bytes(dt, n, heads, max_len), dtype=torch.uint8,
                                     device=self.blocks.device)

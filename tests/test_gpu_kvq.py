@@ -266,6 +266,18 @@ def test_attention_rows_share_sequences_and_lengths_are_bounded():
     assert not out[:3].any() and torch.equal(out[3], got[3])
 
 
+@pytest.mark.parametrize("n", [200, 256])
+def test_many_rows_are_started_longest_first(n):
+    """More work groups than the GPU holds: every row once, whatever the lengths (equal ones, none, the bound's own)."""
+    import paper_2603_12707_amd as hs
+    g = torch.Generator().manual_seed(n)
+    lengths = torch.randint(0, 90, (n,), generator=g).tolist()
+    lengths[n // 2], lengths[3], lengths[n - 1] = 2100, 2048, 2100
+    lengths[10:80] = [33] * 70
+    fill_and_check(hs, "bf16", lengths, 8, 4, 64, 256, seed=18, max_len=2100)
+    fill_and_check(hs, "f16", [7] * n, 4, 4, 64, 64, seed=19, max_len=4096, seqs=[i % 5 for i in range(n)])
+
+
 @pytest.mark.parametrize("scale,spread", [(1.0, 30.0), (1e-6, 1.0), (-0.125, 1.0), (40.0, 8.0), (0.0, 1.0)],
                          ids=["peaked", "flat", "negative", "huge", "zero"])
 def test_attention_of_other_scales(scale, spread):

@@ -224,6 +224,24 @@ def _filled(cfg, slots=3, max_ctx=600):
     return model, pools
 
 
+@pytest.mark.parametrize("length", [2600, 6000])
+def test_long_requests_in_several_splits(length):
+    """Splits joined in the output projection (up to eight) and by the combine kernel."""
+    import paper_2603_12707_amd as hs
+    cfg = small_cfg(**GQA)
+    run = Run(cfg, slots=2, n_blocks=-(-(length + 40) // 256) + 2, max_ctx=length + 40)
+    for slot, n in ((0, length), (1, 300)):
+        run.pool.admit(slot, 0, n + 20)
+        run.pool.set_length(slot, n, n)
+        for l in range(cfg["n_layers"]):
+            for sel in range(2):
+                for j in range(cfg["n_kv_heads"]):
+                    run.pool.write(slot, l, sel, j, 0, synth.kv_block(cfg, slot, l, sel, j, n, device="cuda"))
+        run.len[slot], run.pos[slot] = n, n
+    run.decode(2)
+    run.close()
+
+
 def test_static_step_equals_the_step():
     cfg = small_cfg(**GQA)
     model, (a, b) = _filled(cfg)

@@ -46,7 +46,7 @@ def test_block_bytes():
 
 
 @pytest.mark.parametrize("bad", [(0, 1, 64, 16), (1, 0, 64, 16), (1, 1, 96, 16), (1, 1, 32, 16), (1, 1, 64, 8),
-                                 (1, 1, 64, 48), (1, 1, 64, 32768), (-1, 1, 64, 16), (2 ** 31 - 1, 2 ** 31 - 1, 128, 16384)])
+                                 (1, 1, 64, 48), (1, 1, 64, 32768), (1, 4097, 64, 16), (-1, 1, 64, 16), (2 ** 31 - 1, 2 ** 31 - 1, 128, 16384)])
 def test_block_bytes_refuses(bad):
     with pytest.raises(hs.HsError) as e:
         hs.kvq_block_bytes(*bad)
@@ -94,6 +94,7 @@ def test_append_values_come_in_pairs_and_aligned():
 def test_attention_refused():
     for fault in (dict(q=None), dict(out=None), dict(lens=None), dict(q=AT + 8), dict(out=AT + 2), dict(ws=AT + 4),
                   dict(heads=0), dict(heads=3), dict(heads=34), dict(heads=-2), dict(max_len=0), dict(max_len=-5),
+                  dict(max_len=2 ** 30 + 1),
                   dict(ld_q=255), dict(ld_q=128), dict(ld_out=128), dict(n=2 ** 30)):
         assert attend(cache(), **fault) == H.HS_E_INVALID, fault
 
@@ -114,7 +115,7 @@ def test_attention_workspace_is_checked():
 def test_logprobs_refused():
     for fault in (dict(dtype=3), dict(logits=None), dict(logits=AT + 2), dict(rows=-1), dict(rows=1 << 40),
                   dict(vocab=0), dict(vocab=-7), dict(ld=99), dict(ld=1 << 50), dict(tokens=None), dict(top=-1),
-                  dict(top=65), dict(vocab=2), dict(ws=AT + 4)):
+                  dict(top=65), dict(vocab=2), dict(ws=AT + 4), dict(vocab=2 ** 30 + 1, ld=2 ** 31)):
         assert logprobs(**fault) == H.HS_E_INVALID, fault
     assert logprobs(dtype=H.HS_F16, logits=AT + 1) == H.HS_E_INVALID
     assert logprobs(rows=0) == H.HS_OK
@@ -128,6 +129,15 @@ def test_logprobs_workspace_is_checked():
         assert logprobs(rows=16, vocab=152064, ld=152064, top=20, ws=None) == H.HS_E_BUFFER
         assert logprobs(rows=16, vocab=152064, ld=152064, top=20, ws_bytes=need.value - 1) == H.HS_E_BUFFER
     assert ask(16, 152064, 20, None) == H.HS_E_INVALID
+
+
+def test_pool_and_step_refuse_what_is_missing():
+    """(What needs a model is refused in the GPU tests.)"""
+    out = ctypes.c_void_p(7)
+    L = hs.lib()
+    assert L.hs_kvq_pool_create(None, 1, 256, AT, 1 << 20, ctypes.byref(out)) == H.HS_E_INVALID and not out.value
+    assert L.hs_kvq_pool_create(None, 1, 256, AT, 1 << 20, None) == H.HS_E_INVALID
+    assert L.hs_decode_step_logprobs(None, None, AT, AT, None, 1, None, None, AT, AT, AT, AT, None) == H.HS_E_INVALID
 
 
 def test_binding_refuses_wrong_tensors():
