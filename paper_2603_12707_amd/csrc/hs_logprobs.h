@@ -60,19 +60,23 @@ __device__ __forceinline__ uint64_t block_max(uint64_t v, uint64_t *s_tmp) {
   return v;
 }
 
+template <int PER>
+__device__ __forceinline__ int wave_count(const uint32_t (&v)[PER], uint32_t c) {  // values from c on
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) n += (int)__popcll(__ballot(v[i] >= c));
+  return n;
+}
 // The k-th largest of PER * 64 values, PER to a lane, bit by bit: bits `from` down
 // to `to` of it, those above given.
 template <int PER>
 __device__ __forceinline__ uint32_t wave_kth(const uint32_t (&v)[PER], int k, int from, int to, uint32_t t = 0) {
-  for (int b = from; b >= to; --b) {
-    const uint32_t c = t | 1u << b;
-    int n = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) n += (int)__popcll(__ballot(v[i] >= c));
-    if (n >= k) t = c;
-  }
+  for (int b = from; b >= to; --b)
+    if (wave_count(v, t | 1u << b) >= k) t |= 1u << b;
   return t;
 }
+
+constexpr uint32_t ORD_LEAST = 0x007FFFFFu;  // -inf's order bits
 
 // Hands the `top` largest of the work group's keys to put(rank, key), each once.
 // for_each(floor, f) calls f(key) for those of the thread's own keys whose value
@@ -262,7 +266,8 @@ __global__ __launch_bounds__(LP_THREADS, 5) void k_logprobs(LogprobArgs a) {
   __shared__ float s_m[LP_WAVES], s_r[LP_WAVES], s_1[LP_WAVES];
   __shared__ int s_lead[LP_WAVES], s_last;
   __shared__ uint32_t s_ord[LP_THREADS];
-  __shared__ int s_first[LP_WAVES];
+  __shared__ uint32_t s_kth;
+  __shared__ int s_first[LP_WAVES], s_tie;
   const int64_t row = blockIdx.x / (uint32_t)a.parts;
   const int part = (int)(blockIdx.x % (uint32_t)a.parts), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   // the last of several parts is read from further ahead, so that it is whole; what
@@ -333,82 +338,94 @@ __global__ __launch_bounds__(LP_THREADS, 5) void k_logprobs(LogprobArgs a) {
   float M = s_m[0];
 #pragma unroll
   for (int w2 = 1; w2 < LP_WAVES; ++w2) M = fmaxf(M, s_m[w2]);
-  // the lowest place of value v among the thread's elements
+  // the place of the first of the thread's elements that is v (there is one)
   auto first_of = [&](float v) {
-    int first = 0x7FFFFFFF;
+    int at = 0;
 #pragma unroll
-    for (int i = VPT - 1; i >= 0; --i)
-      if (raw_elem<DT, NW>(w, i) == v) first = min(first, place(i));
+    for (int i = VPT - 1; i >= 0; --i) at = raw_elem<DT, NW>(w, i) == v ? i : at;
     keep();
-    return first;
+    return place(at);
   };
-  uint64_t floor_key = 0;
-  if (a.top > 1) {
+  // The floor: one wave finds it while the others sum, another one in the next work group.
+  // Among threads that share the top-th largest maximum the lowest places would come
+  // first; where many share it, s_tie has the others wait for that.
+  if (a.top > 1 && wave == (int)(blockIdx.x & (LP_WAVES - 1))) {
     uint32_t all[LP_WAVES];
 #pragma unroll
     for (int i = 0; i < LP_WAVES; ++i) all[i] = s_ord[i * 64 + lane];
-    auto count = [&](uint32_t c, bool equal) {
-      int n2 = 0;
-#pragma unroll
-      for (int i = 0; i < LP_WAVES; ++i) n2 += (int)__popcll(__ballot(equal ? all[i] == c : all[i] >= c));
-      return n2;
-    };
     // the upper half of the bits does, unless many threads share it
     // (no number orders below -inf, whose lower bits are set)
-    constexpr uint32_t LEAST = 0x007FFFFFu;
-    uint32_t kth = max(wave_kth(all, a.top, 31, 16), LEAST);
-    if (count(kth, false) > a.top + 16) kth = max(wave_kth(all, a.top, 15, 0, kth & 0xFFFF0000u), LEAST);
-    floor_key = (uint64_t)kth << 32;
-    const int reach = count(kth, false), share = count(kth, true);
-    if (reach > a.top + 16) {
-      // threads that share all of it: the lowest places among them come first
-      __syncthreads();
-      s_ord[threadIdx.x] = ord == kth ? (uint32_t)~first_of(tm) : 0u;
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < LP_WAVES; ++i) all[i] = s_ord[i * 64 + lane];
-      floor_key |= wave_kth(all, a.top - (reach - share), 31, 0);  // the largest complement is the lowest place
-    }
+    uint32_t kth = max(wave_kth(all, a.top, 31, 16), ORD_LEAST);
+    if (wave_count(all, kth) > a.top + 16) kth = max(wave_kth(all, a.top, 15, 0, kth & 0xFFFF0000u), ORD_LEAST);
+    if (lane == 0) s_kth = kth, s_tie = wave_count(all, kth) > a.top + 16;
   }
+  // every e^(x - M), the maximum's own 1 among them
   float r = 0.f, s1 = 0.f;
-  bool lead = false;  // leaves one instance of the maximum out of its sum
   if (M > -INFINITY) {
-    if (__ballot(tm == M)) {
-      // a wave that holds the maximum: a thread's first instance of it is left out
 #pragma unroll
-      for (int i = 0; i < VPT; ++i) {
-        const float v = raw_elem<DT, NW>(w, i), d = v - M;
-        const bool out = v == M && !lead;
-        const float e = out ? 0.f : __expf(d);
-        lead |= out;
-        r += e;
-        s1 = __builtin_fmaf(fmaxf(d, LOGPROB_FAR), e, s1);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < VPT; ++i) {
-        const float d = raw_elem<DT, NW>(w, i) - M, e = __expf(d);
-        r += e;
-        s1 = __builtin_fmaf(fmaxf(d, LOGPROB_FAR), e, s1);
-      }
+    for (int i = 0; i < VPT; ++i) {
+      const float d = raw_elem<DT, NW>(w, i) - M, e = __expf(d);
+      r += e;
+      s1 = __builtin_fmaf(fmaxf(d, LOGPROB_FAR), e, s1);
     }
     keep();
   }
   r = wave_sum(r);
   s1 = wave_sum(s1);
-  const int wlead = (int)__popcll(__ballot(lead));
   int first = 0x7FFFFFFF;
   if (a.top == 1 && wm == M) {
-    first = first_of(M);
+    if (tm == M) first = first_of(M);
     for (int off = 32; off >= 1; off >>= 1) first = min(first, __shfl_xor(first, off));
   }
-  if (lane == 0) s_r[wave] = r, s_1[wave] = s1, s_lead[wave] = wlead, s_first[wave] = first;
+  if (lane == 0) s_r[wave] = r, s_1[wave] = s1, s_first[wave] = first;
   __syncthreads();
   r = s1 = 0.f;
-  int leads = 0;
 #pragma unroll
-  for (int w2 = 0; w2 < LP_WAVES; ++w2) r += s_r[w2], s1 += s_1[w2], leads += s_lead[w2];
-  r += (float)max(leads - 1, 0);
+  for (int w2 = 0; w2 < LP_WAVES; ++w2) r += s_r[w2], s1 += s_1[w2];
+  uint64_t floor_key = 0;
+  if (a.top > 1) {
+    const uint32_t kth = s_kth;
+    floor_key = (uint64_t)kth << 32;
+    if (s_tie) {
+      uint32_t all[LP_WAVES];
+#pragma unroll
+      for (int i = 0; i < LP_WAVES; ++i) all[i] = s_ord[i * 64 + lane];
+      const int above = kth == ~0u ? 0 : wave_count(all, kth + 1);
+      __syncthreads();
+      s_ord[threadIdx.x] = ord == kth ? (uint32_t)~first_of(tm) : 0u;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < LP_WAVES; ++i) all[i] = s_ord[i * 64 + lane];
+      floor_key |= wave_kth(all, a.top - above, 31, 0);  // the largest complement is the lowest place
+    }
+  }
+  if (M > -INFINITY && M < INFINITY && r < 1.f + 0x1p-4f) {
+    // nearly certain: the difference would lose the rest's digits, so the rest is summed by
+    // itself.  A thread with the maximum leaves its first instance out.
+    const bool lead = tm == M;
+    float rest = 0.f;
+    bool out = lead;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const float v = raw_elem<DT, NW>(w, i);
+      const bool skip = out && v == M;
+      out &= !skip;
+      rest += skip ? 0.f : __expf(v - M);
+    }
+    keep();
+    rest = wave_sum(rest);
+    const int leads = (int)__popcll(__ballot(lead));
+    __syncthreads();
+    if (lane == 0) s_r[wave] = rest, s_lead[wave] = leads;
+    __syncthreads();
+    r = 0.f;
+    int n2 = 0;
+#pragma unroll
+    for (int w2 = 0; w2 < LP_WAVES; ++w2) r += s_r[w2], n2 += s_lead[w2];
+    r += (float)(n2 - 1);
+  } else {
+    r -= 1.f;
+  }
   const bool bad = !(r < INFINITY) || M == INFINITY;
   const bool whole = a.parts == 1, none = bad || M == -INFINITY;
   LogprobPart *mine = row_parts(a, row) + part;
