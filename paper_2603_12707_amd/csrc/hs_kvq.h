@@ -197,17 +197,19 @@ __global__ __launch_bounds__(256) void k_kvq_read(KvqRows a) {
 // and keeps an online softmax for the G query heads of the head in the 16
 // columns of the matrix products.
 //
-// Scores: S^T = K Q^T, the scaled MFMA 16x16x128 with 16 positions as rows.  It
-// takes K as it lies in memory: lane (li, lg) = (lane % 16, lane / 16) supplies
-// group lg of its position and the group's exponent byte.  Q enters as the sum of
-// e4m3 parts, each with what the parts before left, times 16 (two hold a bf16
-// number, three an f16), scaled by a power of two of the head's largest element:
-// every product is exact, an element below 2^-13 of the largest is off by at most
-// 2^-17 of 16^-parts of it.  The instruction's sums are good to about 2^-20 of the
-// largest product (measured), which is short of fp32: fp32 rows convert K to bf16
-// and take Q as three bf16 parts through the MFMA 16x16x32.  Row r of the tile's product t is
-// position 16 (r / 4) + 4 t + r % 4, so that a lane ends up with the scores of
-// the 16 consecutive positions 16 lg .. for head li, which is the B operand of
+// Scores: S^T = K Q^T with 16 positions as rows.  Lane (li, lg) = (lane % 16,
+// lane / 16).  bf16 rows take the scaled MFMA 16x16x128, which reads K as it lies
+// in memory: a lane supplies group lg of its position and the group's exponent
+// byte.  Q enters as the sum of two e4m3 parts (the second what the first left,
+// times 16), scaled by a power of two of the head's largest element: every product
+// is exact, and an element below 2^-13 of the largest is off by at most 2^-21 of
+// it.  The instruction's own sums are good to 2^-16 of the largest product
+// (measured; 2^-19 on average), well below what rounding Q and K to bf16 left.  f16
+// and fp32 rows, which that would cost digits, convert K (HD / 4 elements of a
+// position a lane, one group's scale) and take Q as one f16 or three bf16 parts
+// through the MFMA 16x16x32.  Row r of the tile's product t is position
+// 16 (r / 4) + 4 t + r % 4, so that a lane ends up with the scores of the 16
+// consecutive positions 16 lg .. for head li, which is the B operand of
 // O^T += V^T P^T (MFMA 16x16x32): positions 8 m .. 8 m + 7 of each lane group are
 // the k range of MFMA m.  For V^T a lane reads its HD / 16 channels of those 16
 // positions, converts pairs of channels (exact in the 16-bit type) and pairs the
@@ -225,7 +227,10 @@ constexpr int KVQ_MMA = DT == HS_F16 ? HS_F16 : HS_BF16;
 template <int DT>
 constexpr int KVQ_P_PARTS = DT == HS_F32 ? 3 : 2;
 template <int DT>
-constexpr int KVQ_Q_PARTS = DT == HS_BF16 ? 2 : 3;
+constexpr int KVQ_Q_PARTS = DT == HS_BF16 ? 2 : DT == HS_F16 ? 1 : 3;
+// bf16 rows' scores come from the scaled MFMA
+template <int DT>
+constexpr bool KVQ_SCALED = DT == HS_BF16;
 constexpr int KVQ_TILE = 64, KVQ_PLANES = 3;
 // Rows are started longest first where the GPU does not hold all work groups at
 // once and the longest rows take a while: up to this many rows, and from so many
@@ -455,8 +460,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
   const float sign = a.scale < 0.f ? -1.f : 1.f;
   [[maybe_unused]] i32x8 qb[QP];               // scaled MFMA: e4m3 parts
   [[maybe_unused]] int qs = 0;                 // and their scale bytes
-  [[maybe_unused]] u32x4 qh[QP][HD / 32];      // fp32 rows: bf16 parts
-  if constexpr (DT == HS_F32) {
+  [[maybe_unused]] u32x4 qh[QP][HD / 32];      // else: parts in the 16-bit type
+  if constexpr (!KVQ_SCALED<DT>) {
 #pragma unroll
     for (int c = 0; c < HD / 32; ++c) {
       float f[8] = {};
@@ -515,13 +520,13 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
     if (one) wait_copies<2 * COPIES>();  // V, and the next tile's K
     else wait_copies<COPIES>();
     f32x4 sc[4];
-    if constexpr (DT == HS_F32) {
+    if constexpr (!KVQ_SCALED<DT>) {
       constexpr int FGRP = HD == 128 ? 0 : 1;  // lane groups to a group of 32, as a shift
       const u32x4 ks = *(const u32x4 *)(kp + kspan * SPAN + HD * 8 + (lg >> FGRP) * 16);
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         const uint32_t *at = (const uint32_t *)(kp + kspan * SPAN + (4 * x + (li & 3)) * (HD / 2) + lg * (HD / 8));
-        const float s = kvq_scale((ks[x] >> (8 * (li & 3))) & 255u);
+        const float s = __uint_as_float((ks[x] >> (8 * (li & 3))) << 23);  // (exponent bits alone)
         sc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < HD / 32; ++c) {
