@@ -369,6 +369,13 @@ __global__ __launch_bounds__(LP_THREADS, 5) void k_logprobs(LogprobArgs a) {
       s1 = __builtin_fmaf(fmaxf(d, LOGPROB_FAR), e, s1);
     }
     keep();
+  } else {  // -inf and NaN only: the maximum passes a NaN over
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const float v = raw_elem<DT, NW>(w, i);
+      r = v != v ? v : r;
+    }
+    keep();
   }
   r = wave_sum(r);
   s1 = wave_sum(s1);

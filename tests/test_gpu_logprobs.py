@@ -90,6 +90,22 @@ def test_banned_words_and_rows_without_a_distribution(vocab):
     check(hs, x.cuda(), torch.tensor([vocab, vocab + 5, 2 ** 31 - 1, -2 ** 31] * 3), 1)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("vocab", [700, 40000])
+def test_nan_among_banned_words(dtype, vocab):
+    """A NaN counts too where the numbers about it are all -inf, or where there are none."""
+    import paper_2603_12707_amd as hs
+    x = torch.full((6, vocab), -math.inf)
+    x[:, vocab - 1] = 1.0
+    x[0, :] = math.nan
+    x[1, 3] = math.nan
+    x[2, :vocab // 2] = math.nan
+    x[3, vocab // 2:] = math.nan
+    x[4, :vocab - 1] = math.nan
+    for top in (0, 1, 5):
+        check(hs, x.to(R.DT[dtype]).cuda(), torch.tensor([vocab - 1, 0, vocab - 1, 0, vocab - 1, vocab - 1]), top)
+
+
 def test_nearly_certain_tokens_keep_their_digits():
     """log Z of a row with one likely word: as small as e^-40, and within a few 2^-22 of itself."""
     import paper_2603_12707_amd as hs
