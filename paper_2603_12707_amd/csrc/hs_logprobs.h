@@ -10,6 +10,8 @@
 
 #include "hs_device.h"
 
+#include <cfloat>
+
 namespace hs {
 namespace {
 
@@ -359,24 +361,18 @@ __global__ __launch_bounds__(LP_THREADS, 5) void k_logprobs(LogprobArgs a) {
     if (wave_count(all, kth) > a.top + 16) kth = max(wave_kth(all, a.top, 15, 0, kth & 0xFFFF0000u), ORD_LEAST);
     if (lane == 0) s_kth = kth, s_tie = wave_count(all, kth) > a.top + 16;
   }
-  // every e^(x - M), the maximum's own 1 among them
+  // every e^(x - M), the maximum's own 1 among them; without a number above -inf
+  // the difference is to the lowest one, so that only a NaN, which the maximum passed
+  // over, gives a NaN
   float r = 0.f, s1 = 0.f;
-  if (M > -INFINITY) {
+  const float ref = fmaxf(M, -FLT_MAX);
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      const float d = raw_elem<DT, NW>(w, i) - M, e = __expf(d);
-      r += e;
-      s1 = __builtin_fmaf(fmaxf(d, LOGPROB_FAR), e, s1);
-    }
-    keep();
-  } else {  // -inf and NaN only: the maximum passes a NaN over
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      const float v = raw_elem<DT, NW>(w, i);
-      r = v != v ? v : r;
-    }
-    keep();
+  for (int i = 0; i < VPT; ++i) {
+    const float d = raw_elem<DT, NW>(w, i) - ref, e = __expf(d);
+    r += e;
+    s1 = __builtin_fmaf(fmaxf(d, LOGPROB_FAR), e, s1);
   }
+  keep();
   r = wave_sum(r);
   s1 = wave_sum(s1);
   int first = 0x7FFFFFFF;
