@@ -257,9 +257,19 @@ __device__ __forceinline__ float raw_elem(const uint32_t (&w)[NW], int i) {
 // registers as they are: read once, all loads in flight together.  First the
 // maximum, then the sums, then the alternatives: the top-th largest of the 256
 // threads' own maxima is a value that at least `top` elements reach, and few more
-// (every wave finds it, bit by bit with ballots).  A single alternative is the
-// maximum's first place.  A NaN makes the sum NaN.  A row of one part is finished here; of several, by the last
-// of its work groups to arrive, or by k_logprobs_join.
+// (one wave finds it, bit by bit with ballots, while the others sum).  A single
+// alternative is the maximum's first place.  A NaN makes the sum NaN.  A row of one
+// part is finished here; of several, by the last of its work groups to arrive, or by
+// k_logprobs_join.
+//
+// Measured: 256 rows of 152064 fp32 logits (156 MB), no alternatives 34 us, one 39,
+// five 45, twenty 54; 1531 rows of 32003 bf16 logits (98 MB) 32, 38, 41, 44.  The sums
+// are bound by the vector unit (an exponential, a conversion and four more operations an
+// element, half of its cycles) and by each work group's chain of load, maximum and sum,
+// of which five share a CU; the alternatives add the floor's 16 ballots and the
+// ranking.  16 rows of 152064: 9, 12, 15, 17 us, one row of 32000: 6, 8, 9.5, 11, the
+// chain of one part and of the join.  A work group to a row that read it again for each
+// pass took 1204 us for the 256 rows with twenty.
 template <int DT, int NW>
 __global__ __launch_bounds__(LP_THREADS, 5) void k_logprobs(LogprobArgs a) {
   constexpr int VEC = DT == HS_F32 ? 4 : 8, VPT = NW * VEC / 4, NV = NW / 4, PART = LP_THREADS * VPT;
@@ -476,7 +486,9 @@ __global__ __launch_bounds__(LP_THREADS, 5) void k_logprobs(LogprobArgs a) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (threadIdx.x == 0) {
-    uint32_t *c = (uint32_t *)a.ws + row;
+    // (as far apart as they may lie: counters in one cache line wait for each other,
+    // 16.7 us against 14.2 for 16 rows of 19 parts)
+    uint32_t *c = (uint32_t *)a.ws + row * min(32, LOGPROB_COUNTERS / (int)a.rows);
     const bool last = __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(a.parts - 1);
     if (last) st_part(true, c, 0u);  // for the next call
     s_last = last;
@@ -485,6 +497,8 @@ __global__ __launch_bounds__(LP_THREADS, 5) void k_logprobs(LogprobArgs a) {
   if (s_last) join_parts<true>(a, row, given, s_sel);
 }
 
+// Rows past one launch's: 6.4 us for 1531 rows of two parts with one alternative, 8 .. 15
+// for 256 rows of 19 parts with twenty, two dependent reads and the ranking.
 template <int DT>
 __global__ __launch_bounds__(LP_THREADS) void k_logprobs_join(LogprobArgs a) {
   __shared__ SelectLds s_sel;
@@ -494,14 +508,17 @@ __global__ __launch_bounds__(LP_THREADS) void k_logprobs_join(LogprobArgs a) {
 template <int DT>
 hipError_t logprobs_dt(LogprobArgs a, hipStream_t st) {
   constexpr int CE = Ty<DT>::CE / 4;  // elements of a word
-  // rows that eight words a thread hold: fewer registers, and no thread without an element
+  // rows that eight words a thread hold: fewer registers, and no thread without an
+  // element (1531 rows of 2048 fp32 logits 7.4 us, with 32 words 11.2; one row 3.6 and 5.0)
   const bool small = a.vocab <= LP_THREADS * 8 * CE;
   a.parts = small ? 1 : (int)(((int64_t)a.vocab + LP_THREADS * 32 * CE - 1) / (LP_THREADS * 32 * CE));
   const int64_t groups = a.rows * a.parts;
   if (groups > INT32_MAX) return hipErrorInvalidValue;
-  // One launch while the GPU holds all work groups at once: where more wait, joining
-  // at the end of a work group keeps its place for longer than a second launch takes.
-  a.count = a.parts > 1 && groups <= 1024 && a.rows <= LOGPROB_COUNTERS;
+  // One launch while the GPU holds all work groups at once, five to a CU: where more
+  // wait, joining at the end of a work group keeps its place for longer than a second
+  // launch takes (twenty alternatives, one launch against two: 64 rows of 152064 fp32
+  // logits 21.7 and 22.6 us, 128 rows 32.6 and 31.1; one row of 32000 12.0 and 14.1).
+  a.count = a.parts > 1 && groups <= 5 * 256 && a.rows <= LOGPROB_COUNTERS;
   if (small) HS_LAUNCH((k_logprobs<DT, 8>), dim3((uint32_t)groups), dim3(LP_THREADS), 0, st, a);
   else HS_LAUNCH((k_logprobs<DT, 32>), dim3((uint32_t)groups), dim3(LP_THREADS), 0, st, a);
   if (a.parts > 1 && !a.count) HS_LAUNCH((k_logprobs_join<DT>), dim3((uint32_t)a.rows), dim3(LP_THREADS), 0, st, a);
