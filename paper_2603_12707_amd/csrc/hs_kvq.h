@@ -130,7 +130,12 @@ __device__ __forceinline__ void kvq_place(const KvqRows &a, int row, int &seq, i
 
 // One thread takes eight elements; a work group takes one head of K or V of
 // 2048 / HD consecutive rows, so that a prefill pass's rows fill whole spans of 16
-// positions in one place.
+// positions in one place (with all heads of a row in one work group, whose spans
+// other work groups share, the pass below took 11.4 us).
+// Bound by the bytes: 14370 bf16 rows of 4 heads of 128 (29 MB in, 7.8 MB out) are
+// stored in 10.1 us, 3.7 TB/s both ways together, and fetched in 9.5; a copy of
+// gigabytes moves 4.8.  A step's 32 rows of 32 heads take 2.6 and 2.4 us, a launch's
+// least.
 template <int DT, int HD>
 struct KvqLine {
   static constexpr int CPR = HD / 8, ROWS = 256 / CPR, SB = DT == HS_F32 ? 4 : 2;
@@ -217,11 +222,21 @@ __global__ __launch_bounds__(256) void k_kvq_read(KvqRows a) {
 // and more; fp32: three, 24 bits), every sum is fp32.
 //
 // Each wave copies its tiles straight into LDS, K and V alike as they lie in
-// memory, a tile and a half ahead, through buffer ranges that end at the last span with a
-// position (past it LDS gets zeros and nothing is fetched).  The waits count the
-// wave's own copies, so that the waves never meet before the end.  Blocks of 64
-// positions and more (WIDE) hold a tile whole; smaller ones are copied span by
-// span.
+// memory, a tile and a half ahead, through buffer ranges that end at the last span
+// with a position (past it LDS gets zeros and nothing is fetched).  The waits count
+// the wave's own copies, so that the waves never meet before the end.  Blocks of 64
+// positions and more (WIDE) hold a tile whole; smaller ones are copied span by span.
+//
+// Measured: 256 rows of 1024 .. 8192 positions (bf16, 28/4 heads of 128; 645 MB)
+// 109 us, 5.9 TB/s, bound by memory (the copies alone take 115 us where copies and
+// arithmetic take 116, the arithmetic alone 83).  32 rows of 608 .. 960 (f16, 32/32
+// heads; 110 MB) 27 us, bound by the arithmetic and by 1024 work groups of uneven
+// length on 768 places (without copies 27).  Two rows of 120000 .. 131072 (bf16; 137 MB)
+// 33 us, of which 13 are the ramp, the last tiles and the join of 32 splits.  One
+// row of 700 8 us: the length, the block number and the first tile's copy one
+// after the other, 2 us a tile, the merge.  Before: K and V through registers and K
+// converted for bf16 too took 139 us for the first, and 131 as it is now but with two
+// kernels and splits everywhere.
 template <int DT>
 constexpr int KVQ_MMA = DT == HS_F16 ? HS_F16 : HS_BF16;
 template <int DT>
@@ -232,10 +247,11 @@ constexpr int KVQ_Q_PARTS = DT == HS_BF16 ? 2 : DT == HS_F16 ? 1 : 3;
 template <int DT>
 constexpr bool KVQ_SCALED = DT == HS_BF16;
 constexpr int KVQ_TILE = 64, KVQ_PLANES = 3;
-// Rows are started longest first where the GPU does not hold all work groups at
-// once and the longest rows take a while: up to this many rows, and from so many
-// positions on.
-constexpr int KVQ_RESIDENT = 3 * 256, KVQ_RANK_MOST = 256, KVQ_RANK_FROM = 2048;
+// Rows are started longest first where some CU takes more than one work group and the
+// longest rows take a while: up to this many rows, from more positions on.  28/4 heads, in
+// their own order and longest first: 250 rows of 1024 .. 8192 125 and 112 us, 66 rows 53.6
+// and 48.8, 160 rows of 400 .. 2000 29.2 and 27.1, of 200 .. 1000 19.1 and 19.3.
+constexpr int KVQ_CUS = 256, KVQ_RANK_MOST = 256, KVQ_RANK_FROM = 1024;
 typedef const __attribute__((address_space(4))) int64_t ConstI64;
 
 // as dma_1k_stream, four bytes a lane
@@ -729,7 +745,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (threadIdx.x == 0) {
-    uint32_t *c = a.count + (int64_t)row * a.c.n_kv + j;
+    // (counters as far apart as they may lie, so that few share a cache line)
+    uint32_t *c = a.count + (row * a.c.n_kv + j) * min(32, KVQ_COUNTERS / (a.n * a.c.n_kv));
     const bool last = __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(live - 1);
     if (last) __hip_atomic_store(c, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next call
     s_last = last;
@@ -768,7 +785,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
 
 // o = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s over the splits of a (row,
 // head); zeros where none holds a position.  HD / 4 threads take a split's
-// partial, 1024 / HD splits at a time, several of them in flight.
+// partial, 1024 / HD splits at a time, several of them in flight.  64 splits of 28
+// heads: 4.6 us, two dependent reads (beside 17.1 us of attention over 131072 positions).
 template <int DT, int HD>
 __global__ __launch_bounds__(256) void k_kvq_combine(KvqAttn a) {
   constexpr int TPS = HD / 4, PARTS = 256 / TPS, AHEAD = 4;
@@ -843,7 +861,8 @@ hipError_t kvq_rows_any(int dtype, int hd, const KvqRows &a, bool read, hipStrea
 }
 
 // Waves of a work group: eight while there are no more pairs than CUs, four where
-// several work groups share a CU (their LDS holds three).
+// several work groups share a CU (their LDS holds three).  Rows of 3000 .. 4000 in 256
+// pairs take 28.6 us with eight and 30.8 with four, in 288 pairs 43.9 and 39.6.
 int kvq_waves(int64_t pairs) { return pairs <= 256 ? 8 : 4; }
 
 template <int DT, int HD, int NW>
@@ -855,8 +874,8 @@ template <int DT, int HD>
 hipError_t kvq_attn_hd(KvqAttn a, hipStream_t st) {
   const int64_t grid = (int64_t)a.n * a.c.n_kv * a.n_split;
   if (grid > INT32_MAX || a.n_split > KVQ_MAX_SPLITS) return hipErrorInvalidValue;
-  a.rank = !a.order && a.n_split == 1 && a.n > 1 && a.n <= KVQ_RANK_MOST && a.max_len >= KVQ_RANK_FROM &&
-           grid > KVQ_RESIDENT;
+  a.rank = !a.order && a.n_split == 1 && a.n > 1 && a.n <= KVQ_RANK_MOST && a.max_len > KVQ_RANK_FROM &&
+           grid > KVQ_CUS;
   if (kvq_waves((int64_t)a.n * a.c.n_kv) == 8) kvq_attn_start<DT, HD, 8>(a, (uint32_t)grid, st);
   else kvq_attn_start<DT, HD, 4>(a, (uint32_t)grid, st);
   return hipGetLastError();
