@@ -50,6 +50,8 @@ __device__ __forceinline__ void add_part(const LogprobPart &p, float M, bool lea
 constexpr int LP_THREADS = 256, LP_WAVES = LP_THREADS / 64;
 // candidates that the selection's fast path holds
 constexpr int LP_CAND = 1024;
+// keys of a row's parts up to which all are candidates
+constexpr int LP_FEW = 64;
 
 // largest of the work group's values, in every thread
 __device__ __forceinline__ uint64_t block_max(uint64_t v, uint64_t *s_tmp) {
@@ -183,9 +185,11 @@ __device__ __forceinline__ uint64_t *row_keys(const LogprobArgs &a, int64_t row)
 
 // A work group joins a row's parts.  Every part gave its `top` largest keys in
 // order (elements past the row's end among them: they have the lowest keys).
-// The k-th keys of all parts, k = ceil(top / parts): at least `top` keys reach the
-// least of them.  Every wave joins the sums by itself, the keys are asked for
-// beside them.
+// The floor is the top-th largest of as many of the parts' first keys as a wave holds
+// two to a lane, at least `top`: hardly more of all reach it (with the least of the
+// parts' second keys 256 rows of 19 parts and twenty alternatives took 53.6 us, not
+// 47.5).  Few keys are ranked without one, as fast as it is found.  Every wave joins
+// the sums and finds the floor by itself; the keys are asked for beside them.
 template <bool SAME>
 __device__ __forceinline__ void join_parts(const LogprobArgs &a, int64_t row, const Given &given, SelectLds &lds) {
   constexpr int HOLD = 4;  // keys of a thread that stay in registers
@@ -199,17 +203,23 @@ __device__ __forceinline__ void join_parts(const LogprobArgs &a, int64_t row, co
     const int64_t i = u * LP_THREADS + threadIdx.x;
     hold[u] = i < n_keys ? ld_part<SAME>(&keys[i]) : 0;
   }
-  const int kth = a.top > 0 ? (a.top + a.parts - 1) / a.parts - 1 : 0;
+  // the first keys of the parts, part by part
+  constexpr int PER = 2;
+  const int n_first = min(a.parts, 64 * PER) * (a.top > 0 ? min(a.top, max(64 * PER / a.parts, 1)) : 0);
+  uint64_t key[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int e = i * 64 + lane, k = e / a.parts;
+    key[i] = n_keys > LP_FEW && e < n_first ? ld_part<SAME>(&keys[(int64_t)(e - k * a.parts) * a.top + k]) : 0;
+  }
   // parts lane, lane + 64, ..; the first of them kept
   auto part = [&](int c) { return LogprobPart{ld_part<SAME>(&p[c].m), ld_part<SAME>(&p[c].r), ld_part<SAME>(&p[c].s1), ld_part<SAME>(&p[c].bad)}; };
   const LogprobPart mine = lane < a.parts ? part(lane) : LogprobPart{-INFINITY, 0.f, 0.f, 0.f};
-  uint64_t low = a.top > 0 && lane < a.parts ? ld_part<SAME>(&keys[(int64_t)lane * a.top + kth]) : ~0ull;
   float m = mine.m;
   bool bad = mine.bad != 0.f;
   for (int c = lane + 64; c < a.parts; c += 64) {
     m = fmaxf(m, ld_part<SAME>(&p[c].m));
     bad |= ld_part<SAME>(&p[c].bad) != 0.f;
-    if (a.top > 0) low = min(low, ld_part<SAME>(&keys[(int64_t)c * a.top + kth]));
   }
   const float M = wave_max(m);
   if (__ballot(bad) || M == -INFINITY) {
@@ -217,7 +227,6 @@ __device__ __forceinline__ void join_parts(const LogprobArgs &a, int64_t row, co
     put_no_top(a, row);
     return;
   }
-  for (int off = 32; off >= 1; off >>= 1) low = min(low, (uint64_t)__shfl_xor((unsigned long long)low, off));
   // the first part that holds the maximum leads
   int lead = mine.m == M ? lane : 0x7FFFFFFF;
   for (int c = lane + 64; c < a.parts && lead == 0x7FFFFFFF; c += 64)
@@ -233,6 +242,24 @@ __device__ __forceinline__ void join_parts(const LogprobArgs &a, int64_t row, co
     lds.n = 0;
   }
   if (a.top <= 0) return;
+  uint64_t low = 0;
+  if (n_keys > LP_FEW) {
+    uint32_t ord[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) ord[i] = (uint32_t)(key[i] >> 32);
+    // as in k_logprobs: the upper half of the value's bits, all of them, the lowest places
+    uint32_t kth = max(wave_kth(ord, a.top, 31, 16), ORD_LEAST), place = 0;
+    if (wave_count(ord, kth) > a.top + 16) {
+      kth = max(wave_kth(ord, a.top, 15, 0, kth & 0xFFFF0000u), ORD_LEAST);
+      if (wave_count(ord, kth) > a.top + 16) {
+        const int above = kth == ~0u ? 0 : wave_count(ord, kth + 1);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) ord[i] = ord[i] == kth ? (uint32_t)key[i] : 0u;
+        place = wave_kth(ord, a.top - above, 31, 0);
+      }
+    }
+    low = (uint64_t)kth << 32 | place;
+  }
   __syncthreads();
   const float lz = log1pf(r);
   select_top(
@@ -262,12 +289,12 @@ __device__ __forceinline__ float raw_elem(const uint32_t (&w)[NW], int i) {
 // part is finished here; of several, by the last of its work groups to arrive, or by
 // k_logprobs_join.
 //
-// Measured: 256 rows of 152064 fp32 logits (156 MB), no alternatives 34 us, one 39,
-// five 45, twenty 54; 1531 rows of 32003 bf16 logits (98 MB) 32, 38, 41, 44.  The sums
+// Measured: 256 rows of 152064 fp32 logits (156 MB), no alternatives 33 us, one 39,
+// five 44, twenty 47; 1531 rows of 32003 bf16 logits (98 MB) 32, 38, 41, 44.  The sums
 // are bound by the vector unit (an exponential, a conversion and four more operations an
 // element, half of its cycles) and by each work group's chain of load, maximum and sum,
 // of which five share a CU; the alternatives add the floor's 16 ballots and the
-// ranking.  16 rows of 152064: 9, 12, 15, 17 us, one row of 32000: 6, 8, 9.5, 11, the
+// ranking.  16 rows of 152064: 7, 9.5, 12, 13 us, one row of 32000: 6, 8, 9.5, 11, the
 // chain of one part and of the join.  A work group to a row that read it again for each
 // pass took 1204 us for the 256 rows with twenty.
 template <int DT, int NW>
@@ -486,8 +513,8 @@ __global__ __launch_bounds__(LP_THREADS, 5) void k_logprobs(LogprobArgs a) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (threadIdx.x == 0) {
-    // (as far apart as they may lie: counters in one cache line wait for each other,
-    // 16.7 us against 14.2 for 16 rows of 19 parts)
+    // (as far apart as they may lie: counters in one cache line wait for each other, 9.4 us
+    // against 7.3 for 16 rows of 19 parts without alternatives)
     uint32_t *c = (uint32_t *)a.ws + row * min(32, LOGPROB_COUNTERS / (int)a.rows);
     const bool last = __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(a.parts - 1);
     if (last) st_part(true, c, 0u);  // for the next call
@@ -497,8 +524,8 @@ __global__ __launch_bounds__(LP_THREADS, 5) void k_logprobs(LogprobArgs a) {
   if (s_last) join_parts<true>(a, row, given, s_sel);
 }
 
-// Rows past one launch's: 6.4 us for 1531 rows of two parts with one alternative, 8 .. 15
-// for 256 rows of 19 parts with twenty, two dependent reads and the ranking.
+// Rows past one launch's: 6.0 us for 1531 rows of two parts with one alternative, 5.4 for
+// 256 rows of 19 parts with twenty, two dependent reads and the ranking.
 template <int DT>
 __global__ __launch_bounds__(LP_THREADS) void k_logprobs_join(LogprobArgs a) {
   __shared__ SelectLds s_sel;
@@ -516,8 +543,8 @@ hipError_t logprobs_dt(LogprobArgs a, hipStream_t st) {
   if (groups > INT32_MAX) return hipErrorInvalidValue;
   // One launch while the GPU holds all work groups at once, five to a CU: where more
   // wait, joining at the end of a work group keeps its place for longer than a second
-  // launch takes (twenty alternatives, one launch against two: 64 rows of 152064 fp32
-  // logits 21.7 and 22.6 us, 128 rows 32.6 and 31.1; one row of 32000 12.0 and 14.1).
+  // launch takes (no alternatives, one launch against two: 64 rows of 152064 fp32
+  // logits 12.4 and 13.1 us, 400 rows 54.8 and 46.3; one row of 32000 8.7 and 11.1).
   a.count = a.parts > 1 && groups <= 5 * 256 && a.rows <= LOGPROB_COUNTERS;
   if (small) HS_LAUNCH((k_logprobs<DT, 8>), dim3((uint32_t)groups), dim3(LP_THREADS), 0, st, a);
   else HS_LAUNCH((k_logprobs<DT, 32>), dim3((uint32_t)groups), dim3(LP_THREADS), 0, st, a);

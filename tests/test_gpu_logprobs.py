@@ -40,7 +40,7 @@ def test_logprobs_of_every_size(dtype, rows, vocab):
         check(hs, x, tokens, top)
 
 
-@pytest.mark.parametrize("vocab", [3, 100, 4099, 40000])
+@pytest.mark.parametrize("vocab", [3, 100, 4099, 40000, 300000])
 def test_equal_logits_come_by_index(vocab):
     """Ties everywhere: rows of one value, of two values, of zeros of both signs."""
     import paper_2603_12707_amd as hs
@@ -88,6 +88,18 @@ def test_banned_words_and_rows_without_a_distribution(vocab):
     check(hs, x.cuda(), tokens, 5)
     check(hs, x.cuda(), torch.full((12,), -1), 3)
     check(hs, x.cuda(), torch.tensor([vocab, vocab + 5, 2 ** 31 - 1, -2 ** 31] * 3), 1)
+
+
+@pytest.mark.parametrize("dtype,vocab", [("f32", 600001), ("f32", 1100003), ("bf16", 2200007)])
+def test_rows_of_more_parts_than_a_wave_has_lanes(dtype, vocab):
+    import paper_2603_12707_amd as hs
+    g = torch.Generator().manual_seed(vocab)
+    x = torch.randn(3, vocab, generator=g).to(R.DT[dtype])
+    x[1] = torch.tensor([0.5, -0.25])[torch.randint(0, 2, (vocab,), generator=g)].to(x.dtype)  # ties everywhere
+    x[2] = -math.inf
+    x[2, vocab - 3 :] = torch.tensor([1.0, 2.0, 1.0]).to(x.dtype)
+    for top in (0, 1, 20, 64):
+        check(hs, x.cuda(), torch.tensor([vocab - 1, 5, vocab - 2]), top)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
