@@ -483,7 +483,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
       float f[8] = {};
       if (li < G) ld8<DT>((const char *)a.q + ((int64_t)row * a.ld_q + (j * G + li) * HD + lg * (HD / 4) + c * 8) * SB, f);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] *= sign;
+      for (int e = 0; e < 8; ++e) f[e] = __builtin_fmaf(f[e], 0.f, f[e] * sign);  // (an infinity becomes a NaN, as below)
 #pragma unroll
       for (int p = 0; p < QP; ++p)
 #pragma unroll

@@ -323,6 +323,31 @@ def test_attention_passes_a_nan_group_on_to_its_own_heads():
         assert torch.isfinite(out).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("heads,n_kv,hd", [(4, 4, 64), (14, 2, 128)])
+def test_queries_that_are_not_finite_reach_their_own_head_alone(dtype, heads, n_kv, hd):
+    """An infinity or a NaN in a query head makes its output NaN (also where every score would be -inf), no other's.
+    The others are within their tolerance and not always what they were bit for bit: a wave moves the references of
+    its heads together, and a NaN score moves none, so that o and l are rounded at other places."""
+    import paper_2603_12707_amd as hs
+    cache, blocks, table = make(hs, 1, 8, 1, n_kv, hd, 16)
+    k = rows(100, n_kv, hd, dtype, 30).abs() + 1.0
+    v = rows(100, n_kv, hd, dtype, 31)
+    pos = torch.arange(100, dtype=torch.int32, device="cuda")
+    zero = torch.zeros_like(pos)
+    cache.append(0, k, v, pos, seqs=zero)
+    q = rows(4, heads, hd, dtype, 32)
+    lens = torch.full((4,), 100, dtype=torch.int32)
+    want, mass, reach = R.attention(R.Layout(blocks, table, 1, n_kv, hd, 16), 0, q.cpu(), lens, [0] * 4, None, None)
+    tol = R.attention_tolerance(want, mass, reach, dtype, hd)
+    q[0, 1, hd - 1], q[1, 0, 0], q[2, heads - 1, 33] = -math.inf, math.inf, math.nan
+    got = cache.attention(0, q, lens.cuda(), seqs=zero[:4]).double().cpu()
+    bad = torch.zeros(4, heads, dtype=torch.bool)
+    bad[0, 1] = bad[1, 0] = bad[2, heads - 1] = True
+    assert torch.isnan(got[bad]).all()
+    assert ((got - want).abs() <= tol)[~bad].all()
+
+
 def test_offsets_past_32_bits():
     """A cache of more than 4 GiB whose rows live in its last blocks."""
     import paper_2603_12707_amd as hs
