@@ -480,14 +480,28 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
   if constexpr (!KVQ_SCALED<DT>) {
 #pragma unroll
     for (int c = 0; c < HD / 32; ++c) {
-      float f[8] = {};
-      if (li < G) ld8<DT>((const char *)a.q + ((int64_t)row * a.ld_q + (j * G + li) * HD + lg * (HD / 4) + c * 8) * SB, f);
+      const char *at = (const char *)a.q + ((int64_t)row * a.ld_q + (j * G + li) * HD + lg * (HD / 4) + c * 8) * SB;
+      if constexpr (DT == HS_F16) {
+        typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+        u32x4 w{0u, 0u, 0u, 0u};
+        if (li < G) w = ld16(at);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = __builtin_fmaf(f[e], 0.f, f[e] * sign);  // (an infinity becomes a NaN, as below)
+        for (int x = 0; x < 4; ++x) {  // (an infinity becomes a NaN, as in the other types)
+          const uint32_t word = w[x];
+          const f16x2 v = __builtin_bit_cast(f16x2, word);
+          const f16x2 zero{(_Float16)0.f, (_Float16)0.f}, sg{(_Float16)sign, (_Float16)sign};
+          qh[0][c][x] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(v, zero, v * sg));
+        }
+      } else {
+        float f[8] = {};
+        if (li < G) ld8<DT>(at, f);
 #pragma unroll
-      for (int p = 0; p < QP; ++p)
+        for (int e = 0; e < 8; ++e) f[e] *= sign;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) qh[p][c][x] = take_part<MT>(f[2 * x], f[2 * x + 1]);
+        for (int p = 0; p < QP; ++p)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) qh[p][c][x] = take_part<MT>(f[2 * x], f[2 * x + 1]);
+      }
     }
   } else {
     // the MFMA's byte e of lane group lg is channel 16 lg + e, from byte 16 on 64 further
