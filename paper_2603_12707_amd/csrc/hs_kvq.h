@@ -230,8 +230,8 @@ __global__ __launch_bounds__(256) void k_kvq_read(KvqRows a) {
 // Measured: 256 rows of 1024 .. 8192 positions (bf16, 28/4 heads of 128; 645 MB)
 // 109 us, 5.9 TB/s, bound by memory (the copies alone take 115 us where copies and
 // arithmetic take 116, the arithmetic alone 83).  32 rows of 608 .. 960 (f16, 32/32
-// heads; 110 MB) 27 us, bound by the arithmetic and by 1024 work groups of uneven
-// length on 768 places (without copies 27).  Two rows of 120000 .. 131072 (bf16; 137 MB)
+// heads; 110 MB) 25 us, bound by the arithmetic (with the queries through fp32 27, and as
+// much without any copy) and by 1024 work groups of uneven length on 768 places.  Two rows of 120000 .. 131072 (bf16; 137 MB)
 // 33 us, of which 13 are the ramp, the last tiles and the join of 32 splits.  One
 // row of 700 8 us: the length, the block number and the first tile's copy one
 // after the other, 2 us a tile, the merge.  Before: K and V through registers and K
