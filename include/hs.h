@@ -394,9 +394,9 @@ int hs_kvq_read(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, int32_t
  * sequence seqs[r] (NULL: r), query head i reading KV head
  * i / (n_heads / n_kv_heads), at most 16 heads to a KV head:
  *   out[r][i] = sum_p softmax_p(scale * q_i . k_p) v_p
- * over the positions that have a block, in fp32, rounded once to `dtype`; a row
- * without one (length 0 or negative) gives zeros, a query head that holds a NaN or
- * an infinity NaNs.  max_len (host, 1..2^30) bounds the lengths and shapes the
+ * over the positions that have a block, in fp32 (exact products; the weights keep 22
+ * bits for HS_F16, 24 else), rounded once to `dtype`; a row without one (length 0 or
+ * negative) gives zeros, a query head that holds a NaN or an infinity NaNs.  max_len (host, 1..2^30) bounds the lengths and shapes the
  * launch; positions from it on are not attended.
  * q, out, ld_q and ld_out are aligned as in hs_kvq_append.  workspace is device
  * memory of hs_kvq_attention_workspace bytes (which may be 0: then it may be

@@ -16,7 +16,7 @@
 
 #include <algorithm>
 #include <cfloat>
-#include <utility>
+#include <type_traits>
 
 namespace hs {
 namespace {
@@ -203,23 +203,19 @@ __global__ __launch_bounds__(256) void k_kvq_read(KvqRows a) {
 // columns of the matrix products.
 //
 // Scores: S^T = K Q^T with 16 positions as rows.  Lane (li, lg) = (lane % 16,
-// lane / 16).  bf16 rows take the scaled MFMA 16x16x128, which reads K as it lies
-// in memory: a lane supplies group lg of its position and the group's exponent
-// byte.  Q enters as the sum of two e4m3 parts (the second what the first left,
-// times 16), scaled by a power of two of the head's largest element: every product
-// is exact, and an element below 2^-13 of the largest is off by at most 2^-21 of
-// it.  The instruction's own sums are good to 2^-16 of the largest product
-// (measured; 2^-19 on average), well below what rounding Q and K to bf16 left.  f16
-// and fp32 rows, which that would cost digits, convert K (HD / 4 elements of a
-// position a lane, one group's scale) and take Q as one f16 or three bf16 parts
-// through the MFMA 16x16x32.  Row r of the tile's product t is position
+// lane / 16).  K is converted (HD / 4 elements of a position a lane, one group's
+// scale) and Q enters the MFMA 16x16x32 as it is in the 16-bit types, as three bf16
+// parts in fp32: every product is exact, every sum fp32.  (The scaled MFMA
+// 16x16x128 would take K as it lies in memory, but its own sums are good to 2^-16 of
+// the largest product only, measured, and its Q would be e4m3 parts under one power of
+// two a head: a loud channel took the others' digits.)  Row r of the tile's product t is position
 // 16 (r / 4) + 4 t + r % 4, so that a lane ends up with the scores of the 16
 // consecutive positions 16 lg .. for head li, which is the B operand of
 // O^T += V^T P^T (MFMA 16x16x32): positions 8 m .. 8 m + 7 of each lane group are
 // the k range of MFMA m.  For V^T a lane reads its HD / 16 channels of those 16
 // positions, converts pairs of channels (exact in the 16-bit type) and pairs the
-// positions with v_perm.  P enters as the sum of parts in that type (two: 16 bits
-// and more; fp32: three, 24 bits), every sum is fp32.
+// positions with v_perm.  P enters as the sum of parts in that type: two of f16 (22
+// bits), three of bf16 (24 bits); every sum is fp32.
 //
 // Each wave copies its tiles straight into LDS, K and V alike as they lie in
 // memory, a tile and a half ahead, through buffer ranges that end at the last span
@@ -228,24 +224,19 @@ __global__ __launch_bounds__(256) void k_kvq_read(KvqRows a) {
 // positions and more (WIDE) hold a tile whole; smaller ones are copied span by span.
 //
 // Measured: 256 rows of 1024 .. 8192 positions (bf16, 28/4 heads of 128; 645 MB)
-// 109 us, 5.9 TB/s, bound by memory (the copies alone take 115 us where copies and
-// arithmetic take 116, the arithmetic alone 83).  32 rows of 608 .. 960 (f16, 32/32
-// heads; 110 MB) 25 us, bound by the arithmetic (with the queries through fp32 27, and as
-// much without any copy) and by 1024 work groups of uneven length on 768 places.  Two rows of 120000 .. 131072 (bf16; 137 MB)
-// 33 us, of which 13 are the ramp, the last tiles and the join of 32 splits.  One
-// row of 700 8 us: the length, the block number and the first tile's copy one
-// after the other, 2 us a tile, the merge.  Before: K and V through registers and K
-// converted for bf16 too took 139 us for the first, and 131 as it is now but with two
-// kernels and splits everywhere.
+// 115 us, 5.6 TB/s (109 with the scaled MFMA and P in two parts, for scores off by up to
+// 2^-16 of their largest product and P's bits from the 17th on).  32 rows of 608 .. 960 (f16, 32/32
+// heads; 110 MB) 25 us, on 1024 work groups of uneven length in 768 places.  Two rows of
+// 120000 .. 131072 (bf16; 137 MB) 35 us, of which 13 are the ramp, the last tiles and the join of
+// 32 splits.  One row of 700 8 us: the length, the block number and the first tile's copy one
+// after the other, 2 us a tile, the merge.  Before: K and V through registers took 139 us for
+// the first.
 template <int DT>
 constexpr int KVQ_MMA = DT == HS_F16 ? HS_F16 : HS_BF16;
 template <int DT>
-constexpr int KVQ_P_PARTS = DT == HS_F32 ? 3 : 2;
+constexpr int KVQ_P_PARTS = DT == HS_F16 ? 2 : 3;
 template <int DT>
-constexpr int KVQ_Q_PARTS = DT == HS_BF16 ? 2 : DT == HS_F16 ? 1 : 3;
-// bf16 rows' scores come from the scaled MFMA
-template <int DT>
-constexpr bool KVQ_SCALED = DT == HS_BF16;
+constexpr int KVQ_Q_PARTS = DT == HS_F32 ? 3 : 1;
 constexpr int KVQ_TILE = 64, KVQ_PLANES = 3;
 // Rows are started longest first where some CU takes more than one work group and the
 // longest rows take a while: up to this many rows, from more positions on.  28/4 heads, in
@@ -281,15 +272,6 @@ constexpr float KVQ_SLACK = DT == HS_F16 ? 4.f : 11.5f;
 // prefill attention: below it one fma leaves s - m off by at most half an ulp of
 // m, 2^-5, the same factor in o and l).
 constexpr float KVQ_ROUND_FROM = 0x1p20f;
-
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-// sc += K Q^T over the parts P of Q: K fp4 with its group's exponent byte, Q e4m3 with byte P of qs
-template <int QP, int... P>
-__device__ __forceinline__ void score_parts(f32x4 &sc, u32x4 k, int byte, const i32x8 (&qb)[QP], int qs,
-                                            std::integer_sequence<int, P...>) {
-  const i32x8 kv{(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
-  ((sc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kv, qb[P], sc, 4, 0, 0, byte, P, qs)), ...);
-}
 
 // word x of a matrix operand of parts: R(f0) | R(f1) << 16, and what is left
 template <int MT>
@@ -417,7 +399,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
   constexpr int COPIES = WIDE ? PLANE / 1024 + 1 : 8;  // of a plane
   unsigned char *ring = s_mem + wave * (KVQ_PLANES * PLANE);
   const uint32_t ring0 = __builtin_amdgcn_readfirstlane(lds_addr(ring));
-  const int kspan = li >> 2, kgrp = HD == 128 ? lg : lg & 1, vgrp = HD == 128 ? li >> 2 : li >> 3;
+  const int kspan = li >> 2, vgrp = HD == 128 ? li >> 2 : li >> 3;
   // K (v = 0) or V of tile t into plane `slot` of the ring
   auto copy = [&](int t, const Ids &w, int v, int slot) {
     const int p0 = t0 + t * KVQ_TILE;
@@ -474,69 +456,30 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
   // Q^T operand: head li of the group (zeros past it)
   // (a negative scale's sign goes to Q, so that the scores' order is that of the products)
   const float sign = a.scale < 0.f ? -1.f : 1.f;
-  [[maybe_unused]] i32x8 qb[QP];               // scaled MFMA: e4m3 parts
-  [[maybe_unused]] int qs = 0;                 // and their scale bytes
-  [[maybe_unused]] u32x4 qh[QP][HD / 32];      // else: parts in the 16-bit type
-  if constexpr (!KVQ_SCALED<DT>) {
+  u32x4 qh[QP][HD / 32];  // in the 16-bit type, or its parts
 #pragma unroll
-    for (int c = 0; c < HD / 32; ++c) {
-      const char *at = (const char *)a.q + ((int64_t)row * a.ld_q + (j * G + li) * HD + lg * (HD / 4) + c * 8) * SB;
-      if constexpr (DT == HS_F16) {
-        typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-        u32x4 w{0u, 0u, 0u, 0u};
-        if (li < G) w = ld16(at);
+  for (int c = 0; c < HD / 32; ++c) {
+    const char *at = (const char *)a.q + ((int64_t)row * a.ld_q + (j * G + li) * HD + lg * (HD / 4) + c * 8) * SB;
+    if constexpr (DT == HS_F16) {
+      typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+      u32x4 w{0u, 0u, 0u, 0u};
+      if (li < G) w = ld16(at);
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {  // (an infinity becomes a NaN, as in the other types)
-          const uint32_t word = w[x];
-          const f16x2 v = __builtin_bit_cast(f16x2, word);
-          const f16x2 zero{(_Float16)0.f, (_Float16)0.f}, sg{(_Float16)sign, (_Float16)sign};
-          qh[0][c][x] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(v, zero, v * sg));
-        }
-      } else {
-        float f[8] = {};
-        if (li < G) ld8<DT>(at, f);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] *= sign;
-#pragma unroll
-        for (int p = 0; p < QP; ++p)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) qh[p][c][x] = take_part<MT>(f[2 * x], f[2 * x + 1]);
+      for (int x = 0; x < 4; ++x) {  // (an infinity becomes a NaN, as in the other types)
+        const uint32_t word = w[x];
+        const f16x2 v = __builtin_bit_cast(f16x2, word);
+        const f16x2 zero{(_Float16)0.f, (_Float16)0.f}, sg{(_Float16)sign, (_Float16)sign};
+        qh[0][c][x] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(v, zero, v * sg));
       }
-    }
-  } else {
-    // the MFMA's byte e of lane group lg is channel 16 lg + e, from byte 16 on 64 further
-    float f[32];
+    } else {
+      float f[8] = {};
+      if (li < G) ld8<DT>(at, f);
 #pragma unroll
-    for (int e = 0; e < 32; ++e) f[e] = 0.f;
-    if (li < G) {
-      const char *at = (const char *)a.q + ((int64_t)row * a.ld_q + (j * G + li) * HD + lg * 16) * SB;
+      for (int e = 0; e < 8; ++e) f[e] = __builtin_fmaf(f[e], 0.f, f[e] * sign);
 #pragma unroll
-      for (int x = 0; x < HD / 32; ++x) ld8<DT>(at + ((x >> 1) * 64 + (x & 1) * 8) * SB, f + 8 * x);
-    }
-    uint32_t top = 0;
+      for (int p = 0; p < QP; ++p)
 #pragma unroll
-    for (int e = 0; e < 32; ++e) top = max(top, __float_as_uint(f[e]) & 0x7FFFFFFFu);
-    top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-    // 2^s puts the largest into 128 .. 256 (e4m3 ends at 448); a NaN or an infinity makes the head's scores NaN
-    const int s = min(max((int)(top >> 23) - 127 - 7, -100), 120);
-    const float mul = __uint_as_float((uint32_t)(127 - s) << 23) * sign;
-#pragma unroll
-    for (int e = 0; e < 32; ++e) f[e] *= mul;
-#pragma unroll
-    for (int p = 0; p < QP; ++p) {
-#pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        int w = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * x], f[4 * x + 1], 0, false);
-        w = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * x + 2], f[4 * x + 3], w, true);
-        qb[p][x] = w;
-        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-        f[4 * x] = (f[4 * x] - lo[0]) * 16.f;
-        f[4 * x + 1] = (f[4 * x + 1] - lo[1]) * 16.f;
-        f[4 * x + 2] = (f[4 * x + 2] - hi[0]) * 16.f;
-        f[4 * x + 3] = (f[4 * x + 3] - hi[1]) * 16.f;
-      }
-      qs |= (top >= 0x7F800000u ? 255 : 127 + s - 4 * p) << (8 * p);
+        for (int x = 0; x < 4; ++x) qh[p][c][x] = take_part<MT>(f[2 * x], f[2 * x + 1]);
     }
   }
   const float c2 = fabsf(a.scale) * 1.44269504088896341f;
@@ -550,40 +493,19 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
     if (one) wait_copies<2 * COPIES>();  // V, and the next tile's K
     else wait_copies<COPIES>();
     f32x4 sc[4];
-    if constexpr (!KVQ_SCALED<DT>) {
-      constexpr int FGRP = HD == 128 ? 0 : 1;  // lane groups to a group of 32, as a shift
-      const u32x4 ks = *(const u32x4 *)(kp + kspan * SPAN + HD * 8 + (lg >> FGRP) * 16);
+    constexpr int FGRP = HD == 128 ? 0 : 1;  // lane groups to a group of 32, as a shift
+    const u32x4 ks = *(const u32x4 *)(kp + kspan * SPAN + HD * 8 + (lg >> FGRP) * 16);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const uint32_t *at = (const uint32_t *)(kp + kspan * SPAN + (4 * x + (li & 3)) * (HD / 2) + lg * (HD / 8));
-        const float s = __uint_as_float((ks[x] >> (8 * (li & 3))) << 23);  // (exponent bits alone)
-        sc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int x = 0; x < 4; ++x) {
+      const uint32_t *at = (const uint32_t *)(kp + kspan * SPAN + (4 * x + (li & 3)) * (HD / 2) + lg * (HD / 8));
+      const float s = __uint_as_float((ks[x] >> (8 * (li & 3))) << 23);  // (exponent bits alone)
+      sc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int c = 0; c < HD / 32; ++c) {
-          const uint32_t w = at[c];
-          const u32x4 kv{kvq_pair<MT, 0>(w, s), kvq_pair<MT, 1>(w, s), kvq_pair<MT, 2>(w, s), kvq_pair<MT, 3>(w, s)};
+      for (int c = 0; c < HD / 32; ++c) {
+        const uint32_t w = at[c];
+        const u32x4 kv{kvq_pair<MT, 0>(w, s), kvq_pair<MT, 1>(w, s), kvq_pair<MT, 2>(w, s), kvq_pair<MT, 3>(w, s)};
 #pragma unroll
-          for (int p = QP - 1; p >= 0; --p) sc[x] = mma<MT>(kv, qh[p][c], sc[x]);
-        }
-      }
-    } else {
-      u32x4 kc[4];
-#pragma unroll
-      for (int x = 0; x < 4; ++x)
-        kc[x] = *(const u32x4 *)(kp + kspan * SPAN + (4 * x + (li & 3)) * (HD / 2) + kgrp * 16);
-      u32x4 ks = *(const u32x4 *)(kp + kspan * SPAN + HD * 8 + kgrp * 16);
-      if constexpr (HD == 64) {  // the upper half of the contraction: zeros, times 1
-        if (lg >= 2) {
-#pragma unroll
-          for (int x = 0; x < 4; ++x) kc[x] = u32x4{0u, 0u, 0u, 0u};
-          ks = u32x4{0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu};
-        }
-      }
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int byte = (int)(ks[x] >> (8 * (li & 3)));  // the MFMA reads the lowest byte
-        sc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-        score_parts<QP>(sc[x], kc[x], byte, qb, qs, std::make_integer_sequence<int, QP>{});
+        for (int p = QP - 1; p >= 0; --p) sc[x] = mma<MT>(kv, qh[p][c], sc[x]);
       }
     }
     if (one) {

@@ -231,6 +231,56 @@ def test_fp32_rows_keep_fp32_precision(heads, n_kv, hd):
     assert float((got.double().cpu() - want).norm() / want.norm()) < 2.0 ** -20
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_a_loud_query_channel_costs_the_others_nothing(dtype, hd):
+    """One query channel 2^14 above the others, over a group of K 2^14 below the others: both ends of the product count
+    alike, and every element keeps all its bits.  Each head against a tolerance of its own."""
+    import paper_2603_12707_amd as hs
+    cache, blocks, table = make(hs, 1, 2, 1, 1, hd, 64)
+    g = torch.Generator().manual_seed(hd)
+    k, v = torch.randn(100, 1, hd, generator=g) * 0.5, torch.randn(100, 1, hd, generator=g)
+    k[..., :32] *= 2.0 ** -14
+    q = torch.randn(2, 2, hd, generator=g)
+    q[:, 0, 5] = torch.tensor([1.25, -1.75]) * 2.0 ** 14
+    k, v, q = (x.to(R.DT[dtype]).cuda() for x in (k, v, q))
+    pos = torch.arange(100, dtype=torch.int32, device="cuda")
+    cache.append(0, k, v, pos, seqs=torch.zeros_like(pos))
+    lens = torch.tensor([100, 61], dtype=torch.int32)
+    got = cache.attention(0, q, lens.cuda(), seqs=torch.zeros(2, dtype=torch.int32, device="cuda"), scale=1.0)
+    lay = R.Layout(blocks, table, 1, 1, hd, 64)
+    for h in range(2):
+        want, mass, reach = R.attention(lay, 0, q[:, h : h + 1].cpu(), lens, [0, 0], 1.0)
+        err = (got[:, h : h + 1].double().cpu() - want).abs()
+        assert (err <= R.attention_tolerance(want, mass, reach, dtype, hd)).all(), (h, float(err.max()))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_probabilities_keep_their_bits(dtype):
+    """Two values that all but cancel: a position with most of the weight whose value is 0, and two with 1 and -1 whose
+    scores differ by 2^-13.  A score is at most two exact products whose sum is exact; scaling it by log2(e) and taking
+    the reference away leaves it off by less than 2^-23, the exponential by 2^-23 of itself, and the sums of three terms
+    and the division by a few 2^-24 more: the weights by less than 2^-21 of themselves, and the output by 2^-20 of the sum
+    of their sizes.  (With the probabilities in 16 bits it would be off by up to 2^-18.)"""
+    import paper_2603_12707_amd as hs
+    hd, n, heads = 64, 8, 16
+    cache, blocks, table = make(hs, 1, 1, 1, 1, hd, 16)
+    k, v = torch.zeros(3, 1, hd), torch.zeros(3, 1, hd)
+    k[1:, 0, 0], k[1, 0, 32], k[2, 0, 32] = -1.0, 1.0, -1.0
+    v[1], v[2] = 1.0, -1.0
+    q = torch.zeros(n, heads, hd)
+    q[..., 0] = (0.05 + 0.65 * torch.arange(n * heads).reshape(n, heads) / (n * heads)).to(R.DT[dtype]).float()
+    q[..., 32] = 2.0 ** -14
+    k, v, q = (x.to(R.DT[dtype]).cuda() for x in (k, v, q))
+    pos = torch.arange(3, dtype=torch.int32, device="cuda")
+    cache.append(0, k, v, pos, seqs=torch.zeros_like(pos))
+    lens, seqs = torch.full((n,), 3, dtype=torch.int32), torch.zeros(n, dtype=torch.int32)
+    got = cache.attention(0, q, lens.cuda(), seqs=seqs.cuda(), scale=1.0).double().cpu()
+    want, mass, _ = R.attention(R.Layout(blocks, table, 1, 1, hd, 16), 0, q.cpu(), lens, seqs, 1.0)
+    tol = R.HALF_STEP[dtype] * want.abs() + 2.0 ** -20 * mass
+    assert ((got - want).abs() <= tol).all(), float(((got - want).abs() - tol).max())
+
+
 def test_attention_over_very_long_rows():
     import paper_2603_12707_amd as hs
     fill_and_check(hs, "bf16", [70001, 3], 7, 1, 128, 1024, seed=6)
