@@ -282,6 +282,15 @@ __device__ __forceinline__ uint32_t take_part(float &f0, float &f1) {
   return w;
 }
 
+// The same of fp32 numbers of any size, cut to their upper 16 bits and not rounded: three
+// parts hold all 24 bits either way, and the largest numbers do not round to infinity.
+__device__ __forceinline__ uint32_t cut_part(float &f0, float &f1) {
+  const uint32_t a = __float_as_uint(f0), b = __float_as_uint(f1);
+  f0 -= __uint_as_float(a & 0xFFFF0000u);
+  f1 -= __uint_as_float(b & 0xFFFF0000u);
+  return __builtin_amdgcn_perm(b, a, 0x07060302u);
+}
+
 // past the caches of one XCD
 __device__ __forceinline__ void st_agent(float *p, float v) {
   __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -479,7 +488,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
 #pragma unroll
       for (int p = 0; p < QP; ++p)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) qh[p][c][x] = take_part<MT>(f[2 * x], f[2 * x + 1]);
+        for (int x = 0; x < 4; ++x)
+          qh[p][c][x] = DT == HS_F32 ? cut_part(f[2 * x], f[2 * x + 1]) : pack2<MT>(f[2 * x], f[2 * x + 1]);
     }
   }
   const float c2 = fabsf(a.scale) * 1.44269504088896341f;

@@ -281,6 +281,27 @@ def test_probabilities_keep_their_bits(dtype):
     assert ((got - want).abs() <= tol).all(), float(((got - want).abs() - tol).max())
 
 
+@pytest.mark.parametrize("heads", [2, 8])
+def test_fp32_queries_reach_to_the_largest_number(heads):
+    """A query element of the largest finite number over keys small enough for finite scores: not an infinity on the way."""
+    import paper_2603_12707_amd as hs
+    hd, big = 128, torch.finfo(torch.float32).max
+    cache, blocks, table = make(hs, 1, 3, 1, 2, hd, 16)
+    g = torch.Generator().manual_seed(heads)
+    k, v = torch.randn(40, 2, hd, generator=g), torch.randn(40, 2, hd, generator=g)
+    k[..., 32:64] *= 2.0 ** -124
+    q = torch.randn(2, heads, hd, generator=g)
+    q[0, :, 40], q[1, 0, 33], q[1, 1, 63] = big, -big, big * (1 - 2.0 ** -9)
+    k, v, q = k.cuda(), v.cuda(), q.cuda()
+    pos = torch.arange(40, dtype=torch.int32, device="cuda")
+    cache.append(0, k, v, pos, seqs=torch.zeros_like(pos))
+    lens = torch.tensor([40, 33], dtype=torch.int32)
+    got = cache.attention(0, q, lens.cuda(), seqs=torch.zeros(2, dtype=torch.int32, device="cuda"))
+    want, mass, reach = R.attention(R.Layout(blocks, table, 1, 2, hd, 16), 0, q.cpu(), lens, [0, 0])
+    assert torch.isfinite(got).all()
+    assert ((got.double().cpu() - want).abs() <= R.attention_tolerance(want, mass, reach, "f32", hd)).all()
+
+
 def test_attention_over_very_long_rows():
     import paper_2603_12707_amd as hs
     fill_and_check(hs, "bf16", [70001, 3], 7, 1, 128, 1024, seed=6)
