@@ -372,7 +372,8 @@ int hs_kvq_block_bytes(int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, i
 
 /* Stores n rows of K and V of one layer.  Element (row r, head j, channel c) of
  * K is k[r * ld + j * ld_head + c] in `dtype` (v alike; device, 16-byte aligned;
- * ld and ld_head multiples of 8, HS_F32 4, and rows and heads do not overlap).
+ * ld and ld_head multiples of 8, HS_F32 4, and rows and heads do not overlap; a
+ * single row's ld and a single head's ld_head are not looked at).
  * Row r goes to position positions[r] (device int32) of sequence seqs[r] (device
  * int32; NULL: sequence r).  A row whose position is negative, whose sequence is
  * outside the table or whose place has no block is not stored, which is how a
@@ -396,8 +397,9 @@ int hs_kvq_read(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, int32_t
  *   out[r][i] = sum_p softmax_p(scale * q_i . k_p) v_p
  * over the positions that have a block, in fp32 (exact products; the weights keep 22
  * bits for HS_F16, 24 else), rounded once to `dtype`; a row without one (length 0 or
- * negative) gives zeros, a query head that holds a NaN or an infinity NaNs.  max_len (host, 1..2^30) bounds the lengths and shapes the
- * launch; positions from it on are not attended.
+ * negative) gives zeros, a query head that holds a NaN or an infinity NaNs.
+ * max_len (host, 1..2^30) bounds the lengths and shapes the launch; positions from
+ * it on are not attended.
  * q, out, ld_q and ld_out are aligned as in hs_kvq_append.  workspace is device
  * memory of hs_kvq_attention_workspace bytes (which may be 0: then it may be
  * NULL), 16-byte aligned, whose first 2048 bytes are zero before its first use;

@@ -1449,10 +1449,12 @@ int kvq_ref(const hs_kvq_cache *c, int layer, const char *fn, KvqRef *out) {
   return HS_OK;
 }
 
-// rows of n_heads heads of head_dim elements: the strides keep them apart and
-// aligned to 16 bytes (one row needs no row stride)
+// rows of `heads` heads of hd elements: the strides keep them apart and aligned to 16 bytes
+// (a single row's stride and a single head's are used by nothing, and not looked at)
 int kvq_strides(const char *fn, int dtype, int64_t n, int64_t ld, int64_t ld_head, int heads, int hd) {
   const int ce = 16 / dtype_bytes(dtype);
+  if (n <= 1) ld = 0;
+  if (heads <= 1) ld_head = 0;
   if (ld % ce || ld_head % ce) return fail(HS_E_INVALID, "%s: strides must be multiples of %d elements", fn, ce);
   // far below 64 bits in bytes, so that no offset wraps
   if (ld < 0 || ld_head < 0 || ld > (1ll << 40) || ld_head > (1ll << 40)) return fail(HS_E_INVALID, "%s: stride out of range", fn);

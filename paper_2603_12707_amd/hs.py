@@ -502,14 +502,16 @@ class QuantCache:
         self._ref = ctypes.addressof(self._c)
 
     def _check_rows(self, func: str, k, v):
-        """k, v: [n][n_kv_heads][head_dim], equal strides, channels contiguous; returns (n, strides)."""
+        """k, v: [n][n_kv_heads][head_dim], equal strides, channels contiguous; returns (n, strides), the strides of
+        a single row or head, which nothing uses, as 0."""
         shape, stride = k.shape, k.stride()
         if len(shape) != 3 or shape[1] != self.n_kv_heads or shape[2] != self.head_dim or v.shape != shape or \
-                v.dtype != k.dtype or stride[2] != 1 or v.stride() != stride or \
+                v.dtype != k.dtype or stride[2] != 1 or v.stride(2) != 1 or \
+                (shape[0] > 1 and v.stride(0) != stride[0]) or (shape[1] > 1 and v.stride(1) != stride[1]) or \
                 k.get_device() != self._index or v.get_device() != self._index:
             raise ValueError(f"{func}: k and v must be [n][{self.n_kv_heads}][{self.head_dim}] on {self.blocks.device}, "
                              "of one type and equal strides, channels contiguous")
-        return shape[0], stride
+        return shape[0], (stride[0] if shape[0] > 1 else 0, stride[1] if shape[1] > 1 else 0)
 
     def append(self, layer: int, k, v, positions, seqs=None, k_values=None, v_values=None) -> None:
         """Stores rows of K and V ([n][n_kv_heads][head_dim]) at positions (int32 [n]) of sequences seqs (int32 [n];

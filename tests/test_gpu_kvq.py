@@ -372,6 +372,36 @@ def test_attention_takes_strides_and_leaves_other_memory_alone():
     assert one.shape == (1, 2, 64)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_strides_that_nothing_uses_are_not_looked_at(dtype):
+    """One row has no row stride, one head no head stride, whatever the tensors say of them."""
+    import paper_2603_12707_amd as hs
+    hd = 64
+    odd = lambda x, st: torch.as_strided(x, x.shape, st)  # noqa: E731
+    cache, blocks, table = make(hs, 2, 2, 1, 1, hd, 16)
+    k, v = rows(20, 1, hd, dtype, 50), rows(20, 1, hd, dtype, 51)
+    pos = torch.arange(20, dtype=torch.int32, device="cuda")
+    zero = torch.zeros_like(pos)
+    ko, vo = torch.empty_like(k), torch.empty_like(v)
+    cache.append(0, odd(k, (hd, 5, 1)), odd(v, (hd, 7, 1)), pos, seqs=zero, k_values=odd(ko, (hd, 1, 1)), v_values=vo)
+    want = [R.quantize(x.cpu(), dtype)[2] for x in (k, v)]
+    for got, w in zip((ko, vo), want):
+        assert torch.equal(got.double().cpu(), w)
+    rk, rv = cache.read(0, pos, k.dtype, seqs=zero, k=odd(torch.empty_like(k), (hd, 3, 1)), v=torch.empty_like(v))
+    assert torch.equal(rk.double().cpu(), want[0]) and torch.equal(rv.double().cpu(), want[1])
+    q = rows(1, 4, hd, dtype, 52)
+    one = cache.attention(0, q, pos[19:])
+    out = torch.empty_like(q)
+    cache.attention(0, odd(q, (1, hd, 1)), pos[19:], out=odd(out, (37, hd, 1)))
+    assert torch.equal(out, one)
+    wide, blocks, table = make(hs, 1, 1, 1, 3, hd, 16)
+    k, v = rows(1, 3, hd, dtype, 53), rows(1, 3, hd, dtype, 54)
+    wide.append(0, odd(k, (3, hd, 1)), odd(v, (1, hd, 1)), pos[:1], seqs=zero[:1])
+    rk, rv = wide.read(0, pos[:1], k.dtype, seqs=zero[:1], k=odd(torch.empty_like(k), (11, hd, 1)))
+    for got, x in ((rk, k), (rv, v)):
+        assert torch.equal(got.double().cpu(), R.quantize(x.cpu(), dtype)[2])
+
+
 def test_attention_passes_a_nan_group_on_to_its_own_heads():
     """A NaN stored in a row that is attended reaches the outputs of its KV head's rows and of no other; one behind
     the last position reaches none."""
