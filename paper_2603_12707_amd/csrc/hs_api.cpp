@@ -1456,8 +1456,9 @@ int kvq_strides(const char *fn, int dtype, int64_t n, int64_t ld, int64_t ld_hea
   if (n <= 1) ld = 0;
   if (heads <= 1) ld_head = 0;
   if (ld % ce || ld_head % ce) return fail(HS_E_INVALID, "%s: strides must be multiples of %d elements", fn, ce);
-  // far below 64 bits in bytes, so that no offset wraps
-  if (ld < 0 || ld_head < 0 || ld > (1ll << 40) || ld_head > (1ll << 40)) return fail(HS_E_INVALID, "%s: stride out of range", fn);
+  // offsets far below 64 bits in bytes, so that none wraps
+  if (ld < 0 || ld_head < 0 || ld > std::min(1ll << 40, (1ll << 58) / std::max<int64_t>(n, 1)) || ld_head > 1ll << 40)
+    return fail(HS_E_INVALID, "%s: stride out of range", fn);
   if (heads > 1 && ld_head < hd) return fail(HS_E_INVALID, "%s: heads overlap", fn);
   // rows of heads side by side, or heads of rows side by side
   const int64_t per_head = n > 1 ? (n - 1) * ld + hd : hd, per_row = (int64_t)(heads - 1) * ld_head + hd;
@@ -1610,7 +1611,7 @@ int hs_token_logprobs(int32_t dtype, const void *logits, int64_t rows, int32_t v
   if (rows == 0) return HS_OK;
   if (!logits) return fail(HS_E_INVALID, "%s: logits is NULL", fn);
   if (((uintptr_t)logits) % dtype_bytes(dtype)) return fail(HS_E_INVALID, "%s: logits are not aligned to their type", fn);
-  if (rows > 1 && (ld < vocab || ld > (1ll << 40))) return fail(HS_E_INVALID, "%s: rows overlap, or ld out of range", fn);
+  if (rows > 1 && (ld < vocab || ld > std::min<int64_t>(1ll << 40, (1ll << 58) / rows))) return fail(HS_E_INVALID, "%s: rows overlap, or ld out of range", fn);
   if (logprob && !tokens) return fail(HS_E_INVALID, "%s: logprob needs tokens", fn);
   if (need && (!workspace || workspace_bytes < need))
     return fail(HS_E_BUFFER, "%s: the workspace holds %llu bytes, %llu are needed", fn,

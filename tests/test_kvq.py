@@ -99,6 +99,17 @@ def test_attention_refused():
         assert attend(cache(), **fault) == H.HS_E_INVALID, fault
 
 
+def test_strides_whose_last_row_lies_past_64_bits_are_refused():
+    far, n = 1 << 40, 1 << 26
+    assert append(cache(), n=n, ld=far) == H.HS_E_INVALID
+    assert read(cache(), n=n, ld=far) == H.HS_E_INVALID
+    assert read(cache(n_kv_heads=4096, bytes=1 << 40), n=2, ld=64, ld_head=1 << 50) == H.HS_E_INVALID
+    c = cache(n_seqs=1 << 30)
+    assert attend(c, n=n, ld_q=far) == H.HS_E_INVALID
+    assert attend(c, n=n, ld_out=far) == H.HS_E_INVALID
+    assert logprobs(rows=n, ld=far) == H.HS_E_INVALID
+
+
 def test_attention_workspace_is_checked():
     c, need = cache(n_seqs=1, table_ld=1 << 16), ctypes.c_uint64()
     ask = hs.lib().hs_kvq_attention_workspace
