@@ -194,7 +194,11 @@ int hs_kv_free(hs_kv *kv);
  * prefilled request, in slot order; tokens_in / tokens_out are indexed by
  * slot ([slots]; other entries untouched) and logits / hidden_out rows
  * follow that order.  Host-side checks refuse a prefill or step the free
- * blocks cannot cover (HS_E_CAPACITY) before launching anything. */
+ * blocks cannot cover (HS_E_CAPACITY) before launching anything.  A graph
+ * captured from a decode step cuts the positions as the largest capacity
+ * admitted until then asks for: after admitting a larger one, capture it again
+ * (a pool held in 4 bits, hs_kvq_pool_create, attends over all positions even
+ * so). */
 int hs_kv_pool_create(hs_model *m, int32_t slots, int32_t block_tokens, void *dev_buf, uint64_t buf_bytes,
                       hs_kv **out);
 /* Puts a request (n_v vision rows, at most `capacity` positions,

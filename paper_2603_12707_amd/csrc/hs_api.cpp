@@ -311,7 +311,7 @@ struct Step {
     a.cap = kv->d_cap;
     a.len_by_seq = 1;
     a.len_add = 1;
-    a.max_len = kv->max_cap;
+    a.max_len = INT32_MAX;  // the capacities bound the lengths, those of requests admitted after a capture too
     a.scale = b.scale;
     a.out = b.out;
     a.ld_out = b.ld_q;

@@ -346,7 +346,7 @@ struct KvqAttn {
   int64_t ld_out;
   const int *order;  // the z-th row to be started is order[z]; NULL: z
   int rank;          // (set by the launcher) the z-th longest row
-  int S, n_split;    // positions per split (a multiple of 256), splits
+  int S, n_split;    // positions per split (a multiple of 256; the last one takes all that are left), splits
   float *part_o;     // [n][n_heads][n_split][head_dim]
   float *part_ml;    // [n][n_heads][n_split][2]: maximum (-inf: no position), sum
   uint32_t *count;

@@ -398,7 +398,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
     }
     return;
   }
-  const int end = min(t0 + a.S, len);  // the split's positions: t0 .. end - 1
+  // the split's positions: t0 .. end - 1.  The last one takes what is left: a replayed step may
+  // serve a request of a larger capacity than any that S was made for.
+  const int end = split == a.n_split - 1 ? len : min(t0 + a.S, len);
   const int n_tiles = (end - t0 + KVQ_TILE - 1) / KVQ_TILE;
   const int64_t kin = ((int64_t)(a.c.layer * 2) * a.c.n_kv + j) << (a.c.bt_log2 - 4);  // spans before the head's
   const int64_t vin = kin + ((int64_t)a.c.n_kv << (a.c.bt_log2 - 4));

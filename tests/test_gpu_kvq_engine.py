@@ -286,6 +286,44 @@ def test_replayed_steps_take_blocks_and_equal_eager_ones():
     assert model.status() == 0
 
 
+def test_a_replayed_step_serves_a_longer_request_than_at_its_capture():
+    """A slot released and filled with a request of a larger capacity than any at the capture: the replayed step attends
+    over all of its positions, in one split and in several."""
+    import paper_2603_12707_amd as hs
+    cfg = small_cfg(**GQA)
+    model = hs.Model(cfg, synth.make_weights(cfg, device="cuda"), 1, 5200)
+    for first, later in ((300, 1500), (2600, 5100)):
+        pools = [hs.QuantKVPool(model, 1, 256, 21) for _ in range(2)]
+
+        def fill(p, n, cap):
+            p.admit(0, 0, cap)
+            p.set_length(0, n, n)
+            for l in range(cfg["n_layers"]):
+                for sel in range(2):
+                    for j in range(cfg["n_kv_heads"]):
+                        p.write(0, l, sel, j, 0, synth.kv_block(cfg, 0, l, sel, j, n, device="cuda"))
+
+        fill(pools[0], first - 10, first)
+        tin, tout = torch.tensor([5], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+        logits, want = (torch.empty(1, cfg["vocab"], device="cuda") for _ in range(2))
+        graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(graph, stream=side):
+            pools[0].decode(tin, tout, logits)
+        pools[0].sync()
+        pools[0].release(0)
+        for p in pools:
+            fill(p, later - 40, later)
+        for i in range(3):
+            pools[1].decode(tin, torch.empty_like(tout), want)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert rel_err(logits[0].cpu(), want[0].cpu()) <= 2.0 ** -6, (first, i)
+        pools[0].sync()
+        assert pools[0].lengths() == pools[1].lengths() == [later - 37]
+    assert model.status() == 0
+
+
 def test_write_and_read_round_and_give_stored_values():
     cfg = small_cfg(**MHA)
     import paper_2603_12707_amd as hs
