@@ -459,7 +459,9 @@ int hs_token_logprobs(int32_t dtype, const void *logits, int64_t rows, int32_t v
  * NULL: of the tokens that the step chooses), the entropy and the `top`
  * alternatives.  logprob, entropy, top_ids and top_logprobs have a row for each
  * decoded request, in the order of the logits' rows; each may be NULL.  Feeding a
- * given text's tokens and asking for each next one scores the text. */
+ * given text's tokens and asking for each next one scores the text.  targets is
+ * read after tokens_out is written: it may be tokens_in, and tokens_out stands for
+ * the chosen tokens. */
 int hs_decode_step_logprobs(hs_model *m, hs_kv *kv, const int32_t *tokens_in, int32_t *tokens_out,
                             const int32_t *targets, int32_t top, float *logits, float *hidden_out, float *logprob,
                             float *entropy, int32_t *top_ids, float *top_logprobs, hs_stream_t stream);

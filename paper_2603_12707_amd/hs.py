@@ -339,9 +339,16 @@ class KVCache:
     def decode_logprobs(self, tokens_in, tokens_out, targets=None, top: int = 0, logits=None, hidden_out=None,
                         model=None):
         """The same step, and of its logits (logprob, entropy, top_ids, top_logprobs) as token_logprobs gives them,
-        a row for each decoded request: of the tokens in targets (int32, indexed like tokens_in; None: the chosen
-        ones), with `top` alternatives (None without)."""
+        a row for each decoded request: of the tokens in targets (int32, one for each request of the handle, like
+        tokens_in; None: the chosen ones), with `top` alternatives (None without)."""
         import torch
+        func = "decode_logprobs"
+        index = -1 if tokens_in is None else tokens_in.get_device()
+        if index < 0:
+            raise ValueError(f"{func}: tokens_in must be on the GPU")
+        # the kernels read and write an entry for every request of the handle
+        for name, t in (("tokens_in", tokens_in), ("tokens_out", tokens_out), ("targets", targets)):
+            _int32(func, name, t, self.batch, index)
         m = model or self.model
         device = tokens_in.device
         # as many rows as requests can be decoded; a pool that decodes fewer leaves the last ones unwritten

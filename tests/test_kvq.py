@@ -189,3 +189,40 @@ def test_binding_refuses_wrong_tensors():
         hs.token_logprobs(x.double())
     with pytest.raises(ValueError):
         hs.token_logprobs(x, torch.zeros(2, dtype=torch.int64))
+
+
+class _Tokens:
+    """What the binding looks at of a token tensor on a GPU."""
+
+    def __init__(self, n, dtype=None, index=0, contiguous=True):
+        import torch
+        self.n, self.dtype, self.index, self.contiguous, self.device = n, dtype or torch.int32, index, contiguous, "cuda"
+
+    def numel(self):
+        return self.n
+
+    def is_contiguous(self):
+        return self.contiguous
+
+    def get_device(self):
+        return self.index
+
+    def data_ptr(self):
+        return 0
+
+
+def test_steps_with_log_probabilities_refuse_wrong_tokens():
+    """One int32 token for each request of the handle, on the GPU: the kernels read by request number."""
+    import types
+
+    import torch
+    pool = object.__new__(hs.KVPool)
+    pool.batch, pool.handle, pool.model = 4, None, types.SimpleNamespace(max_batch=2, handle=None)
+    good = dict(tokens_in=_Tokens(4), tokens_out=_Tokens(4))
+    for bad in (_Tokens(4, torch.int64), _Tokens(2), _Tokens(5), _Tokens(4, index=-1), _Tokens(4, index=1),
+                _Tokens(4, contiguous=False), torch.zeros(4, dtype=torch.int64), torch.zeros(2, dtype=torch.int32)):
+        for name in ("targets", "tokens_in", "tokens_out"):
+            with pytest.raises(ValueError):
+                pool.decode_logprobs(**{**good, name: bad})
+    with pytest.raises(ValueError):
+        pool.decode_logprobs(None, _Tokens(4))
