@@ -340,7 +340,8 @@ class KVCache:
                         model=None):
         """The same step, and of its logits (logprob, entropy, top_ids, top_logprobs) as token_logprobs gives them,
         a row for each decoded request: of the tokens in targets (int32, one for each request of the handle, like
-        tokens_in; None: the chosen ones), with `top` alternatives (None without)."""
+        tokens_in; None: the chosen ones), with `top` alternatives (None without).  The rows come first; a pool that
+        decodes fewer requests than it could (slots, max_batch) has NaN, and -1 for tokens, in the others."""
         import torch
         func = "decode_logprobs"
         index = -1 if tokens_in is None else tokens_in.get_device()
@@ -351,11 +352,16 @@ class KVCache:
             _int32(func, name, t, self.batch, index)
         m = model or self.model
         device = tokens_in.device
-        # as many rows as requests can be decoded; a pool that decodes fewer leaves the last ones unwritten
-        rows = min(self.batch, m.max_batch)
-        lp, entropy = (torch.empty(rows, dtype=torch.float32, device=device) for _ in range(2))
-        ids = torch.empty(rows, top, dtype=torch.int32, device=device) if top > 0 else None
-        tops = torch.empty(rows, top, dtype=torch.float32, device=device) if top > 0 else None
+        # as many rows as requests can be decoded; those that a pool decodes fewer keep NaN and -1
+        rows, alts = min(self.batch, m.max_batch), max(top, 0)
+        if isinstance(self, KVPool):
+            numbers = torch.full((rows * (2 + alts),), float("nan"), dtype=torch.float32, device=device)
+            ids = torch.full((rows, alts), -1, dtype=torch.int32, device=device) if alts else None
+        else:
+            numbers = torch.empty(rows * (2 + alts), dtype=torch.float32, device=device)
+            ids = torch.empty(rows, alts, dtype=torch.int32, device=device) if alts else None
+        lp, entropy = numbers[:rows], numbers[rows : 2 * rows]
+        tops = numbers[2 * rows :].view(rows, alts) if alts else None
         _call("hs_decode_step_logprobs", m.handle, self.handle, _ptr(tokens_in), _ptr(tokens_out), _ptr(targets), top,
               _ptr(logits), _ptr(hidden_out), _ptr(lp), _ptr(entropy), _ptr(ids), _ptr(tops), _stream())
         return lp, entropy, ids, tops

@@ -431,6 +431,28 @@ def test_scoring_a_text_with_log_probabilities(quant):
     assert model.status() == 0
 
 
+def test_log_probabilities_of_a_partly_filled_pool():
+    """Rows past the decoded requests say so: NaN, and -1 for tokens."""
+    import paper_2603_12707_amd as hs
+    cfg = small_cfg(**GQA)
+    model = hs.Model(cfg, synth.make_weights(cfg, device="cuda"), 4, 300)
+    pool = hs.KVPool(model, 5, 256, 5)
+    for s in (1, 3):
+        pool.admit(s, 0, 60)
+        pool.prefill(s, None, synth.text_ids(cfg, s, 9).cuda(), synth.mrope_positions(0, 9).cuda())
+    tin, tout = torch.zeros(5, dtype=torch.int32, device="cuda"), torch.zeros(5, dtype=torch.int32, device="cuda")
+    junk = [torch.full((64,), 7.0, device="cuda") for _ in range(8)]  # what new memory may hold
+    del junk
+    for top in (0, 1, 3):
+        lp, ent, ids, tops = pool.decode_logprobs(tin, tout, top=top)
+        assert lp.shape == ent.shape == (4,) and torch.isfinite(lp[:2]).all() and torch.isfinite(ent[:2]).all()
+        assert torch.isnan(lp[2:]).all() and torch.isnan(ent[2:]).all()
+        if top:
+            assert ids.shape == tops.shape == (4, top) and (ids[:2] >= 0).all() and (ids[2:] == -1).all()
+            assert torch.isfinite(tops[:2]).all() and torch.isnan(tops[2:]).all()
+    assert model.status() == 0
+
+
 def test_contiguous_caches_have_log_probabilities_too():
     import paper_2603_12707_amd as hs
     cfg = small_cfg(n_layers=1, dtype="f32")
