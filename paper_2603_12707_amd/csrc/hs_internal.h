@@ -389,10 +389,11 @@ struct LogprobArgs {
   void *ws;   // logprob_workspace bytes, its counters zero between calls
   int count;  // (set by the launcher) the last work group of a row joins its parts
 };
-// a row is cut into parts of this many elements at least
+// a row is cut into parts of this many fp32 elements, or twice as many 16-bit ones
 constexpr int LOGPROB_PART = 8192;
 constexpr int LOGPROB_TOP = 64;  // most alternatives
 constexpr int LOGPROB_COUNTERS = 512;  // rows up to which they are joined in one launch
+constexpr int LOGPROB_ONE_LAUNCH = 5 * 256;  // and work groups
 inline int logprob_parts(int vocab) { return (int)(((int64_t)vocab + LOGPROB_PART - 1) / LOGPROB_PART); }
 uint64_t logprob_workspace(int64_t rows, int vocab, int top);
 hipError_t launch_logprobs(int dtype, const LogprobArgs &a, hipStream_t st);

@@ -538,14 +538,16 @@ hipError_t logprobs_dt(LogprobArgs a, hipStream_t st) {
   // rows that eight words a thread hold: fewer registers, and no thread without an
   // element (1531 rows of 2048 fp32 logits 7.4 us, with 32 words 11.2; one row 3.6 and 5.0)
   const bool small = a.vocab <= LP_THREADS * 8 * CE;
-  a.parts = small ? 1 : (int)(((int64_t)a.vocab + LP_THREADS * 32 * CE - 1) / (LP_THREADS * 32 * CE));
+  constexpr int PART = LOGPROB_PART * CE;
+  static_assert(LOGPROB_PART == LP_THREADS * 32, "a part is 32 words a thread");
+  a.parts = small ? 1 : (int)(((int64_t)a.vocab + PART - 1) / PART);
   const int64_t groups = a.rows * a.parts;
   if (groups > INT32_MAX) return hipErrorInvalidValue;
   // One launch while the GPU holds all work groups at once, five to a CU: where more
   // wait, joining at the end of a work group keeps its place for longer than a second
   // launch takes (no alternatives, one launch against two: 64 rows of 152064 fp32
   // logits 12.4 and 13.1 us, 400 rows 54.8 and 46.3; one row of 32000 8.7 and 11.1).
-  a.count = a.parts > 1 && groups <= 5 * 256 && a.rows <= LOGPROB_COUNTERS;
+  a.count = a.parts > 1 && groups <= LOGPROB_ONE_LAUNCH && a.rows <= LOGPROB_COUNTERS;
   if (small) HS_LAUNCH((k_logprobs<DT, 8>), dim3((uint32_t)groups), dim3(LP_THREADS), 0, st, a);
   else HS_LAUNCH((k_logprobs<DT, 32>), dim3((uint32_t)groups), dim3(LP_THREADS), 0, st, a);
   if (a.parts > 1 && !a.count) HS_LAUNCH((k_logprobs_join<DT>), dim3((uint32_t)a.rows), dim3(LP_THREADS), 0, st, a);

@@ -424,6 +424,28 @@ def test_attention_passes_a_nan_group_on_to_its_own_heads():
         assert torch.isfinite(out).all()
 
 
+@pytest.mark.parametrize("length,n_kv", [(3000, 2), (40000, 1)], ids=["joined", "combined"])
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+def test_a_nan_in_one_of_several_splits_reaches_the_output(length, n_kv, dtype):
+    """A NaN key group in one split alone, through the join of the last work group and through the combine kernel:
+    the outputs of its head are NaN, the other heads' and rows' are not."""
+    import paper_2603_12707_amd as hs
+    hd = 64
+    cache, blocks, table = make(hs, 2, -(-length // 64), 1, n_kv, hd, 64, fill=0)
+    for at in (length // 3, length - 5, 7):
+        blocks.zero_()  # rows of zeros but for a few, the one at `at` with a NaN
+        pos = torch.arange(at - 5, min(at + 11, length), dtype=torch.int32, device="cuda")
+        k, v = rows(len(pos), n_kv, hd, dtype, 60), rows(len(pos), n_kv, hd, dtype, 61)
+        k[5, n_kv - 1, 3] = math.nan
+        cache.append(0, k, v, pos, seqs=torch.zeros_like(pos))
+        q = rows(2, 4 * n_kv, hd, dtype, 62)
+        out = cache.attention(0, q, torch.tensor([length, length], dtype=torch.int32, device="cuda"))
+        assert torch.isnan(out[0, -4:]).all()
+        assert torch.isfinite(out[0, :-4]).all() and torch.isfinite(out[1]).all()
+        short = cache.attention(0, q, torch.tensor([at, length], dtype=torch.int32, device="cuda"))
+        assert torch.isfinite(short).all()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("heads,n_kv,hd", [(4, 4, 64), (14, 2, 128)])
 def test_queries_that_are_not_finite_reach_their_own_head_alone(dtype, heads, n_kv, hd):

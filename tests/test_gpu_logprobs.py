@@ -2,6 +2,8 @@
 from __future__ import annotations
 
 import math
+import os
+import re
 
 import pytest
 import torch
@@ -161,6 +163,65 @@ def test_rows_of_several_parts_on_both_sides_of_the_one_launch_limit(rows):
     order = torch.sort(x.float(), descending=True, stable=True)
     assert torch.equal(ids.long(), order.indices[:, :3])
     assert ((tops.double() - ref.gather(1, order.indices[:, :3])).abs() <= 2.0 ** -16).all()
+
+
+def _constant(name):
+    """An integer constant of the library's sources, or a product of two."""
+    src = os.path.join(os.path.dirname(__file__), "..", "paper_2603_12707_amd", "csrc", "hs_internal.h")
+    with open(src) as f:
+        value = re.search(rf"constexpr int {name} = ([0-9* ]+);", f.read()).group(1)
+    return math.prod(int(x) for x in value.split("*"))
+
+
+@pytest.mark.parametrize("dtype,vocab,rows,one", [("f32", 8200, 511, True), ("f32", 8200, 513, False),
+                                                  ("bf16", 16400, 512, True), ("bf16", 16400, 513, False),
+                                                  ("f16", 40000, 426, True), ("f16", 40000, 427, False),
+                                                  ("f32", 152064, 67, True), ("f32", 152064, 68, False),
+                                                  ("bf16", 32003, 700, False)])
+def test_rows_of_several_parts_joined_in_the_launch_and_after_it(dtype, vocab, rows, one):
+    """Both sides of the limits up to which one launch does, with rows whose parts hold ties, nothing but -inf, a NaN or
+    +inf in one part alone, and the largest value in the last elements."""
+    import paper_2603_12707_amd as hs
+    part = _constant("LOGPROB_PART") * (1 if dtype == "f32" else 2)
+    parts = -(-vocab // part)
+    assert parts > 1
+    assert one == (rows * parts <= _constant("LOGPROB_ONE_LAUNCH") and rows <= _constant("LOGPROB_COUNTERS"))
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x = (torch.randn(rows, vocab, device="cuda", generator=g) * 2).to(R.DT[dtype])
+    tail = part * (parts - 1)
+    x[::3, tail:] = 30.0            # the largest, and equal, in the last part
+    x[1::7, :tail] = -math.inf      # parts of nothing else
+    x[2::11, tail:] = -math.inf
+    x[3::13] = x[3::13].round()     # ties across parts
+    for r, (at, bad) in enumerate(((3, math.nan), (vocab - 1, math.nan), (part, math.inf), (tail - 1, math.nan))):
+        x[5 + 9 * r, at] = bad
+    x[50] = -math.inf
+    x[51] = -math.inf
+    x[51, vocab - 2] = 1.5
+    none = torch.isnan(x).any(1) | (x == math.inf).any(1) | (x == -math.inf).all(1)
+    assert none.sum() >= 5
+    tokens = torch.randint(-1, vocab, (rows,), device="cuda", generator=g)
+    tokens[51] = vocab - 2
+    ref = torch.log_softmax(x.double(), -1)
+    want = torch.where(tokens >= 0, ref.gather(1, tokens.clamp(min=0)[:, None])[:, 0], 0.0)
+    want[none & (tokens >= 0)] = math.nan
+    ent = -torch.where(ref > -math.inf, ref.exp() * ref, 0.0).sum(-1)
+    order = torch.sort(x.float() + 0.0, descending=True, stable=True).indices
+    for top in (0, 1, 20):
+        lp, e, ids, tops = hs.token_logprobs(x, tokens.int(), top=top)
+        assert torch.equal(torch.isnan(lp), torch.isnan(want)) and torch.equal(torch.isinf(lp), torch.isinf(want))
+        fine = torch.isfinite(want)
+        assert ((lp.double() - want).abs()[fine] <= R.logprob_tolerance(want)[fine]).all()
+        assert torch.equal(torch.isnan(e), none)
+        assert ((e.double() - ent).abs()[~none] <= 2.0 ** -16).all()
+        if not top:
+            continue
+        assert (ids[none] == -1).all() and torch.isnan(tops[none]).all()
+        assert torch.equal(ids.long()[~none], order[~none][:, :top])
+        t = ref.gather(1, order[:, :top])[~none]
+        got = tops.double()[~none]
+        assert torch.equal(torch.isinf(got), torch.isinf(t))
+        assert ((got - t).abs()[torch.isfinite(t)] <= R.logprob_tolerance(t)[torch.isfinite(t)]).all()
 
 
 def test_many_rows():
