@@ -374,7 +374,7 @@ typedef struct hs_kvq_cache {
 
 int hs_kvq_block_bytes(int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, int32_t block_tokens, uint64_t *bytes);
 
-/* Stores n rows of K and V of one layer.  Element (row r, head j, channel c) of
+/* Stores n rows (n * n_kv_heads below 2^28) of K and V of one layer.  Element (row r, head j, channel c) of
  * K is k[r * ld + j * ld_head + c] in `dtype` (v alike; device, 16-byte aligned;
  * ld and ld_head multiples of 8, HS_F32 4, and rows and heads do not overlap; a
  * single row's ld and a single head's ld_head are not looked at).
@@ -397,7 +397,8 @@ int hs_kvq_read(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, int32_t
 /* Decode attention: row r of q ([n_heads][head_dim] in `dtype`, rows ld_q
  * elements apart) attends over the first lengths[r] positions (device int32) of
  * sequence seqs[r] (NULL: r), query head i reading KV head
- * i / (n_heads / n_kv_heads), at most 16 heads to a KV head:
+ * i / (n_heads / n_kv_heads), at most 16 heads to a KV head (n * n_kv_heads below
+ * 2^24):
  *   out[r][i] = sum_p softmax_p(scale * q_i . k_p) v_p
  * over the positions that have a block, in fp32 (exact products; the weights keep 22
  * bits for HS_F16, 24 else), rounded once to `dtype`; a row without one (length 0 or
@@ -434,7 +435,8 @@ int hs_kvq_pool_create(hs_model *m, int32_t slots, int32_t block_tokens, void *d
 
 /* ---- log probabilities of tokens ----
  *
- * For each of `rows` rows of logits (device, `dtype`, vocab elements, 1..2^30, rows
+ * For each of `rows` rows of logits (rows times vocab / 8192, rounded up, is below
+ * 2^24; device, `dtype`, vocab elements, 1..2^30, rows
  * ld elements apart, aligned to their elements), with M = max x, Z = sum e^(x - M):
  *   logprob[r]  = x[tokens[r]] - M - log Z, the log probability of the given
  *                 token (device int32 [rows]); 0 for a negative token (none is

@@ -1476,7 +1476,8 @@ int kvq_rows_args(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, int32
   if (n == 0) return HS_OK;
   if (!k || !v || !positions) return fail(HS_E_INVALID, "%s: NULL argument", fn);
   if (((uintptr_t)k | (uintptr_t)v) % 16) return fail(HS_E_INVALID, "%s: rows must be 16-byte aligned", fn);
-  if ((int64_t)n * cache->n_kv_heads > (1ll << 30)) return fail(HS_E_INVALID, "%s: too many rows", fn);
+  // (a launch takes less than 2^32 threads: 16 rows of a head to 256 of them at least)
+  if ((int64_t)n * cache->n_kv_heads >= 1 << 28) return fail(HS_E_INVALID, "%s: too many rows", fn);
   return kvq_strides(fn, dtype, n, ld, ld_head, cache->n_kv_heads, cache->head_dim);
 }
 
@@ -1539,7 +1540,8 @@ int hs_kvq_attention_workspace(const hs_kvq_cache *cache, int32_t dtype, int32_t
     return fail(HS_E_INVALID, "%s: negative row count, or max_len not in 1..2^30", fn);
   if (n_heads <= 0 || n_heads % cache->n_kv_heads || n_heads / cache->n_kv_heads > 16)
     return fail(HS_E_INVALID, "%s: n_heads %d is not 1..16 times n_kv_heads %d", fn, n_heads, cache->n_kv_heads);
-  if ((int64_t)n * n_heads > (1 << 30)) return fail(HS_E_INVALID, "%s: too many rows", fn);
+  // (a launch takes less than 2^32 threads: 256 to a row and KV head)
+  if ((int64_t)n * cache->n_kv_heads >= 1 << 24) return fail(HS_E_INVALID, "%s: too many rows", fn);
   int S, ns;
   kvq_split_policy(n, cache->n_kv_heads, max_len, &S, &ns);
   *bytes = ns > 1 ? KVQ_COUNTERS * 4 + (uint64_t)n * n_heads * ns * (cache->head_dim + 2) * 4 : 0;
@@ -1595,7 +1597,8 @@ int hs_token_logprobs_workspace(int64_t rows, int32_t vocab, int32_t top, uint64
   if (rows < 0 || rows > INT32_MAX || vocab <= 0 || vocab > (1 << 30)) return fail(HS_E_INVALID, "%s: rows or vocab out of range", fn);
   if (top < 0 || top > LOGPROB_TOP || top > vocab)
     return fail(HS_E_INVALID, "%s: top %d is not in 0..%d or exceeds vocab", fn, top, LOGPROB_TOP);
-  if (rows * logprob_parts(vocab) > INT32_MAX) return fail(HS_E_INVALID, "%s: too many rows", fn);
+  // (a launch takes less than 2^32 threads: 256 to a part of a row)
+  if (rows * logprob_parts(vocab) >= 1 << 24) return fail(HS_E_INVALID, "%s: too many rows", fn);
   *bytes = logprob_workspace(rows, vocab, top);
   return HS_OK;
 }

@@ -110,6 +110,17 @@ def test_strides_whose_last_row_lies_past_64_bits_are_refused():
     assert logprobs(rows=n, ld=far) == H.HS_E_INVALID
 
 
+def test_more_rows_than_a_launch_takes_are_refused():
+    """A launch has less than 2^32 threads in a dimension; what would need more is refused before it."""
+    one = cache(n_kv_heads=1, n_seqs=1 << 30)
+    for call in (append, read):
+        assert call(one, n=1 << 28, ld=64) == H.HS_E_INVALID
+        assert call(cache(n_kv_heads=4096, bytes=1 << 40), n=1 << 16, ld=4096 * 64) == H.HS_E_INVALID
+    assert attend(one, n=1 << 24, heads=1, ld_q=64, ld_out=64) == H.HS_E_INVALID
+    assert logprobs(rows=1 << 24) == H.HS_E_INVALID
+    assert logprobs(rows=1 << 20, vocab=16 * 8192, ld=16 * 8192) == H.HS_E_INVALID
+
+
 def test_attention_workspace_is_checked():
     c, need = cache(n_seqs=1, table_ld=1 << 16), ctypes.c_uint64()
     ask = hs.lib().hs_kvq_attention_workspace
