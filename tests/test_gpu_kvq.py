@@ -357,6 +357,18 @@ def test_attention_of_other_scales(scale, spread):
         fill_and_check(hs, dtype, [513, 70], 8, 2, 64, 64, scale=scale, spread=spread, seed=12)
 
 
+def test_many_rows_and_many_heads():
+    """More rows than a grid's second dimension takes, each as in a smaller call; and a cache of hundreds of heads."""
+    import paper_2603_12707_amd as hs
+    cache, q, lens, want = fill_and_check(hs, "bf16", [(37 * i) % 90 for i in range(300)], 4, 1, 64, 32, seed=22,
+                                          seqs=[i % 7 for i in range(300)])
+    n = 70000
+    at = torch.arange(n, device="cuda") % 300
+    got = cache.attention(0, q[at], lens[at], seqs=(at % 7).int())
+    assert torch.equal(got, want[at])
+    fill_and_check(hs, "f16", [70, 0, 33], 600, 300, 64, 16, seed=23)
+
+
 def test_attention_takes_strides_and_leaves_other_memory_alone():
     import paper_2603_12707_amd as hs
     cache, q, lens, want = fill_and_check(hs, "bf16", [200, 31, 0, 77], 4, 2, 64, 32, seed=13)

@@ -324,6 +324,46 @@ def test_a_replayed_step_serves_a_longer_request_than_at_its_capture():
     assert model.status() == 0
 
 
+def test_a_pool_that_runs_dry_inside_replays():
+    """Request 0 enters a block that is not there: the step says so, keeps its new rows unstored and masks their places,
+    in one split and where they are all that a split holds; request 1 goes on as in a pool with room."""
+    import paper_2603_12707_amd as hs
+    cfg = small_cfg(**GQA)
+    model = hs.Model(cfg, synth.make_weights(cfg, device="cuda"), 2, 2700)
+    for first, cap in ((250, 400), (2558, 2700)):
+        blocks = -(-first // 256) + 1
+        pools = [hs.QuantKVPool(model, 2, 256, blocks + room) for room in (0, 1)]
+        for p in pools:
+            for r, n in ((0, first), (1, 100)):
+                p.admit(r, 0, cap)
+                p.set_length(r, n, n)
+                for l in range(cfg["n_layers"]):
+                    for sel in range(2):
+                        for j in range(cfg["n_kv_heads"]):
+                            p.write(r, l, sel, j, 0, synth.kv_block(cfg, r, l, sel, j, n, device="cuda"))
+        assert pools[0].blocks() == (0, blocks)
+        tin, tout = torch.tensor([3, 4], dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+        logits, want = (torch.empty(2, cfg["vocab"], device="cuda") for _ in range(2))
+        graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(graph, stream=side):
+            pools[0].decode(tin, tout, logits)
+        pools[0].sync()
+        steps = 256 - first % 256
+        for i in range(steps + 3):
+            pools[1].decode(tin, torch.empty_like(tout), want)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert model.status() == (4 if i >= steps else 0), i
+            assert torch.isfinite(logits).all()
+            assert torch.equal(logits[1], want[1]), i
+            assert (i >= steps) or torch.equal(logits[0], want[0]), i
+        pools[0].sync()
+        assert pools[0].lengths() == [first + steps + 3, 100 + steps + 3]
+        with pytest.raises(hs.HsError):
+            pools[0].decode(tin, tout)
+
+
 def test_write_and_read_round_and_give_stored_values():
     cfg = small_cfg(**MHA)
     import paper_2603_12707_amd as hs
