@@ -401,8 +401,9 @@ int hs_kvq_read(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, int32_t
  * 2^24):
  *   out[r][i] = sum_p softmax_p(scale * q_i . k_p) v_p
  * over the positions that have a block, in fp32 (exact products; the weights keep 22
- * bits for HS_F16, 24 else), rounded once to `dtype`; a row without one (length 0 or
- * negative) gives zeros, a query head that holds a NaN or an infinity NaNs.
+ * bits for HS_F16, 24 else; scores have to be finite there), rounded once to `dtype`; a
+ * row without one (length 0 or negative) gives zeros, a query head that holds a NaN or
+ * an infinity NaNs.
  * max_len (host, 1..2^30) bounds the lengths and shapes the launch; positions from
  * it on are not attended.
  * q, out, ld_q and ld_out are aligned as in hs_kvq_append.  workspace is device
@@ -435,9 +436,9 @@ int hs_kvq_pool_create(hs_model *m, int32_t slots, int32_t block_tokens, void *d
 
 /* ---- log probabilities of tokens ----
  *
- * For each of `rows` rows of logits (rows times vocab / 8192, rounded up, is below
- * 2^24; device, `dtype`, vocab elements, 1..2^30, rows
- * ld elements apart, aligned to their elements), with M = max x, Z = sum e^(x - M):
+ * For each of `rows` rows of logits (device, `dtype`, vocab elements, 1..2^30, rows
+ * ld elements apart, aligned to their elements; rows times vocab / 8192 rounded up is
+ * below 2^24), with M = max x, Z = sum e^(x - M):
  *   logprob[r]  = x[tokens[r]] - M - log Z, the log probability of the given
  *                 token (device int32 [rows]); 0 for a negative token (none is
  *                 asked for: a padded batch), NaN for one from vocab on;

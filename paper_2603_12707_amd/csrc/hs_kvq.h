@@ -4,10 +4,10 @@
 // A row's elements are E2M1 numbers (sign, 2 exponent bits, 1 mantissa bit:
 // 0, 1/2, 1, 3/2, 2, 3, 4, 6) in groups of 32 that share one power of two, a
 // byte holding its exponent + 127.  With a = max |x| of a group the power is
-// the least 2^e with a < 7 * 2^e: the group's largest element then rounds to
-// 4 or 6 (or to 3 below 3.5), and as 7 lies half way between 6 and the next
-// step, saturating at 6 moves an element by less than 2^e, which is half of
-// the widest step.  Rounding is to nearest, ties to even.  A value takes at most
+// the least 2^e with a < 7 * 2^e: a is then 3.5 * 2^e at least (but where e is the
+// least that there is) and rounds to 4 or 6, and as 7 lies half way between 6 and
+// the next step, saturating at 6 moves an element by less than 2^e, which is half
+// of the widest step.  Rounding is to nearest, ties to even.  A value takes at most
 // 2 significant bits, so it is exact in f16 and in bf16, and gfx950 converts
 // both ways in one full-rate instruction for two elements.
 #pragma once
@@ -215,7 +215,7 @@ __global__ __launch_bounds__(256) void k_kvq_read(KvqRows a) {
 // the k range of MFMA m.  For V^T a lane reads its HD / 16 channels of those 16
 // positions, converts pairs of channels (exact in the 16-bit type) and pairs the
 // positions with v_perm.  P enters as the sum of parts in that type: two of f16 (22
-// bits), three of bf16 (24 bits); every sum is fp32.
+// bits), three of bf16 (24 bits); every sum is fp32, that of P taken before it is cut.
 //
 // Each wave copies its tiles straight into LDS, K and V alike as they lie in
 // memory, a tile and a half ahead, through buffer ranges that end at the last span
@@ -224,13 +224,17 @@ __global__ __launch_bounds__(256) void k_kvq_read(KvqRows a) {
 // positions and more (WIDE) hold a tile whole; smaller ones are copied span by span.
 //
 // Measured: 256 rows of 1024 .. 8192 positions (bf16, 28/4 heads of 128; 645 MB)
-// 115 us, 5.6 TB/s (109 with the scaled MFMA and P in two parts, for scores off by up to
-// 2^-16 of their largest product and P's bits from the 17th on).  32 rows of 608 .. 960 (f16, 32/32
-// heads; 110 MB) 25 us, on 1024 work groups of uneven length in 768 places.  Two rows of
-// 120000 .. 131072 (bf16; 137 MB) 35 us, of which 13 are the ramp, the last tiles and the join of
-// 32 splits.  One row of 700 8 us: the length, the block number and the first tile's copy one
-// after the other, 2 us a tile, the merge.  Before: K and V through registers took 139 us for
-// the first.
+// 115 us, 5.6 TB/s; from a graph 121, of which the copies alone take 105 and the
+// arithmetic alone 89: they overlap for the most part.  (109 with the scaled MFMA and P in
+// two parts, for scores off by up to 2^-16 of their largest product and P's bits from the
+// 17th on; K and V through registers took 139.)  32 rows of 608 .. 960 (f16, 32/32
+// heads; 110 MB) 25 us, from a graph 27: the copies alone 19, the arithmetic alone 21, the
+// vector unit a third busy and the matrix cores a ninth: 1024 work groups of uneven length
+// in 768 places, each a chain of few tiles.  Two rows of 120000 .. 131072 (bf16; 137 MB)
+// 35 us, 37 from a graph, the copies alone 31 and the arithmetic 32, 20 at the read rate:
+// the ramp, the last tiles and the join of 32 splits are in each.  One row of 700 8 us: the
+// length, the block number and the first tile's copy one after the other, 2 us a tile, the
+// merge.
 template <int DT>
 constexpr int KVQ_MMA = DT == HS_F16 ? HS_F16 : HS_BF16;
 template <int DT>
@@ -240,8 +244,8 @@ constexpr int KVQ_Q_PARTS = DT == HS_F32 ? 3 : 1;
 constexpr int KVQ_TILE = 64, KVQ_PLANES = 3;
 // Rows are started longest first where some CU takes more than one work group and the
 // longest rows take a while: up to this many rows, from more positions on.  28/4 heads, in
-// their own order and longest first: 250 rows of 1024 .. 8192 125 and 112 us, 66 rows 53.6
-// and 48.8, 160 rows of 400 .. 2000 29.2 and 27.1, of 200 .. 1000 19.1 and 19.3.
+// their own order and longest first: 250 rows of 1024 .. 8192 140 and 121 us, 66 rows 64.6
+// and 57.1, 160 rows of 400 .. 2000 34.9 and 30.2, of 200 .. 1000 22.7 and 21.8.
 constexpr int KVQ_CUS = 256, KVQ_RANK_MOST = 256, KVQ_RANK_FROM = 1024;
 typedef const __attribute__((address_space(4))) int64_t ConstI64;
 
@@ -734,7 +738,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DT == H
 // o = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s over the splits of a (row,
 // head); zeros where none holds a position.  HD / 4 threads take a split's
 // partial, 1024 / HD splits at a time, several of them in flight.  64 splits of 28
-// heads: 4.6 us, two dependent reads (beside 17.1 us of attention over 131072 positions).
+// heads: 4.6 us, two dependent reads (beside 20 us of attention over 131072 positions).
 template <int DT, int HD>
 __global__ __launch_bounds__(256) void k_kvq_combine(KvqAttn a) {
   constexpr int TPS = HD / 4, PARTS = 256 / TPS, AHEAD = 4;
@@ -809,8 +813,9 @@ hipError_t kvq_rows_any(int dtype, int hd, const KvqRows &a, bool read, hipStrea
 }
 
 // Waves of a work group: eight while there are no more pairs than CUs, four where
-// several work groups share a CU (their LDS holds three).  Rows of 3000 .. 4000 in 256
-// pairs take 28.6 us with eight and 30.8 with four, in 288 pairs 43.9 and 39.6.
+// several work groups share a CU (their LDS holds three).  bf16 rows of 3000 .. 4000 in 256
+// pairs take 29.8 us with eight and 33.0 with four, in 288 pairs 48.2 and 42.9 (f16: 27.2
+// and 30.7, 41.8 and 38.4).
 int kvq_waves(int64_t pairs) { return pairs <= 256 ? 8 : 4; }
 
 template <int DT, int HD, int NW>

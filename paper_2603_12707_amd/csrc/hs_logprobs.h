@@ -285,16 +285,18 @@ __device__ __forceinline__ float raw_elem(const uint32_t (&w)[NW], int i) {
 // maximum, then the sums, then the alternatives: the top-th largest of the 256
 // threads' own maxima is a value that at least `top` elements reach, and few more
 // (one wave finds it, bit by bit with ballots, while the others sum).  A single
-// alternative is the maximum's first place.  A NaN makes the sum NaN.  A row of one
+// alternative is the maximum's first place.  A NaN makes the sum NaN.  The exponentials
+// are 2^(d log2 e) with the product rounded: off by |d| 2^-24 of themselves,
+// as much as the rounding of d = x - M moves them.  A row of one
 // part is finished here; of several, by the last of its work groups to arrive, or by
 // k_logprobs_join.
 //
 // Measured: 256 rows of 152064 fp32 logits (156 MB), no alternatives 33 us, one 39,
-// five 44, twenty 47; 1531 rows of 32003 bf16 logits (98 MB) 32, 38, 41, 44.  The sums
-// are bound by the vector unit (an exponential, a conversion and four more operations an
-// element, half of its cycles) and by each work group's chain of load, maximum and sum,
-// of which five share a CU; the alternatives add the floor's 16 ballots and the
-// ranking.  16 rows of 152064: 7, 9.5, 12, 13 us, one row of 32000: 6, 8, 9.5, 11, the
+// five 44, twenty 47; 1531 rows of 32003 bf16 logits (98 MB) 32, 38, 41, 44.  Neither the
+// vector unit (issue 48 % of the cycles for fp32, 57 % for bf16) nor memory (3.8 TB/s) is
+// full: each work group's load, maximum, barrier and sum come one after the other, five
+// share a CU, and no register is left for the next part meanwhile; the alternatives add the
+// floor's 16 ballots and the ranking.  16 rows of 152064: 7, 9.5, 12, 13 us, one row of 32000: 6, 8, 9.5, 11, the
 // chain of one part and of the join.  A work group to a row that read it again for each
 // pass took 1204 us for the 256 rows with twenty.
 template <int DT, int NW>
