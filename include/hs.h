@@ -434,6 +434,99 @@ int hs_kvq_attention(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, in
 int hs_kvq_pool_create(hs_model *m, int32_t slots, int32_t block_tokens, void *dev_buf, uint64_t buf_bytes,
                        hs_kv **out);
 
+/* ---- a paged KV cache in the model's own type ----
+ *
+ * The operators of serving many answers to one prompt: rows stored with their
+ * positions turned into them, and attention that reads what sequences have in
+ * common once.  The cache is caller-owned device memory in `dtype`, cut into
+ * blocks of block_tokens positions (a power of two in 16..16384), and a table of
+ * their numbers.  A block is [n_layers][K, V][n_kv_heads][block_tokens][head_dim].
+ * Position p of sequence s lives in block table[s * table_ld + p / block_tokens];
+ * a number that is negative or not below bytes / block_bytes means that there is
+ * no block: nothing is stored there, and attention masks it.  Tables may share
+ * blocks.  blocks: 16-byte aligned; head_dim 64 or 128, n_kv_heads 1..4096. */
+typedef struct hs_paged_cache {
+  void *blocks;         /* device */
+  uint64_t bytes;       /* of blocks; at least one block */
+  const int64_t *table; /* device [n_seqs][table_ld] */
+  int32_t n_seqs, table_ld;
+  int32_t n_layers, n_kv_heads, head_dim, block_tokens;
+  int32_t dtype;
+} hs_paged_cache;
+
+int hs_paged_block_bytes(int32_t dtype, int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, int32_t block_tokens,
+                         uint64_t *bytes);
+
+/* A rotation by position.  Pair i (i < n_pairs, a multiple of 8, at most head_dim /
+ * 2) of a head's channels, (i, i + n_pairs) or, with `adjacent`, (2 i, 2 i + 1), is
+ * turned by angles_at[axes[i]][row] * frequencies[i] radians; channels from 2
+ * n_pairs on stay.  frequencies: device, 64 bits; axes: device, NULL for axis 0
+ * throughout, numbers outside 0..n_axes - 1 are taken into it; n_axes 1..8 (time,
+ * height and width of a multimodal row are three).  n_pairs 0: no rotation. */
+typedef struct hs_rope {
+  const double *frequencies; /* [n_pairs] */
+  const int32_t *axes;       /* [n_pairs] */
+  int32_t n_pairs, n_axes, adjacent;
+} hs_rope;
+
+/* New rows of one layer, n of them (n * (n_heads + 2 n_kv_heads) below 2^28): keys
+ * normalised (k_gain not NULL: x / sqrt(mean x^2 + eps) * k_gain over the head's
+ * channels), turned (rope not NULL) and stored, values stored as they are, and
+ * with n_heads > 0 queries normalised (q_gain) and turned alike into q_out.  Angles
+ * are taken in 64 bits, the rest in fp32, rounded once.  Element (row r, head j,
+ * channel c) of k is k[r * ld + j * ld_head + c] (v alike), of q q[r * ld_q + j *
+ * ld_q_head + c], of q_out alike; all device, the cache's dtype, 16-byte aligned,
+ * strides multiples of 16 bytes (a single row's and a single head's are not looked
+ * at), rows and heads apart.  q_out may be q, with its strides; else it overlaps
+ * no input.  Row r goes to position positions[r] (device int32) of sequence seqs[r]
+ * (device int32; NULL: sequence r); a row whose position is negative, whose sequence
+ * is outside the table or whose place has no block is not stored (its query is
+ * turned all the same), which is how a padded batch is passed.  No two stored rows
+ * of a call may name the same place.  angles_at: device int32 [n_axes][n], any
+ * numbers; NULL: positions, for a rope of one axis.  q_gain, k_gain: device
+ * [head_dim], 16-byte aligned. */
+int hs_paged_append(const hs_paged_cache *cache, int32_t layer, int32_t n, int32_t n_heads, const void *q,
+                    int64_t ld_q, int64_t ld_q_head, void *q_out, int64_t ld_q_out, int64_t ld_q_out_head,
+                    const void *k, const void *v, int64_t ld, int64_t ld_head, const int32_t *seqs,
+                    const int32_t *positions, const hs_rope *rope, const int32_t *angles_at, const void *q_gain,
+                    const void *k_gain, float eps, hs_stream_t stream);
+
+/* Attention: row r of q ([n_heads][head_dim] in the cache's dtype, rows ld_q
+ * elements apart) attends over the first lengths[r] positions (device int32) of
+ * sequence seqs[r] (NULL: r), query head i reading KV head i / (n_heads /
+ * n_kv_heads), at most 16 heads to a KV head (n * n_heads below 2^22):
+ *   out[r][i] = sum_p softmax_p(scale * q_i . k_p) v_p
+ * over the positions that have a block, rounded once; a row without one (length 0
+ * or negative, a sequence outside the table) gives zeros.  Several rows may be of
+ * one sequence: rows of lengths L + 1, L + 2, ... are its next tokens, each of
+ * which sees those before it.
+ *
+ * Groups.  With n_groups > 0 (at most n), rows group_starts[g] .. group_starts[g +
+ * 1] - 1 (device int32 [n_groups + 1], not falling, within 0..n) are group g and have
+ * their first shared[g] positions (device int32) in common: those are read through
+ * the table row of the group's first row, once for all its rows.  Rows before
+ * group_starts[0] or from group_starts[n_groups] on are in no group.  A row whose
+ * length is less than shared[g] attends over its length of them.  The arrays may
+ * change between replays of a captured call.
+ *
+ * max_len and max_shared (host, max_len 1..2^30, max_shared 0..max_len) bound the
+ * lengths and the shared positions and shape the launch; positions from max_len on
+ * are not attended, and of shared[g] more than max_shared is not taken as shared.
+ * Scores and sums are fp32, and have to be finite; weights enter the second product
+ * with 22 bits for HS_F16, 16 for HS_BF16, 24 for HS_F32; values have to be finite.
+ * q, out, ld_q and ld_out are aligned as in hs_paged_append.  workspace: device
+ * memory of hs_paged_attention_workspace bytes (which may be 0: then it may be
+ * NULL), 16-byte aligned; nothing in it is kept from call to call.  Calls that may
+ * run at the same time (on several streams, or two graphs) do not share one.
+ * Both calls only enqueue kernels and can be captured. */
+int hs_paged_attention_workspace(const hs_paged_cache *cache, int32_t n, int32_t n_heads, int32_t max_len,
+                                 int32_t n_groups, int32_t max_shared, uint64_t *bytes);
+int hs_paged_attention(const hs_paged_cache *cache, int32_t layer, int32_t n, int32_t n_heads, const void *q,
+                       int64_t ld_q, const int32_t *seqs, const int32_t *lengths, int32_t n_groups,
+                       const int32_t *group_starts, const int32_t *shared, int32_t max_len, int32_t max_shared,
+                       float scale, void *out, int64_t ld_out, void *workspace, uint64_t workspace_bytes,
+                       hs_stream_t stream);
+
 /* ---- log probabilities of tokens ----
  *
  * For each of `rows` rows of logits (device, `dtype`, vocab elements, 1..2^30, rows
@@ -468,6 +561,39 @@ int hs_token_logprobs(int32_t dtype, const void *logits, int64_t rows, int32_t v
 int hs_decode_step_logprobs(hs_model *m, hs_kv *kv, const int32_t *tokens_in, int32_t *tokens_out,
                             const int32_t *targets, int32_t top, float *logits, float *hidden_out, float *logprob,
                             float *entropy, int32_t *top_ids, float *top_logprobs, hs_stream_t stream);
+
+/* ---- tokens drawn ----
+ *
+ * For each of `rows` rows of logits (laid out as for hs_token_logprobs, and as
+ * many): with the logits in falling order (the lowest index first among equals) and
+ * w = e^((x - max x) / temperature),
+ *   the first top_k[r] stay (0 or less, or more than vocab: all);
+ *   of these the shortest beginning whose weights sum to at least top_p[r] times
+ *   theirs (1 or more: all);
+ *   of these the ones with w >= min_p[r] (0 or less: all);
+ * the first always stays.  tokens[r] is the first token whose weights, summed up to
+ * it, exceed u[r] times the sum of those that stay, and logprob[r] (may be NULL) its
+ * log probability among them.  temperature 0 takes the first (logprob 0).  u: device
+ * fp32 in [0, 1), a number below is taken as 0 and one above as just less than 1;
+ * temperature (NULL: 1), top_p (NULL: 1), min_p (NULL: 0): device fp32 [rows]; top_k
+ * (NULL: 0): device int32 [rows].  Logits of -inf are never drawn.  A row of logits
+ * that holds a NaN or +inf, or nothing but -inf, or whose temperature is negative
+ * or infinite, or with a NaN among its parameters, has token -1 and logprob NaN.
+ * Weights and their sums are held in 64 bits, and results are the same from call to
+ * call.  workspace: device memory of hs_sample_tokens_workspace bytes under the rules
+ * of hs_kvq_attention's, its first 2048 bytes zero before its first use. */
+int hs_sample_tokens_workspace(int64_t rows, int32_t vocab, uint64_t *bytes);
+int hs_sample_tokens(int32_t dtype, const void *logits, int64_t rows, int32_t vocab, int64_t ld, const float *u,
+                     const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                     int32_t *tokens, float *logprob, void *workspace, uint64_t workspace_bytes, hs_stream_t stream);
+
+/* hs_decode_step that draws its tokens as hs_sample_tokens does instead of taking the
+ * largest logit.  u, temperature, top_k, top_p and min_p are indexed like tokens_in;
+ * logprob (may be NULL) has a row for each decoded request, in the order of the
+ * logits' rows.  A captured step reads them at each replay. */
+int hs_decode_step_sample(hs_model *m, hs_kv *kv, const int32_t *tokens_in, int32_t *tokens_out, const float *u,
+                          const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                          float *logits, float *hidden_out, float *logprob, hs_stream_t stream);
 
 /* Reads and clears the device-side flags.  Synchronises the device.
  *   bit 0 (1): a token id outside [0, vocab) was replaced by 0;

@@ -165,7 +165,7 @@ hipError_t rebuild_active(hs_kv *kv, hipStream_t st) {
 void free_model(hs_model *m) {
   if (!m) return;
   void *ptrs[] = {m->x,      m->q,      m->attn,    m->act,      m->hnorm,  m->splitk, m->xlast,
-                  m->pk_dev, m->pk_order, m->lp_ws, m->logits, m->part_o, m->part_ml, m->rope_tab, m->status};
+                  m->pk_dev, m->pk_order, m->lp_ws, m->sm_ws, m->logits, m->part_o, m->part_ml, m->rope_tab, m->status};
   for (void *p : ptrs)
     if (p) (void)hipFree(p);
   delete m;
@@ -717,6 +717,7 @@ int hs_model_create(const hs_config *cfg, const hs_weights *w, int32_t max_batch
       {(void **)&m->pk_dev, sizeof(PackedRows)},
       {(void **)&m->pk_order, (size_t)prefill_groups_max(rows) * sizeof(PrefillGroup)},
       {&m->lp_ws, w->lm_head ? (size_t)logprob_workspace(max_batch, c.vocab, LOGPROB_TOP) : 0},
+      {&m->sm_ws, w->lm_head ? (size_t)sample_workspace(max_batch, c.vocab) : 0},
       {(void **)&m->logits, w->lm_head ? (size_t)max_batch * c.vocab * 4 : 0},
       {(void **)&m->part_o, (size_t)std::max<int64_t>(entries, 1) * hd * 4},
       {(void **)&m->part_ml, (size_t)std::max<int64_t>(entries, 1) * 2 * 4},
@@ -745,7 +746,8 @@ int hs_model_create(const hs_config *cfg, const hs_weights *w, int32_t max_batch
   // (they are never written, so cleared once here)
   if (hipMemcpy(m->rope_tab, tab.data(), tab.size() * 4, hipMemcpyHostToDevice) != hipSuccess ||
       hipMemset(m->status, 0, 4) != hipSuccess ||
-      (m->lp_ws && hipMemset(m->lp_ws, 0, LOGPROB_COUNTERS * 4) != hipSuccess) || hipMemset(m->attn, 0, (size_t)act_elems(rows, nh * hd) * b) ||
+      (m->lp_ws && hipMemset(m->lp_ws, 0, LOGPROB_COUNTERS * 4) != hipSuccess) ||
+      (m->sm_ws && hipMemset(m->sm_ws, 0, SAMPLE_COUNTERS * 4) != hipSuccess) || hipMemset(m->attn, 0, (size_t)act_elems(rows, nh * hd) * b) ||
       hipMemset(m->act, 0, (size_t)act_elems(rows, c.ffn_dim) * b) ||
       hipMemset(m->hnorm, 0, (size_t)act_elems(rows, c.d_model) * b)) {
     free_model(m);
@@ -1063,10 +1065,11 @@ int hs_model_reserve_rows(hs_model *m, int64_t rows) {
 
 // One decode step (hs_decode_step); ovr, when given, replaces the model's
 // workspaces as the step's scratch; lp, when given, asks for log probabilities
-// (its outputs, top and given tokens; tokens NULL: the chosen ones).
+// (its outputs, top and given tokens; tokens NULL: the chosen ones); sm, when
+// given, has the tokens drawn (its parameters and logprob).
 static int decode_impl(hs_model *m, hs_kv *kv, const int32_t *tokens_in, int32_t *tokens_out, float *logits,
                        float *hidden_out, hs_stream_t stream, const StepWs *ovr, const char *fn,
-                       const LogprobArgs *lp = nullptr) {
+                       const LogprobArgs *lp = nullptr, const SampleArgs *sm = nullptr) {
   if (!kv_matches(kv, m)) return fail(HS_E_INVALID, "%s: model/handle mismatch", fn);
   if (!tokens_in) return fail(HS_E_INVALID, "%s: tokens_in is NULL", fn);
   const hs_config &c = m->cfg;
@@ -1095,7 +1098,20 @@ static int decode_impl(hs_model *m, hs_kv *kv, const int32_t *tokens_in, int32_t
   if (m->w.lm_head) {
     float *lg = logits ? logits : step.ws.logits;
     HIP_TRY(step.head(step.ws.x, lg, pend));
-    HIP_TRY(launch_argmax(lg, c.vocab, c.vocab, B, tokens_out, act, kv->d_len, kv->d_rope, 1, st));
+    if (sm) {
+      SampleArgs a = *sm;
+      a.logits = lg;
+      a.rows = B;
+      a.ld = c.vocab;
+      a.vocab = c.vocab;
+      a.act = act;
+      a.tokens = tokens_out;
+      a.ws = m->sm_ws;
+      HIP_TRY(launch_sample(HS_F32, a, st));
+      HIP_TRY(launch_advance(kv->d_len, kv->d_rope, act, B, st));
+    } else {
+      HIP_TRY(launch_argmax(lg, c.vocab, c.vocab, B, tokens_out, act, kv->d_len, kv->d_rope, 1, st));
+    }
     if (lp) {
       LogprobArgs a = *lp;
       a.logits = lg;
@@ -1145,6 +1161,23 @@ int hs_decode_step_logprobs(hs_model *m, hs_kv *kv, const int32_t *tokens_in, in
   lp.top_ids = top_ids;
   lp.top_logprobs = top_logprobs;
   return decode_impl(m, kv, tokens_in, tokens_out, logits, hidden_out, stream, nullptr, fn, &lp);
+}
+
+int hs_decode_step_sample(hs_model *m, hs_kv *kv, const int32_t *tokens_in, int32_t *tokens_out, const float *u,
+                          const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                          float *logits, float *hidden_out, float *logprob, hs_stream_t stream) {
+  static const char *fn = "hs_decode_step_sample";
+  if (!kv_matches(kv, m)) return fail(HS_E_INVALID, "%s: model/handle mismatch", fn);
+  if (!m->w.lm_head) return fail(HS_E_STATE, "%s: model has no LM head", fn);
+  if (!u) return fail(HS_E_INVALID, "%s: u is NULL", fn);
+  SampleArgs sm{};
+  sm.u = u;
+  sm.temperature = temperature;
+  sm.top_k = top_k;
+  sm.top_p = top_p;
+  sm.min_p = min_p;
+  sm.logprob = logprob;
+  return decode_impl(m, kv, tokens_in, tokens_out, logits, hidden_out, stream, nullptr, fn, nullptr, &sm);
 }
 
 // ---- the decode step with its scratch in a static device array ----
@@ -1586,6 +1619,215 @@ int hs_kvq_attention(const hs_kvq_cache *cache, int32_t layer, int32_t dtype, in
   a.ld_out = ld_out;
   HIP_TRY(launch_kvq_attention(dtype, cache->head_dim, a, (hipStream_t)stream));
   if (!a.count) HIP_TRY(launch_kvq_combine(dtype, cache->head_dim, a, (hipStream_t)stream));
+  return HS_OK;
+}
+
+// ---- a paged cache in the model's type ----
+
+int hs_paged_block_bytes(int32_t dtype, int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, int32_t block_tokens,
+                         uint64_t *bytes) {
+  static const char *fn = "hs_paged_block_bytes";
+  if (!bytes) return fail(HS_E_INVALID, "%s: bytes is NULL", fn);
+  if (dtype < HS_F32 || dtype > HS_BF16) return fail(HS_E_INVALID, "%s: unknown dtype", fn);
+  if (n_layers <= 0 || n_kv_heads <= 0 || n_kv_heads > 4096)
+    return fail(HS_E_INVALID, "%s: n_layers must be positive, n_kv_heads in 1..4096", fn);
+  if (head_dim != 64 && head_dim != 128) return fail(HS_E_INVALID, "%s: head_dim %d is not 64 or 128", fn, head_dim);
+  if (block_tokens < 16 || block_tokens > 16384 || (block_tokens & (block_tokens - 1)))
+    return fail(HS_E_INVALID, "%s: block_tokens must be a power of two in 16..16384", fn);
+  uint64_t b = 2ull * (uint64_t)block_tokens * (uint64_t)head_dim * (uint64_t)dtype_bytes(dtype);
+  if (__builtin_mul_overflow(b, (uint64_t)n_layers * (uint64_t)n_kv_heads, &b) || b > (uint64_t)INT64_MAX)
+    return fail(HS_E_INVALID, "%s: size overflows 63 bits", fn);
+  *bytes = b;
+  return HS_OK;
+}
+
+static int paged_ref(const hs_paged_cache *c, int layer, const char *fn, PagedRef *out) {
+  if (!c || !c->blocks || !c->table) return fail(HS_E_INVALID, "%s: NULL argument", fn);
+  uint64_t bb;
+  const int rc = hs_paged_block_bytes(c->dtype, c->n_layers, c->n_kv_heads, c->head_dim, c->block_tokens, &bb);
+  if (rc) return rc;
+  if (((uintptr_t)c->blocks) % 16 || ((uintptr_t)c->table) % 8)
+    return fail(HS_E_INVALID, "%s: blocks must be 16-byte aligned, the table 8-byte", fn);
+  if (c->n_seqs <= 0 || c->table_ld <= 0) return fail(HS_E_INVALID, "%s: non-positive table size", fn);
+  if (layer < 0 || layer >= c->n_layers) return fail(HS_E_INVALID, "%s: layer %d out of range", fn, layer);
+  if (c->bytes / bb < 1) return fail(HS_E_BUFFER, "%s: the buffer holds no block of %llu bytes", fn, (unsigned long long)bb);
+  *out = PagedRef{c->blocks,   (int64_t)(c->bytes / bb), (int64_t)(bb / dtype_bytes(c->dtype)),
+                  c->table,    c->n_seqs,                c->table_ld,
+                  __builtin_ctz(c->block_tokens),        c->n_kv_heads,
+                  layer};
+  return HS_OK;
+}
+
+int hs_paged_append(const hs_paged_cache *cache, int32_t layer, int32_t n, int32_t n_heads, const void *q,
+                    int64_t ld_q, int64_t ld_q_head, void *q_out, int64_t ld_q_out, int64_t ld_q_out_head,
+                    const void *k, const void *v, int64_t ld, int64_t ld_head, const int32_t *seqs,
+                    const int32_t *positions, const hs_rope *rope, const int32_t *angles_at, const void *q_gain,
+                    const void *k_gain, float eps, hs_stream_t stream) {
+  static const char *fn = "hs_paged_append";
+  PagedRows a{};
+  int rc = paged_ref(cache, layer, fn, &a.c);
+  if (rc) return rc;
+  if (n < 0 || n_heads < 0) return fail(HS_E_INVALID, "%s: negative row or head count", fn);
+  if (n_heads > 65536) return fail(HS_E_INVALID, "%s: more than 65536 query heads", fn);
+  if (rope && rope->n_pairs) {
+    if (rope->n_pairs < 0 || rope->n_pairs % 8 || rope->n_pairs > cache->head_dim / 2)
+      return fail(HS_E_INVALID, "%s: %d pairs are no multiple of 8 up to head_dim / 2", fn, rope->n_pairs);
+    if (rope->n_axes < 1 || rope->n_axes > 8) return fail(HS_E_INVALID, "%s: n_axes must be in 1..8", fn);
+    if (!rope->frequencies || ((uintptr_t)rope->frequencies) % 8)
+      return fail(HS_E_INVALID, "%s: frequencies are NULL or not 8-byte aligned", fn);
+    if (!angles_at && rope->n_axes > 1) return fail(HS_E_INVALID, "%s: a rope of several axes needs angles_at", fn);
+  }
+  if (!(eps >= 0.f) || eps > 3e38f) return fail(HS_E_INVALID, "%s: eps must be finite and not negative", fn);
+  if (n == 0) return HS_OK;
+  if (!k || !v || !positions || (n_heads && (!q || !q_out))) return fail(HS_E_INVALID, "%s: NULL argument", fn);
+  if (((uintptr_t)k | (uintptr_t)v) % 16 || (n_heads && ((uintptr_t)q | (uintptr_t)q_out) % 16) ||
+      ((uintptr_t)q_gain | (uintptr_t)k_gain) % 16)
+    return fail(HS_E_INVALID, "%s: rows and gains must be 16-byte aligned", fn);
+  // (a launch takes less than 2^32 threads: 8 or 16 to a head)
+  if ((int64_t)n * (n_heads + 2 * cache->n_kv_heads) >= 1 << 28) return fail(HS_E_INVALID, "%s: too many rows", fn);
+  rc = kvq_strides(fn, cache->dtype, n, ld, ld_head, cache->n_kv_heads, cache->head_dim);
+  if (!rc && n_heads) rc = kvq_strides(fn, cache->dtype, n, ld_q, ld_q_head, n_heads, cache->head_dim);
+  if (!rc && n_heads) rc = kvq_strides(fn, cache->dtype, n, ld_q_out, ld_q_out_head, n_heads, cache->head_dim);
+  if (rc) return rc;
+  if (n_heads && q == q_out && ((n > 1 && ld_q != ld_q_out) || (n_heads > 1 && ld_q_head != ld_q_out_head)))
+    return fail(HS_E_INVALID, "%s: q_out is q, with other strides", fn);
+  a.n = n;
+  a.n_heads = n_heads;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_out = q_out;
+  a.ld_q = n > 1 ? ld_q : 0;
+  a.ld_q_head = n_heads > 1 ? ld_q_head : 0;
+  a.ld_q_out = n > 1 ? ld_q_out : 0;
+  a.ld_q_out_head = n_heads > 1 ? ld_q_out_head : 0;
+  a.ld = n > 1 ? ld : 0;
+  a.ld_head = cache->n_kv_heads > 1 ? ld_head : 0;
+  a.seqs = seqs;
+  a.pos = positions;
+  a.q_gain = q_gain;
+  a.k_gain = k_gain;
+  a.eps = eps;
+  if (rope && rope->n_pairs) {
+    a.freq = rope->frequencies;
+    a.axes = rope->axes;
+    a.angles_at = angles_at ? angles_at : positions;
+    a.pairs = rope->n_pairs;
+    a.n_axes = rope->n_axes;
+    a.adjacent = rope->adjacent != 0;
+  }
+  HIP_TRY(launch_paged_append(cache->dtype, cache->head_dim, a, (hipStream_t)stream));
+  return HS_OK;
+}
+
+int hs_paged_attention_workspace(const hs_paged_cache *cache, int32_t n, int32_t n_heads, int32_t max_len,
+                                 int32_t n_groups, int32_t max_shared, uint64_t *bytes) {
+  static const char *fn = "hs_paged_attention_workspace";
+  if (!cache || !bytes) return fail(HS_E_INVALID, "%s: NULL argument", fn);
+  uint64_t bb;
+  const int rc = hs_paged_block_bytes(cache->dtype, cache->n_layers, cache->n_kv_heads, cache->head_dim,
+                                      cache->block_tokens, &bb);
+  if (rc) return rc;
+  if (n < 0 || max_len <= 0 || max_len > (1 << 30))
+    return fail(HS_E_INVALID, "%s: negative row count, or max_len not in 1..2^30", fn);
+  if (n_groups < 0 || n_groups > n || max_shared < 0 || max_shared > max_len)
+    return fail(HS_E_INVALID, "%s: n_groups is not in 0..n, or max_shared not in 0..max_len", fn);
+  if (n_heads <= 0 || n_heads % cache->n_kv_heads || n_heads / cache->n_kv_heads > 16)
+    return fail(HS_E_INVALID, "%s: n_heads %d is not 1..16 times n_kv_heads %d", fn, n_heads, cache->n_kv_heads);
+  // (a launch takes less than 2^32 threads: 256 to a row, KV head and split)
+  if ((int64_t)n * n_heads >= 1 << 22) return fail(HS_E_INVALID, "%s: too many rows", fn);
+  PagedAttn a{};
+  paged_plan(n, n_heads, cache->n_kv_heads, max_len, n_groups, max_shared, &a);
+  const int slots = a.n_own + a.n_pre;
+  *bytes = slots > 1 ? (uint64_t)n * n_heads * slots * (cache->head_dim + 2) * 4 : 0;
+  return HS_OK;
+}
+
+int hs_paged_attention(const hs_paged_cache *cache, int32_t layer, int32_t n, int32_t n_heads, const void *q,
+                       int64_t ld_q, const int32_t *seqs, const int32_t *lengths, int32_t n_groups,
+                       const int32_t *group_starts, const int32_t *shared, int32_t max_len, int32_t max_shared,
+                       float scale, void *out, int64_t ld_out, void *workspace, uint64_t workspace_bytes,
+                       hs_stream_t stream) {
+  static const char *fn = "hs_paged_attention";
+  PagedAttn a{};
+  int rc = paged_ref(cache, layer, fn, &a.c);
+  if (rc) return rc;
+  uint64_t need;
+  rc = hs_paged_attention_workspace(cache, n, n_heads, max_len, n_groups, max_shared, &need);
+  if (rc || n == 0) return rc;
+  if (!q || !out || !lengths || (n_groups && (!group_starts || !shared)))
+    return fail(HS_E_INVALID, "%s: NULL argument", fn);
+  if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)workspace) % 16)
+    return fail(HS_E_INVALID, "%s: q, out and workspace must be 16-byte aligned", fn);
+  rc = kvq_strides(fn, cache->dtype, n, ld_q, cache->head_dim, n_heads, cache->head_dim);
+  if (!rc) rc = kvq_strides(fn, cache->dtype, n, ld_out, cache->head_dim, n_heads, cache->head_dim);
+  if (rc) return rc;
+  if (need && (!workspace || workspace_bytes < need))
+    return fail(HS_E_BUFFER, "%s: the workspace holds %llu bytes, %llu are needed", fn,
+                (unsigned long long)(workspace ? workspace_bytes : 0), (unsigned long long)need);
+  a.q = q;
+  a.ld_q = n > 1 ? ld_q : 0;
+  a.n = n;
+  a.n_heads = n_heads;
+  a.seqs = seqs;
+  a.lens = lengths;
+  a.starts = group_starts;
+  a.shared = shared;
+  a.max_len = max_len;
+  a.max_shared = max_shared;
+  a.scale = scale;
+  a.out = out;
+  a.ld_out = n > 1 ? ld_out : 0;
+  paged_plan(n, n_heads, cache->n_kv_heads, max_len, n_groups, max_shared, &a);
+  if (!a.n_pre) a.n_groups = 0;
+  a.part_o = (float *)workspace;
+  a.part_ml = a.part_o + (int64_t)n * n_heads * (a.n_own + a.n_pre) * cache->head_dim;
+  HIP_TRY(launch_paged_attention(cache->dtype, cache->head_dim, a, (hipStream_t)stream));
+  return HS_OK;
+}
+
+// ---- tokens drawn ----
+
+int hs_sample_tokens_workspace(int64_t rows, int32_t vocab, uint64_t *bytes) {
+  static const char *fn = "hs_sample_tokens_workspace";
+  if (!bytes) return fail(HS_E_INVALID, "%s: bytes is NULL", fn);
+  if (rows < 0 || rows > INT32_MAX || vocab <= 0 || vocab > (1 << 30)) return fail(HS_E_INVALID, "%s: rows or vocab out of range", fn);
+  // (a launch takes less than 2^32 threads)
+  if (rows * logprob_parts(vocab) >= 1 << 22) return fail(HS_E_INVALID, "%s: too many rows", fn);
+  *bytes = sample_workspace(rows, vocab);
+  return HS_OK;
+}
+
+int hs_sample_tokens(int32_t dtype, const void *logits, int64_t rows, int32_t vocab, int64_t ld, const float *u,
+                     const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                     int32_t *tokens, float *logprob, void *workspace, uint64_t workspace_bytes, hs_stream_t stream) {
+  static const char *fn = "hs_sample_tokens";
+  uint64_t need;
+  const int rc = hs_sample_tokens_workspace(rows, vocab, &need);
+  if (rc) return rc;
+  if (dtype < HS_F32 || dtype > HS_BF16) return fail(HS_E_INVALID, "%s: unknown dtype", fn);
+  if (rows == 0) return HS_OK;
+  if (!logits || !u || !tokens) return fail(HS_E_INVALID, "%s: NULL argument", fn);
+  if (((uintptr_t)logits) % dtype_bytes(dtype)) return fail(HS_E_INVALID, "%s: logits are not aligned to their type", fn);
+  if (rows > 1 && (ld < vocab || ld > std::min<int64_t>(1ll << 40, (1ll << 58) / rows))) return fail(HS_E_INVALID, "%s: rows overlap, or ld out of range", fn);
+  if (need && (!workspace || workspace_bytes < need))
+    return fail(HS_E_BUFFER, "%s: the workspace holds %llu bytes, %llu are needed", fn,
+                (unsigned long long)(workspace ? workspace_bytes : 0), (unsigned long long)need);
+  if (((uintptr_t)workspace) % 16) return fail(HS_E_INVALID, "%s: workspace must be 16-byte aligned", fn);
+  SampleArgs a{};
+  a.logits = logits;
+  a.rows = rows;
+  a.ld = rows > 1 ? ld : 0;
+  a.vocab = vocab;
+  a.u = u;
+  a.temperature = temperature;
+  a.top_k = top_k;
+  a.top_p = top_p;
+  a.min_p = min_p;
+  a.tokens = tokens;
+  a.logprob = logprob;
+  a.ws = workspace;
+  HIP_TRY(launch_sample(dtype, a, (hipStream_t)stream));
   return HS_OK;
 }
 

@@ -398,6 +398,72 @@ inline int logprob_parts(int vocab) { return (int)(((int64_t)vocab + LOGPROB_PAR
 uint64_t logprob_workspace(int64_t rows, int vocab, int top);
 hipError_t launch_logprobs(int dtype, const LogprobArgs &a, hipStream_t st);
 
+// ---- a paged cache in the model's type (layout: hs_paged_cache in hs.h) ----
+struct PagedRef {
+  void *blocks;
+  int64_t n_blocks, block_elems;
+  const int64_t *table;  // [n_seqs][table_ld] block numbers
+  int n_seqs, table_ld;
+  int bt_log2;           // log2 of the positions of a block
+  int n_kv, layer;
+};
+// new rows: element (row, head, e) of q at q + row * ld_q + head * ld_q_head + e, of
+// k and v alike; row r goes to position pos[r] of sequence seqs[r] (NULL: r)
+struct PagedRows {
+  PagedRef c;
+  int n, n_heads;        // n_heads 0: no queries
+  const void *q, *k, *v;
+  void *q_out;
+  int64_t ld_q, ld_q_head, ld_q_out, ld_q_out_head, ld, ld_head;
+  const int *seqs, *pos;
+  const void *q_gain, *k_gain;
+  float eps;
+  const double *freq;    // [pairs]
+  const int *axes;       // [pairs], NULL: axis 0
+  const int *angles_at;  // [n_axes][n]
+  int pairs, n_axes, adjacent;
+};
+// Row r of q attends over the first lens[r] positions of sequence seqs[r] (NULL:
+// r); rows starts[g] .. starts[g + 1] - 1 share the first shared[g] of them.
+struct PagedAttn {
+  PagedRef c;
+  const void *q;
+  int64_t ld_q;
+  int n, n_heads;
+  const int *seqs, *lens, *starts, *shared;
+  int n_groups, max_len, max_shared;
+  float scale;
+  void *out;
+  int64_t ld_out;
+  // the plan (paged_plan): columns of a tile, tiles at most, splits of the
+  // shared (0: none are) and of the own positions
+  int tile;
+  int64_t pre_units;
+  int n_pre, n_own;
+  float *part_o;   // [n][n_heads][n_own + n_pre][head_dim]
+  float *part_ml;  // [n][n_heads][n_own + n_pre][2]: base-2 maximum (-inf: no position), sum
+};
+constexpr int PAGED_MAX_SPLITS = 64;
+void paged_plan(int64_t n, int n_heads, int n_kv, int max_len, int n_groups, int max_shared, PagedAttn *a);
+hipError_t launch_paged_append(int dtype, int head_dim, const PagedRows &a, hipStream_t st);
+hipError_t launch_paged_attention(int dtype, int head_dim, const PagedAttn &a, hipStream_t st);
+
+// tokens drawn from rows of logits (hs_sample_tokens); u, temperature, top_k,
+// top_p, min_p and tokens are indexed by act[row] (act NULL: row), logprob by row
+struct SampleArgs {
+  const void *logits;
+  int64_t rows, ld;
+  int vocab;
+  const float *u, *temperature, *top_p, *min_p;
+  const int *top_k, *act;
+  int *tokens;
+  float *logprob;
+  void *ws;  // sample_workspace bytes, its counters zero between calls
+};
+constexpr int SAMPLE_COUNTERS = 512;
+uint64_t sample_workspace(int64_t rows, int vocab);
+hipError_t launch_sample(int dtype, const SampleArgs &a, hipStream_t st);
+
 // records the thread's error message (hs_last_error) and returns code
 int fail(int code, const char *fmt, ...);
 
@@ -423,6 +489,7 @@ struct hs_model {
   hs::PackedRows *pk_dev = nullptr;  // the rows of the current prefill pass
   hs::PrefillGroup *pk_order = nullptr;  // [prefill_groups_max(max_rows)] its attention groups, longest first
   void *lp_ws = nullptr;    // logprob_workspace(max_batch, V, LOGPROB_TOP)
+  void *sm_ws = nullptr;    // sample_workspace(max_batch, V)
   float *logits = nullptr;  // [max_batch][V] (used when the caller passes no logits buffer)
   float *part_o = nullptr;
   float *part_ml = nullptr;

@@ -1,0 +1,618 @@
+// hs_paged.hip — a paged KV cache in the model's own type (gfx950): new rows
+// normalised, turned and stored, and attention over it where rows of a group
+// share their first positions.
+#include "hs_device.h"
+
+#include <algorithm>
+#include <cfloat>
+
+namespace hs {
+namespace {
+
+using namespace dev;
+
+// element offset of layer a.layer's K (sel 0) or V (1) of head j in a block
+__device__ __forceinline__ int64_t paged_slab(const PagedRef &c, int64_t block, int sel, int j, int hd) {
+  return block * c.block_elems + ((((int64_t)c.layer * 2 + sel) * c.n_kv + j) << c.bt_log2) * hd;
+}
+// The block of (sequence, position), or -1: outside the table, without a
+// block, or a number that is no block of the cache.
+__device__ __forceinline__ int64_t paged_block(const PagedRef &c, int seq, int pos) {
+  const int k = pos >> c.bt_log2;
+  if ((uint32_t)seq >= (uint32_t)c.n_seqs || pos < 0 || k >= c.table_ld) return -1;
+  const int64_t b = c.table[(int64_t)seq * c.table_ld + k];
+  return (uint64_t)b < (uint64_t)c.n_blocks ? b : -1;
+}
+
+// ---------------------------------------------------------------------------
+// rows stored
+// ---------------------------------------------------------------------------
+constexpr int APPEND_THREADS = 256;
+constexpr int APPEND_ROWS = 4;  // most rows of a work group
+
+// cos and sin of the angle at * freq.  The product and the whole turns taken off
+// it are in 64 bits (an angle of 2^30 keeps 2^-23 of a radian); what is left, half a
+// turn at most, goes through fp32.
+__device__ __forceinline__ void turn(int at, double freq, float &c, float &s) {
+  const double t = (double)at * freq * 0.15915494309189535;  // turns
+  const float r = 2.f * (float)(t - rint(t));                // half turns
+  sincospif(r, &s, &c);
+}
+
+// New rows of a layer.  x of query and key heads becomes x / sqrt(mean x^2 + eps) * gain
+// (with a gain), then pair i of its first 2 pairs channels, (i, i + pairs) or
+// (2 i, 2 i + 1), is turned by angles_at[axis[i]][row] * freq[i]: all in fp32, rounded
+// once.  Keys and values go to the row's place in the cache, queries to q_out.
+//
+// The work is a copy.  A work group takes some rows (or a part of one row's
+// heads), computes the rows' cosines and sines once for all heads (64 bits, into
+// LDS) and gives each head to HD / 8 lanes, 8 channels a lane; a half-apart pair's
+// other channel comes from the lane that holds it.  All loads of a lane are asked
+// for before the first is used.
+template <int DT, int HD>
+__global__ __launch_bounds__(APPEND_THREADS) void k_paged_append(PagedRows a, int rows_wg, int heads_wg) {
+  constexpr int B = DT == HS_F32 ? 4 : 2, L = HD / 8, GROUPS = APPEND_THREADS / L;
+  constexpr int W = DT == HS_F32 ? 8 : 4;  // words of a lane's 8 channels
+  __shared__ float2 cs[APPEND_ROWS][HD / 2];
+  const int parts = (a.n_heads + 2 * a.c.n_kv + heads_wg - 1) / heads_wg;
+  const int row0 = blockIdx.x / parts * rows_wg, h0 = blockIdx.x % parts * heads_wg;
+  const int rows = min(rows_wg, a.n - row0), heads = min(heads_wg, a.n_heads + 2 * a.c.n_kv - h0);
+  const int items = rows * heads;
+  const int lane = threadIdx.x % L, e0 = lane * 8;
+  for (int i = threadIdx.x; i < rows * a.pairs; i += APPEND_THREADS) {
+    const int r = i / a.pairs, p = i - r * a.pairs;
+    const int axis = a.axes ? min(max(a.axes[p], 0), a.n_axes - 1) : 0;
+    float c, s;
+    turn(a.angles_at[(int64_t)axis * a.n + row0 + r], a.freq[p], c, s);
+    cs[r][p] = float2{c, s};
+  }
+  __syncthreads();
+  for (int it = threadIdx.x / L; it < items; it += GROUPS) {
+    const int r = it / heads, h = h0 + it - r * heads;
+    const int64_t row = row0 + r;
+    const bool is_q = h < a.n_heads, is_k = !is_q && h < a.n_heads + a.c.n_kv;
+    const int j = is_q ? h : is_k ? h - a.n_heads : h - a.n_heads - a.c.n_kv;
+    const char *src = (const char *)(is_q ? a.q : is_k ? a.k : a.v) +
+                      (is_q ? row * a.ld_q + j * a.ld_q_head : row * a.ld + j * a.ld_head) * B + e0 * B;
+    uint32_t w[W];
+#pragma unroll
+    for (int u = 0; u < W; u += 4) {
+      const u32x4 t = ld16(src + u * 4);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) w[u + x] = t[x];
+    }
+    char *dst;
+    if (is_q) {
+      dst = (char *)a.q_out + (row * a.ld_q_out + j * a.ld_q_out_head) * B;
+    } else {
+      const int pos = a.pos[row];
+      const int64_t b = paged_block(a.c, a.seqs ? a.seqs[row] : (int)row, pos);
+      dst = b < 0 ? nullptr
+                  : (char *)a.c.blocks + (paged_slab(a.c, b, is_k ? 0 : 1, j, HD) +
+                                          (int64_t)(pos & ((1 << a.c.bt_log2) - 1)) * HD) * B;
+    }
+    if (is_q || is_k) {
+      float f[8], g[8];
+      auto widen = [&](const uint32_t(&v)[W], float *o) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if constexpr (DT == HS_F32) o[e] = __uint_as_float(v[e]);
+          else o[e] = e & 1 ? hi_f32<DT>(v[e / 2]) : lo_f32<DT>(v[e / 2]);
+        }
+      };
+      widen(w, f);
+      const void *gain = is_q ? a.q_gain : a.k_gain;
+      float rs = 1.f;
+      if (gain) {
+        float ss = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(f[e], f[e], ss);
+        ss = group_sum<L>(ss);
+        rs = 1.f / sqrtf(ss * (1.f / HD) + a.eps);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] *= rs * ld_elem<DT>(gain, e0 + e);
+      }
+      if (a.adjacent) {
+#pragma unroll
+        for (int e = 0; e < 8; e += 2)
+          if (e0 + e < 2 * a.pairs) {
+            const float2 t = cs[r][(e0 + e) / 2];
+            const float x = f[e], y = f[e + 1];
+            f[e] = x * t.x - y * t.y;
+            f[e + 1] = x * t.y + y * t.x;
+          }
+      } else if (a.pairs) {
+        // the partner's channels, 8 of them in one lane as pairs is a multiple of 8
+        const bool first = e0 < a.pairs, in = e0 < 2 * a.pairs;
+        const int d = a.pairs / 8, other = in ? (first ? lane + d : lane - d) : lane;
+        const int from = (int)(threadIdx.x & 63) - lane + other;
+        uint32_t v[W];
+#pragma unroll
+        for (int u = 0; u < W; ++u) v[u] = (uint32_t)__shfl((int)w[u], from);
+        widen(v, g);
+        if (in) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            if (gain) g[e] *= rs * ld_elem<DT>(gain, other * 8 + e);
+            const float2 t = cs[r][(first ? e0 : e0 - a.pairs) + e];
+            f[e] = first ? f[e] * t.x - g[e] * t.y : g[e] * t.y + f[e] * t.x;
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < W; ++u) {
+        if constexpr (DT == HS_F32) w[u] = __float_as_uint(f[u]);
+        else w[u] = pack2<DT>(f[2 * u], f[2 * u + 1]);
+      }
+    }
+    if (dst) {
+#pragma unroll
+      for (int u = 0; u < W; u += 4) *(u32x4 *)(dst + e0 * B + u * 4) = u32x4{w[u], w[u + 1], w[u + 2], w[u + 3]};
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// attention
+// ---------------------------------------------------------------------------
+constexpr int PG_WAVES = 4;
+constexpr int PG_STRIPE = PG_WAVES * 32;  // positions that a work group takes at a time
+
+// the group of a row: starts[g] <= row < starts[g + 1] (-1: none), by every lane of the wave
+__device__ __forceinline__ int paged_group(const PagedAttn &a, int row) {
+  int n = 0;
+  for (int b = 0; b <= a.n_groups; b += 64) {
+    const int i = b + (int)(threadIdx.x & 63);
+    n += (int)__popcll(__ballot(i <= a.n_groups && a.starts[min(i, a.n_groups)] <= row));
+  }
+  return n >= 1 && n <= a.n_groups ? n - 1 : -1;
+}
+__device__ __forceinline__ int paged_most(const PagedRef &c) {
+  return (int)min((int64_t)c.table_ld << c.bt_log2, (int64_t)INT32_MAX);
+}
+__device__ __forceinline__ int paged_shared(const PagedAttn &a, int g) {
+  return max(0, min(min(a.shared[g], a.max_shared), paged_most(a.c)));
+}
+__device__ __forceinline__ int paged_seq(const PagedAttn &a, int row) { return a.seqs ? a.seqs[row] : row; }
+__device__ __forceinline__ int paged_length(const PagedAttn &a, int row, int seq) {
+  if ((uint32_t)seq >= (uint32_t)a.c.n_seqs) return 0;
+  return max(0, min(min(a.lens[row], a.max_len), paged_most(a.c)));
+}
+// What a row attends over: positions [lo, hi) of its own (or of its group's
+// first sequence, where it is shorter than what the group shares), and whether
+// the shared ones before them come from the group.
+struct PagedRow {
+  int seq, lo, hi;
+  bool grouped;
+};
+__device__ __forceinline__ PagedRow paged_row(const PagedAttn &a, int row) {
+  PagedRow r;
+  r.seq = paged_seq(a, row);
+  r.lo = 0;
+  r.hi = paged_length(a, row, r.seq);
+  r.grouped = false;
+  const int g = a.n_groups ? paged_group(a, row) : -1;
+  if (g >= 0) {
+    const int sh = paged_shared(a, g);
+    if (sh > 0 && r.hi >= sh) {
+      r.lo = sh;
+      r.grouped = true;
+    } else if (sh > 0) {
+      r.seq = paged_seq(a, min(max(a.starts[g], 0), a.n - 1));
+    }
+  }
+  return r;
+}
+
+// a row's partials: [row][head][slot], slots 0 .. n_own - 1 of its own
+// positions, then n_pre of the shared ones
+__device__ __forceinline__ int64_t paged_slot(const PagedAttn &a, int64_t row, int head, int slot) {
+  return (row * a.n_heads + head) * (a.n_own + a.n_pre) + slot;
+}
+
+// Attention of up to 16 CT query columns (a column is a head of a row) over a
+// range of positions of one KV head: a row's own positions (PRE false: the
+// columns are the heads of one row, CT 1), or the positions that a group of rows
+// shares.  One work group takes a split of the range, each wave stripes of 32
+// positions on its own, straight from memory into registers.
+//
+// Scores are S^T = K Q^T, 16 positions x 16 columns: lane (g, c) then holds those
+// of positions 4 g .. 4 g + 3 for column c, which is how the second product, O^T +=
+// V^T P^T, takes them.  Its k slots of lane group g are positions 4 g .. 4 g + 3 of
+// both tiles of a stripe; its rows are channels: a lane loads VE = HD / 16
+// consecutive channels of those positions, and row m of tile dt is channel VE m +
+// dt.  P enters as two parts of the type, hi + lo: 22 bits of it in f16, 16 in bf16,
+// whose rounding (2^-17) is 1/256 of the output's.  fp32 runs on the fp32 products.
+//
+// Loads go through buffer descriptors made for a tile of 16 positions, which
+// end where the positions do: what lies past them reads as zeros.
+template <int DT, int HD, int CT, bool PRE>
+__global__ __launch_bounds__(64 * PG_WAVES) void k_paged_attn(PagedAttn a) {
+  constexpr int B = DT == HS_F32 ? 4 : 2;
+  constexpr int KCH = HD * B / 64;  // 16-byte chunks of a K row's quarter
+  constexpr int VE = HD / 16, VW = VE * B / 4;  // channels of a lane, and their words
+  constexpr int PITCH = HD + 4;
+  __shared__ __align__(16) float s_o[PG_WAVES][16][PITCH];
+  __shared__ float s_m[PG_WAVES][16], s_l[PG_WAVES][16];
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = a.n_heads / a.c.n_kv;
+  const int ns = PRE ? a.n_pre : a.n_own;
+  const int j = blockIdx.x % a.c.n_kv, split = blockIdx.x / a.c.n_kv % ns, unit = blockIdx.x / a.c.n_kv / ns;
+  int row0 = unit, rows = 1, seq, lo = 0, hi;
+  if constexpr (PRE) {
+    // the unit-th tile of columns, counted group by group
+    const int per = 16 * CT / G;
+    int left = unit, grp = -1, first = 0;
+    for (int b = 0; b < a.n_groups && grp < 0; b += 64) {
+      const int i = b + lane;
+      int s = 0, e = 0;
+      if (i < a.n_groups) {
+        s = min(max(a.starts[i], 0), a.n);
+        e = min(max(a.starts[i + 1], s), a.n);
+      }
+      int sum = (e - s + per - 1) / per;
+      const int mine = sum;
+      for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(sum, o);
+        if (lane >= o) sum += v;
+      }
+      const uint64_t in = __ballot(left < sum);
+      if (in) {
+        const int at = (int)__builtin_ctzll(in);
+        left -= __shfl(sum, at) - __shfl(mine, at);
+        first = __shfl(s, at);
+        rows = __shfl(e, at) - first;
+        grp = b + at;
+      } else {
+        left -= __shfl(sum, 63);
+      }
+    }
+    if (grp < 0) return;
+    grp = __builtin_amdgcn_readfirstlane(grp);
+    first = __builtin_amdgcn_readfirstlane(first);
+    left = __builtin_amdgcn_readfirstlane(left);
+    row0 = first + left * per;
+    rows = min(__builtin_amdgcn_readfirstlane(rows) - left * per, per);
+    seq = paged_seq(a, first);
+    hi = paged_shared(a, grp);
+  } else {
+    const PagedRow r = paged_row(a, unit);
+    seq = __builtin_amdgcn_readfirstlane(r.seq);
+    lo = __builtin_amdgcn_readfirstlane(r.lo);
+    hi = __builtin_amdgcn_readfirstlane(r.hi);
+  }
+  seq = __builtin_amdgcn_readfirstlane(seq);
+  const int cols = rows * G;
+  // this split's stripes, of whole ones from the tile of the first position on
+  const int base = lo & ~15;
+  const int per = max(0, (int)((((int64_t)hi - base + ns - 1) / ns + PG_STRIPE - 1) / PG_STRIPE * PG_STRIPE));
+  const int s0 = (int)min((int64_t)hi, base + (int64_t)split * per), s1 = (int)min((int64_t)hi, (int64_t)s0 + per);
+
+  u32x4 q[CT][KCH];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const int cc = ct * 16 + c;
+    const int r = cc / G, h = j * G + cc - r * G;
+    const char *src = (const char *)a.q + (((int64_t)row0 + r) * a.ld_q + (int64_t)h * HD) * B + g * 16;
+#pragma unroll
+    for (int k = 0; k < KCH; ++k) q[ct][k] = cc < cols ? ld16(src + k * 64) : u32x4{0u, 0u, 0u, 0u};
+  }
+
+  struct Buf {
+    u32x4 k[2][KCH];
+    uint32_t v[2][4][VW];
+    bool any[2];
+  };
+  const bool known = (uint32_t)seq < (uint32_t)a.c.n_seqs;
+  const int64_t *trow = a.c.table + (known ? (int64_t)seq * a.c.table_ld : 0);
+  const int in_block = (1 << a.c.bt_log2) - 1;
+  auto load = [&](Buf &b, int pos) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int p0 = pos + 16 * u, at = p0 >> a.c.bt_log2;
+      const bool ask = known && p0 < s1 && at < a.c.table_ld;
+      const int64_t num = ask ? trow[at] : -1;
+      b.any[u] = (uint64_t)num < (uint64_t)a.c.n_blocks;
+      const int64_t blk = b.any[u] ? num : 0;
+      const uint32_t bytes = b.any[u] ? (uint32_t)min(16, s1 - p0) * (HD * B) : 0u;
+      const int64_t inner = (int64_t)(p0 & in_block) * HD;
+      const rsrc_t kr = make_rsrc((const char *)a.c.blocks + (paged_slab(a.c, blk, 0, j, HD) + inner) * B, bytes);
+      const rsrc_t vr = make_rsrc((const char *)a.c.blocks + (paged_slab(a.c, blk, 1, j, HD) + inner) * B, bytes);
+      const int skip = PRE ? 0 : lo - p0;  // rows before the first position
+      const uint32_t ko = !PRE && c < skip ? BUF_OOB : (uint32_t)(c * HD * B + g * 16);
+#pragma unroll
+      for (int k = 0; k < KCH; ++k) b.k[u][k] = PRE ? bld16(kr, ko + k * 64) : bld16_stream(kr, ko + k * 64);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t vo = !PRE && 4 * g + i < skip ? BUF_OOB : (uint32_t)((4 * g + i) * HD * B + c * VE * B);
+        if constexpr (VW == 2) {
+          const u32x2 t = bld8(vr, vo);
+          b.v[u][i][0] = t[0];
+          b.v[u][i][1] = t[1];
+        } else {
+#pragma unroll
+          for (int x = 0; x < VW; x += 4) {
+            const u32x4 t = PRE ? bld16(vr, vo + x * 4) : bld16_stream(vr, vo + x * 4);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) b.v[u][i][x + y] = t[y];
+          }
+        }
+      }
+    }
+  };
+
+  const float c2 = a.scale * 1.4426950408889634f;
+  float m[CT], l[CT];
+  f32x4 o[CT][VE];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    m[ct] = -INFINITY;
+    l[ct] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < VE; ++dt) o[ct][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  auto step = [&](const Buf &b, int pos) {
+    f32x4 s[CT][2];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        s[ct][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < KCH; ++k) s[ct][u] = mma<DT>(b.k[u][k], q[ct][k], s[ct][u]);
+        s[ct][u] *= c2;
+      }
+    if (!b.any[0] || !b.any[1] || pos < lo || pos + 32 > s1) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int p = pos + 16 * u + 4 * g + i;
+          if (!b.any[u] || p < lo || p >= s1) {
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) s[ct][u][i] = -INFINITY;
+          }
+        }
+    }
+    uint32_t ph[CT][4], pl[CT][4];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[ct][u][i]);
+      // m, the same for the four lanes of a column, is raised only where a score
+      // passes it by more than 2^8: o / l does not depend on it
+      if (__ballot(top > m[ct] + 8.f)) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float mn = fmaxf(m[ct], top);
+        const float corr = m[ct] == mn ? 1.f : __builtin_amdgcn_exp2f(m[ct] - mn);
+        l[ct] *= corr;
+#pragma unroll
+        for (int dt = 0; dt < VE; ++dt) o[ct][dt] *= corr;
+        m[ct] = mn;
+      }
+      const float ref = m[ct] == -INFINITY ? 0.f : m[ct];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[ct][u][i] = __builtin_amdgcn_exp2f(s[ct][u][i] - ref);
+          l[ct] += s[ct][u][i];
+        }
+      if constexpr (DT != HS_F32) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const float p0 = s[ct][x >> 1][2 * (x & 1)], p1 = s[ct][x >> 1][2 * (x & 1) + 1];
+          ph[ct][x] = pack2<DT>(p0, p1);
+          pl[ct][x] = pack2<DT>(p0 - lo_f32<DT>(ph[ct][x]), p1 - hi_f32<DT>(ph[ct][x]));
+        }
+      }
+    }
+    if constexpr (DT == HS_F32) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int dt = 0; dt < VE; ++dt)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+              o[ct][dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b.v[u][i][dt]), s[ct][u][i], o[ct][dt],
+                                                               0, 0, 0);
+    } else {
+#pragma unroll
+      for (int dt = 0; dt < VE; ++dt) {
+        u32x4 av;
+        const uint32_t sel = dt & 1 ? 0x07060302u : 0x05040100u;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          av[2 * u] = __builtin_amdgcn_perm(b.v[u][1][dt / 2], b.v[u][0][dt / 2], sel);
+          av[2 * u + 1] = __builtin_amdgcn_perm(b.v[u][3][dt / 2], b.v[u][2][dt / 2], sel);
+        }
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          o[ct][dt] = mma<DT>(av, u32x4{ph[ct][0], ph[ct][1], ph[ct][2], ph[ct][3]}, o[ct][dt]);
+          o[ct][dt] = mma<DT>(av, u32x4{pl[ct][0], pl[ct][1], pl[ct][2], pl[ct][3]}, o[ct][dt]);
+        }
+      }
+    }
+  };
+  Buf b0, b1;
+  int pos = s0 + wave * 32;
+  load(b0, pos);
+  for (; pos < s1; pos += 2 * PG_STRIPE) {
+    load(b1, pos + PG_STRIPE);
+    step(b0, pos);
+    if (pos + PG_STRIPE >= s1) break;
+    load(b0, pos + 2 * PG_STRIPE);
+    step(b1, pos + PG_STRIPE);
+  }
+
+  // the waves' results, 16 columns at a time
+  const bool whole = a.n_own + a.n_pre == 1;
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    if (ct * 16 >= cols) break;
+    if (ct) __syncthreads();
+    l[ct] += __shfl_xor(l[ct], 16);
+    l[ct] += __shfl_xor(l[ct], 32);
+    if (g == 0) {
+      s_m[wave][c] = m[ct];
+      s_l[wave][c] = l[ct];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int dt = 0; dt < VE; dt += 4)
+        *(f32x4 *)&s_o[wave][c][VE * (4 * g + i) + dt] =
+            f32x4{o[ct][dt][i], o[ct][dt + 1][i], o[ct][dt + 2][i], o[ct][dt + 3][i]};
+    __syncthreads();
+    for (int x = tid; x < 16 * HD / 4; x += 64 * PG_WAVES) {
+      const int cc = x / (HD / 4), e = x % (HD / 4) * 4;
+      if (ct * 16 + cc >= cols) continue;
+      float M = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < PG_WAVES; ++w) M = fmaxf(M, s_m[w][cc]);
+      float den = 0.f;
+      f32x4 num = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < PG_WAVES; ++w) {
+        // (a wave that saw no score keeps -inf and zeros; one that saw NaN alone has NaN sums)
+        const float k = s_m[w][cc] == M ? 1.f : __builtin_amdgcn_exp2f(s_m[w][cc] - M);
+        den += k * s_l[w][cc];
+        num += k * *(const f32x4 *)&s_o[w][cc][e];
+      }
+      const int r = (ct * 16 + cc) / G, h = j * G + ct * 16 + cc - r * G;
+      const int64_t row = row0 + r;
+      if (whole) {
+        float f[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = den == 0.f ? 0.f : num[i] / den;
+        const int64_t at = row * a.ld_out + (int64_t)h * HD + e;
+        st_elem2<DT>(a.out, at, f[0], f[1]);
+        st_elem2<DT>(a.out, at + 2, f[2], f[3]);
+      } else {
+        const int64_t at = paged_slot(a, row, h, PRE ? a.n_own + split : split);
+        *(f32x4 *)(a.part_o + at * HD + e) = num;
+        if (e == 0) {
+          a.part_ml[at * 2] = M;
+          a.part_ml[at * 2 + 1] = den;
+        }
+      }
+    }
+  }
+}
+
+// A row's partials joined, in the order of their slots.
+template <int DT, int HD>
+__global__ __launch_bounds__(256) void k_paged_join(PagedAttn a) {
+  const int row = blockIdx.x;
+  const int slots = paged_row(a, row).grouped ? a.n_own + a.n_pre : a.n_own;
+  for (int x = threadIdx.x; x < a.n_heads * (HD / 4); x += 256) {
+    const int h = x / (HD / 4), e = x % (HD / 4) * 4;
+    const int64_t at = paged_slot(a, row, h, 0);
+    float M = -INFINITY;
+    for (int s = 0; s < slots; ++s) M = fmaxf(M, a.part_ml[(at + s) * 2]);
+    float den = 0.f;
+    f32x4 num = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < slots; ++s) {
+      const float ms = a.part_ml[(at + s) * 2];
+      const float k = ms == M ? 1.f : __builtin_amdgcn_exp2f(ms - M);
+      den += k * a.part_ml[(at + s) * 2 + 1];
+      num += k * *(const f32x4 *)(a.part_o + (at + s) * HD + e);
+    }
+    float f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = den == 0.f ? 0.f : num[i] / den;
+    const int64_t to = (int64_t)row * a.ld_out + (int64_t)h * HD + e;
+    st_elem2<DT>(a.out, to, f[0], f[1]);
+    st_elem2<DT>(a.out, to + 2, f[2], f[3]);
+  }
+}
+
+template <int DT, int HD>
+hipError_t attn_launch(const PagedAttn &a, hipStream_t st) {
+  const dim3 block(64 * PG_WAVES);
+  if (a.n_pre) {
+    const dim3 grid((uint32_t)(a.pre_units * a.n_pre * a.c.n_kv));
+    if (a.tile == 16) HS_LAUNCH((k_paged_attn<DT, HD, 1, true>), grid, block, 0, st, a);
+    else if (a.tile == 32) HS_LAUNCH((k_paged_attn<DT, HD, 2, true>), grid, block, 0, st, a);
+    else HS_LAUNCH((k_paged_attn<DT, HD, 4, true>), grid, block, 0, st, a);
+  }
+  HS_LAUNCH((k_paged_attn<DT, HD, 1, false>), dim3((uint32_t)((int64_t)a.n * a.n_own * a.c.n_kv)), block, 0, st, a);
+  if (a.n_own + a.n_pre > 1) HS_LAUNCH((k_paged_join<DT, HD>), dim3(a.n), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+template <int DT, int HD>
+hipError_t append_launch(const PagedRows &a, hipStream_t st) {
+  const int heads = a.n_heads + 2 * a.c.n_kv, at_once = APPEND_THREADS / (HD / 8);
+  // one row's heads over several work groups while those are few, then several rows a work group
+  const int64_t spread = (int64_t)a.n * ((heads + at_once - 1) / at_once);
+  const int heads_wg = spread <= 1024 ? std::min(heads, at_once) : heads;
+  const int rows_wg = spread <= 1024 ? 1 : APPEND_ROWS;
+  const int parts = (heads + heads_wg - 1) / heads_wg;
+  const int64_t groups = ((int64_t)a.n + rows_wg - 1) / rows_wg * parts;
+  HS_LAUNCH((k_paged_append<DT, HD>), dim3((uint32_t)groups), dim3(APPEND_THREADS), 0, st, a, rows_wg, heads_wg);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// columns of a tile, splits of the shared and of the own positions
+void paged_plan(int64_t n, int n_heads, int n_kv, int max_len, int n_groups, int max_shared, PagedAttn *a) {
+  const int G = n_heads / n_kv;
+  a->n_groups = n_groups;
+  a->n_pre = a->n_own = 1;
+  const int64_t target = 512;  // work groups: two to a CU
+  auto splits = [&](int64_t groups, int64_t positions) {
+    int64_t s = std::max<int64_t>(1, target / std::max<int64_t>(groups, 1));
+    s = std::min(s, (positions + 2 * PG_STRIPE - 1) / (2 * PG_STRIPE));
+    return (int)std::min<int64_t>(std::max<int64_t>(s, 1), PAGED_MAX_SPLITS);
+  };
+  if (n_groups && max_shared > 0) {
+    const int64_t mean = (n + n_groups - 1) / n_groups * G;
+    a->tile = mean <= 16 ? 16 : mean <= 32 ? 32 : 64;
+    const int per = a->tile / G;
+    a->pre_units = std::min<int64_t>(n, n / per + n_groups);
+    a->n_pre = splits(a->pre_units * n_kv, max_shared);
+    a->n_own = splits(n * n_kv, std::max(1, max_len - max_shared));
+  } else {
+    a->tile = 16;
+    a->pre_units = 0;
+    a->n_pre = 0;
+    a->n_own = splits(n * n_kv, max_len);
+  }
+}
+
+hipError_t launch_paged_attention(int dtype, int head_dim, const PagedAttn &a, hipStream_t st) {
+  if (head_dim == 64) {
+    if (dtype == HS_F32) return attn_launch<HS_F32, 64>(a, st);
+    if (dtype == HS_F16) return attn_launch<HS_F16, 64>(a, st);
+    if (dtype == HS_BF16) return attn_launch<HS_BF16, 64>(a, st);
+  } else if (head_dim == 128) {
+    if (dtype == HS_F32) return attn_launch<HS_F32, 128>(a, st);
+    if (dtype == HS_F16) return attn_launch<HS_F16, 128>(a, st);
+    if (dtype == HS_BF16) return attn_launch<HS_BF16, 128>(a, st);
+  }
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_paged_append(int dtype, int head_dim, const PagedRows &a, hipStream_t st) {
+  if (head_dim == 64) {
+    if (dtype == HS_F32) return append_launch<HS_F32, 64>(a, st);
+    if (dtype == HS_F16) return append_launch<HS_F16, 64>(a, st);
+    if (dtype == HS_BF16) return append_launch<HS_BF16, 64>(a, st);
+  } else if (head_dim == 128) {
+    if (dtype == HS_F32) return append_launch<HS_F32, 128>(a, st);
+    if (dtype == HS_F16) return append_launch<HS_F16, 128>(a, st);
+    if (dtype == HS_BF16) return append_launch<HS_BF16, 128>(a, st);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace hs

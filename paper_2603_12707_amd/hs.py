@@ -27,7 +27,9 @@ EXPORTS = ("hs_last_error", "hs_kv_bytes", "hs_model_create", "hs_model_free", "
            "hs_kv_pool_blocks", "hs_handoff_create", "hs_handoff_free", "hs_handoff_push", "hs_handoff_pop",
            "hs_handoff_pending", "hs_stream_read", "hs_decode_step_static", "hs_kvq_block_bytes", "hs_kvq_append",
            "hs_kvq_read", "hs_kvq_attention_workspace", "hs_kvq_attention", "hs_token_logprobs_workspace",
-           "hs_token_logprobs", "hs_kvq_pool_create", "hs_decode_step_logprobs")
+           "hs_token_logprobs", "hs_kvq_pool_create", "hs_decode_step_logprobs", "hs_paged_block_bytes",
+           "hs_paged_append", "hs_paged_attention_workspace", "hs_paged_attention", "hs_sample_tokens_workspace",
+           "hs_sample_tokens", "hs_decode_step_sample")
 
 # projection matrices the library reads in its packed layout
 PACKED = ("wq", "wk", "wv", "wo", "w_gate", "w_up", "w_down", "lm_head")
@@ -63,6 +65,15 @@ class hs_kvq_cache(ctypes.Structure):
     _fields_ = [("blocks", ctypes.c_void_p), ("bytes", ctypes.c_uint64), ("table", ctypes.c_void_p),
                 ("n_seqs", ctypes.c_int32), ("table_ld", ctypes.c_int32), ("n_layers", ctypes.c_int32),
                 ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("block_tokens", ctypes.c_int32)]
+
+
+class hs_paged_cache(ctypes.Structure):
+    _fields_ = hs_kvq_cache._fields_ + [("dtype", ctypes.c_int32)]
+
+
+class hs_rope(ctypes.Structure):
+    _fields_ = [("frequencies", ctypes.c_void_p), ("axes", ctypes.c_void_p), ("n_pairs", ctypes.c_int32),
+                ("n_axes", ctypes.c_int32), ("adjacent", ctypes.c_int32)]
 
 
 _lib = None
@@ -124,6 +135,14 @@ def lib() -> ctypes.CDLL:
         "hs_token_logprobs_workspace": [I64, I32, I32, ctypes.POINTER(U64)],
         "hs_kvq_pool_create": [P, I32, I32, P, U64, ctypes.POINTER(P)],
         "hs_decode_step_logprobs": [P, P, P, P, P, I32, P, P, P, P, P, P, P],
+        "hs_paged_block_bytes": [I32, I32, I32, I32, I32, ctypes.POINTER(U64)],
+        "hs_paged_append": [P, I32, I32, I32, P, I64, I64, P, I64, I64, P, P, I64, I64, P, P, P, P, P, P,
+                            ctypes.c_float, P],
+        "hs_paged_attention_workspace": [P, I32, I32, I32, I32, I32, ctypes.POINTER(U64)],
+        "hs_paged_attention": [P, I32, I32, I32, P, I64, P, P, I32, P, P, I32, I32, ctypes.c_float, P, I64, P, U64, P],
+        "hs_sample_tokens_workspace": [I64, I32, ctypes.POINTER(U64)],
+        "hs_sample_tokens": [I32, P, I64, I32, I64, P, P, P, P, P, P, P, P, U64, P],
+        "hs_decode_step_sample": [P, P, P, P, P, P, P, P, P, P, P, P, P],
         "hs_token_logprobs": [I32, P, I64, I32, I64, P, I32, P, P, P, P, P, U64, P],
     }
     for name, args in sig.items():
@@ -366,6 +385,31 @@ class KVCache:
               _ptr(logits), _ptr(hidden_out), _ptr(lp), _ptr(entropy), _ptr(ids), _ptr(tops), _stream())
         return lp, entropy, ids, tops
 
+    def decode_sample(self, tokens_in, tokens_out, u, temperature=None, top_k=None, top_p=None, min_p=None,
+                      logits=None, hidden_out=None, model=None):
+        """The same step with its tokens drawn as sample_tokens draws them, instead of the largest logit; u, temperature,
+        top_p, min_p (float32) and top_k (int32) have an entry for each request of the handle, like tokens_in.  Returns
+        the log probabilities of the drawn tokens, a row for each decoded request (the rows come first; a pool that
+        decodes fewer than it could has NaN in the others)."""
+        import torch
+        func = "decode_sample"
+        index = -1 if tokens_in is None else tokens_in.get_device()
+        if index < 0:
+            raise ValueError(f"{func}: tokens_in must be on the GPU")
+        if u is None:
+            raise ValueError(f"{func}: u must be {self.batch} contiguous float32 values")
+        for name, t in (("tokens_in", tokens_in), ("tokens_out", tokens_out), ("top_k", top_k)):
+            _int32(func, name, t, self.batch, index)
+        for name, t in (("u", u), ("temperature", temperature), ("top_p", top_p), ("min_p", min_p)):
+            _float32(func, name, t, self.batch, index)
+        m = model or self.model
+        rows = min(self.batch, m.max_batch)
+        lp = torch.full((rows,), float("nan"), dtype=torch.float32, device=tokens_in.device)
+        _call("hs_decode_step_sample", m.handle, self.handle, _ptr(tokens_in), _ptr(tokens_out), _ptr(u),
+              _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(logits), _ptr(hidden_out), _ptr(lp),
+              _stream())
+        return lp
+
     def sync(self) -> None:
         """Host mirrors of the lengths from the device (after graph replays)."""
         _call("hs_kv_sync", self.handle)
@@ -467,6 +511,16 @@ def _int32(func: str, name: str, t, n: int, index: int):
         return None
     if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous() or t.get_device() != index:
         raise ValueError(f"{func}: {name} must be {n} contiguous int32 values on GPU {index}")
+    return t.data_ptr()
+
+
+def _float32(func: str, name: str, t, n: int, index: int):
+    """Address of a contiguous float32 tensor of n values on GPU `index` (None: NULL)."""
+    import torch
+    if t is None:
+        return None
+    if t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous() or t.get_device() != index:
+        raise ValueError(f"{func}: {name} must be {n} contiguous float32 values on GPU {index}")
     return t.data_ptr()
 
 
@@ -605,6 +659,211 @@ class QuantCache:
                    hd ** -0.5 if scale is None else scale, out.data_ptr(), out.stride(0), workspace.data_ptr(),
                    workspace.nbytes)
         return out
+
+
+def rope_frequencies(theta: float, n_pairs: int, device="cuda"):
+    """theta^(-i / n_pairs) for the n_pairs pairs of a rotation, in float64."""
+    import torch
+    return theta ** (-torch.arange(n_pairs, dtype=torch.float64, device=device) / n_pairs)
+
+
+class Rope:
+    """A rotation by position (hs_rope): pair i of a head's channels, (i, i + pairs) or, with adjacent, (2 i, 2 i + 1),
+    is turned by position[axes[i]] * frequencies[i].  frequencies: contiguous float64 [pairs], pairs a multiple of 8;
+    axes: contiguous int32 [pairs] (None: one axis); n_axes: how many axes there are (None: what axes names, which is
+    looked up once, here)."""
+
+    def __init__(self, frequencies, axes=None, adjacent: bool = False, n_axes=None):
+        import torch
+        if frequencies.dtype is not torch.float64 or frequencies.dim() != 1 or not frequencies.is_contiguous():
+            raise ValueError("Rope: frequencies must be a contiguous float64 vector")
+        self._index, pairs = frequencies.get_device(), frequencies.numel()
+        at = _int32("Rope", "axes", axes, pairs, self._index)
+        if n_axes is None:
+            n_axes = 1 if axes is None else int(axes.max()) + 1
+        self.frequencies, self.axes, self.n_axes = frequencies, axes, n_axes  # keeps the tensors alive
+        self._c = hs_rope(frequencies.data_ptr(), at, pairs, n_axes, int(adjacent))
+        self._ref = ctypes.addressof(self._c)
+
+
+def paged_block_bytes(dtype, n_layers: int, n_kv_heads: int, head_dim: int, block_tokens: int) -> int:
+    """Bytes of one block of a paged cache of a torch dtype."""
+    import torch
+    out = ctypes.c_uint64()
+    _call("hs_paged_block_bytes", _dtype_code("paged_block_bytes", torch.empty(0, dtype=dtype)), n_layers, n_kv_heads,
+          head_dim, block_tokens, ctypes.byref(out))
+    return out.value
+
+
+class PagedCache:
+    """A paged KV cache in the model's own type (hs_paged_cache) over caller-owned tensors: blocks, contiguous
+    [blocks][layers][2][n_kv_heads][block_tokens][head_dim] of float32, float16 or bfloat16, and table, a contiguous
+    int64 tensor [sequences][blocks per sequence] of block numbers, negative where there is none.  The table may be
+    rewritten between calls, and sequences may share blocks."""
+
+    def __init__(self, blocks, table):
+        import torch
+        if blocks.dim() != 6 or blocks.shape[2] != 2 or not blocks.is_contiguous():
+            raise ValueError("PagedCache: blocks must be contiguous [blocks][layers][2][n_kv_heads][block_tokens]"
+                             "[head_dim]")
+        if table.dtype is not torch.int64 or table.dim() != 2 or not table.is_contiguous() or \
+                table.device != blocks.device:
+            raise ValueError("PagedCache: table must be a contiguous int64 matrix on the blocks' device")
+        self.dtype = blocks.dtype
+        _, self.n_layers, _, self.n_kv_heads, self.block_tokens, self.head_dim = blocks.shape
+        paged_block_bytes(self.dtype, self.n_layers, self.n_kv_heads, self.head_dim, self.block_tokens)  # checks
+        self.blocks, self.table = blocks, table  # keeps the tensors alive
+        self._index, self._align = blocks.get_device(), 16 // blocks.element_size()
+        self._c = hs_paged_cache(blocks.data_ptr(), blocks.nbytes, table.data_ptr(), table.shape[0], table.shape[1],
+                                 self.n_layers, self.n_kv_heads, self.head_dim, self.block_tokens,
+                                 _dtype_code("PagedCache", blocks))
+        self._ref = ctypes.addressof(self._c)
+
+    def _rows(self, func: str, name: str, t, n, heads):
+        """Strides of t ([n][heads][head_dim], channels contiguous); those of a single row or head, which nothing
+        uses, as 0."""
+        shape, stride = t.shape, t.stride()
+        if len(shape) != 3 or (n is not None and shape[0] != n) or (heads is not None and shape[1] != heads) or \
+                shape[2] != self.head_dim or stride[2] != 1 or t.dtype is not self.dtype or \
+                t.get_device() != self._index:
+            raise ValueError(f"{func}: {name} must be [{'n' if n is None else n}][{heads or 'heads'}]"
+                             f"[{self.head_dim}] of {self.dtype} on {self.blocks.device}, channels contiguous")
+        return stride[0] if shape[0] > 1 else 0, stride[1] if shape[1] > 1 else 0
+
+    def append(self, layer: int, k, v, positions, seqs=None, q=None, rope=None, angles_at=None, q_gain=None,
+               k_gain=None, eps: float = 1e-6, q_out=None):
+        """Stores rows of K and V ([n][n_kv_heads][head_dim]) at positions (int32 [n]) of sequences seqs (int32 [n];
+        None: row i is sequence i), K normalised with k_gain ([head_dim]; None: not) and turned by rope (None: not) at
+        angles_at (int32 [axes][n]; None: positions).  Queries q ([n][heads][head_dim]) are normalised and turned
+        alike into q_out (None: a new tensor; may be q), which is returned."""
+        import torch
+        func = "PagedCache.append"
+        n, index = k.shape[0], self._index
+        ld, ldh = self._rows(func, "k", k, None, self.n_kv_heads)
+        if self._rows(func, "v", v, n, self.n_kv_heads) != (ld, ldh):
+            raise ValueError(f"{func}: k and v must have equal strides")
+        heads = lq = lqh = lo = loh = 0
+        if q is not None:
+            lq, lqh = self._rows(func, "q", q, n, None)
+            heads = q.shape[1]
+            if q_out is None:
+                q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            lo, loh = self._rows(func, "q_out", q_out, n, heads)
+        elif q_out is not None or q_gain is not None:
+            raise ValueError(f"{func}: q_out and q_gain are given with q")
+        for name, t in (("q_gain", q_gain), ("k_gain", k_gain)):
+            if t is not None and (t.dtype is not self.dtype or t.shape != (self.head_dim,) or not t.is_contiguous() or
+                                  t.get_device() != index):
+                raise ValueError(f"{func}: {name} must be {self.head_dim} contiguous values of {self.dtype}")
+        ref = None
+        if rope is not None:
+            if rope._index != index:
+                raise ValueError(f"{func}: the rope's tensors must be on {self.blocks.device}")
+            ref = rope._ref
+        elif angles_at is not None:
+            raise ValueError(f"{func}: angles_at is given with a rope")
+        _on_device(func, "hs_paged_append", index, self._ref, layer, n, heads, None if q is None else q.data_ptr(), lq,
+                   lqh, None if q_out is None else q_out.data_ptr(), lo, loh, k.data_ptr(), v.data_ptr(), ld, ldh,
+                   _int32(func, "seqs", seqs, n, index), _int32(func, "positions", positions, n, index), ref,
+                   None if rope is None else _int32(func, "angles_at", angles_at, rope.n_axes * n, index),
+                   None if q_gain is None else q_gain.data_ptr(), None if k_gain is None else k_gain.data_ptr(), eps)
+        return q_out
+
+    def _workspace_bytes(self, n: int, n_heads: int, max_len: int, n_groups: int, max_shared: int) -> int:
+        out = ctypes.c_uint64()
+        _call("hs_paged_attention_workspace", self._ref, n, n_heads, max_len, n_groups, max_shared, ctypes.byref(out))
+        return out.value
+
+    def attention_workspace(self, n: int, n_heads: int, max_len: int, n_groups: int = 0, max_shared: int = 0):
+        """A workspace for attention over n rows of n_heads heads, max_len positions, n_groups groups of rows and
+        max_shared shared positions."""
+        import torch
+        return torch.zeros(self._workspace_bytes(n, n_heads, max_len, n_groups, max_shared), dtype=torch.uint8,
+                           device=self.blocks.device)
+
+    def attention(self, layer: int, q, lengths, seqs=None, group_starts=None, shared=None, max_len=None,
+                  max_shared=None, scale=None, out=None, workspace=None):
+        """Attention of q ([n][n_heads][head_dim]) over the first lengths (int32 [n]) positions of sequences seqs.
+        Rows group_starts[g] .. group_starts[g + 1] - 1 (int32 [groups + 1], not falling) have their first shared[g]
+        (int32 [groups]) positions in common, which are read once, through the first row's sequence.  max_len bounds
+        the lengths (None: what the table holds), max_shared the shared positions (None: max_len); scale None:
+        head_dim ** -0.5.  A workspace (attention_workspace) may be kept from call to call; calls on several streams
+        do not share one."""
+        import torch
+        func = "PagedCache.attention"
+        index, hd = self._index, self.head_dim
+        ld, ldh = self._rows(func, "q", q, None, None)
+        n, heads = q.shape[0], q.shape[1]
+        if out is None:
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        lo, loh = self._rows(func, "out", out, n, heads)
+        if heads > 1 and (ldh != hd or loh != hd):
+            raise ValueError(f"{func}: each row of q and out must be contiguous")
+        groups = 0
+        if group_starts is not None or shared is not None:
+            if group_starts is None or shared is None:
+                raise ValueError(f"{func}: group_starts and shared are given together")
+            groups = shared.numel()
+        if max_len is None:
+            max_len = min(self.table.shape[1] * self.block_tokens, 1 << 30)
+        if max_shared is None:
+            max_shared = max_len if groups else 0
+        if workspace is None:
+            workspace = torch.empty(self._workspace_bytes(n, heads, max_len, groups, max_shared), dtype=torch.uint8,
+                                    device=self.blocks.device)
+        elif workspace.get_device() != index or not workspace.is_contiguous():
+            raise ValueError(f"{func}: workspace must be contiguous on {self.blocks.device}")
+        _on_device(func, "hs_paged_attention", index, self._ref, layer, n, heads, q.data_ptr(), ld,
+                   _int32(func, "seqs", seqs, n, index), _int32(func, "lengths", lengths, n, index), groups,
+                   _int32(func, "group_starts", group_starts, groups + 1, index),
+                   _int32(func, "shared", shared, groups, index), max_len, max_shared,
+                   hd ** -0.5 if scale is None else scale, out.data_ptr(), lo, workspace.data_ptr(), workspace.nbytes)
+        return out
+
+
+def _sample_bytes(rows: int, vocab: int) -> int:
+    out = ctypes.c_uint64()
+    _call("hs_sample_tokens_workspace", rows, vocab, ctypes.byref(out))
+    return out.value
+
+
+def sample_tokens_workspace(rows: int, vocab: int, device="cuda"):
+    """A workspace for sample_tokens over rows of vocab logits, which may be kept from call to call."""
+    import torch
+    return torch.zeros(_sample_bytes(rows, vocab), dtype=torch.uint8, device=device)
+
+
+def sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None, workspace=None):
+    """(tokens, logprob) of rows of logits ([rows][vocab]; float32, float16 or bfloat16): a token (int32) for each row,
+    drawn with the row's uniform number u (float32 [rows], in [0, 1)), and its log probability among the tokens that the
+    row's temperature, top_p, min_p (float32 [rows]) and top_k (int32 [rows]) leave, each None for none.  Of the logits
+    in falling order the first top_k stay, of these the shortest beginning with top_p of their weight, of these the
+    ones with at least min_p of the largest weight; temperature 0 takes the largest logit.  A row without a distribution
+    has token -1 and logprob NaN.  tokens: written there (None: a new tensor)."""
+    import torch
+    func = "sample_tokens"
+    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError(f"{func}: logits must be [rows][vocab], each row contiguous")
+    rows, vocab = logits.shape
+    index, dt = logits.get_device(), _dtype_code(func, logits)
+    if u is None:
+        raise ValueError(f"{func}: u must be {rows} contiguous float32 values")
+    at = [_float32(func, name, t, rows, index) for name, t in
+          (("u", u), ("temperature", temperature), ("top_p", top_p), ("min_p", min_p))]
+    tk = _int32(func, "top_k", top_k, rows, index)
+    if tokens is None:
+        tokens = logits.new_empty((rows,), dtype=torch.int32)
+    out = _int32(func, "tokens", tokens, rows, index)
+    logprob = torch.empty_like(u)
+    if workspace is None:
+        workspace = logits.new_empty((_sample_bytes(rows, vocab),), dtype=torch.uint8)
+        if workspace.numel():
+            workspace[:2048].zero_()
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError(f"{func}: workspace must be contiguous on the logits' device")
+    _on_device(func, "hs_sample_tokens", index, dt, logits.data_ptr(), rows, vocab, logits.stride(0), at[0], at[1], tk,
+               at[2], at[3], out, logprob.data_ptr(), workspace.data_ptr(), workspace.nbytes)
+    return tokens, logprob
 
 
 def _logprobs_bytes(rows: int, vocab: int, top: int) -> int:

@@ -1,0 +1,207 @@
+"""Tokens drawn on the GPU against the definition in 64 bits."""
+from __future__ import annotations
+
+import math
+
+import pytest
+import torch
+
+import paged_ref as R
+
+pytestmark = pytest.mark.gpu
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def check(hs, x, u, temperature=None, top_k=None, top_p=None, min_p=None, workspace=None):
+    gpu = lambda t, d=torch.float32: None if t is None else t.to(d).cuda()  # noqa: E731
+    f = lambda t: None if t is None else t.float()  # noqa: E731
+    got, lp = hs.sample_tokens(x.cuda(), gpu(u), gpu(temperature), top_k=gpu(top_k, torch.int32), top_p=gpu(top_p),
+                               min_p=gpu(min_p), workspace=workspace)
+    want, ref = R.draw(x.float(), f(u), f(temperature), top_k, f(top_p), f(min_p))
+    assert torch.equal(got.cpu(), want), (got.cpu() != want).nonzero()[:5]
+    lp = lp.double().cpu()
+    assert torch.equal(torch.isnan(lp), torch.isnan(ref))
+    fine = ~torch.isnan(ref)
+    # computed in 64 bits, rounded once
+    assert ((lp - ref).abs()[fine] <= ref.abs()[fine] * 2.0 ** -24 + 1e-12).all()
+    return got, lp
+
+
+def params(rows, g, greedy=False):
+    pick = lambda *v: torch.tensor(v)[torch.randint(0, len(v), (rows,), generator=g)]  # noqa: E731
+    t = 0.3 + 1.5 * torch.rand(rows, generator=g)
+    if greedy:
+        t *= torch.rand(rows, generator=g) > 0.2
+    return t, pick(0, 1, 2, 20, 50, 1000), pick(1.0, 0.5, 0.9, 0.95), pick(0.0, 0.01, 0.2)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(1, 1), (3, 2), (4, 63), (4, 64), (4, 65), (9, 997), (5, 4096), (5, 8191),
+                                        (5, 8192), (5, 8193), (4, 16384), (6, 16385), (8, 32000), (7, 152064),
+                                        (3, 200001)])
+def test_draws_of_every_size(dtype, rows, vocab):
+    import paper_2603_12707_amd as hs
+    g = gen(vocab)
+    x = (torch.randn(rows, vocab, generator=g) * 3).to(R.DT[dtype])
+    t, k, p, m = params(rows, g)
+    u = torch.rand(rows, generator=g)
+    check(hs, x, u)
+    check(hs, x, u, t)
+    check(hs, x, u, t, top_k=k)
+    check(hs, x, u, t, top_p=p)
+    check(hs, x, u, t, min_p=m)
+    check(hs, x, u, t, k, p, m)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("spread", [0.02, 0.5, 1.0, 8.0, 60.0])
+def test_flat_and_peaked_rows(dtype, spread):
+    import paper_2603_12707_amd as hs
+    g = gen(int(spread * 100))
+    x = (torch.randn(24, 40000, generator=g) * spread).to(R.DT[dtype])
+    t, k, p, m = params(24, g, greedy=True)
+    k[::3] = 30000
+    p[::5] = 0.9999
+    check(hs, x, torch.rand(24, generator=g), t, k, p, m)
+    check(hs, x, torch.rand(24, generator=g), t, None, p)
+    check(hs, x, torch.rand(24, generator=g))
+
+
+@pytest.mark.parametrize("vocab", [40, 5000, 70000])
+def test_equal_logits_come_by_index(vocab):
+    """Ties everywhere, also at each of the borders and the draw: weights that are powers of two, sums that are exact."""
+    import paper_2603_12707_amd as hs
+    x = torch.zeros(8, vocab)
+    x[1] = -2.5
+    x[2, 1::2] = 1.0
+    x[3, ::2] = -0.0
+    x[4] = (torch.arange(vocab) // 7).float() * -0.25
+    x[5] = torch.randint(0, 3, (vocab,), generator=gen(vocab)).float()
+    x[6, 3:] = -math.inf
+    x[7, vocab // 2 :] = 1.0
+    for u in (0.0, 0.3125, 0.75, 1.0 - 2.0 ** -24):
+        uu = torch.full((8,), u)
+        for dtype in ("f32", "bf16"):
+            y = x.to(R.DT[dtype])
+            check(hs, y, uu)
+            check(hs, y, uu, top_k=torch.tensor([3, 20, vocab // 2, 5, 9, vocab // 3, 2, 7]))
+            check(hs, y, uu, min_p=torch.full((8,), 0.3))
+            check(hs, y[[0, 1, 3, 6]], uu[:4], top_p=torch.tensor([0.5, 0.25, 0.125, 0.5]))
+            check(hs, y[[0, 1, 3]], uu[:3], top_k=torch.tensor([32, 16, 8]), top_p=torch.tensor([0.5, 0.25, 0.125]))
+
+
+@pytest.mark.parametrize("vocab", [6, 9001, 70001])
+def test_rows_without_a_distribution_and_banned_words(vocab):
+    import paper_2603_12707_amd as hs
+    g = gen(1)
+    x = torch.randn(12, vocab, generator=g)
+    x[0, torch.rand(vocab, generator=g) < 0.9] = -math.inf
+    x[0, 2] = 0.0
+    x[1] = -math.inf
+    x[1, vocab - 1] = -300.0  # one word left
+    x[2] = -math.inf          # none
+    x[3, 1] = math.nan
+    x[4, vocab - 1] = math.inf
+    x[5] = torch.finfo(torch.float32).min  # the lowest number, everywhere: an even distribution
+    x[6] = torch.finfo(torch.float32).min
+    x[6, 3] = 0.0
+    x[7, vocab // 2] = -math.nan
+    x[8] = math.inf
+    x[9] = -math.inf
+    x[9, :2] = torch.tensor([1.0, 1.0])
+    x[10, 0] = 80.0
+    x[11] *= 1e30
+    t, k, p, m = params(12, g, greedy=True)
+    u = torch.rand(12, generator=g)
+    for args in ((), (t,), (t, k), (t, None, p), (t, None, None, m), (t, k, p, m), (0 * t,)):
+        check(hs, x, u, *args)
+
+
+def test_parameters_at_their_ends():
+    import paper_2603_12707_amd as hs
+    g = gen(5)
+    n, vocab = 18, 3000
+    x = torch.randn(n, vocab, generator=g) * 2
+    t, k = torch.full((n,), 0.8), torch.zeros(n, dtype=torch.int64)
+    p, m = torch.ones(n), torch.zeros(n)
+    u = torch.rand(n, generator=g)
+    t[0], t[1], t[2], t[3], t[4] = -1.0, math.inf, math.nan, 1e-45, 3e38
+    k[5], k[6], k[7] = -5, vocab, 2 ** 31 - 1
+    p[8], p[9], p[10], p[11] = 0.0, -1.0, 2.0, math.nan
+    m[12], m[13], m[14] = 1.0, 7.0, math.nan
+    u[15], u[16], u[17] = 1.0, -0.5, math.nan
+    check(hs, x, u, t, k, p, m)
+    check(hs, x, u, None, k, p, m)
+
+
+def test_draws_follow_the_distribution():
+    """A sweep of u over one row gives every token its share, to within the sweep's step."""
+    import paper_2603_12707_amd as hs
+    n = 4096
+    x = torch.randn(1, 50, generator=gen(3)).expand(n, -1).contiguous()
+    u = (torch.arange(n) + 0.5) / n
+    got, _ = check(hs, x, u)
+    share = torch.bincount(got.cpu().long(), minlength=50) / n
+    assert (share - torch.softmax(x[0].double(), 0)).abs().max() <= 1.0 / n + 1e-9
+
+
+@pytest.mark.parametrize("rows", [1, 3, 300])
+def test_a_kept_workspace_and_strides(rows):
+    import paper_2603_12707_amd as hs
+    g = gen(rows)
+    ws = hs.sample_tokens_workspace(rows, 33000)
+    wide = torch.randn(rows, 40000, generator=g).cuda() * 3
+    u = torch.rand(rows, generator=g).cuda()
+    for vocab in (33000, 20000, 100, 33000):
+        part = wide[:, 3 : 3 + vocab]
+        one = hs.sample_tokens(part, u, workspace=ws)
+        two = hs.sample_tokens(part.contiguous(), u)
+        assert torch.equal(one[0], two[0]) and torch.equal(one[1], two[1])
+        check(hs, part.cpu(), u.cpu(), workspace=ws)
+
+
+def test_replayed_draws_read_new_numbers():
+    import paper_2603_12707_amd as hs
+    g = gen(9)
+    rows, vocab = 5, 40000
+    x = (torch.randn(rows, vocab, generator=g) * 2).cuda()
+    u, t, p = torch.rand(rows, generator=g).cuda(), torch.full((rows,), 0.9).cuda(), torch.full((rows,), 0.95).cuda()
+    ws = hs.sample_tokens_workspace(rows, vocab)
+    tokens = torch.empty(rows, dtype=torch.int32, device="cuda")
+    hs.sample_tokens(x, u, t, top_p=p, tokens=tokens, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        hs.sample_tokens(x, u, t, top_p=p, tokens=tokens, workspace=ws)
+    for turn in range(5):
+        u.copy_(torch.rand(rows, generator=g))
+        x.copy_(torch.randn(rows, vocab, generator=g) * (0.5 + turn))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager, _ = check(hs, x.cpu(), u.cpu(), t.cpu(), top_p=p.cpu())
+        assert torch.equal(tokens, eager)
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    import paper_2603_12707_amd as hs
+    g = gen(11)
+    x = (torch.randn(40, 50000, generator=g) * 2).cuda()
+    u = torch.rand(40, generator=g).cuda()
+    want = hs.sample_tokens(x, u)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = [hs.sample_tokens(x, u) for _ in range(3)]
+    here = [hs.sample_tokens(x, u) for _ in range(3)]
+    torch.cuda.synchronize()
+    for one in got + here:
+        assert torch.equal(one[0], want[0]) and torch.equal(one[1], want[1])
+
+
+def test_no_rows():
+    import paper_2603_12707_amd as hs
+    t, lp = hs.sample_tokens(torch.empty(0, 100, device="cuda"), torch.empty(0, device="cuda"))
+    assert t.shape == lp.shape == (0,)
