@@ -574,14 +574,14 @@ int hs_decode_step_logprobs(hs_model *m, hs_kv *kv, const int32_t *tokens_in, in
  * the first always stays.  tokens[r] is the first token whose weights, summed up to
  * it, exceed u[r] times the sum of those that stay, and logprob[r] (may be NULL) its
  * log probability among them.  temperature 0 takes the first (logprob 0).  u: device
- * fp32 in [0, 1), a number below is taken as 0 and one above as just less than 1;
+ * fp32 in [0, 1), a number below is taken as 0 and one above as 1 - 2^-24;
  * temperature (NULL: 1), top_p (NULL: 1), min_p (NULL: 0): device fp32 [rows]; top_k
  * (NULL: 0): device int32 [rows].  Logits of -inf are never drawn.  A row of logits
  * that holds a NaN or +inf, or nothing but -inf, or whose temperature is negative
  * or infinite, or with a NaN among its parameters, has token -1 and logprob NaN.
  * Weights and their sums are held in 64 bits, and results are the same from call to
  * call.  workspace: device memory of hs_sample_tokens_workspace bytes under the rules
- * of hs_kvq_attention's, its first 2048 bytes zero before its first use. */
+ * of hs_paged_attention's. */
 int hs_sample_tokens_workspace(int64_t rows, int32_t vocab, uint64_t *bytes);
 int hs_sample_tokens(int32_t dtype, const void *logits, int64_t rows, int32_t vocab, int64_t ld, const float *u,
                      const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,

@@ -746,8 +746,7 @@ int hs_model_create(const hs_config *cfg, const hs_weights *w, int32_t max_batch
   // (they are never written, so cleared once here)
   if (hipMemcpy(m->rope_tab, tab.data(), tab.size() * 4, hipMemcpyHostToDevice) != hipSuccess ||
       hipMemset(m->status, 0, 4) != hipSuccess ||
-      (m->lp_ws && hipMemset(m->lp_ws, 0, LOGPROB_COUNTERS * 4) != hipSuccess) ||
-      (m->sm_ws && hipMemset(m->sm_ws, 0, SAMPLE_COUNTERS * 4) != hipSuccess) || hipMemset(m->attn, 0, (size_t)act_elems(rows, nh * hd) * b) ||
+      (m->lp_ws && hipMemset(m->lp_ws, 0, LOGPROB_COUNTERS * 4) != hipSuccess) || hipMemset(m->attn, 0, (size_t)act_elems(rows, nh * hd) * b) ||
       hipMemset(m->act, 0, (size_t)act_elems(rows, c.ffn_dim) * b) ||
       hipMemset(m->hnorm, 0, (size_t)act_elems(rows, c.d_model) * b)) {
     free_model(m);

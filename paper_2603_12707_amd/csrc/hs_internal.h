@@ -458,9 +458,9 @@ struct SampleArgs {
   const int *top_k, *act;
   int *tokens;
   float *logprob;
-  void *ws;  // sample_workspace bytes, its counters zero between calls
+  void *ws;   // sample_workspace bytes
+  int parts;  // (set by the launcher) parts of a row
 };
-constexpr int SAMPLE_COUNTERS = 512;
 uint64_t sample_workspace(int64_t rows, int vocab);
 hipError_t launch_sample(int dtype, const SampleArgs &a, hipStream_t st);
 

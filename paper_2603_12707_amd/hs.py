@@ -778,7 +778,7 @@ class PagedCache:
         """A workspace for attention over n rows of n_heads heads, max_len positions, n_groups groups of rows and
         max_shared shared positions."""
         import torch
-        return torch.zeros(self._workspace_bytes(n, n_heads, max_len, n_groups, max_shared), dtype=torch.uint8,
+        return torch.empty(self._workspace_bytes(n, n_heads, max_len, n_groups, max_shared), dtype=torch.uint8,
                            device=self.blocks.device)
 
     def attention(self, layer: int, q, lengths, seqs=None, group_starts=None, shared=None, max_len=None,
@@ -830,7 +830,7 @@ def _sample_bytes(rows: int, vocab: int) -> int:
 def sample_tokens_workspace(rows: int, vocab: int, device="cuda"):
     """A workspace for sample_tokens over rows of vocab logits, which may be kept from call to call."""
     import torch
-    return torch.zeros(_sample_bytes(rows, vocab), dtype=torch.uint8, device=device)
+    return torch.empty(_sample_bytes(rows, vocab), dtype=torch.uint8, device=device)
 
 
 def sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None, workspace=None):
@@ -857,8 +857,6 @@ def sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=Non
     logprob = torch.empty_like(u)
     if workspace is None:
         workspace = logits.new_empty((_sample_bytes(rows, vocab),), dtype=torch.uint8)
-        if workspace.numel():
-            workspace[:2048].zero_()
     elif workspace.get_device() != index or not workspace.is_contiguous():
         raise ValueError(f"{func}: workspace must be contiguous on the logits' device")
     _on_device(func, "hs_sample_tokens", index, dt, logits.data_ptr(), rows, vocab, logits.stride(0), at[0], at[1], tk,

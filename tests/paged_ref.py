@@ -121,7 +121,7 @@ def draw(x, u, temperature=None, top_k=None, top_p=None, min_p=None):
             keep = max(1, int((w >= least).sum()))
             w, logw = w[:keep], logw[:keep]
         upto = torch.cumsum(w, 0)
-        uu = min(max(uu, 0.0), 1.0 - 2.0 ** -53)
+        uu = min(max(uu, 0.0), 1.0 - 2.0 ** -24)
         i = min(int((upto <= uu * upto[-1]).sum()), int((w > 0).sum()) - 1)
         tokens.append(int(order[i]))
         lps.append(float(logw[i] - torch.log(upto[-1])))
