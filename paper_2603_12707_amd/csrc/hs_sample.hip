@@ -7,11 +7,12 @@
 // of up to all the weights before it, and in 32 bits one in some ten thousand would
 // fall on its neighbour.
 //
-// No row is sorted.  A first launch cuts rows into parts that stay in registers
-// and sums the weights of bins 1/16 wide in x / T, aligned to the same grid in every
-// part.  A second one, a work group for a row, joins the bins, finds those in which
-// the three borders and the draw lie, gathers their logits from the row, and sorts
-// those few.
+// No row is sorted.  The weights of bins 1/16 wide in x / T are summed, which says
+// in which few of them the three borders and the draw lie; the logits of those are
+// found in the row, cut into 64 parts a bin, and the same said of the parts; what is
+// left is sorted.  A work group draws from a row, which it reads three or four times
+// (L2 holds it).  The bins of long rows are summed by a launch before, in parts that
+// stay in registers, on one grid.
 #include "hs_device.h"
 
 #include <algorithm>
@@ -78,7 +79,7 @@ constexpr double SM_EQUAL = 0x1p-44;
 // Bin b holds the logits with floor(x * 16 / T) = b; the product is rounded, but
 // alike everywhere, and rounding keeps the order.  Counted from the bin of a
 // part's (a row's) largest downward, the last of SM_BINS holds all that is lower.
-constexpr int SM_BINS = 512;
+constexpr int SM_BINS = 1024;
 constexpr double SM_FINE = 16.0;
 // A weight relative to its bin's upper end, in (e^-1/16, 1], as a whole multiple of
 // 2^-49: a part's 2^14 of them sum in 63 bits, in any order to the same.
@@ -96,8 +97,8 @@ __device__ __forceinline__ uint64_t bin_weight(double xs, double b) {
   e = __builtin_fma(e, r, 1.0);
   return __builtin_bit_cast(uint64_t, e + SM_ONE) - __builtin_bit_cast(uint64_t, SM_ONE);
 }
-// The same in the last bin, where all lies 32 below the part's largest: its whole
-// sum is 1e-10 of that one's weight, and fp32 does for it.
+// The same in the last bin, where all lies 63 below the part's largest: its whole
+// sum is 2^14 e^-63 of that one's weight, and fp32 does for it.
 __device__ __forceinline__ uint64_t tail_weight(double xs, double b) {
 #pragma clang fp contract(off)
   const float e = __expf((float)fmax((xs - (b + 1.0)) * (1.0 / SM_FINE), -200.0));
@@ -115,9 +116,24 @@ __host__ __device__ inline char *sample_ws(void *ws, int64_t row, int parts, int
   return (char *)ws + (row * parts + part) * SM_PART_BYTES;
 }
 
-constexpr int SP_THREADS = 256, SP_WAVES = SP_THREADS / 64;
 constexpr int SP_WORDS = 32;  // 4-byte words of a thread
 
+// sum over the work group's threads up to this one
+template <int WAVES>
+__device__ __forceinline__ int block_scan(int v, int *s_tmp) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(v, o);
+    if (lane >= o) v += y;
+  }
+  __syncthreads();
+  if (lane == 63) s_tmp[wave] = v;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w)
+    if (w < wave) v += s_tmp[w];
+  return v;
+}
 // largest of the work group's values, in every thread
 template <int WAVES>
 __device__ __forceinline__ uint64_t block_most(uint64_t v, uint64_t *s_tmp) {
@@ -130,122 +146,230 @@ __device__ __forceinline__ uint64_t block_most(uint64_t v, uint64_t *s_tmp) {
   return v;
 }
 
-// A part of a row: its largest, and its bins.  One read of the logits, which stay
-// in registers; the sums go through LDS, whole numbers that are added in any order.
+// Up to 32 words of logits for each of a work group's threads, in registers.
+template <int DT, int THREADS>
+struct Held {
+  static constexpr int B = DT == HS_F32 ? 4 : 2, CE = 16 / B, PER = 4 / B, N = SP_WORDS * PER, ALL = THREADS * N;
+  uint32_t w[SP_WORDS];
+  int n;
+  // n of them from x on; -inf past them
+  __device__ __forceinline__ Held(const char *x, int n_) : n(n_) {
+    constexpr uint32_t NEG = DT == HS_F32 ? 0xFF800000u : DT == HS_F16 ? 0xFC00FC00u : 0xFF80FF80u;
+#pragma unroll
+    for (int c = 0; c < SP_WORDS / 4; ++c) {
+      const int i = (c * THREADS + (int)threadIdx.x) * CE;
+      u32x4 t = {NEG, NEG, NEG, NEG};
+      if (i + CE <= n) {
+        t = ld_loose<DT>(x + i * B);
+      } else {
+#pragma unroll
+        for (int e = 0; e < CE; ++e)
+          if (i + e < n) {
+            if constexpr (DT == HS_F32) {
+              t[e] = ((const uint32_t *)x)[i + e];
+            } else {
+              const uint32_t h = ((const uint16_t *)x)[i + e];
+              t[e / 2] = e & 1 ? (t[e / 2] & 0xFFFFu) | h << 16 : (t[e / 2] & 0xFFFF0000u) | h;
+            }
+          }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[4 * c + k] = t[k];
+    }
+  }
+  // f(values of a chunk, the first one's index), in order
+  template <class F>
+  __device__ __forceinline__ void chunks(F f) {
+#pragma unroll
+    for (int c = 0; c < SP_WORDS / 4; ++c) {
+      float v[CE];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        // opaque from one use to the next: what is made of a word is made again, not
+        // kept in registers
+        asm volatile("" : "+v"(w[4 * c + k]));
+      }
+      unpack<DT>(u32x4{w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]}, v);
+      f(v, (c * THREADS + (int)threadIdx.x) * CE);
+    }
+  }
+};
+// The same of a row in memory, of any length.
+template <int DT, int THREADS>
+struct Read {
+  static constexpr int B = DT == HS_F32 ? 4 : 2, CE = 16 / B;
+  const char *x;
+  int n;
+  template <class F>
+  __device__ __forceinline__ void chunks(F f) const {
+    const int whole = n / CE, tid = (int)threadIdx.x;
+    constexpr int U = 4;  // loads in flight
+    u32x4 q[U];
+    for (int c = tid; c - tid < whole; c += U * THREADS) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) q[u] = ld_loose<DT>(x + (int64_t)min(c + u * THREADS, whole - 1) * 16);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float v[CE];
+        unpack<DT>(q[u], v);
+        if (c + u * THREADS >= whole) {
+#pragma unroll
+          for (int e = 0; e < CE; ++e) v[e] = -INFINITY;
+        }
+        f(v, (c + u * THREADS) * CE);
+      }
+    }
+    // what is left, less than a chunk
+    float v[CE];
+#pragma unroll
+    for (int e = 0; e < CE; ++e) v[e] = -INFINITY;
+    if (whole * CE + tid < n) v[0] = ld_elem<DT>(x, whole * CE + tid);
+    f(v, whole * CE + tid);
+  }
+};
+
+struct BinLds {
+  unsigned long long mass[SM_BINS];
+  uint32_t count[SM_BINS];
+  uint64_t tmp[16];
+  int tmp_n[16];
+  int last;
+};
+// The largest of some logits (value key and ~index, counted from `first` on), and
+// whether one is NaN or +inf.
+template <class H, int THREADS>
+__device__ __forceinline__ uint64_t row_best(H &h, int first, BinLds &lds, bool &odd) {
+  float m = -INFINITY;
+  int at = 0;
+  odd = false;
+  h.chunks([&](const float *v, int i) {
+#pragma unroll
+    for (int e = 0; e < H::CE; ++e) {
+      odd |= !(v[e] < INFINITY);
+      at = v[e] > m ? i + e : at;
+      m = fmaxf(m, v[e]);
+    }
+  });
+  odd = __syncthreads_or(odd);
+  return block_most<THREADS / 64>((uint64_t)value_key(m) << 32 | (uint32_t)~(first + at), lds.tmp);
+}
+// Their bins from b0 down, in LDS.  The sums are of whole numbers, added in any
+// order.  With top_k: among the largest of every chunk (16 bytes) there is a bin up
+// to which top_k of them lie; what lies lower is left out.
+template <class H, int THREADS>
+__device__ __forceinline__ void row_bins(H &h, double s, double b0, int top_k, bool counts, BinLds &lds) {
+  const int tid = threadIdx.x;
+  for (int i = tid; i < SM_BINS; i += THREADS) {
+    lds.mass[i] = 0;
+    lds.count[i] = 0;
+  }
+  double most = INFINITY;
+  __syncthreads();
+  if (counts && top_k <= h.n / H::CE / 2) {
+    h.chunks([&](const float *v, int) {
+      float m = v[0];
+#pragma unroll
+      for (int e = 1; e < H::CE; ++e) m = fmaxf(m, v[e]);
+      const double d = b0 - floor((double)m * s);
+      if (d < SM_BINS - 1) atomicAdd(&lds.count[(int)d], 1u);
+    });
+    if (tid == 0) lds.last = SM_BINS;
+    __syncthreads();
+    constexpr int EACH = SM_BINS / THREADS;
+    int own[EACH], sum = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) sum += own[i] = (int)lds.count[tid * EACH + i];
+    int n = block_scan<THREADS / 64>(sum, lds.tmp_n) - sum;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      if (n < top_k && n + own[i] >= top_k) lds.last = tid * EACH + i;
+      n += own[i];
+      lds.count[tid * EACH + i] = 0;
+    }
+    __syncthreads();
+    most = lds.last;
+  }
+  h.chunks([&](const float *v, int) {
+#pragma unroll
+    for (int e = 0; e < H::CE; ++e) {
+      const double xs = (double)v[e] * s, b = floor(xs), d = b0 - b;
+      if (d <= most) {
+        if (d < SM_BINS - 1) {
+          const int g = (int)d;
+          atomicAdd(&lds.mass[g], (unsigned long long)bin_weight(xs, b));
+          if (counts) atomicAdd(&lds.count[g], 1u);
+        } else if (v[e] > -INFINITY) {
+          atomicAdd(&lds.mass[SM_BINS - 1], (unsigned long long)tail_weight(xs, b0 - (SM_BINS - 1)));
+          if (counts) atomicAdd(&lds.count[SM_BINS - 1], 1u);
+        }
+      }
+    }
+  });
+  __syncthreads();
+}
+
+// A part of a row: its largest, and its bins.
+constexpr int SP_THREADS = 512;
 template <int DT>
 __global__ __launch_bounds__(SP_THREADS) void k_sample_parts(SampleArgs a) {
-  constexpr int B = DT == HS_F32 ? 4 : 2, PER = 4 / B, PART = SP_THREADS * SP_WORDS * PER;
-  __shared__ unsigned long long s_mass[SM_BINS];
-  __shared__ uint32_t s_count[SM_BINS];
-  __shared__ uint64_t s_tmp[SP_WAVES];
+  using H = Held<DT, SP_THREADS>;
+  __shared__ BinLds lds;
   const int64_t row = blockIdx.x / a.parts;
   const int part = (int)(blockIdx.x - row * a.parts), tid = threadIdx.x;
   const SampleRow p = sample_row(a, a.act ? a.act[row] : row);
-  const int first = part * PART, n = min(PART, a.vocab - first);
-  const char *x = (const char *)a.logits + (row * a.ld + first) * B;
-  // chunks of 16 bytes to a thread
-  constexpr int CE = 16 / B, NC = SP_WORDS / 4;
-  constexpr uint32_t NEG = DT == HS_F32 ? 0xFF800000u : DT == HS_F16 ? 0xFC00FC00u : 0xFF80FF80u;  // -inf
-  u32x4 w[NC];
-#pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const int i = (c * SP_THREADS + tid) * CE;
-    w[c] = u32x4{NEG, NEG, NEG, NEG};
-    if (n == PART || i + CE <= n) {
-      w[c] = ld_loose<DT>(x + i * B);
-    } else {
-#pragma unroll
-      for (int e = 0; e < CE; ++e)
-        if (i + e < n) {
-          if constexpr (DT == HS_F32) {
-            w[c][e] = ((const uint32_t *)x)[i + e];
-          } else {
-            const uint32_t h = ((const uint16_t *)x)[i + e];
-            w[c][e / 2] = e & 1 ? (w[c][e / 2] & 0xFFFFu) | h << 16 : (w[c][e / 2] & 0xFFFF0000u) | h;
-          }
-        }
-    }
-  }
-  const auto value = [&](int i) {  // element i of the thread's
-    const uint32_t u = w[i / CE][i % CE / PER];
-    if constexpr (DT == HS_F32) return __uint_as_float(u);
-    else return i & 1 ? hi_f32<DT>(u) : lo_f32<DT>(u);
-  };
-  for (int i = tid; i < SM_BINS; i += SP_THREADS) {
-    s_mass[i] = 0;
-    s_count[i] = 0;
-  }
-  float m = -INFINITY;
-  bool odd = false;
-#pragma unroll
-  for (int i = 0; i < SP_WORDS * PER; ++i) {
-    m = fmaxf(m, value(i));
-    odd |= !(value(i) < INFINITY);
-  }
-  int at = INT32_MAX;
-#pragma unroll
-  for (int i = SP_WORDS * PER - 1; i >= 0; --i)
-    if (value(i) == m) at = first + ((i / CE) * SP_THREADS + tid) * CE + i % CE;
-  // (a part that ends early has -inf behind its end, which is not looked for)
-  const uint64_t best = block_most<SP_WAVES>((uint64_t)value_key(m) << 32 | (uint32_t)~at, s_tmp);
-  const bool any_odd = __syncthreads_or(odd);
+  const int first = part * H::ALL;
+  H h((const char *)a.logits + (row * a.ld + first) * H::B, min(H::ALL, a.vocab - first));
+  bool odd;
+  const uint64_t best = row_best<H, SP_THREADS>(h, first, lds, odd);
   const float top = key_float((uint32_t)(best >> 32));
   const double s = p.inv_t * SM_FINE, b0 = floor((double)top * s);
   char *ws = sample_ws(a.ws, row, a.parts, part);
-  if (tid == 0) *(SamplePart *)ws = SamplePart{b0, best, any_odd ? 1ull : 0ull};
-  if (p.bad || p.greedy || any_odd || top == -INFINITY) return;
+  if (tid == 0) *(SamplePart *)ws = SamplePart{b0, best, odd ? 1ull : 0ull};
+  if (p.bad || p.greedy || odd || top == -INFINITY) return;
   const bool counts = p.top_k < a.vocab;
-#pragma unroll
-  for (int i = 0; i < SP_WORDS * PER; ++i) {
-    const float v = value(i);
-    const double xs = (double)v * s, b = floor(xs);
-    const double d = b0 - b;
-    if (d < SM_BINS - 1) {
-      const int g = (int)d;
-      atomicAdd(&s_mass[g], (unsigned long long)bin_weight(xs, b));
-      if (counts) atomicAdd(&s_count[g], 1u);
-    } else if (v > -INFINITY) {
-      atomicAdd(&s_mass[SM_BINS - 1], (unsigned long long)tail_weight(xs, b0 - (SM_BINS - 1)));
-      if (counts) atomicAdd(&s_count[SM_BINS - 1], 1u);
-    }
-  }
-  __syncthreads();
+  row_bins<H, SP_THREADS>(h, s, b0, p.top_k, counts, lds);
   uint64_t *mass = (uint64_t *)(ws + sizeof(SamplePart));
   uint32_t *count = (uint32_t *)(mass + SM_BINS);
   for (int i = tid; i < SM_BINS; i += SP_THREADS) {
-    mass[i] = s_mass[i];
-    if (counts) count[i] = s_count[i];
+    mass[i] = lds.mass[i];
+    if (counts) count[i] = lds.count[i];
   }
 }
 
 // ---------------------------------------------------------------------------
 // draws
 // ---------------------------------------------------------------------------
-constexpr int SD_THREADS = 512, SD_WAVES = SD_THREADS / 64;
-constexpr int SD_LIST = 4096;  // logits that are sorted
-static_assert(SD_THREADS == SM_BINS, "a thread for each bin");
+constexpr int SD_THREADS = 1024, SD_WAVES = SD_THREADS / 64;
+constexpr int SD_LIST = 2048;  // gathered logits that stay at hand
+constexpr int SD_SUB = 64;     // parts that a bin is cut into
+constexpr int SD_FEW = 512;    // logits that are sorted
+constexpr int SD_RUNS = 3;     // ranges of values that are looked for
+static_assert(SD_THREADS == SM_BINS && SD_WAVES * SD_SUB == SD_THREADS, "a thread for each");
 
 struct DrawLds {
+  BinLds bins;                    // of the row, then the parts of its needed bins
   union {
-    uint64_t list[SD_LIST];       // value key and ~index, sorted downward
-    struct {                      // a row by itself
-      unsigned long long mass[256];
-      uint32_t count[256];
-    } radix;
+    struct {
+      uint64_t queue[SD_WAVES][128];  // a wave's logits (value key and ~index) that wait for 64 lanes
+      int slot[SM_BINS];              // of a bin that is cut further, -1: not
+    };
+    struct {
+      double few_before[SD_THREADS];
+      int start[SD_THREADS];
+    };
   };
-  uint64_t sorted[1024];          // (ranked by counting)
-  double upto[SM_BINS], before[SM_BINS], scale[SM_BINS];
-  int count_before[SM_BINS];
-  int start[SM_BINS];
-  double list_before[SM_BINS];
-  uint8_t need[SM_BINS];
+  uint64_t list[SD_LIST];
+  __align__(16) uint64_t few[SD_FEW + 8];
+  uint64_t sorted[SD_FEW];
+  double upto[SD_THREADS], before[SD_THREADS];
+  int count_before[SD_THREADS];
+  int slot_bin[SD_WAVES];
+  uint8_t need[SD_THREADS];
   double tmp[SD_WAVES];
-  uint64_t tmp_u[SD_WAVES];
-  int tmp_n[SD_WAVES];
-  int bk, bp0, bp1, bt0, bt1, n, pick, last;
+  float run_lo[SD_RUNS], run_hi[SD_RUNS];
+  int bk, bp0, bp1, bt0, bt1, n, n_few, pick, last;
   uint32_t digit;
-  double above;
-  uint64_t above_u, ties;
+  uint64_t above_u, number, ties;
 };
 
 // sums over the threads before this one and up to it
@@ -269,20 +393,6 @@ __device__ __forceinline__ double block_scan(double v, double *s_tmp, double &to
   const double prev = __shfl_up(x, 1);
   before = lane ? base + prev : base;
   return base + x;
-}
-__device__ __forceinline__ int block_scan(int v, int *s_tmp) {  // up to this thread
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(v, o);
-    if (lane >= o) v += y;
-  }
-  __syncthreads();
-  if (lane == 63) s_tmp[wave] = v;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < SD_WAVES; ++w)
-    if (w < wave) v += s_tmp[w];
-  return v;
 }
 __device__ __forceinline__ double block_largest(double v, double *s_tmp) {
   for (int o = 32; o; o >>= 1) v = fmax(v, __shfl_xor(v, o));
@@ -316,16 +426,16 @@ __device__ __attribute__((noinline)) void draw_alone(const SampleArgs &a, DrawLd
     for (int shift = 24; shift >= 0; shift -= 8) {
       __syncthreads();
       if (tid < 256) {
-        lds.radix.mass[tid] = 0;
-        lds.radix.count[tid] = 0;
+        lds.bins.mass[tid] = 0;
+        lds.bins.count[tid] = 0;
       }
       __syncthreads();
       for (int i = tid; i < V; i += SD_THREADS) {
         const float v = ld_elem<DT>(x, i);
         const uint32_t k = value_key(v);
         if (shift == 24 || (k >> (shift + 8)) == (edge >> (shift + 8))) {
-          atomicAdd(&lds.radix.count[k >> shift & 255], 1u);
-          atomicAdd(&lds.radix.mass[k >> shift & 255], (unsigned long long)weight(v));
+          atomicAdd(&lds.bins.count[k >> shift & 255], 1u);
+          atomicAdd(&lds.bins.mass[k >> shift & 255], (unsigned long long)weight(v));
         }
       }
       __syncthreads();
@@ -334,23 +444,23 @@ __device__ __attribute__((noinline)) void draw_alone(const SampleArgs &a, DrawLd
         int d = 255, last = -1;
         uint64_t lm = m, ln = n;
         for (; d >= 0; --d) {
-          const uint64_t c = lds.radix.count[d];
+          const uint64_t c = lds.bins.count[d];
           if (!c) continue;
-          if (!by_weight || lds.radix.mass[d]) last = d, lm = m, ln = n;
-          if (cross(n + c, m + lds.radix.mass[d])) break;
+          if (!by_weight || lds.bins.mass[d]) last = d, lm = m, ln = n;
+          if (cross(n + c, m + lds.bins.mass[d])) break;
           n += c;
-          m += lds.radix.mass[d];
+          m += lds.bins.mass[d];
         }
         if (d < 0) d = last, m = lm, n = ln;  // (rounding: the last that counts)
         lds.digit = (uint32_t)d;
         lds.above_u = m;
-        lds.tmp_u[0] = n;
-        lds.ties = lds.radix.count[d];
+        lds.number = n;
+        lds.ties = lds.bins.count[d];
       }
       __syncthreads();
       edge |= lds.digit << shift;
       above = lds.above_u;
-      number = lds.tmp_u[0];
+      number = lds.number;
       ties = lds.ties;
     }
   };
@@ -376,7 +486,7 @@ __device__ __attribute__((noinline)) void draw_alone(const SampleArgs &a, DrawLd
     const uint32_t k = value_key(min_p_floor(p, M));
     // how many reach it, and their weight
     __syncthreads();
-    if (tid == 0) lds.radix.mass[0] = lds.radix.mass[1] = 0;
+    if (tid == 0) lds.bins.mass[0] = lds.bins.mass[1] = 0;
     __syncthreads();
     unsigned long long n = 0, m = 0;
     for (int i = tid; i < V; i += SD_THREADS) {
@@ -386,12 +496,12 @@ __device__ __attribute__((noinline)) void draw_alone(const SampleArgs &a, DrawLd
         m += weight(v);
       }
     }
-    atomicAdd(&lds.radix.mass[0], n);
-    atomicAdd(&lds.radix.mass[1], m);
+    atomicAdd(&lds.bins.mass[0], n);
+    atomicAdd(&lds.bins.mass[1], m);
     __syncthreads();
-    if (lds.radix.mass[0] < kept) {
-      kept = lds.radix.mass[0];
-      total = lds.radix.mass[1];
+    if (lds.bins.mass[0] < kept) {
+      kept = lds.bins.mass[0];
+      total = lds.bins.mass[1];
     }
   }
   const double want = (p.u + SM_EQUAL) * (double)total;
@@ -406,12 +516,12 @@ __device__ __attribute__((noinline)) void draw_alone(const SampleArgs &a, DrawLd
     const bool is = i < V && value_key(ld_elem<DT>(x, i)) == edge;
     const uint64_t in = __ballot(is);
     __syncthreads();
-    if ((tid & 63) == 0) lds.tmp_n[tid >> 6] = (int)__popcll(in);
+    if ((tid & 63) == 0) lds.bins.tmp_n[tid >> 6] = (int)__popcll(in);
     __syncthreads();
     int before = 0, all = 0;
     for (int o = 0; o < SD_WAVES; ++o) {
-      if (o < tid >> 6) before += lds.tmp_n[o];
-      all += lds.tmp_n[o];
+      if (o < tid >> 6) before += lds.bins.tmp_n[o];
+      all += lds.bins.tmp_n[o];
     }
     if (left < all) {
       if (is && before + (int)__popcll(in & ((1ull << (tid & 63)) - 1)) == left) {
@@ -424,285 +534,366 @@ __device__ __attribute__((noinline)) void draw_alone(const SampleArgs &a, DrawLd
   }
 }
 
-// A row's draw.  The sums of its bins say in which bins top-k and min-p end, and
-// between which bounds the weight that top-k leaves, hence in which bins top-p ends,
-// hence between which bounds the weight that is drawn from, and so the draw.  The
-// logits of those bins (a few hundred, mostly) are gathered from the row and sorted;
-// with the sums of the bins before theirs that gives each its place and the weight
-// up to it, and with these the borders and the draw.  Bounds are wider by 1e-12 than
-// sums are off.
-template <int DT>
+// What a thread knows of its bin (or part of one): the weight and the number before
+// it and up to it, in the row's falling order.
+struct DrawBin {
+  double before, upto, weight;
+  int count_before, count;
+};
+struct DrawCuts {
+  bool k, p, m;
+  int bk, e0, e1;   // the bin in which top-k ends; bounds of the one in which all that stays ends (SD_THREADS: none)
+  bool need, past;  // whether the thread's bin may hold a border or the draw; whether some bin could not be found
+};
+// Which bins top-k and min-p end in; between which bounds the weight lies that top-k
+// leaves, hence the bins that top-p may end in; hence the bounds of the weight that
+// is drawn from, and the bins that the draw may fall in.  Bounds are wider by 1e-12
+// than sums are off.  bm: the bin that min-p's floor lies in.
+__device__ __forceinline__ DrawCuts draw_cuts(DrawLds &lds, const SampleRow &p, const DrawBin &b, double total, int vocab,
+                                              int bm) {
+  constexpr int NONE = SD_THREADS;
+  const int tid = threadIdx.x;
+  DrawCuts c;
+  c.k = p.top_k < vocab;
+  c.p = p.top_p < 1.f;
+  c.m = p.min_p > 0.f;
+  __syncthreads();
+  lds.before[tid] = b.before;
+  lds.upto[tid] = b.upto;
+  lds.count_before[tid] = b.count_before;
+  if (tid == 0) lds.bk = lds.bp0 = lds.bp1 = lds.bt0 = lds.bt1 = NONE;
+  __syncthreads();
+  if (c.k && b.count && b.count_before < p.top_k && b.count_before + b.count >= p.top_k) lds.bk = tid;
+  __syncthreads();
+  c.bk = lds.bk;
+  const auto bound = [&](int at, bool after) { return at >= NONE ? total : after ? lds.upto[at] : lds.before[at]; };
+  const double wider = 1e-12;
+  if (c.p) {
+    const double lo = fmax((double)p.top_p * bound(c.bk, false) * (1 - wider), 0x1p-1070),
+                 hi = fmax((double)p.top_p * bound(c.bk, true) * (1 + wider), 0x1p-1070);
+    if (b.upto >= lo && b.before < lo) lds.bp0 = tid;
+    if (b.upto >= hi && b.before < hi) lds.bp1 = tid;
+    __syncthreads();
+  }
+  const int bp0 = lds.bp0, bp1 = lds.bp1;
+  c.e0 = min(bm, min(c.bk, bp0));
+  c.e1 = min(bm, min(c.bk, bp1));
+  const double lo = p.u * bound(c.e0, false) * (1 - wider), hi = p.u * bound(c.e1, true) * (1 + wider);
+  if (b.upto > lo && b.before <= lo) lds.bt0 = tid;
+  if (b.upto > hi && b.before <= hi) lds.bt1 = tid;
+  __syncthreads();
+  const int bt0 = min(lds.bt0, c.e1), bt1 = min(lds.bt1, c.e1);
+  // (a top-p that ends past what the others leave says nothing, nor then does top-k)
+  c.need = (tid == c.bk && ((c.p && bp0 <= c.e1) || c.bk <= c.e1)) || (tid == bm && bm <= c.e1) ||
+           (b.weight > 0.0 && ((c.p && tid >= bp0 && tid <= bp1 && tid <= c.e1) || (tid >= bt0 && tid <= bt1)));
+  c.past = bt1 >= NONE || (c.p && c.e1 >= NONE);
+  return c;
+}
+
+// A row's draw.  WHOLE: its bins are summed here; else its parts' are joined.
+template <int DT, bool WHOLE>
 __global__ __launch_bounds__(SD_THREADS) void k_sample_draw(SampleArgs a) {
-  constexpr int B = DT == HS_F32 ? 4 : 2, CE = 16 / B;
+  using H = Read<DT, SD_THREADS>;
   __shared__ DrawLds lds;
   const int64_t row = blockIdx.x, slot = a.act ? a.act[row] : row;
-  const int tid = threadIdx.x, V = a.vocab;
+  const int tid = threadIdx.x, V = a.vocab, lane = tid & 63, wave = tid >> 6;
+  H h{(const char *)a.logits + row * a.ld * H::B, V};
   const SampleRow p = sample_row(a, slot);
-  // the parts' largest
-  uint64_t best = 0, odd = 0;
-  for (int i = tid; i < a.parts; i += SD_THREADS) {
-    const SamplePart h = *(const SamplePart *)sample_ws(a.ws, row, a.parts, i);
-    best = max(best, h.best);
-    odd |= h.odd;
+  uint64_t best = 0;
+  bool odd = false;
+  if constexpr (WHOLE) {
+    best = row_best<H, SD_THREADS>(h, 0, lds.bins, odd);
+  } else {
+    for (int i = tid; i < a.parts; i += SD_THREADS) {
+      const SamplePart h = *(const SamplePart *)sample_ws(a.ws, row, a.parts, i);
+      best = max(best, h.best);
+      odd |= h.odd != 0;
+    }
+    odd = __syncthreads_or(odd);
+    best = block_most<SD_WAVES>(best, lds.bins.tmp);
   }
-  best = block_most<SD_WAVES>(best, lds.tmp_u);
-  const bool any_odd = __syncthreads_or(odd != 0);
   const float M = key_float((uint32_t)(best >> 32));
-  if (p.bad || any_odd || M == -INFINITY || p.greedy) {
+  if (p.bad || odd || M == -INFINITY || p.greedy) {
     if (tid == 0) {
-      const bool none = p.bad || any_odd || M == -INFINITY;
+      const bool none = p.bad || odd || M == -INFINITY;
       a.tokens[slot] = none ? -1 : (int)~(uint32_t)best;
       if (a.logprob) a.logprob[row] = none ? NAN : 0.f;
     }
     return;
   }
   const double s = p.inv_t * SM_FINE, b0 = floor((double)M * s);
-  const bool cut_k = p.top_k < V, cut_p = p.top_p < 1.f, cut_m = p.min_p > 0.f;
+  const bool cut_k = p.top_k < V;
 
-  // the row's bins, bin tid of each thread: from part i's bin tid - off
-  const double scale = exp(-(double)tid / SM_FINE) * 0x1p-49;
-  double w = 0.0;
+  // the row's bins, one of each thread
+  const auto bin_scale = [](int b) { return exp(-(double)b / SM_FINE) * 0x1p-49; };
+  const double scale = bin_scale(tid);
+  double w = 0.0, total, before;
   int count = 0;
-  for (int i = 0; i < a.parts; ++i) {
-    const char *ws = sample_ws(a.ws, row, a.parts, i);
-    const SamplePart *h = (const SamplePart *)ws;
-    if ((uint32_t)(h->best >> 32) == value_key(-INFINITY)) continue;
-    const uint64_t *mass = (const uint64_t *)(ws + sizeof(SamplePart));
-    const uint32_t *cnt = (const uint32_t *)(mass + SM_BINS);
-    const int off = (int)fmin(b0 - h->top, (double)SM_BINS);
-    if (tid < SM_BINS - 1 && tid >= off) {
-      w += (double)mass[tid - off] * scale;
-      if (cut_k) count += (int)cnt[tid - off];
-    }
-  }
-  // what lies in the last one: bins of parts that reach past it
-  double far = 0.0;
-  int far_count = 0;
-  for (int i = 0; i < a.parts; ++i) {
-    const char *ws = sample_ws(a.ws, row, a.parts, i);
-    const SamplePart *h = (const SamplePart *)ws;
-    if ((uint32_t)(h->best >> 32) == value_key(-INFINITY)) continue;
-    const uint64_t *mass = (const uint64_t *)(ws + sizeof(SamplePart));
-    const uint32_t *cnt = (const uint32_t *)(mass + SM_BINS);
-    const double off = b0 - h->top;
-    if (tid + off >= SM_BINS - 1) {
-      far += (double)mass[tid] * (exp(-(tid + off) / SM_FINE) * 0x1p-49);
-      if (cut_k) far_count += (int)cnt[tid];
-    }
-  }
-  double total, before;
-  (void)block_scan(far, lds.tmp, total, before);
-  if (tid == SM_BINS - 1) w = total;
-  const double upto = block_scan(w, lds.tmp, total, before);
-  lds.upto[tid] = upto;
-  lds.before[tid] = before;
-  lds.scale[tid] = scale;
-  lds.need[tid] = 0;
-  int count_upto = 0;
-  if (cut_k) {
-    // (-inf is not counted: a border past the last bin's numbers lies among them)
-    const int fars = block_scan(far_count, lds.tmp_n);
-    if (tid == SM_BINS - 1) count = fars;
-    count_upto = block_scan(count, lds.tmp_n);
-    lds.count_before[tid] = count_upto - count;
-  }
-  if (tid == 0) {
-    lds.bk = lds.bp0 = lds.bp1 = lds.bt0 = lds.bt1 = SM_BINS;
-    lds.n = 0;
-    lds.pick = INT32_MAX;
-    lds.last = -1;
-  }
-  __syncthreads();
-  if (cut_k && count && count_upto >= p.top_k && count_upto - count < p.top_k) lds.bk = tid;
-  __syncthreads();
-  const int bk = lds.bk;  // SM_BINS: none
-  const auto bound = [&](int b, bool after) {  // weight before, or after, bin b
-    return b >= SM_BINS ? total : after ? lds.upto[b] : lds.before[b];
-  };
-  const double wider = 1e-12;
-  if (cut_p) {
-    const double lo = fmax((double)p.top_p * bound(bk, false) * (1 - wider), 0x1p-1070),
-                 hi = fmax((double)p.top_p * bound(bk, true) * (1 + wider), 0x1p-1070);
-    if (upto >= lo && before < lo) lds.bp0 = tid;
-    if (upto >= hi && before < hi) lds.bp1 = tid;
-  }
-  const float floor_x = cut_m ? min_p_floor(p, M) : -INFINITY;
-  const int bm = cut_m ? (int)fmin(b0 - floor((double)floor_x * s), (double)(SM_BINS - 1)) : SM_BINS;
-  __syncthreads();
-  const int bp0 = lds.bp0, bp1 = lds.bp1;
-  const int e0 = min(bm, min(bk, bp0)), e1 = min(bm, min(bk, bp1));
-  const double lo = p.u * bound(e0, false) * (1 - wider), hi = p.u * bound(e1, true) * (1 + wider);
-  if (upto > lo && before <= lo) lds.bt0 = tid;
-  if (upto > hi && before <= hi) lds.bt1 = tid;
-  __syncthreads();
-  const int bt0 = min(lds.bt0, e1), bt1 = min(lds.bt1, e1);
-  const bool need = (tid == bk && (cut_p || bk <= e1)) || (cut_p && tid >= bp0 && tid <= bp1 && tid <= e1) ||
-                    (tid == bm && bm <= e1) || (tid >= bt0 && tid <= bt1);
-  if (need) lds.need[tid] = 1;
-  // the last bin is not gathered, nor is what no bin holds
-  const bool past = (need && tid == SM_BINS - 1) || bt1 >= SM_BINS || (cut_p && bp1 >= SM_BINS) ||
-                    (cut_m && bm >= SM_BINS - 1 && bm <= e1);
-  if (__syncthreads_or(past)) {
-    draw_alone<DT>(a, lds, p, row, slot, M);
-    return;
-  }
-  // the lowest bin that is asked for
-  const int lowest = (int)block_most<SD_WAVES>(need ? (uint64_t)tid : 0, lds.tmp_u);
-  // (a first sieve: a bin and more lower, for the roundings)
-  const double edge = (b0 - lowest - 1.0) / s;
-  const float sieve = (float)fmax(edge - fabs(edge) * 1e-6, -(double)FLT_MAX);
-  const char *x = (const char *)a.logits + row * a.ld * B;
-  const auto take = [&](float v, int i) {
-    if (v >= sieve) {
-      const double d = b0 - floor((double)v * s);
-      if (d < SM_BINS - 1 && lds.need[(int)d]) {
-        const int at = atomicAdd(&lds.n, 1);
-        if (at < SD_LIST) lds.list[at] = (uint64_t)value_key(v) << 32 | (uint32_t)~i;
+  if constexpr (WHOLE) {
+    row_bins<H, SD_THREADS>(h, s, b0, p.top_k, cut_k, lds.bins);
+    w = (double)lds.bins.mass[tid] * scale;
+    count = (int)lds.bins.count[tid];
+  } else {
+    // from part i's bin tid - off, and what reaches past the last
+    double far = 0.0;
+    int far_count = 0;
+    for (int i = 0; i < a.parts; ++i) {
+      const char *ws = sample_ws(a.ws, row, a.parts, i);
+      const SamplePart *h = (const SamplePart *)ws;
+      if ((uint32_t)(h->best >> 32) == value_key(-INFINITY)) continue;
+      const uint64_t *mass = (const uint64_t *)(ws + sizeof(SamplePart));
+      const uint32_t *cnt = (const uint32_t *)(mass + SM_BINS);
+      const int off = (int)fmin(b0 - h->top, (double)SM_BINS);
+      if (tid < SM_BINS - 1 && tid >= off) {
+        w += (double)mass[tid - off] * scale;
+        if (cut_k) count += (int)cnt[tid - off];
+      }
+      if (tid + off >= SM_BINS - 1) {
+        far += (double)mass[tid] * (exp(-(tid + (b0 - h->top)) / SM_FINE) * 0x1p-49);
+        if (cut_k) far_count += (int)cnt[tid];
       }
     }
-  };
-  const int chunks = V / CE;
-  for (int c = tid; c < chunks; c += 4 * SD_THREADS) {
-    u32x4 q[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) q[u] = ld_loose<DT>(x + (int64_t)min(c + u * SD_THREADS, chunks - 1) * 16);
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (c + u * SD_THREADS < chunks) {
-        float f[CE];
-        unpack<DT>(q[u], f);
-#pragma unroll
-        for (int e = 0; e < CE; ++e) take(f[e], (c + u * SD_THREADS) * CE + e);
-      }
+    (void)block_scan(far, lds.tmp, total, before);
+    if (tid == SM_BINS - 1) w = total;
+    if (cut_k) {
+      const int fars = block_scan<SD_WAVES>(far_count, lds.bins.tmp_n);
+      if (tid == SM_BINS - 1) count = fars;
+    }
   }
-  for (int i = chunks * CE + tid; i < V; i += SD_THREADS) take(ld_elem<DT>(x, i), i);
-  __syncthreads();
-  const int n = lds.n;
-  if (n > SD_LIST) {
+  DrawBin bin;
+  bin.upto = block_scan(w, lds.tmp, total, bin.before);
+  bin.weight = w;
+  bin.count = count;
+  // (-inf is not counted: top_k may end past the last number)
+  bin.count_before = cut_k ? block_scan<SD_WAVES>(count, lds.bins.tmp_n) - count : 0;
+  const float floor_x = p.min_p > 0.f ? min_p_floor(p, M) : -INFINITY;
+  const int bm = p.min_p > 0.f ? (int)fmin(b0 - floor((double)floor_x * s), (double)(SM_BINS - 1)) : SD_THREADS;
+  DrawCuts cut = draw_cuts(lds, p, bin, total, V, bm);
+  // the needed bins in order; the last one is not cut further
+  const uint64_t needed = __ballot(cut.need);
+  if (lane == 0) lds.bins.tmp_n[wave] = (int)__popcll(needed);
+  if (tid == 0) lds.n = lds.n_few = 0;
+  const bool alone = __syncthreads_or(cut.past || (cut.need && tid == SM_BINS - 1));
+  int mine = (int)__popcll(needed & ((1ull << lane) - 1)), slots = 0;
+  for (int o = 0; o < SD_WAVES; ++o) {
+    if (o < wave) mine += lds.bins.tmp_n[o];
+    slots += lds.bins.tmp_n[o];
+  }
+  if (alone || slots > SD_WAVES) {
     __syncthreads();
     draw_alone<DT>(a, lds, p, row, slot, M);
     return;
   }
-  const uint64_t *sorted = lds.list;
-  if (n <= 1024) {
-    for (int i = tid; i < n; i += SD_THREADS) {
-      const uint64_t mine = lds.list[i];
-      int rank = 0;
-      for (int o = 0; o < n; ++o) rank += lds.list[o] > mine;
-      lds.sorted[rank] = mine;
+  lds.slot[tid] = cut.need ? mine : -1;
+  if (cut.need) lds.slot_bin[mine] = tid;
+  lds.bins.mass[tid] = 0;
+  lds.bins.count[tid] = 0;
+  __syncthreads();
+  // ranges of values that cover them, wider than roundings: few logits outside the
+  // bins are in them
+  if (tid == 0) {
+    for (int r = 0; r < SD_RUNS; ++r) {
+      lds.run_lo[r] = INFINITY;
+      lds.run_hi[r] = -INFINITY;
     }
-    sorted = lds.sorted;
+    int r = -1;
+    for (int i = 0; i < slots; ++i) {
+      const int b = lds.slot_bin[i];
+      if (r < 0 || (b != lds.slot_bin[i - 1] + 1 && r < SD_RUNS - 1)) {
+        const double hi = (b0 - b + 1.0) / s;
+        lds.run_hi[++r] = (float)fmin(hi + fabs(hi) * 0x1p-20 + 1e-37, (double)FLT_MAX);
+      }
+      const double lo = (b0 - b) / s;
+      lds.run_lo[r] = (float)fmax(lo - fabs(lo) * 0x1p-20 - 1e-37, -(double)FLT_MAX);
+    }
+  }
+  __syncthreads();
+  float run_lo[SD_RUNS], run_hi[SD_RUNS];
+#pragma unroll
+  for (int r = 0; r < SD_RUNS; ++r) {
+    run_lo[r] = lds.run_lo[r];
+    run_hi[r] = lds.run_hi[r];
+  }
+  // Calls take(value, ~index), a wave's lanes together, for the row's logits in the
+  // ranges.  They wait in a queue of the wave's until they fill its lanes.
+  const auto each = [&](auto take) {
+    int waiting = 0;
+    const auto offer = [&](float v, int i) {
+      bool in = v >= run_lo[0] && v <= run_hi[0];
+#pragma unroll
+      for (int r = 1; r < SD_RUNS; ++r) in |= v >= run_lo[r] && v <= run_hi[r];
+      const uint64_t all = __ballot(in);
+      if (!all) return;
+      if (in)
+        lds.queue[wave][waiting + (int)__popcll(all & ((1ull << lane) - 1))] = (uint64_t)value_key(v) << 32 | (uint32_t)~i;
+      waiting += (int)__popcll(all);
+      if (waiting >= 64) {
+        waiting -= 64;
+        const uint64_t k = lds.queue[wave][waiting + lane];
+        take(key_float((uint32_t)(k >> 32)), (uint32_t)k);
+      }
+    };
+    h.chunks([&](const float *v, int i) {
+#pragma unroll
+      for (int e = 0; e < H::CE; ++e) offer(v[e], i + e);
+    });
+    if (lane < waiting) {
+      const uint64_t k = lds.queue[wave][lane];
+      take(key_float((uint32_t)(k >> 32)), (uint32_t)k);
+    }
+  };
+  // the part of a bin that a logit lies in, -1: in none that is needed
+  const auto part = [&](float v, double &xs, double &b) {
+    xs = (double)v * s;
+    b = floor(xs);
+    const double d = b0 - b;
+    const int at = d < SM_BINS - 1 ? lds.slot[(int)d] : -1;
+    return at < 0 ? -1 : at * SD_SUB + SD_SUB - 1 - (int)((xs - b) * SD_SUB);
+  };
+  each([&](float v, uint32_t low) {
+    double xs, b;
+    const int at = part(v, xs, b);
+    if (at < 0) return;
+    atomicAdd(&lds.bins.mass[at], (unsigned long long)bin_weight(xs, b));
+    atomicAdd(&lds.bins.count[at], 1u);
+    const int to = atomicAdd(&lds.n, 1);
+    if (to < SD_LIST) lds.list[to] = (uint64_t)value_key(v) << 32 | low;
+  });
+  __syncthreads();
+  // the parts, each wave's of one bin
+  w = count = 0;
+  bin.before = bin.upto = total;
+  bin.count_before = INT32_MAX / 2;
+  if (wave < slots) {
+    const int of = lds.slot_bin[wave];
+    w = (double)lds.bins.mass[tid] * bin_scale(of);
+    count = (int)lds.bins.count[tid];
+    double up = w;
+    int n = count;
+    for (int o = 1; o < 64; o <<= 1) {
+      const double y = __shfl_up(up, o);
+      const int z = __shfl_up(n, o);
+      if (lane >= o) {
+        up += y;
+        n += z;
+      }
+    }
+    const double prev = __shfl_up(up, 1);
+    bin.before = lds.before[of] + (lane ? prev : 0.0);
+    bin.upto = lds.before[of] + up;
+    bin.count_before = lds.count_before[of] + n - count;
+  }
+  bin.count = count;
+  bin.weight = w;
+  double floor_s, floor_b;
+  int bm2 = p.min_p > 0.f ? part(floor_x, floor_s, floor_b) : -1;
+  if (bm2 < 0) bm2 = SD_THREADS;
+  cut = draw_cuts(lds, p, bin, total, V, bm2);
+  lds.need[tid] = cut.need;
+  // (2^14 weights of a part sum in 63 bits)
+  if (__syncthreads_or(cut.past || count > 1 << 14)) {
+    draw_alone<DT>(a, lds, p, row, slot, M);
+    return;
+  }
+  // what is left
+  const auto pick_up = [&](float v, uint32_t low) {
+    double xs, b;
+    const int at = part(v, xs, b);
+    if (at >= 0 && lds.need[at]) {
+      const int to = atomicAdd(&lds.n_few, 1);
+      if (to < SD_FEW) lds.few[to] = (uint64_t)value_key(v) << 32 | low;
+    }
+  };
+  if (lds.n <= SD_LIST) {
+    for (int i = tid; i < lds.n; i += SD_THREADS) pick_up(key_float((uint32_t)(lds.list[i] >> 32)), (uint32_t)lds.list[i]);
   } else {
-    int m = 2048;
-    while (m < n) m *= 2;
-    for (int i = n + tid; i < m; i += SD_THREADS) lds.list[i] = 0;
-    for (int k = 2; k <= m; k *= 2)
-      for (int j = k / 2; j; j /= 2) {
-        __syncthreads();
-        for (int i = tid; i < m / 2; i += SD_THREADS) {
-          const int lo_i = i / j * 2 * j + i % j, hi_i = lo_i + j;
-          const uint64_t u = lds.list[lo_i], v = lds.list[hi_i];
-          if ((u < v) == ((lo_i & k) == 0)) {
-            lds.list[lo_i] = v;
-            lds.list[hi_i] = u;
-          }
-        }
-      }
+    each(pick_up);
   }
   __syncthreads();
-  // each thread's run of the list: weights, and the weight before it in the list
-  constexpr int PER = SD_LIST / SD_THREADS;
-  const int run = (n + SD_THREADS - 1) / SD_THREADS, i0 = min(n, tid * run), mine = min(n, i0 + run) - i0;
-  double wt[PER], sum = 0.0;
-  int bin[PER];
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    wt[i] = 0.0;
-    bin[i] = 0;
-    if (i < mine) {
-      const double xs = (double)key_float((uint32_t)(sorted[i0 + i] >> 32)) * s, b = floor(xs);
-      bin[i] = (int)(b0 - b);
-      wt[i] = (double)bin_weight(xs, b) * lds.scale[bin[i]];
-      sum += wt[i];
-    }
+  const int n = lds.n_few;
+  if (n > SD_FEW) {
+    __syncthreads();
+    draw_alone<DT>(a, lds, p, row, slot, M);
+    return;
   }
-  double list_total, run_before;
-  (void)block_scan(sum, lds.tmp, list_total, run_before);
-  {
-    double c = run_before;
-    int prev = -1;
-    if (mine && i0) prev = (int)(b0 - floor((double)key_float((uint32_t)(sorted[i0 - 1] >> 32)) * s));
+  if (tid < n) {
+    const uint64_t key = lds.few[tid];
+    int rank = 0;
+    for (int o = 0; o < n; o += 8) {
+      u32x4 two[4];
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
-      if (i < mine) {
-        if (bin[i] != prev) {
-          lds.start[bin[i]] = i0 + i;
-          lds.list_before[bin[i]] = c;
-        }
-        prev = bin[i];
-        c += wt[i];
+      for (int u = 0; u < 4; ++u) two[u] = *(const u32x4 *)&lds.few[o + 2 * u];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        rank += o + 2 * u < n && ((uint64_t)two[u][1] << 32 | two[u][0]) > key;
+        rank += o + 2 * u + 1 < n && ((uint64_t)two[u][3] << 32 | two[u][2]) > key;
       }
+    }
+    lds.sorted[rank] = key;
+  }
+  if (tid == 0) {
+    lds.pick = INT32_MAX;
+    lds.last = -1;
   }
   __syncthreads();
-  // weight before each and its place in the row
-  double ahead[PER];
-  bool in[PER];
-  double c = run_before, kept = 0.0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    in[i] = i < mine;
-    ahead[i] = 0.0;
-    if (in[i]) {
-      ahead[i] = lds.before[bin[i]] + (c - lds.list_before[bin[i]]);
-      c += wt[i];
-      if (cut_k) in[i] = lds.count_before[bin[i]] + (i0 + i - lds.start[bin[i]]) < p.top_k;
-      if (in[i] && bin[i] == bk) kept = fmax(kept, ahead[i] + wt[i]);
-    }
+  // each one's weight, and the weight before it and its place in the row
+  double wt = 0.0, xs, b, all;
+  int at = -1, at_prev = -1;
+  float v = 0.f;
+  if (tid < n) {
+    v = key_float((uint32_t)(lds.sorted[tid] >> 32));
+    if (tid) at_prev = part(key_float((uint32_t)(lds.sorted[tid - 1] >> 32)), xs, b);
+    at = part(v, xs, b);
+    wt = (double)bin_weight(xs, b) * bin_scale((int)(b0 - b));
   }
-  if (cut_p) {
-    const double zk = bk < SM_BINS ? fmax(block_largest(kept, lds.tmp), lds.before[bk]) : total;
-    const double want = fmax((double)p.top_p * zk * (1 - SM_EQUAL), 0x1p-1070);
-#pragma unroll
-    for (int i = 0; i < PER; ++i) in[i] = in[i] && ahead[i] < want;
+  (void)block_scan(wt, lds.tmp, all, before);  // (its barriers end the use of `slot`)
+  if (tid < n && at != at_prev) {
+    lds.start[at] = tid;
+    lds.few_before[at] = before;
   }
-  kept = 0.0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i)
-    if (in[i]) {
-      in[i] = key_float((uint32_t)(sorted[i0 + i] >> 32)) >= floor_x;
-      if (in[i]) kept = fmax(kept, ahead[i] + wt[i]);
-    }
-  const double z = e1 < SM_BINS ? fmax(block_largest(kept, lds.tmp), bound(e0, false)) : total;
+  __syncthreads();
+  bool in = tid < n;
+  double ahead = 0.0;
+  if (in) {
+    ahead = lds.before[at] + (before - lds.few_before[at]);
+    if (cut.k) in = lds.count_before[at] + (tid - lds.start[at]) < p.top_k;
+  }
+  if (cut.p) {
+    const double kept = block_largest(in && at == cut.bk ? ahead + wt : 0.0, lds.tmp);
+    const double zk = cut.bk < SD_THREADS ? fmax(kept, lds.before[cut.bk]) : total;
+    in = in && ahead < fmax((double)p.top_p * zk * (1 - SM_EQUAL), 0x1p-1070);
+  }
+  in = in && v >= floor_x;
+  const double kept = block_largest(in ? ahead + wt : 0.0, lds.tmp);
+  const double z = cut.e1 < SD_THREADS ? fmax(kept, lds.before[cut.e0]) : total;
   const double want = (p.u + SM_EQUAL) * z;
-  int pick = INT32_MAX, last = -1;
-#pragma unroll
-  for (int i = PER - 1; i >= 0; --i)
-    if (in[i] && wt[i] > 0.0) {
-      last = max(last, i0 + i);
-      if (ahead[i] + wt[i] > want) pick = i0 + i;
-    }
-  if (pick < INT32_MAX) atomicMin(&lds.pick, pick);
-  if (last >= 0) atomicMax(&lds.last, last);
+  if (in && wt > 0.0) {
+    atomicMax(&lds.last, tid);
+    if (ahead + wt > want) atomicMin(&lds.pick, tid);
+  }
   __syncthreads();
-  const int at = lds.pick < INT32_MAX ? lds.pick : lds.last;
-#pragma unroll
-  for (int i = 0; i < PER; ++i)
-    if (i < mine && i0 + i == at) {
-      a.tokens[slot] = (int)~(uint32_t)sorted[at];
-      if (a.logprob) a.logprob[row] = (float)log(wt[i] / z);
-    }
+  if (tid == (lds.pick < INT32_MAX ? lds.pick : lds.last)) {
+    a.tokens[slot] = (int)~(uint32_t)lds.sorted[tid];
+    if (a.logprob) a.logprob[row] = (float)log(wt / z);
+  }
 }
 
+constexpr int SAMPLE_WHOLE = 32768;
+// parts of a row; 0: it has none
 inline int sample_parts(int vocab, int dtype) {
-  const int part = SP_THREADS * SP_WORDS * (dtype == HS_F32 ? 1 : 2);
-  return (int)(((int64_t)vocab + part - 1) / part);
+  const int per = SP_WORDS * SP_THREADS * (dtype == HS_F32 ? 1 : 2);
+  return vocab <= SAMPLE_WHOLE ? 0 : (int)(((int64_t)vocab + per - 1) / per);
 }
 
 template <int DT>
 hipError_t sample_launch(SampleArgs a, hipStream_t st) {
   a.parts = sample_parts(a.vocab, DT);
-  HS_LAUNCH((k_sample_parts<DT>), dim3((uint32_t)(a.rows * a.parts)), dim3(SP_THREADS), 0, st, a);
-  HS_LAUNCH((k_sample_draw<DT>), dim3((uint32_t)a.rows), dim3(SD_THREADS), 0, st, a);
+  if (!a.parts) {
+    HS_LAUNCH((k_sample_draw<DT, true>), dim3((uint32_t)a.rows), dim3(SD_THREADS), 0, st, a);
+  } else {
+    HS_LAUNCH((k_sample_parts<DT>), dim3((uint32_t)(a.rows * a.parts)), dim3(SP_THREADS), 0, st, a);
+    HS_LAUNCH((k_sample_draw<DT, false>), dim3((uint32_t)a.rows), dim3(SD_THREADS), 0, st, a);
+  }
   return hipGetLastError();
 }
 
