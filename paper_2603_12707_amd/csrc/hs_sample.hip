@@ -634,23 +634,42 @@ __global__ __launch_bounds__(SD_THREADS) void k_sample_draw(SampleArgs a) {
     w = (double)lds.bins.mass[tid] * scale;
     count = (int)lds.bins.count[tid];
   } else {
-    // from part i's bin tid - off, and what reaches past the last
+    // from part i's bin tid - off, and what reaches past the last; `list` holds the
+    // parts' offsets
     double far = 0.0;
     int far_count = 0;
-    for (int i = 0; i < a.parts; ++i) {
-      const char *ws = sample_ws(a.ws, row, a.parts, i);
-      const SamplePart *h = (const SamplePart *)ws;
-      if ((uint32_t)(h->best >> 32) == value_key(-INFINITY)) continue;
-      const uint64_t *mass = (const uint64_t *)(ws + sizeof(SamplePart));
-      const uint32_t *cnt = (const uint32_t *)(mass + SM_BINS);
-      const int off = (int)fmin(b0 - h->top, (double)SM_BINS);
-      if (tid < SM_BINS - 1 && tid >= off) {
-        w += (double)mass[tid - off] * scale;
-        if (cut_k) count += (int)cnt[tid - off];
+    for (int i0 = 0; i0 < a.parts; i0 += SD_LIST) {
+      const int n = min(a.parts - i0, SD_LIST);
+      __syncthreads();
+      for (int i = tid; i < n; i += SD_THREADS) {
+        const SamplePart *h = (const SamplePart *)sample_ws(a.ws, row, a.parts, i0 + i);
+        const double off = (uint32_t)(h->best >> 32) == value_key(-INFINITY) ? -1.0 : b0 - h->top;
+        lds.list[i] = __builtin_bit_cast(uint64_t, off);
       }
-      if (tid + off >= SM_BINS - 1) {
-        far += (double)mass[tid] * (exp(-(tid + (b0 - h->top)) / SM_FINE) * 0x1p-49);
-        if (cut_k) far_count += (int)cnt[tid];
+      __syncthreads();
+      constexpr int U = 4;
+      for (int j = 0; j < n; j += U) {
+        uint64_t near_w[U], far_w[U];
+        uint32_t near_n[U], far_n[U];
+        double off[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          off[u] = j + u < n ? __builtin_bit_cast(double, lds.list[j + u]) : -1.0;
+          const char *ws = sample_ws(a.ws, row, a.parts, i0 + min(j + u, n - 1)) + sizeof(SamplePart);
+          const int to = (int)fmin(off[u], (double)SM_BINS);
+          const bool near = to >= 0 && tid < SM_BINS - 1 && tid >= to, past = to >= 0 && tid + to >= SM_BINS - 1;
+          near_w[u] = near ? ((const uint64_t *)ws)[tid - to] : 0;
+          far_w[u] = past ? ((const uint64_t *)ws)[tid] : 0;
+          near_n[u] = near && cut_k ? ((const uint32_t *)((const uint64_t *)ws + SM_BINS))[tid - to] : 0;
+          far_n[u] = past && cut_k ? ((const uint32_t *)((const uint64_t *)ws + SM_BINS))[tid] : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          w += (double)near_w[u] * scale;
+          if (far_w[u]) far += (double)far_w[u] * (exp(-(tid + off[u]) / SM_FINE) * 0x1p-49);
+          count += (int)near_n[u];
+          far_count += (int)far_n[u];
+        }
       }
     }
     (void)block_scan(far, lds.tmp, total, before);
@@ -714,6 +733,7 @@ __global__ __launch_bounds__(SD_THREADS) void k_sample_draw(SampleArgs a) {
     run_lo[r] = lds.run_lo[r];
     run_hi[r] = lds.run_hi[r];
   }
+  const float lowest = fminf(run_lo[0], fminf(run_lo[1], run_lo[2]));
   // Calls take(value, ~index), a wave's lanes together, for the row's logits in the
   // ranges.  They wait in a queue of the wave's until they fill its lanes.
   const auto each = [&](auto take) {
@@ -734,6 +754,10 @@ __global__ __launch_bounds__(SD_THREADS) void k_sample_draw(SampleArgs a) {
       }
     };
     h.chunks([&](const float *v, int i) {
+      float top = v[0];
+#pragma unroll
+      for (int e = 1; e < H::CE; ++e) top = fmaxf(top, v[e]);
+      if (!__ballot(top >= lowest)) return;
 #pragma unroll
       for (int e = 0; e < H::CE; ++e) offer(v[e], i + e);
     });
