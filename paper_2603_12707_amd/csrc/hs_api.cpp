@@ -1736,7 +1736,7 @@ int hs_paged_attention_workspace(const hs_paged_cache *cache, int32_t n, int32_t
   // (a launch takes less than 2^32 threads: 256 to a row, KV head and split)
   if ((int64_t)n * n_heads >= 1 << 22) return fail(HS_E_INVALID, "%s: too many rows", fn);
   PagedAttn a{};
-  paged_plan(n, n_heads, cache->n_kv_heads, max_len, n_groups, max_shared, &a);
+  paged_plan(cache->dtype, n, n_heads, cache->n_kv_heads, max_len, n_groups, max_shared, &a);
   const int slots = a.n_own + a.n_pre;
   *bytes = slots > 1 ? (uint64_t)n * n_heads * slots * (cache->head_dim + 2) * 4 : 0;
   return HS_OK;
@@ -1777,7 +1777,7 @@ int hs_paged_attention(const hs_paged_cache *cache, int32_t layer, int32_t n, in
   a.scale = scale;
   a.out = out;
   a.ld_out = n > 1 ? ld_out : 0;
-  paged_plan(n, n_heads, cache->n_kv_heads, max_len, n_groups, max_shared, &a);
+  paged_plan(cache->dtype, n, n_heads, cache->n_kv_heads, max_len, n_groups, max_shared, &a);
   if (!a.n_pre) a.n_groups = 0;
   a.part_o = (float *)workspace;
   a.part_ml = a.part_o + (int64_t)n * n_heads * (a.n_own + a.n_pre) * cache->head_dim;

@@ -168,6 +168,20 @@ __device__ __forceinline__ f32x4 mma16(u32x2 a, u32x2 b, f32x4 c) {
   }
 }
 
+// The 32x32x16 MFMA: lane l supplies row (A) / column (B) l % 32 and the 8 k values
+// of half l / 32; row 8 (i / 4) + 4 (l / 32) + i % 4 of its column is c[i].
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+template <int DT>
+__device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c) {
+  if constexpr (DT == HS_F16) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  } else {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
+                                                   0);
+  }
+}
+
 __device__ __forceinline__ u32x4 ld16(const void *p) { return *(const u32x4 *)p; }
 __device__ __forceinline__ u32x4 ld16_stream(const void *p) {
   return __builtin_nontemporal_load((const u32x4 *)p);

@@ -444,7 +444,7 @@ struct PagedAttn {
   float *part_ml;  // [n][n_heads][n_own + n_pre][2]: base-2 maximum (-inf: no position), sum
 };
 constexpr int PAGED_MAX_SPLITS = 64;
-void paged_plan(int64_t n, int n_heads, int n_kv, int max_len, int n_groups, int max_shared, PagedAttn *a);
+void paged_plan(int dtype, int64_t n, int n_heads, int n_kv, int max_len, int n_groups, int max_shared, PagedAttn *a);
 hipError_t launch_paged_append(int dtype, int head_dim, const PagedRows &a, hipStream_t st);
 hipError_t launch_paged_attention(int dtype, int head_dim, const PagedAttn &a, hipStream_t st);
 

@@ -210,6 +210,40 @@ __device__ __forceinline__ int64_t paged_slot(const PagedAttn &a, int64_t row, i
   return (row * a.n_heads + head) * (a.n_own + a.n_pre) + slot;
 }
 
+// The unit-th tile of a group's rows, `per` rows at most to a tile, counted group by
+// group: its first row, rows, the group's first row and number (-1: there is none).
+struct PagedUnit {
+  int row0, rows, first, group;
+};
+__device__ __forceinline__ PagedUnit paged_unit(const PagedAttn &a, int unit, int per) {
+  const int lane = threadIdx.x & 63;
+  int left = unit;
+  for (int b = 0; b < a.n_groups; b += 64) {
+    const int i = b + lane;
+    int s = 0, e = 0;
+    if (i < a.n_groups) {
+      s = min(max(a.starts[i], 0), a.n);
+      e = min(max(a.starts[i + 1], s), a.n);
+    }
+    int sum = (e - s + per - 1) / per;
+    const int mine = sum;
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(sum, o);
+      if (lane >= o) sum += v;
+    }
+    const uint64_t in = __ballot(left < sum);
+    if (in) {
+      const int at = (int)__builtin_ctzll(in);
+      left -= __builtin_amdgcn_readfirstlane(__shfl(sum, at) - __shfl(mine, at));
+      const int first = __builtin_amdgcn_readfirstlane(__shfl(s, at)), end = __builtin_amdgcn_readfirstlane(__shfl(e, at));
+      const int row0 = first + left * per;
+      return PagedUnit{row0, min(end - row0, per), first, b + at};
+    }
+    left -= __builtin_amdgcn_readfirstlane(__shfl(sum, 63));
+  }
+  return PagedUnit{0, 0, 0, -1};
+}
+
 // Attention of up to 16 CT query columns (a column is a head of a row) over a
 // range of positions of one KV head: a row's own positions (PRE false: the
 // columns are the heads of one row, CT 1), or the positions that a group of rows
@@ -241,41 +275,12 @@ __global__ __launch_bounds__(64 * PG_WAVES) void k_paged_attn(PagedAttn a) {
   const int j = blockIdx.x % a.c.n_kv, split = blockIdx.x / a.c.n_kv % ns, unit = blockIdx.x / a.c.n_kv / ns;
   int row0 = unit, rows = 1, seq, lo = 0, hi;
   if constexpr (PRE) {
-    // the unit-th tile of columns, counted group by group
-    const int per = 16 * CT / G;
-    int left = unit, grp = -1, first = 0;
-    for (int b = 0; b < a.n_groups && grp < 0; b += 64) {
-      const int i = b + lane;
-      int s = 0, e = 0;
-      if (i < a.n_groups) {
-        s = min(max(a.starts[i], 0), a.n);
-        e = min(max(a.starts[i + 1], s), a.n);
-      }
-      int sum = (e - s + per - 1) / per;
-      const int mine = sum;
-      for (int o = 1; o < 64; o <<= 1) {
-        const int v = __shfl_up(sum, o);
-        if (lane >= o) sum += v;
-      }
-      const uint64_t in = __ballot(left < sum);
-      if (in) {
-        const int at = (int)__builtin_ctzll(in);
-        left -= __shfl(sum, at) - __shfl(mine, at);
-        first = __shfl(s, at);
-        rows = __shfl(e, at) - first;
-        grp = b + at;
-      } else {
-        left -= __shfl(sum, 63);
-      }
-    }
-    if (grp < 0) return;
-    grp = __builtin_amdgcn_readfirstlane(grp);
-    first = __builtin_amdgcn_readfirstlane(first);
-    left = __builtin_amdgcn_readfirstlane(left);
-    row0 = first + left * per;
-    rows = min(__builtin_amdgcn_readfirstlane(rows) - left * per, per);
-    seq = paged_seq(a, first);
-    hi = paged_shared(a, grp);
+    const PagedUnit t = paged_unit(a, unit, 16 * CT / G);
+    if (t.group < 0) return;
+    row0 = t.row0;
+    rows = t.rows;
+    seq = paged_seq(a, t.first);
+    hi = __builtin_amdgcn_readfirstlane(paged_shared(a, t.group));
   } else {
     const PagedRow r = paged_row(a, unit);
     seq = __builtin_amdgcn_readfirstlane(r.seq);
@@ -507,31 +512,240 @@ __global__ __launch_bounds__(64 * PG_WAVES) void k_paged_attn(PagedAttn a) {
   }
 }
 
-// A row's partials joined, in the order of their slots.
+// Attention of a tile of query columns over the positions that their group shares,
+// in 16-bit types.  Four waves of 32 columns each share the K and V of 64 positions,
+// which are copied straight into LDS a tile ahead.  Scores are S^T = K Q^T, 32
+// positions x 32 columns: lane (h, c) holds those of positions 8 i + 4 h + 0 .. 3 for
+// column c, and these are its k slots of the second product, O^T += V^T P^T, with
+// the rows of V taken in the same order.  Output row m of tile dt is channel VE m +
+// dt: a lane reads VE = HD / 32 consecutive channels of eight positions.  P enters
+// as hi + lo, as in k_paged_attn.  16-byte chunk j of K's row p lies at chunk j ^ p, so
+// that the 32 rows that a product reads spread over the banks.
+template <int DT, int HD>
+__global__ __launch_bounds__(64 * PG_WAVES, 2) void k_paged_prefix(PagedAttn a) {
+  constexpr int KK = HD / 16, VE = HD / 32, ROW = HD * 2, CHUNKS = ROW / 16;
+  constexpr int TILE = 64, GROUP = 16 * ROW;  // bytes of 16 positions
+  constexpr int PARTS = GROUP / 1024;         // copies of 1 KB of them
+  constexpr int ROWS = 1024 / ROW;            // rows of a copy
+  __shared__ __align__(16) unsigned char s_kv[2][2][TILE * ROW];
+  __shared__ int s_rows[2][4];
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, c = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = a.n_heads / a.c.n_kv;
+  const int j = blockIdx.x % a.c.n_kv, split = blockIdx.x / a.c.n_kv % a.n_pre, unit = blockIdx.x / a.c.n_kv / a.n_pre;
+  const PagedUnit t = paged_unit(a, unit, 32 * PG_WAVES / G);
+  if (t.group < 0) return;
+  const int seq = __builtin_amdgcn_readfirstlane(paged_seq(a, t.first));
+  const int hi = __builtin_amdgcn_readfirstlane(paged_shared(a, t.group));
+  const int cols = t.rows * G;
+  const int per = ((hi + a.n_pre - 1) / a.n_pre + TILE - 1) / TILE * TILE;
+  const int s0 = min((int64_t)hi, (int64_t)split * per), s1 = min((int64_t)hi, (int64_t)s0 + per);
+  const int col = wave * 32 + c;
+  const bool some = wave * 32 < cols;  // whether the wave has columns
+  const int row = t.row0 + col / G, head = j * G + col % G;
+  u32x4 q[KK];
+#pragma unroll
+  for (int k = 0; k < KK; ++k)
+    q[k] = col < cols ? ld16((const char *)a.q + ((int64_t)row * a.ld_q + (int64_t)head * HD) * 2 + k * 32 + h * 16)
+                      : u32x4{0u, 0u, 0u, 0u};
+
+  // wave w copies the tile's positions 16 w .. 16 w + 15
+  const bool known = (uint32_t)seq < (uint32_t)a.c.n_seqs;
+  const int64_t *trow = a.c.table + (known ? (int64_t)seq * a.c.table_ld : 0);
+  const int in_block = (1 << a.c.bt_log2) - 1;
+  const auto lookup = [&](int pos) -> int64_t {  // of the wave's positions of the tile at pos
+    const int p0 = pos + 16 * wave, at = p0 >> a.c.bt_log2;
+    return known && p0 < s1 && at < a.c.table_ld ? trow[at] : -1;
+  };
+  uint32_t k_off[PARTS];
+#pragma unroll
+  for (int i = 0; i < PARTS; ++i) {
+    const int r = i * ROWS + lane / CHUNKS, ch = lane % CHUNKS;  // row of the 16, chunk of LDS
+    k_off[i] = (uint32_t)(r * ROW + (CHUNKS == 16 ? ch ^ r : ch ^ (r >> 1 & 7)) * 16);
+  }
+  const auto copy = [&](int buf, int pos, int64_t num) {
+    const int p0 = pos + 16 * wave;
+    const bool any = (uint64_t)num < (uint64_t)a.c.n_blocks;
+    const int n = any ? min(16, s1 - p0) : 0;
+    const int64_t blk = any ? num : 0, inner = (int64_t)(p0 & in_block) * HD;
+    const char *base = (const char *)a.c.blocks;
+    const uint64_t ka = (uint64_t)(base + (paged_slab(a.c, blk, 0, j, HD) + inner) * 2);
+    const uint64_t va = (uint64_t)(base + (paged_slab(a.c, blk, 1, j, HD) + inner) * 2);
+    const uint32_t bytes = (uint32_t)n * ROW;
+    const u32x4 kr = {(uint32_t)ka, (uint32_t)(ka >> 32) & 0xFFFFu, bytes, (uint32_t)BUF_WORD3};
+    const u32x4 vr = {(uint32_t)va, (uint32_t)(va >> 32) & 0xFFFFu, bytes, (uint32_t)BUF_WORD3};
+    const uint32_t kl = lds_addr(&s_kv[buf][0][wave * GROUP]), vl = lds_addr(&s_kv[buf][1][wave * GROUP]);
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+      dma_1k(kr, k_off[i], 0, kl + i * 1024);
+      dma_1k(vr, (uint32_t)lane * 16, i * 1024, vl + i * 1024);
+    }
+    if (lane == 0) s_rows[buf][wave] = n;
+  };
+
+  const float c2 = a.scale * 1.4426950408889634f;
+  float m = -INFINITY, l = 0.f;
+  f32x16 o[VE];
+#pragma unroll
+  for (int dt = 0; dt < VE; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+  const auto step = [&](int buf) {
+    const unsigned char *kt = s_kv[buf][0], *vt = s_kv[buf][1];
+    const int n0 = s_rows[buf][0], n1 = s_rows[buf][1], n2 = s_rows[buf][2], n3 = s_rows[buf][3];
+    const bool part = __builtin_amdgcn_readfirstlane(n0 + n1 + n2 + n3) < TILE;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f32x16 s;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+      const unsigned char *kp = kt + (u * 32 + c) * ROW;
+      const int sw = CHUNKS == 16 ? c & 15 : c >> 1 & 7;
+#pragma unroll
+      for (int k = 0; k < KK; ++k) s = mma32<DT>(*(const u32x4 *)(kp + (((2 * k + h) ^ sw) * 16)), q[k], s);
+      if (part) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int in16 = 8 * (i / 4 & 1) + 4 * h + i % 4, n = u ? (i < 8 ? n2 : n3) : i < 8 ? n0 : n1;
+          if (in16 >= n) s[i] = -INFINITY;
+        }
+      }
+      float top = s[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+      float bottom = top;
+      if (c2 < 0.f) {
+        bottom = part ? INFINITY : s[0];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) bottom = s[i] == -INFINITY ? bottom : fminf(bottom, s[i]);
+        top = bottom == INFINITY ? -INFINITY : bottom * c2;
+      } else {
+        top = top == -INFINITY ? top : top * c2;
+      }
+      // m is raised only where a score passes it by more than 2^8: o / l does not
+      // depend on it
+      if (__ballot(top > m + 8.f)) {
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float mn = fmaxf(m, top);
+        const float corr = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+        l *= corr;
+#pragma unroll
+        for (int dt = 0; dt < VE; ++dt) o[dt] *= corr;
+        m = mn;
+      }
+      const float ref = m == -INFINITY ? 0.f : m;
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float x = part && s[i] == -INFINITY ? -INFINITY : __builtin_fmaf(s[i], c2, -ref);
+        s[i] = __builtin_amdgcn_exp2f(x);
+        sum += s[i];
+      }
+      l += sum;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {  // 16 positions
+        u32x4 ph, pl;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const float p0 = s[8 * x + 2 * w], p1 = s[8 * x + 2 * w + 1];
+          ph[w] = pack2<DT>(p0, p1);
+          pl[w] = pack2<DT>(p0 - lo_f32<DT>(ph[w]), p1 - hi_f32<DT>(ph[w]));
+        }
+        const unsigned char *vp = vt + (u * 32 + 16 * x + 4 * h) * ROW + c * (VE * 2);
+        uint32_t v[8][VE / 2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const unsigned char *at = vp + (i < 4 ? i : i + 4) * ROW;
+          if constexpr (VE == 4) {
+            const u32x2 two = *(const u32x2 *)at;
+            v[i][0] = two[0];
+            v[i][1] = two[1];
+          } else {
+            v[i][0] = *(const uint32_t *)at;
+          }
+        }
+#pragma unroll
+        for (int dt = 0; dt < VE; ++dt) {
+          const uint32_t sel = dt & 1 ? 0x07060302u : 0x05040100u;
+          u32x4 av;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) av[w] = __builtin_amdgcn_perm(v[2 * w + 1][dt / 2], v[2 * w][dt / 2], sel);
+          o[dt] = mma32<DT>(av, ph, o[dt]);
+          o[dt] = mma32<DT>(av, pl, o[dt]);
+        }
+      }
+    }
+  };
+  int64_t num = lookup(s0);
+  copy(0, s0, num);
+  num = lookup(s0 + TILE);
+  int buf = 0;
+  for (int pos = s0; pos < s1; pos += TILE) {
+    dma_sync<0>();
+    if (pos + TILE < s1) {
+      copy(buf ^ 1, pos + TILE, num);
+      num = lookup(pos + 2 * TILE);
+    }
+    if (some) step(buf);
+    buf ^= 1;
+  }
+  dma_sync<0>();  // (an empty split has copies under way)
+  l += __shfl_xor(l, 32);
+  if (col >= cols) return;
+  const int64_t at = paged_slot(a, row, head, a.n_own + split);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    float *to = a.part_o + at * HD + VE * (8 * (i / 4) + 4 * h + i % 4);
+    if constexpr (VE == 4) *(f32x4 *)to = f32x4{o[0][i], o[1][i], o[2][i], o[3][i]};
+    else *(f32x2 *)to = f32x2{o[0][i], o[1][i]};
+  }
+  if (h == 0) *(f32x2 *)(a.part_ml + at * 2) = f32x2{m, l};
+}
+
+// A row's partials joined, in the order of their slots; a thread takes four channels.
 template <int DT, int HD>
 __global__ __launch_bounds__(256) void k_paged_join(PagedAttn a) {
-  const int row = blockIdx.x;
+  const int heads_wg = 256 / (HD / 4), parts = (a.n_heads + heads_wg - 1) / heads_wg;
+  const int row = blockIdx.x / parts;
+  const int h = blockIdx.x % parts * heads_wg + threadIdx.x / (HD / 4), e = threadIdx.x % (HD / 4) * 4;
   const int slots = paged_row(a, row).grouped ? a.n_own + a.n_pre : a.n_own;
-  for (int x = threadIdx.x; x < a.n_heads * (HD / 4); x += 256) {
-    const int h = x / (HD / 4), e = x % (HD / 4) * 4;
-    const int64_t at = paged_slot(a, row, h, 0);
-    float M = -INFINITY;
-    for (int s = 0; s < slots; ++s) M = fmaxf(M, a.part_ml[(at + s) * 2]);
-    float den = 0.f;
-    f32x4 num = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < slots; ++s) {
-      const float ms = a.part_ml[(at + s) * 2];
-      const float k = ms == M ? 1.f : __builtin_amdgcn_exp2f(ms - M);
-      den += k * a.part_ml[(at + s) * 2 + 1];
-      num += k * *(const f32x4 *)(a.part_o + (at + s) * HD + e);
-    }
-    float f[4];
+  if (h >= a.n_heads) return;
+  const int64_t at = paged_slot(a, row, h, 0);
+  const f32x2 *ml = (const f32x2 *)(a.part_ml + at * 2);
+  const f32x4 *po = (const f32x4 *)(a.part_o + at * HD + e);
+  float M = -INFINITY, den = 0.f;
+  f32x4 num = {0.f, 0.f, 0.f, 0.f};
+  constexpr int U = 8;
+  for (int s0 = 0; s0 < slots; s0 += U) {
+    f32x2 w[U];
+    f32x4 o[U];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = den == 0.f ? 0.f : num[i] / den;
-    const int64_t to = (int64_t)row * a.ld_out + (int64_t)h * HD + e;
-    st_elem2<DT>(a.out, to, f[0], f[1]);
-    st_elem2<DT>(a.out, to + 2, f[2], f[3]);
+    for (int u = 0; u < U; ++u) {
+      const int s = min(s0 + u, slots - 1);
+      w[u] = ml[s];
+      o[u] = po[s * (HD / 4)];
+    }
+    float top = M;
+#pragma unroll
+    for (int u = 0; u < U; ++u) top = fmaxf(top, w[u][0]);
+    const float k0 = M == top ? 1.f : __builtin_amdgcn_exp2f(M - top);
+    M = top;
+    den *= k0;
+    num *= k0;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (s0 + u < slots) {
+        const float k = w[u][0] == M ? 1.f : __builtin_amdgcn_exp2f(w[u][0] - M);
+        den += k * w[u][1];
+        num += k * o[u];
+      }
   }
+  float f[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = den == 0.f ? 0.f : num[i] / den;
+  const int64_t to = (int64_t)row * a.ld_out + (int64_t)h * HD + e;
+  st_elem2<DT>(a.out, to, f[0], f[1]);
+  st_elem2<DT>(a.out, to + 2, f[2], f[3]);
 }
 
 template <int DT, int HD>
@@ -539,12 +753,15 @@ hipError_t attn_launch(const PagedAttn &a, hipStream_t st) {
   const dim3 block(64 * PG_WAVES);
   if (a.n_pre) {
     const dim3 grid((uint32_t)(a.pre_units * a.n_pre * a.c.n_kv));
-    if (a.tile == 16) HS_LAUNCH((k_paged_attn<DT, HD, 1, true>), grid, block, 0, st, a);
-    else if (a.tile == 32) HS_LAUNCH((k_paged_attn<DT, HD, 2, true>), grid, block, 0, st, a);
-    else HS_LAUNCH((k_paged_attn<DT, HD, 4, true>), grid, block, 0, st, a);
+    if constexpr (DT == HS_F32) HS_LAUNCH((k_paged_attn<DT, HD, 2, true>), grid, block, 0, st, a);
+    else HS_LAUNCH((k_paged_prefix<DT, HD>), grid, block, 0, st, a);
   }
   HS_LAUNCH((k_paged_attn<DT, HD, 1, false>), dim3((uint32_t)((int64_t)a.n * a.n_own * a.c.n_kv)), block, 0, st, a);
-  if (a.n_own + a.n_pre > 1) HS_LAUNCH((k_paged_join<DT, HD>), dim3(a.n), dim3(256), 0, st, a);
+  if (a.n_own + a.n_pre > 1) {
+    const int heads_wg = 256 / (HD / 4);
+    const int64_t groups = (int64_t)a.n * ((a.n_heads + heads_wg - 1) / heads_wg);
+    HS_LAUNCH((k_paged_join<DT, HD>), dim3((uint32_t)groups), dim3(256), 0, st, a);
+  }
   return hipGetLastError();
 }
 
@@ -564,28 +781,33 @@ hipError_t append_launch(const PagedRows &a, hipStream_t st) {
 }  // namespace
 
 // columns of a tile, splits of the shared and of the own positions
-void paged_plan(int64_t n, int n_heads, int n_kv, int max_len, int n_groups, int max_shared, PagedAttn *a) {
+void paged_plan(int dtype, int64_t n, int n_heads, int n_kv, int max_len, int n_groups, int max_shared, PagedAttn *a) {
   const int G = n_heads / n_kv;
   a->n_groups = n_groups;
   a->n_pre = a->n_own = 1;
   const int64_t target = 512;  // work groups: two to a CU
-  auto splits = [&](int64_t groups, int64_t positions) {
+  auto splits = [&](int64_t groups, int64_t positions, int64_t least) {
     int64_t s = std::max<int64_t>(1, target / std::max<int64_t>(groups, 1));
-    s = std::min(s, (positions + 2 * PG_STRIPE - 1) / (2 * PG_STRIPE));
+    s = std::min(s, (positions + least - 1) / least);
     return (int)std::min<int64_t>(std::max<int64_t>(s, 1), PAGED_MAX_SPLITS);
   };
   if (n_groups && max_shared > 0) {
-    const int64_t mean = (n + n_groups - 1) / n_groups * G;
-    a->tile = mean <= 16 ? 16 : mean <= 32 ? 32 : 64;
+    a->tile = dtype == HS_F32 ? 32 : 32 * PG_WAVES;
     const int per = a->tile / G;
     a->pre_units = std::min<int64_t>(n, n / per + n_groups);
-    a->n_pre = splits(a->pre_units * n_kv, max_shared);
-    a->n_own = splits(n * n_kv, std::max(1, max_len - max_shared));
+    // groups of one tile each, or one group of many: about so many tiles hold rows
+    const int64_t units = std::max<int64_t>(n_groups, (n + per - 1) / per);
+    a->n_pre = splits(units * n_kv, max_shared, 256);
+    // tiles of a group that read the same positions go to the same XCD (work group
+    // index modulo 8), whose L2 then holds them, where the splits allow it
+    if (units > n_groups && a->n_pre * n_kv > 8)
+      while (a->n_pre > 1 && a->n_pre * n_kv % 8) --a->n_pre;
+    a->n_own = splits(n * n_kv, std::max(1, max_len - max_shared), 256);
   } else {
     a->tile = 16;
     a->pre_units = 0;
     a->n_pre = 0;
-    a->n_own = splits(n * n_kv, max_len);
+    a->n_own = splits(n * n_kv, max_len, 256);
   }
 }
 
