@@ -210,12 +210,13 @@ __device__ __forceinline__ int64_t paged_slot(const PagedAttn &a, int64_t row, i
   return (row * a.n_heads + head) * (a.n_own + a.n_pre) + slot;
 }
 
-// The unit-th tile of a group's rows, `per` rows at most to a tile, counted group by
-// group: its first row, rows, the group's first row and number (-1: there is none).
+// The unit-th tile of columns (the heads of a group's rows that share a KV head, row by
+// row, `per` at most to a tile), counted group by group: the group's first row and
+// number (-1: there is no such tile), the tile's first column and its columns.
 struct PagedUnit {
-  int row0, rows, first, group;
+  int first, group, col0, cols;
 };
-__device__ __forceinline__ PagedUnit paged_unit(const PagedAttn &a, int unit, int per) {
+__device__ __forceinline__ PagedUnit paged_unit(const PagedAttn &a, int unit, int per, int G) {
   const int lane = threadIdx.x & 63;
   int left = unit;
   for (int b = 0; b < a.n_groups; b += 64) {
@@ -225,7 +226,7 @@ __device__ __forceinline__ PagedUnit paged_unit(const PagedAttn &a, int unit, in
       s = min(max(a.starts[i], 0), a.n);
       e = min(max(a.starts[i + 1], s), a.n);
     }
-    int sum = (e - s + per - 1) / per;
+    int sum = ((e - s) * G + per - 1) / per;
     const int mine = sum;
     for (int o = 1; o < 64; o <<= 1) {
       const int v = __shfl_up(sum, o);
@@ -236,12 +237,11 @@ __device__ __forceinline__ PagedUnit paged_unit(const PagedAttn &a, int unit, in
       const int at = (int)__builtin_ctzll(in);
       left -= __builtin_amdgcn_readfirstlane(__shfl(sum, at) - __shfl(mine, at));
       const int first = __builtin_amdgcn_readfirstlane(__shfl(s, at)), end = __builtin_amdgcn_readfirstlane(__shfl(e, at));
-      const int row0 = first + left * per;
-      return PagedUnit{row0, min(end - row0, per), first, b + at};
+      return PagedUnit{first, b + at, left * per, min((end - first) * G - left * per, per)};
     }
     left -= __builtin_amdgcn_readfirstlane(__shfl(sum, 63));
   }
-  return PagedUnit{0, 0, 0, -1};
+  return PagedUnit{0, -1, 0, 0};
 }
 
 // Attention of up to 16 CT query columns (a column is a head of a row) over a
@@ -273,13 +273,14 @@ __global__ __launch_bounds__(64 * PG_WAVES) void k_paged_attn(PagedAttn a) {
   const int G = a.n_heads / a.c.n_kv;
   const int ns = PRE ? a.n_pre : a.n_own;
   const int j = blockIdx.x % a.c.n_kv, split = blockIdx.x / a.c.n_kv % ns, unit = blockIdx.x / a.c.n_kv / ns;
-  int row0 = unit, rows = 1, seq, lo = 0, hi;
+  int first = unit, col0 = 0, cols = G, seq, lo = 0, hi;
   if constexpr (PRE) {
-    const PagedUnit t = paged_unit(a, unit, 16 * CT / G);
+    const PagedUnit t = paged_unit(a, unit, 16 * CT, G);
     if (t.group < 0) return;
-    row0 = t.row0;
-    rows = t.rows;
-    seq = paged_seq(a, t.first);
+    first = t.first;
+    col0 = t.col0;
+    cols = t.cols;
+    seq = paged_seq(a, first);
     hi = __builtin_amdgcn_readfirstlane(paged_shared(a, t.group));
   } else {
     const PagedRow r = paged_row(a, unit);
@@ -288,7 +289,6 @@ __global__ __launch_bounds__(64 * PG_WAVES) void k_paged_attn(PagedAttn a) {
     hi = __builtin_amdgcn_readfirstlane(r.hi);
   }
   seq = __builtin_amdgcn_readfirstlane(seq);
-  const int cols = rows * G;
   // this split's stripes, of whole ones from the tile of the first position on
   const int base = lo & ~15;
   const int per = max(0, (int)((((int64_t)hi - base + ns - 1) / ns + PG_STRIPE - 1) / PG_STRIPE * PG_STRIPE));
@@ -298,8 +298,8 @@ __global__ __launch_bounds__(64 * PG_WAVES) void k_paged_attn(PagedAttn a) {
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
     const int cc = ct * 16 + c;
-    const int r = cc / G, h = j * G + cc - r * G;
-    const char *src = (const char *)a.q + (((int64_t)row0 + r) * a.ld_q + (int64_t)h * HD) * B + g * 16;
+    const int r = (col0 + cc) / G, h = j * G + col0 + cc - r * G;
+    const char *src = (const char *)a.q + (((int64_t)first + r) * a.ld_q + (int64_t)h * HD) * B + g * 16;
 #pragma unroll
     for (int k = 0; k < KCH; ++k) q[ct][k] = cc < cols ? ld16(src + k * 64) : u32x4{0u, 0u, 0u, 0u};
   }
@@ -491,8 +491,8 @@ __global__ __launch_bounds__(64 * PG_WAVES) void k_paged_attn(PagedAttn a) {
         den += k * s_l[w][cc];
         num += k * *(const f32x4 *)&s_o[w][cc][e];
       }
-      const int r = (ct * 16 + cc) / G, h = j * G + ct * 16 + cc - r * G;
-      const int64_t row = row0 + r;
+      const int r = (col0 + ct * 16 + cc) / G, h = j * G + col0 + ct * 16 + cc - r * G;
+      const int64_t row = first + r;
       if (whole) {
         float f[4];
 #pragma unroll
@@ -513,7 +513,7 @@ __global__ __launch_bounds__(64 * PG_WAVES) void k_paged_attn(PagedAttn a) {
 }
 
 // Attention of a tile of query columns over the positions that their group shares,
-// in 16-bit types.  Four waves of 32 columns each share the K and V of 64 positions,
+// in 16-bit types.  The waves, of 32 columns each, share the K and V of 64 positions,
 // which are copied straight into LDS a tile ahead.  Scores are S^T = K Q^T, 32
 // positions x 32 columns: lane (h, c) holds those of positions 8 i + 4 h + 0 .. 3 for
 // column c, and these are its k slots of the second product, O^T += V^T P^T, with
@@ -521,8 +521,8 @@ __global__ __launch_bounds__(64 * PG_WAVES) void k_paged_attn(PagedAttn a) {
 // dt: a lane reads VE = HD / 32 consecutive channels of eight positions.  P enters
 // as hi + lo, as in k_paged_attn.  16-byte chunk j of K's row p lies at chunk j ^ p, so
 // that the 32 rows that a product reads spread over the banks.
-template <int DT, int HD>
-__global__ __launch_bounds__(64 * PG_WAVES, 2) void k_paged_prefix(PagedAttn a) {
+template <int DT, int HD, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void k_paged_prefix(PagedAttn a) {
   constexpr int KK = HD / 16, VE = HD / 32, ROW = HD * 2, CHUNKS = ROW / 16;
   constexpr int TILE = 64, GROUP = 16 * ROW;  // bytes of 16 positions
   constexpr int PARTS = GROUP / 1024;         // copies of 1 KB of them
@@ -533,29 +533,32 @@ __global__ __launch_bounds__(64 * PG_WAVES, 2) void k_paged_prefix(PagedAttn a) 
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int G = a.n_heads / a.c.n_kv;
   const int j = blockIdx.x % a.c.n_kv, split = blockIdx.x / a.c.n_kv % a.n_pre, unit = blockIdx.x / a.c.n_kv / a.n_pre;
-  const PagedUnit t = paged_unit(a, unit, 32 * PG_WAVES / G);
+  const PagedUnit t = paged_unit(a, unit, 32 * WAVES, G);
   if (t.group < 0) return;
   const int seq = __builtin_amdgcn_readfirstlane(paged_seq(a, t.first));
   const int hi = __builtin_amdgcn_readfirstlane(paged_shared(a, t.group));
-  const int cols = t.rows * G;
+  const int cols = t.cols;
   const int per = ((hi + a.n_pre - 1) / a.n_pre + TILE - 1) / TILE * TILE;
   const int s0 = min((int64_t)hi, (int64_t)split * per), s1 = min((int64_t)hi, (int64_t)s0 + per);
   const int col = wave * 32 + c;
   const bool some = wave * 32 < cols;  // whether the wave has columns
-  const int row = t.row0 + col / G, head = j * G + col % G;
+  const int row = t.first + (t.col0 + col) / G, head = j * G + (t.col0 + col) % G;
   u32x4 q[KK];
 #pragma unroll
   for (int k = 0; k < KK; ++k)
     q[k] = col < cols ? ld16((const char *)a.q + ((int64_t)row * a.ld_q + (int64_t)head * HD) * 2 + k * 32 + h * 16)
                       : u32x4{0u, 0u, 0u, 0u};
 
-  // wave w copies the tile's positions 16 w .. 16 w + 15
+  // wave w copies 16 of the tile's positions, K and V of them or, with eight waves, one
   const bool known = (uint32_t)seq < (uint32_t)a.c.n_seqs;
   const int64_t *trow = a.c.table + (known ? (int64_t)seq * a.c.table_ld : 0);
-  const int in_block = (1 << a.c.bt_log2) - 1;
-  const auto lookup = [&](int pos) -> int64_t {  // of the wave's positions of the tile at pos
-    const int p0 = pos + 16 * wave, at = p0 >> a.c.bt_log2;
-    return known && p0 < s1 && at < a.c.table_ld ? trow[at] : -1;
+  const int in_block = (1 << a.c.bt_log2) - 1, part16 = wave & 3;
+  // lane i holds the block of the wave's positions of the i-th tile from pos on (-1: none)
+  const auto blocks64 = [&](int pos) {
+    const int64_t p0 = (int64_t)pos + lane * TILE + 16 * part16, at = p0 >> a.c.bt_log2;
+    int64_t num = -1;
+    if (known && p0 < s1 && at < a.c.table_ld) num = trow[at];
+    return (uint64_t)num < (uint64_t)a.c.n_blocks ? (int)num : -1;
   };
   uint32_t k_off[PARTS];
 #pragma unroll
@@ -563,130 +566,153 @@ __global__ __launch_bounds__(64 * PG_WAVES, 2) void k_paged_prefix(PagedAttn a) 
     const int r = i * ROWS + lane / CHUNKS, ch = lane % CHUNKS;  // row of the 16, chunk of LDS
     k_off[i] = (uint32_t)(r * ROW + (CHUNKS == 16 ? ch ^ r : ch ^ (r >> 1 & 7)) * 16);
   }
-  const auto copy = [&](int buf, int pos, int64_t num) {
-    const int p0 = pos + 16 * wave;
-    const bool any = (uint64_t)num < (uint64_t)a.c.n_blocks;
-    const int n = any ? min(16, s1 - p0) : 0;
-    const int64_t blk = any ? num : 0, inner = (int64_t)(p0 & in_block) * HD;
-    const char *base = (const char *)a.c.blocks;
-    const uint64_t ka = (uint64_t)(base + (paged_slab(a.c, blk, 0, j, HD) + inner) * 2);
-    const uint64_t va = (uint64_t)(base + (paged_slab(a.c, blk, 1, j, HD) + inner) * 2);
+  const auto copy = [&](int buf, int pos, int num) {
+    const int p0 = pos + 16 * part16, n = num >= 0 ? min(16, s1 - p0) : 0;
+    const int64_t blk = max(num, 0), inner = (int64_t)(p0 & in_block) * HD;
     const uint32_t bytes = (uint32_t)n * ROW;
-    const u32x4 kr = {(uint32_t)ka, (uint32_t)(ka >> 32) & 0xFFFFu, bytes, (uint32_t)BUF_WORD3};
-    const u32x4 vr = {(uint32_t)va, (uint32_t)(va >> 32) & 0xFFFFu, bytes, (uint32_t)BUF_WORD3};
-    const uint32_t kl = lds_addr(&s_kv[buf][0][wave * GROUP]), vl = lds_addr(&s_kv[buf][1][wave * GROUP]);
 #pragma unroll
-    for (int i = 0; i < PARTS; ++i) {
-      dma_1k(kr, k_off[i], 0, kl + i * 1024);
-      dma_1k(vr, (uint32_t)lane * 16, i * 1024, vl + i * 1024);
+    for (int sel = 0; sel < 2; ++sel) {
+      if (WAVES == 8 && wave / 4 != sel) continue;
+      const uint64_t at = (uint64_t)((const char *)a.c.blocks + (paged_slab(a.c, blk, sel, j, HD) + inner) * 2);
+      const u32x4 r = {(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, bytes, (uint32_t)BUF_WORD3};
+      const uint32_t to = lds_addr(&s_kv[buf][sel][part16 * GROUP]);
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i)
+        if (sel) dma_1k(r, (uint32_t)lane * 16, i * 1024, to + i * 1024);
+        else dma_1k(r, k_off[i], 0, to + i * 1024);
     }
-    if (lane == 0) s_rows[buf][wave] = n;
+    if (lane == 0 && wave < 4) s_rows[buf][wave] = n;
   };
 
-  const float c2 = a.scale * 1.4426950408889634f;
+  // the scale's sign goes into the queries, so that the largest product has the largest
+  // score; of scale 0 the queries are zeros
+  float c2 = a.scale * 1.4426950408889634f;
+  if (!(c2 > 0.f)) {
+#pragma unroll
+    for (int k = 0; k < KK; ++k)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) q[k][w] = c2 == 0.f ? 0u : q[k][w] ^ 0x80008000u;
+    c2 = c2 == 0.f ? 1.f : -c2;
+  }
   float m = -INFINITY, l = 0.f;
   f32x16 o[VE];
 #pragma unroll
   for (int dt = 0; dt < VE; ++dt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
-  const auto step = [&](int buf) {
+  // `part`: some of the tile's positions have no rows
+  const auto step = [&](int buf, auto part) {
     const unsigned char *kt = s_kv[buf][0], *vt = s_kv[buf][1];
-    const int n0 = s_rows[buf][0], n1 = s_rows[buf][1], n2 = s_rows[buf][2], n3 = s_rows[buf][3];
-    const bool part = __builtin_amdgcn_readfirstlane(n0 + n1 + n2 + n3) < TILE;
+    // chunk 2 k + h of row c, at its place; made anew for every tile, not kept in registers
+    int first = (h ^ (CHUNKS == 16 ? c & 15 : c >> 1 & 7)) * 16 + c * ROW;
+    asm volatile("" : "+v"(first));
+    f32x16 s[2];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      f32x16 s;
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
-      const unsigned char *kp = kt + (u * 32 + c) * ROW;
-      const int sw = CHUNKS == 16 ? c & 15 : c >> 1 & 7;
+      for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
 #pragma unroll
-      for (int k = 0; k < KK; ++k) s = mma32<DT>(*(const u32x4 *)(kp + (((2 * k + h) ^ sw) * 16)), q[k], s);
-      if (part) {
+    for (int k = 0; k < KK; ++k)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int in16 = 8 * (i / 4 & 1) + 4 * h + i % 4, n = u ? (i < 8 ? n2 : n3) : i < 8 ? n0 : n1;
-          if (in16 >= n) s[i] = -INFINITY;
-        }
-      }
-      float top = s[0];
+      for (int u = 0; u < 2; ++u) s[u] = mma32<DT>(*(const u32x4 *)(kt + u * 32 * ROW + (first ^ (k * 32))), q[k], s[u]);
+    if constexpr (part) {
 #pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-      float bottom = top;
-      if (c2 < 0.f) {
-        bottom = part ? INFINITY : s[0];
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) bottom = s[i] == -INFINITY ? bottom : fminf(bottom, s[i]);
-        top = bottom == INFINITY ? -INFINITY : bottom * c2;
-      } else {
-        top = top == -INFINITY ? top : top * c2;
-      }
-      // m is raised only where a score passes it by more than 2^8: o / l does not
-      // depend on it
-      if (__ballot(top > m + 8.f)) {
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float mn = fmaxf(m, top);
-        const float corr = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);
-        l *= corr;
+        for (int i = 0; i < 16; ++i)
+          if (8 * (i / 4 & 1) + 4 * h + i % 4 >= s_rows[buf][2 * u + i / 8]) s[u][i] = -INFINITY;
+    }
+    // scores less m, which is raised only where one passes it by more than 2^8 (or there
+    // is none yet): o / l does not depend on it
+    const float ref = m == -INFINITY ? 0.f : m;
+    float top = -INFINITY;
 #pragma unroll
-        for (int dt = 0; dt < VE; ++dt) o[dt] *= corr;
-        m = mn;
-      }
-      const float ref = m == -INFINITY ? 0.f : m;
-      float sum = 0.f;
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float x = part && s[i] == -INFINITY ? -INFINITY : __builtin_fmaf(s[i], c2, -ref);
-        s[i] = __builtin_amdgcn_exp2f(x);
-        sum += s[i];
+        s[u][i] = __builtin_fmaf(s[u][i], c2, -ref);
+        top = fmaxf(top, s[u][i]);
+      }
+    if (__ballot(top > 8.f || m == -INFINITY)) {
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float mn = fmaxf(m, ref + top), up = mn == -INFINITY ? 0.f : mn - ref;
+      const float corr = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      l *= corr;
+#pragma unroll
+      for (int dt = 0; dt < VE; ++dt) o[dt] *= corr;
+      m = mn;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[u][i] -= up;
+    }
+    u32x4 ph, pl;
+    const auto parts = [&](int x) {  // of 16 positions
+      float sum = 0.f;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const float p0 = __builtin_amdgcn_exp2f(s[x / 2][8 * (x & 1) + 2 * y]);
+        const float p1 = __builtin_amdgcn_exp2f(s[x / 2][8 * (x & 1) + 2 * y + 1]);
+        sum += p0 + p1;
+        ph[y] = pack2<DT>(p0, p1);
+        pl[y] = pack2<DT>(p0 - lo_f32<DT>(ph[y]), p1 - hi_f32<DT>(ph[y]));
       }
       l += sum;
+    };
+    parts(0);
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {  // 16 positions
-        u32x4 ph, pl;
+    for (int x = 0; x < 4; ++x) {
+      const u32x4 hi_x = ph, lo_x = pl;
+      const unsigned char *vp = vt + (16 * x + 4 * h) * ROW + c * (VE * 2);
+      uint32_t v[8][VE / 2];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const float p0 = s[8 * x + 2 * w], p1 = s[8 * x + 2 * w + 1];
-          ph[w] = pack2<DT>(p0, p1);
-          pl[w] = pack2<DT>(p0 - lo_f32<DT>(ph[w]), p1 - hi_f32<DT>(ph[w]));
-        }
-        const unsigned char *vp = vt + (u * 32 + 16 * x + 4 * h) * ROW + c * (VE * 2);
-        uint32_t v[8][VE / 2];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const unsigned char *at = vp + (i < 4 ? i : i + 4) * ROW;
-          if constexpr (VE == 4) {
-            const u32x2 two = *(const u32x2 *)at;
-            v[i][0] = two[0];
-            v[i][1] = two[1];
-          } else {
-            v[i][0] = *(const uint32_t *)at;
-          }
-        }
-#pragma unroll
-        for (int dt = 0; dt < VE; ++dt) {
-          const uint32_t sel = dt & 1 ? 0x07060302u : 0x05040100u;
-          u32x4 av;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) av[w] = __builtin_amdgcn_perm(v[2 * w + 1][dt / 2], v[2 * w][dt / 2], sel);
-          o[dt] = mma32<DT>(av, ph, o[dt]);
-          o[dt] = mma32<DT>(av, pl, o[dt]);
+      for (int i = 0; i < 8; ++i) {
+        const unsigned char *at = vp + (i < 4 ? i : i + 4) * ROW;
+        if constexpr (VE == 4) {
+          const u32x2 two = *(const u32x2 *)at;
+          v[i][0] = two[0];
+          v[i][1] = two[1];
+        } else {
+          v[i][0] = *(const uint32_t *)at;
         }
       }
+      if (x < 3) parts(x + 1);
+      u32x4 av[VE];
+#pragma unroll
+      for (int dt = 0; dt < VE; ++dt) {
+        const uint32_t sel = dt & 1 ? 0x07060302u : 0x05040100u;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) av[dt][y] = __builtin_amdgcn_perm(v[2 * y + 1][dt / 2], v[2 * y][dt / 2], sel);
+      }
+#pragma unroll
+      for (int dt = 0; dt < VE; ++dt) o[dt] = mma32<DT>(av[dt], hi_x, o[dt]);
+#pragma unroll
+      for (int dt = 0; dt < VE; ++dt) o[dt] = mma32<DT>(av[dt], lo_x, o[dt]);
+      // the vector unit works on the next weights while the matrix cores multiply: a
+      // product, then what fits behind it
+#pragma unroll
+      for (int i = 0; i < 2 * VE; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, 6, 0);
+        __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
-  int64_t num = lookup(s0);
-  copy(0, s0, num);
-  num = lookup(s0 + TILE);
+  int nums = blocks64(s0), tile = 0;
+  copy(0, s0, __builtin_amdgcn_readlane(nums, 0));
   int buf = 0;
   for (int pos = s0; pos < s1; pos += TILE) {
     dma_sync<0>();
     if (pos + TILE < s1) {
-      copy(buf ^ 1, pos + TILE, num);
-      num = lookup(pos + 2 * TILE);
+      if ((++tile & 63) == 0) nums = blocks64(pos + TILE);
+      copy(buf ^ 1, pos + TILE, __builtin_amdgcn_readlane(nums, tile & 63));
     }
-    if (some) step(buf);
+    if (some) {
+      const int rows = s_rows[buf][0] + s_rows[buf][1] + s_rows[buf][2] + s_rows[buf][3];
+      if (__builtin_amdgcn_readfirstlane(rows) == TILE) step(buf, std::false_type{});
+      else step(buf, std::true_type{});
+    }
     buf ^= 1;
   }
   dma_sync<0>();  // (an empty split has copies under way)
@@ -754,7 +780,8 @@ hipError_t attn_launch(const PagedAttn &a, hipStream_t st) {
   if (a.n_pre) {
     const dim3 grid((uint32_t)(a.pre_units * a.n_pre * a.c.n_kv));
     if constexpr (DT == HS_F32) HS_LAUNCH((k_paged_attn<DT, HD, 2, true>), grid, block, 0, st, a);
-    else HS_LAUNCH((k_paged_prefix<DT, HD>), grid, block, 0, st, a);
+    else if (a.tile == 256) HS_LAUNCH((k_paged_prefix<DT, HD, 8>), grid, dim3(512), 0, st, a);
+    else HS_LAUNCH((k_paged_prefix<DT, HD, 4>), grid, block, 0, st, a);
   }
   HS_LAUNCH((k_paged_attn<DT, HD, 1, false>), dim3((uint32_t)((int64_t)a.n * a.n_own * a.c.n_kv)), block, 0, st, a);
   if (a.n_own + a.n_pre > 1) {
@@ -792,16 +819,21 @@ void paged_plan(int dtype, int64_t n, int n_heads, int n_kv, int max_len, int n_
     return (int)std::min<int64_t>(std::max<int64_t>(s, 1), PAGED_MAX_SPLITS);
   };
   if (n_groups && max_shared > 0) {
-    a->tile = dtype == HS_F32 ? 32 : 32 * PG_WAVES;
-    const int per = a->tile / G;
-    a->pre_units = std::min<int64_t>(n, n / per + n_groups);
-    // groups of one tile each, or one group of many: about so many tiles hold rows
-    const int64_t units = std::max<int64_t>(n_groups, (n + per - 1) / per);
-    a->n_pre = splits(units * n_kv, max_shared, 256);
+    // eight waves where most groups fill them: each K and V tile is then copied once for
+    // twice the columns
+    a->tile = dtype == HS_F32 ? 32 : n * G > (int64_t)n_groups * 192 ? 256 : 128;
+    a->pre_units = std::min<int64_t>(n, n * G / a->tile + n_groups);
+    // groups of one tile each, or one group of many: about so many tiles hold columns
+    const int64_t units = std::max<int64_t>(n_groups, (n * G + a->tile - 1) / a->tile);
+    a->n_pre = splits(units * n_kv * (a->tile == 256 ? 2 : 1), max_shared, 256);
     // tiles of a group that read the same positions go to the same XCD (work group
-    // index modulo 8), whose L2 then holds them, where the splits allow it
-    if (units > n_groups && a->n_pre * n_kv > 8)
-      while (a->n_pre > 1 && a->n_pre * n_kv % 8) --a->n_pre;
+    // index modulo 8), whose L2 then holds them, where that leaves nine tenths of the
+    // work groups
+    if (units > n_groups) {
+      int s = a->n_pre;
+      while (s > 1 && s * n_kv % 8) --s;
+      if (s * n_kv % 8 == 0 && s * 10 >= a->n_pre * 9) a->n_pre = s;
+    }
     a->n_own = splits(n * n_kv, std::max(1, max_len - max_shared), 256);
   } else {
     a->tile = 16;
