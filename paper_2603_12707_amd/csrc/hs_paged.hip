@@ -212,20 +212,24 @@ __device__ __forceinline__ int64_t paged_slot(const PagedAttn &a, int64_t row, i
 
 // The unit-th tile of columns (the heads of a group's rows that share a KV head, row by
 // row, `per` at most to a tile), counted group by group: the group's first row and
-// number (-1: there is no such tile), the tile's first column and its columns.
+// number (-1: there is no such tile), the tile's first column and its columns, and
+// the positions that the group, and that any group, shares.
 struct PagedUnit {
-  int first, group, col0, cols;
+  int first, group, col0, cols, shared, longest;
 };
 __device__ __forceinline__ PagedUnit paged_unit(const PagedAttn &a, int unit, int per, int G) {
   const int lane = threadIdx.x & 63;
-  int left = unit;
+  PagedUnit u{0, -1, 0, 0, 0, 0};
+  int left = unit, longest = 0;
   for (int b = 0; b < a.n_groups; b += 64) {
     const int i = b + lane;
-    int s = 0, e = 0;
+    int s = 0, e = 0, shared = 0;
     if (i < a.n_groups) {
       s = min(max(a.starts[i], 0), a.n);
       e = min(max(a.starts[i + 1], s), a.n);
+      shared = paged_shared(a, i);
     }
+    longest = max(longest, shared);
     int sum = ((e - s) * G + per - 1) / per;
     const int mine = sum;
     for (int o = 1; o < 64; o <<= 1) {
@@ -233,15 +237,20 @@ __device__ __forceinline__ PagedUnit paged_unit(const PagedAttn &a, int unit, in
       if (lane >= o) sum += v;
     }
     const uint64_t in = __ballot(left < sum);
-    if (in) {
+    if (in && u.group < 0) {
       const int at = (int)__builtin_ctzll(in);
       left -= __builtin_amdgcn_readfirstlane(__shfl(sum, at) - __shfl(mine, at));
-      const int first = __builtin_amdgcn_readfirstlane(__shfl(s, at)), end = __builtin_amdgcn_readfirstlane(__shfl(e, at));
-      return PagedUnit{first, b + at, left * per, min((end - first) * G - left * per, per)};
+      u.first = __builtin_amdgcn_readfirstlane(__shfl(s, at));
+      u.group = b + at;
+      u.col0 = left * per;
+      u.cols = min((__builtin_amdgcn_readfirstlane(__shfl(e, at)) - u.first) * G - u.col0, per);
+      u.shared = __builtin_amdgcn_readfirstlane(__shfl(shared, at));
     }
     left -= __builtin_amdgcn_readfirstlane(__shfl(sum, 63));
   }
-  return PagedUnit{0, -1, 0, 0};
+  for (int o = 32; o; o >>= 1) longest = max(longest, __shfl_xor(longest, o));
+  u.longest = __builtin_amdgcn_readfirstlane(longest);
+  return u;
 }
 
 // Attention of up to 16 CT query columns (a column is a head of a row) over a
@@ -273,7 +282,7 @@ __global__ __launch_bounds__(64 * PG_WAVES) void k_paged_attn(PagedAttn a) {
   const int G = a.n_heads / a.c.n_kv;
   const int ns = PRE ? a.n_pre : a.n_own;
   const int j = blockIdx.x % a.c.n_kv, split = blockIdx.x / a.c.n_kv % ns, unit = blockIdx.x / a.c.n_kv / ns;
-  int first = unit, col0 = 0, cols = G, seq, lo = 0, hi;
+  int first = unit, col0 = 0, cols = G, seq, lo = 0, hi, total;
   if constexpr (PRE) {
     const PagedUnit t = paged_unit(a, unit, 16 * CT, G);
     if (t.group < 0) return;
@@ -281,17 +290,20 @@ __global__ __launch_bounds__(64 * PG_WAVES) void k_paged_attn(PagedAttn a) {
     col0 = t.col0;
     cols = t.cols;
     seq = paged_seq(a, first);
-    hi = __builtin_amdgcn_readfirstlane(paged_shared(a, t.group));
+    hi = t.shared;
+    total = t.longest;
   } else {
     const PagedRow r = paged_row(a, unit);
     seq = __builtin_amdgcn_readfirstlane(r.seq);
     lo = __builtin_amdgcn_readfirstlane(r.lo);
     hi = __builtin_amdgcn_readfirstlane(r.hi);
+    total = hi - (lo & ~15);
   }
   seq = __builtin_amdgcn_readfirstlane(seq);
-  // this split's stripes, of whole ones from the tile of the first position on
+  // this split's stripes, of whole ones from the tile of the first position on; groups
+  // are cut at equal lengths, so that all splits of long and short ones are alike
   const int base = lo & ~15;
-  const int per = max(0, (int)((((int64_t)hi - base + ns - 1) / ns + PG_STRIPE - 1) / PG_STRIPE * PG_STRIPE));
+  const int per = max(0, (int)((((int64_t)total + ns - 1) / ns + PG_STRIPE - 1) / PG_STRIPE * PG_STRIPE));
   const int s0 = (int)min((int64_t)hi, base + (int64_t)split * per), s1 = (int)min((int64_t)hi, (int64_t)s0 + per);
 
   u32x4 q[CT][KCH];
@@ -521,8 +533,11 @@ __global__ __launch_bounds__(64 * PG_WAVES) void k_paged_attn(PagedAttn a) {
 // dt: a lane reads VE = HD / 32 consecutive channels of eight positions.  P enters
 // as hi + lo, as in k_paged_attn.  16-byte chunk j of K's row p lies at chunk j ^ p, so
 // that the 32 rows that a product reads spread over the banks.
-template <int DT, int HD, int WAVES>
+// Few columns (HALVES 2: 64 at most) are two waves' each; the other two take the same
+// columns over the other half of each tile, and the halves are joined in LDS.
+template <int DT, int HD, int WAVES, int HALVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void k_paged_prefix(PagedAttn a) {
+  constexpr int NU = 2 / HALVES;  // runs of 32 positions that a wave takes of a tile
   constexpr int KK = HD / 16, VE = HD / 32, ROW = HD * 2, CHUNKS = ROW / 16;
   constexpr int TILE = 64, GROUP = 16 * ROW;  // bytes of 16 positions
   constexpr int PARTS = GROUP / 1024;         // copies of 1 KB of them
@@ -533,15 +548,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_paged_prefix(PagedAttn a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int G = a.n_heads / a.c.n_kv;
   const int j = blockIdx.x % a.c.n_kv, split = blockIdx.x / a.c.n_kv % a.n_pre, unit = blockIdx.x / a.c.n_kv / a.n_pre;
-  const PagedUnit t = paged_unit(a, unit, 32 * WAVES, G);
+  const PagedUnit t = paged_unit(a, unit, 32 * WAVES / HALVES, G);
   if (t.group < 0) return;
   const int seq = __builtin_amdgcn_readfirstlane(paged_seq(a, t.first));
-  const int hi = __builtin_amdgcn_readfirstlane(paged_shared(a, t.group));
-  const int cols = t.cols;
-  const int per = ((hi + a.n_pre - 1) / a.n_pre + TILE - 1) / TILE * TILE;
+  const int hi = t.shared, cols = t.cols;
+  // (groups are cut at equal lengths, so that all splits of long and short ones are alike)
+  const int per = ((t.longest + a.n_pre - 1) / a.n_pre + TILE - 1) / TILE * TILE;
   const int s0 = min((int64_t)hi, (int64_t)split * per), s1 = min((int64_t)hi, (int64_t)s0 + per);
-  const int col = wave * 32 + c;
-  const bool some = wave * 32 < cols;  // whether the wave has columns
+  const int mine = HALVES == 2 ? wave & 1 : wave, u0 = HALVES == 2 ? wave >> 1 : 0;  // columns, first run
+  const int col = mine * 32 + c;
+  const bool some = mine * 32 < cols;  // whether the wave has columns
   const int row = t.first + (t.col0 + col) / G, head = j * G + (t.col0 + col) % G;
   u32x4 q[KK];
 #pragma unroll
@@ -602,32 +618,32 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_paged_prefix(PagedAttn a) {
     for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
   // `part`: some of the tile's positions have no rows
   const auto step = [&](int buf, auto part) {
-    const unsigned char *kt = s_kv[buf][0], *vt = s_kv[buf][1];
+    const unsigned char *kt = s_kv[buf][0] + u0 * 32 * ROW, *vt = s_kv[buf][1] + u0 * 32 * ROW;
     // chunk 2 k + h of row c, at its place; made anew for every tile, not kept in registers
     int first = (h ^ (CHUNKS == 16 ? c & 15 : c >> 1 & 7)) * 16 + c * ROW;
     asm volatile("" : "+v"(first));
-    f32x16 s[2];
+    f32x16 s[NU];
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < NU; ++u)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
 #pragma unroll
     for (int k = 0; k < KK; ++k)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) s[u] = mma32<DT>(*(const u32x4 *)(kt + u * 32 * ROW + (first ^ (k * 32))), q[k], s[u]);
+      for (int u = 0; u < NU; ++u) s[u] = mma32<DT>(*(const u32x4 *)(kt + u * 32 * ROW + (first ^ (k * 32))), q[k], s[u]);
     if constexpr (part) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < NU; ++u)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (8 * (i / 4 & 1) + 4 * h + i % 4 >= s_rows[buf][2 * u + i / 8]) s[u][i] = -INFINITY;
+          if (8 * (i / 4 & 1) + 4 * h + i % 4 >= s_rows[buf][2 * (u0 + u) + i / 8]) s[u][i] = -INFINITY;
     }
     // scores less m, which is raised only where one passes it by more than 2^8 (or there
     // is none yet): o / l does not depend on it
     const float ref = m == -INFINITY ? 0.f : m;
     float top = -INFINITY;
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < NU; ++u)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         s[u][i] = __builtin_fmaf(s[u][i], c2, -ref);
@@ -642,7 +658,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_paged_prefix(PagedAttn a) {
       for (int dt = 0; dt < VE; ++dt) o[dt] *= corr;
       m = mn;
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < NU; ++u)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[u][i] -= up;
     }
@@ -661,7 +677,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_paged_prefix(PagedAttn a) {
     };
     parts(0);
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
+    for (int x = 0; x < 2 * NU; ++x) {
       const u32x4 hi_x = ph, lo_x = pl;
       const unsigned char *vp = vt + (16 * x + 4 * h) * ROW + c * (VE * 2);
       uint32_t v[8][VE / 2];
@@ -676,7 +692,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_paged_prefix(PagedAttn a) {
           v[i][0] = *(const uint32_t *)at;
         }
       }
-      if (x < 3) parts(x + 1);
+      if (x < 2 * NU - 1) parts(x + 1);
       u32x4 av[VE];
 #pragma unroll
       for (int dt = 0; dt < VE; ++dt) {
@@ -717,6 +733,33 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_paged_prefix(PagedAttn a) {
   }
   dma_sync<0>();  // (an empty split has copies under way)
   l += __shfl_xor(l, 32);
+  if constexpr (HALVES == 2) {
+    f32x4 *half = (f32x4 *)&s_kv[0][0][0] + mine * 64 + lane;  // a wave's 16 bytes a lane, 128 lanes apart
+    f32x2 *half_ml = (f32x2 *)((f32x4 *)&s_kv[0][0][0] + 4 * VE * 128) + mine * 64 + lane;
+    static_assert((4 * VE * 16 + 8) * 128 <= sizeof(s_kv), "the halves fit");
+    if (u0) {
+#pragma unroll
+      for (int dt = 0; dt < VE; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) half[(dt * 4 + i / 4) * 128] = f32x4{o[dt][i], o[dt][i + 1], o[dt][i + 2], o[dt][i + 3]};
+      *half_ml = f32x2{m, l};
+    }
+    __syncthreads();
+    if (u0) return;
+    const f32x2 other = *half_ml;
+    const float top = fmaxf(m, other[0]);
+    const float k0 = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top), k1 = other[0] == top ? 1.f : __builtin_amdgcn_exp2f(other[0] - top);
+    m = top;
+    l = k0 * l + k1 * other[1];
+#pragma unroll
+    for (int dt = 0; dt < VE; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const f32x4 y = half[(dt * 4 + i / 4) * 128];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[dt][i + e] = k0 * o[dt][i + e] + k1 * y[e];
+      }
+  }
   if (col >= cols) return;
   const int64_t at = paged_slot(a, row, head, a.n_own + split);
 #pragma unroll
@@ -780,8 +823,9 @@ hipError_t attn_launch(const PagedAttn &a, hipStream_t st) {
   if (a.n_pre) {
     const dim3 grid((uint32_t)(a.pre_units * a.n_pre * a.c.n_kv));
     if constexpr (DT == HS_F32) HS_LAUNCH((k_paged_attn<DT, HD, 2, true>), grid, block, 0, st, a);
-    else if (a.tile == 256) HS_LAUNCH((k_paged_prefix<DT, HD, 8>), grid, dim3(512), 0, st, a);
-    else HS_LAUNCH((k_paged_prefix<DT, HD, 4>), grid, block, 0, st, a);
+    else if (a.tile == 256) HS_LAUNCH((k_paged_prefix<DT, HD, 8, 1>), grid, dim3(512), 0, st, a);
+    else if (a.tile == 128) HS_LAUNCH((k_paged_prefix<DT, HD, 4, 1>), grid, block, 0, st, a);
+    else HS_LAUNCH((k_paged_prefix<DT, HD, 4, 2>), grid, block, 0, st, a);
   }
   HS_LAUNCH((k_paged_attn<DT, HD, 1, false>), dim3((uint32_t)((int64_t)a.n * a.n_own * a.c.n_kv)), block, 0, st, a);
   if (a.n_own + a.n_pre > 1) {
@@ -812,8 +856,10 @@ void paged_plan(int dtype, int64_t n, int n_heads, int n_kv, int max_len, int n_
   const int G = n_heads / n_kv;
   a->n_groups = n_groups;
   a->n_pre = a->n_own = 1;
-  const int64_t target = 512;  // work groups: two to a CU
+  // work groups: two to a CU.  (Four times as many splits of the own positions took 33 us
+  // against 29 for 67 rows of 1..1664, 29 against 23 for 32 rows of 32..384)
   auto splits = [&](int64_t groups, int64_t positions, int64_t least) {
+    const int64_t target = 512;
     int64_t s = std::max<int64_t>(1, target / std::max<int64_t>(groups, 1));
     s = std::min(s, (positions + least - 1) / least);
     return (int)std::min<int64_t>(std::max<int64_t>(s, 1), PAGED_MAX_SPLITS);
@@ -821,11 +867,13 @@ void paged_plan(int dtype, int64_t n, int n_heads, int n_kv, int max_len, int n_
   if (n_groups && max_shared > 0) {
     // eight waves where most groups fill them: each K and V tile is then copied once for
     // twice the columns
-    a->tile = dtype == HS_F32 ? 32 : n * G > (int64_t)n_groups * 192 ? 256 : 128;
+    const int64_t mean = (n * G + n_groups - 1) / n_groups;
+    a->tile = dtype == HS_F32 ? 32 : mean > 192 ? 256 : mean > 64 ? 128 : 64;
     a->pre_units = std::min<int64_t>(n, n * G / a->tile + n_groups);
     // groups of one tile each, or one group of many: about so many tiles hold columns
     const int64_t units = std::max<int64_t>(n_groups, (n * G + a->tile - 1) / a->tile);
-    a->n_pre = splits(units * n_kv * (a->tile == 256 ? 2 : 1), max_shared, 256);
+    // (several groups are of several lengths: twice the splits, of which some are empty)
+    a->n_pre = splits((units * n_kv * (a->tile == 256 ? 2 : 1) + (n_groups > 1)) / (n_groups > 1 ? 2 : 1), max_shared, 256);
     // tiles of a group that read the same positions go to the same XCD (work group
     // index modulo 8), whose L2 then holds them, where that leaves nine tenths of the
     // work groups
