@@ -158,15 +158,6 @@ __global__ __launch_bounds__(APPEND_THREADS) void k_paged_append(PagedRows a, in
 constexpr int PG_WAVES = 4;
 constexpr int PG_STRIPE = PG_WAVES * 32;  // positions that a work group takes at a time
 
-// the group of a row: starts[g] <= row < starts[g + 1] (-1: none), by every lane of the wave
-__device__ __forceinline__ int paged_group(const PagedAttn &a, int row) {
-  int n = 0;
-  for (int b = 0; b <= a.n_groups; b += 64) {
-    const int i = b + (int)(threadIdx.x & 63);
-    n += (int)__popcll(__ballot(i <= a.n_groups && a.starts[min(i, a.n_groups)] <= row));
-  }
-  return n >= 1 && n <= a.n_groups ? n - 1 : -1;
-}
 __device__ __forceinline__ int paged_most(const PagedRef &c) {
   return (int)min((int64_t)c.table_ld << c.bt_log2, (int64_t)INT32_MAX);
 }
@@ -191,15 +182,20 @@ __device__ __forceinline__ PagedRow paged_row(const PagedAttn &a, int row) {
   r.lo = 0;
   r.hi = paged_length(a, row, r.seq);
   r.grouped = false;
-  const int g = a.n_groups ? paged_group(a, row) : -1;
-  if (g >= 0) {
-    const int sh = paged_shared(a, g);
+  // its group: starts[g] <= row < starts[g + 1]
+  const int lane = threadIdx.x & 63;
+  for (int b = 0; b < a.n_groups; b += 64) {
+    const int i = min(b + lane, a.n_groups - 1), start = a.starts[i], end = a.starts[i + 1], shared = paged_shared(a, i);
+    const uint64_t in = __ballot(b + lane < a.n_groups && start <= row && row < end);
+    if (!in) continue;
+    const int at = (int)__builtin_ctzll(in), sh = __shfl(shared, at), first = __shfl(start, at);
     if (sh > 0 && r.hi >= sh) {
       r.lo = sh;
       r.grouped = true;
     } else if (sh > 0) {
-      r.seq = paged_seq(a, min(max(a.starts[g], 0), a.n - 1));
+      r.seq = paged_seq(a, min(max(first, 0), a.n - 1));
     }
+    break;
   }
   return r;
 }
@@ -269,19 +265,23 @@ __device__ __forceinline__ PagedUnit paged_unit(const PagedAttn &a, int unit, in
 //
 // Loads go through buffer descriptors made for a tile of 16 positions, which
 // end where the positions do: what lies past them reads as zeros.
+template <int HD>
+struct AttnLds {
+  __align__(16) float o[PG_WAVES][16][HD + 4];
+  float m[PG_WAVES][16], l[PG_WAVES][16];
+};
 template <int DT, int HD, int CT, bool PRE>
-__global__ __launch_bounds__(64 * PG_WAVES) void k_paged_attn(PagedAttn a) {
+__device__ __forceinline__ void attn_columns(const PagedAttn &a, uint32_t block, AttnLds<HD> &lds) {
   constexpr int B = DT == HS_F32 ? 4 : 2;
   constexpr int KCH = HD * B / 64;  // 16-byte chunks of a K row's quarter
   constexpr int VE = HD / 16, VW = VE * B / 4;  // channels of a lane, and their words
-  constexpr int PITCH = HD + 4;
-  __shared__ __align__(16) float s_o[PG_WAVES][16][PITCH];
-  __shared__ float s_m[PG_WAVES][16], s_l[PG_WAVES][16];
+  auto &s_o = lds.o;
+  auto &s_m = lds.m, &s_l = lds.l;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int G = a.n_heads / a.c.n_kv;
   const int ns = PRE ? a.n_pre : a.n_own;
-  const int j = blockIdx.x % a.c.n_kv, split = blockIdx.x / a.c.n_kv % ns, unit = blockIdx.x / a.c.n_kv / ns;
+  const int j = block % a.c.n_kv, split = block / a.c.n_kv % ns, unit = block / a.c.n_kv / ns;
   int first = unit, col0 = 0, cols = G, seq, lo = 0, hi, total;
   if constexpr (PRE) {
     const PagedUnit t = paged_unit(a, unit, 16 * CT, G);
@@ -535,19 +535,24 @@ __global__ __launch_bounds__(64 * PG_WAVES) void k_paged_attn(PagedAttn a) {
 // that the 32 rows that a product reads spread over the banks.
 // Few columns (HALVES 2: 64 at most) are two waves' each; the other two take the same
 // columns over the other half of each tile, and the halves are joined in LDS.
+template <int HD>
+struct SharedLds {
+  __align__(16) unsigned char kv[2][2][64 * HD * 2];
+  int rows[2][4];
+};
 template <int DT, int HD, int WAVES, int HALVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void k_paged_prefix(PagedAttn a) {
+__device__ __forceinline__ void shared_columns(const PagedAttn &a, uint32_t block, SharedLds<HD> &lds) {
   constexpr int NU = 2 / HALVES;  // runs of 32 positions that a wave takes of a tile
   constexpr int KK = HD / 16, VE = HD / 32, ROW = HD * 2, CHUNKS = ROW / 16;
   constexpr int TILE = 64, GROUP = 16 * ROW;  // bytes of 16 positions
   constexpr int PARTS = GROUP / 1024;         // copies of 1 KB of them
   constexpr int ROWS = 1024 / ROW;            // rows of a copy
-  __shared__ __align__(16) unsigned char s_kv[2][2][TILE * ROW];
-  __shared__ int s_rows[2][4];
+  auto &s_kv = lds.kv;
+  auto &s_rows = lds.rows;
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, c = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int G = a.n_heads / a.c.n_kv;
-  const int j = blockIdx.x % a.c.n_kv, split = blockIdx.x / a.c.n_kv % a.n_pre, unit = blockIdx.x / a.c.n_kv / a.n_pre;
+  const int j = block % a.c.n_kv, split = block / a.c.n_kv % a.n_pre, unit = block / a.c.n_kv / a.n_pre;
   const PagedUnit t = paged_unit(a, unit, 32 * WAVES / HALVES, G);
   if (t.group < 0) return;
   const int seq = __builtin_amdgcn_readfirstlane(paged_seq(a, t.first));
@@ -771,6 +776,31 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_paged_prefix(PagedAttn a) {
   if (h == 0) *(f32x2 *)(a.part_ml + at * 2) = f32x2{m, l};
 }
 
+// Rows' own positions.
+template <int DT, int HD>
+__global__ __launch_bounds__(64 * PG_WAVES) void k_paged_own(PagedAttn a) {
+  __shared__ AttnLds<HD> lds;
+  attn_columns<DT, HD, 1, false>(a, blockIdx.x, lds);
+}
+// The first `pre` work groups take the shared positions, the others the rows' own: one
+// launch, in which the ones' arithmetic and the others' reads overlap.
+template <int DT, int HD, int HALVES>
+__global__ __launch_bounds__(64 * PG_WAVES, DT == HS_F32 ? 1 : 2) void k_paged_both(PagedAttn a, uint32_t pre) {
+  __shared__ union {
+    AttnLds<HD> own;
+    SharedLds<HD> shared;
+  } lds;
+  if (blockIdx.x >= pre) attn_columns<DT, HD, 1, false>(a, blockIdx.x - pre, lds.own);
+  else if constexpr (DT == HS_F32) attn_columns<DT, HD, 2, true>(a, blockIdx.x, lds.own);
+  else shared_columns<DT, HD, PG_WAVES, HALVES>(a, blockIdx.x, lds.shared);
+}
+// Shared positions of large groups: eight waves, all of a CU's registers.
+template <int DT, int HD>
+__global__ __launch_bounds__(512, 2) void k_paged_shared(PagedAttn a) {
+  __shared__ SharedLds<HD> lds;
+  shared_columns<DT, HD, 8, 1>(a, blockIdx.x, lds);
+}
+
 // A row's partials joined, in the order of their slots; a thread takes four channels.
 template <int DT, int HD>
 __global__ __launch_bounds__(256) void k_paged_join(PagedAttn a) {
@@ -820,14 +850,19 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedAttn a) {
 template <int DT, int HD>
 hipError_t attn_launch(const PagedAttn &a, hipStream_t st) {
   const dim3 block(64 * PG_WAVES);
-  if (a.n_pre) {
-    const dim3 grid((uint32_t)(a.pre_units * a.n_pre * a.c.n_kv));
-    if constexpr (DT == HS_F32) HS_LAUNCH((k_paged_attn<DT, HD, 2, true>), grid, block, 0, st, a);
-    else if (a.tile == 256) HS_LAUNCH((k_paged_prefix<DT, HD, 8, 1>), grid, dim3(512), 0, st, a);
-    else if (a.tile == 128) HS_LAUNCH((k_paged_prefix<DT, HD, 4, 1>), grid, block, 0, st, a);
-    else HS_LAUNCH((k_paged_prefix<DT, HD, 4, 2>), grid, block, 0, st, a);
+  const uint32_t own = (uint32_t)((int64_t)a.n * a.n_own * a.c.n_kv), pre = (uint32_t)(a.pre_units * a.n_pre * a.c.n_kv);
+  if (!a.n_pre) {
+    HS_LAUNCH((k_paged_own<DT, HD>), dim3(own), block, 0, st, a);
+  } else if constexpr (DT == HS_F32) {
+    HS_LAUNCH((k_paged_both<DT, HD, 1>), dim3(pre + own), block, 0, st, a, pre);
+  } else if (a.tile == 256) {
+    HS_LAUNCH((k_paged_shared<DT, HD>), dim3(pre), dim3(512), 0, st, a);
+    HS_LAUNCH((k_paged_own<DT, HD>), dim3(own), block, 0, st, a);
+  } else if (a.tile == 128) {
+    HS_LAUNCH((k_paged_both<DT, HD, 1>), dim3(pre + own), block, 0, st, a, pre);
+  } else {
+    HS_LAUNCH((k_paged_both<DT, HD, 2>), dim3(pre + own), block, 0, st, a, pre);
   }
-  HS_LAUNCH((k_paged_attn<DT, HD, 1, false>), dim3((uint32_t)((int64_t)a.n * a.n_own * a.c.n_kv)), block, 0, st, a);
   if (a.n_own + a.n_pre > 1) {
     const int heads_wg = 256 / (HD / 4);
     const int64_t groups = (int64_t)a.n * ((a.n_heads + heads_wg - 1) / heads_wg);
@@ -883,6 +918,10 @@ void paged_plan(int dtype, int64_t n, int n_heads, int n_kv, int max_len, int n_
       if (s * n_kv % 8 == 0 && s * 10 >= a->n_pre * 9) a->n_pre = s;
     }
     a->n_own = splits(n * n_kv, std::max(1, max_len - max_shared), 256);
+    // one round of work groups rather than a second with a few, while splits are short
+    while (a->tile < 256 && a->n_pre > 1 && (units * a->n_pre + n * a->n_own) * n_kv > 512 &&
+           max_shared / (a->n_pre - 1) <= 512)
+      --a->n_pre;
   } else {
     a->tile = 16;
     a->pre_units = 0;
