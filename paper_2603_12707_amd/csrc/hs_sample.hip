@@ -342,9 +342,9 @@ __global__ __launch_bounds__(SP_THREADS) void k_sample_parts(SampleArgs a) {
 constexpr int SD_THREADS = 1024, SD_WAVES = SD_THREADS / 64;
 constexpr int SD_LIST = 2048;  // gathered logits that stay at hand
 constexpr int SD_SUB = 64;     // parts that a bin is cut into
-constexpr int SD_FEW = 512;    // logits that are sorted
+constexpr int SD_FEW = 1024;   // logits that are sorted
 constexpr int SD_RUNS = 3;     // ranges of values that are looked for
-static_assert(SD_THREADS == SM_BINS && SD_WAVES * SD_SUB == SD_THREADS, "a thread for each");
+static_assert(SD_THREADS == SM_BINS && SD_WAVES * SD_SUB == SD_THREADS && SD_FEW <= SD_THREADS, "a thread for each");
 
 struct DrawLds {
   BinLds bins;                    // of the row, then the parts of its needed bins
@@ -411,11 +411,30 @@ __device__ __forceinline__ double block_largest(double v, double *s_tmp) {
 template <int DT>
 __device__ __attribute__((noinline)) void draw_alone(const SampleArgs &a, DrawLds &lds, const SampleRow &p, int64_t row,
                                                      int64_t slot, float M) {
-  const char *x = (const char *)a.logits + row * a.ld * (DT == HS_F32 ? 4 : 2);
+  using H = Read<DT, SD_THREADS>;
   const int V = a.vocab, tid = threadIdx.x;
+  const H h{(const char *)a.logits + row * a.ld * H::B, V};
+  const char *x = h.x;
   const int bits = 62 - (32 - __clz(V));  // V * 2^bits stays below 2^62
   const double unit = (double)(1ull << bits), least = (double)M;
   const auto weight = [&](float v) { return (uint64_t)rint(exp(((double)v - least) * p.inv_t) * unit); };
+  const auto each = [&](auto f) {
+    h.chunks([&](const float *v, int) {
+      for (int e = 0; e < H::CE; ++e)
+        if (v[e] > -INFINITY) f(v[e]);  // (-inf stands for what is past the row's end, and is never drawn)
+    });
+  };
+  // a number and a weight of every thread, summed
+  const auto sum = [&](unsigned long long &n, unsigned long long &m) {
+    __syncthreads();
+    if (tid == 0) lds.bins.mass[0] = lds.bins.mass[1] = 0;
+    __syncthreads();
+    atomicAdd(&lds.bins.mass[0], n);
+    atomicAdd(&lds.bins.mass[1], m);
+    __syncthreads();
+    n = lds.bins.mass[0];
+    m = lds.bins.mass[1];
+  };
   // the value at which `cross` (of the number and the weight up to it) becomes true
   // first; all above it, and its ties
   uint32_t edge = 0;
@@ -430,14 +449,27 @@ __device__ __attribute__((noinline)) void draw_alone(const SampleArgs &a, DrawLd
         lds.bins.count[tid] = 0;
       }
       __syncthreads();
-      for (int i = tid; i < V; i += SD_THREADS) {
-        const float v = ld_elem<DT>(x, i);
+      // (a run of equal digits, of which there are many, is added at once)
+      uint32_t digit = 0, n = 0;
+      unsigned long long m = 0;
+      const auto put = [&] {
+        if (!n) return;
+        atomicAdd(&lds.bins.count[digit], n);
+        atomicAdd(&lds.bins.mass[digit], m);
+      };
+      each([&](float v) {
         const uint32_t k = value_key(v);
-        if (shift == 24 || (k >> (shift + 8)) == (edge >> (shift + 8))) {
-          atomicAdd(&lds.bins.count[k >> shift & 255], 1u);
-          atomicAdd(&lds.bins.mass[k >> shift & 255], (unsigned long long)weight(v));
+        if (shift != 24 && (k >> (shift + 8)) != (edge >> (shift + 8))) return;
+        if ((k >> shift & 255) != digit) {
+          put();
+          digit = k >> shift & 255;
+          n = 0;
+          m = 0;
         }
-      }
+        ++n;
+        m += weight(v);
+      });
+      put();
       __syncthreads();
       if (tid == 0) {
         uint64_t m = above, n = number;
@@ -464,14 +496,17 @@ __device__ __attribute__((noinline)) void draw_alone(const SampleArgs &a, DrawLd
       ties = lds.ties;
     }
   };
-  if (p.top_k < V) {
+  unsigned long long kept = 0, total = 0;  // of the row's beginning
+  each([&](float v) {
+    ++kept;
+    total += weight(v);
+  });
+  sum(kept, total);
+  if ((uint64_t)p.top_k < kept) {
     find([&](uint64_t n, uint64_t) { return n >= (uint64_t)p.top_k; }, false);
-    ties = (uint64_t)p.top_k - number;
-  } else {
-    find([&](uint64_t n, uint64_t) { return n >= (uint64_t)V; }, false);
+    kept = p.top_k;
+    total = above + (kept - number) * weight(key_float(edge));
   }
-  uint64_t total = above + ties * weight(key_float(edge));
-  uint64_t kept = number + ties;  // of the row's beginning
   if (p.top_p < 1.f) {
     const double want = fmax((double)p.top_p * (double)total * (1 - SM_EQUAL), 0.5);
     const uint64_t most = kept;
@@ -483,25 +518,19 @@ __device__ __attribute__((noinline)) void draw_alone(const SampleArgs &a, DrawLd
     kept = number + ties;
   }
   if (p.min_p > 0.f) {
-    const uint32_t k = value_key(min_p_floor(p, M));
     // how many reach it, and their weight
-    __syncthreads();
-    if (tid == 0) lds.bins.mass[0] = lds.bins.mass[1] = 0;
-    __syncthreads();
+    const float least_x = min_p_floor(p, M);
     unsigned long long n = 0, m = 0;
-    for (int i = tid; i < V; i += SD_THREADS) {
-      const float v = ld_elem<DT>(x, i);
-      if (value_key(v) >= k) {
+    each([&](float v) {
+      if (v >= least_x) {
         ++n;
         m += weight(v);
       }
-    }
-    atomicAdd(&lds.bins.mass[0], n);
-    atomicAdd(&lds.bins.mass[1], m);
-    __syncthreads();
-    if (lds.bins.mass[0] < kept) {
-      kept = lds.bins.mass[0];
-      total = lds.bins.mass[1];
+    });
+    sum(n, m);
+    if (n < kept) {
+      kept = n;
+      total = m;
     }
   }
   const double want = (p.u + SM_EQUAL) * (double)total;
@@ -902,6 +931,87 @@ __global__ __launch_bounds__(SD_THREADS) void k_sample_draw(SampleArgs a) {
   }
 }
 
+// A row of T logits or fewer, a thread for each: sorted by counting, then as the
+// definition has it.
+template <int DT, int T>
+__global__ __launch_bounds__(T) void k_sample_few(SampleArgs a) {
+  constexpr int WAVES = T / 64;
+  __shared__ __align__(16) uint64_t s_key[T + 8], s_sorted[T];
+  __shared__ double s_d[WAVES];
+  __shared__ int s_pick, s_last;
+  const int64_t row = blockIdx.x, slot = a.act ? a.act[row] : row;
+  const int tid = threadIdx.x, V = a.vocab, lane = tid & 63, wave = tid >> 6;
+  const SampleRow p = sample_row(a, slot);
+  const float x = tid < V ? ld_elem<DT>((const char *)a.logits + row * a.ld * (DT == HS_F32 ? 4 : 2), tid) : -INFINITY;
+  const bool odd = __syncthreads_or(!(x < INFINITY));
+  const uint64_t key = (uint64_t)value_key(x) << 32 | (uint32_t)~tid;
+  s_key[tid] = key;
+  if (tid == 0) {
+    s_pick = INT32_MAX;
+    s_last = -1;
+  }
+  __syncthreads();
+  int rank = 0;
+  const int n = (V + 7) / 8 * 8;  // (what lies past the row ranks below it)
+  for (int o = 0; o < n; o += 8) {
+    u32x4 two[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) two[u] = *(const u32x4 *)&s_key[o + 2 * u];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      rank += o + 2 * u < V && ((uint64_t)two[u][1] << 32 | two[u][0]) > key;
+      rank += o + 2 * u + 1 < V && ((uint64_t)two[u][3] << 32 | two[u][2]) > key;
+    }
+  }
+  if (tid < V) s_sorted[rank] = key;
+  __syncthreads();
+  const float M = key_float((uint32_t)(s_sorted[0] >> 32));
+  if (p.bad || odd || M == -INFINITY || p.greedy) {
+    if (tid == 0) {
+      const bool none = p.bad || odd || M == -INFINITY;
+      a.tokens[slot] = none ? -1 : (int)~(uint32_t)s_sorted[0];
+      if (a.logprob) a.logprob[row] = none ? NAN : 0.f;
+    }
+    return;
+  }
+  const float v = tid < V ? key_float((uint32_t)(s_sorted[tid] >> 32)) : -INFINITY;
+  bool in = tid < V && tid < p.top_k;
+  const double w = in ? exp(((double)v - (double)M) * p.inv_t) : 0.0;
+  double upto = w;
+  for (int o = 1; o < 64; o <<= 1) {
+    const double y = __shfl_up(upto, o);
+    if (lane >= o) upto += y;
+  }
+  if (lane == 63) s_d[wave] = upto;
+  __syncthreads();
+  double z = 0.0;
+#pragma unroll
+  for (int o = 0; o < WAVES; ++o) {
+    if (o < wave) upto += s_d[o];
+    z += s_d[o];
+  }
+  if (p.top_p < 1.f) in = in && (tid == 0 || upto - w < (double)p.top_p * z * (1 - SM_EQUAL));
+  if (p.min_p > 0.f) in = in && v >= min_p_floor(p, M);
+  // the weight up to the last that stays
+  double top = in ? upto : 0.0;
+  for (int o = 32; o; o >>= 1) top = fmax(top, __shfl_xor(top, o));
+  __syncthreads();
+  if (lane == 0) s_d[wave] = top;
+  __syncthreads();
+  z = 0.0;
+#pragma unroll
+  for (int o = 0; o < WAVES; ++o) z = fmax(z, s_d[o]);
+  if (in && w > 0.0) {
+    atomicMax(&s_last, tid);
+    if (upto > (p.u + SM_EQUAL) * z) atomicMin(&s_pick, tid);
+  }
+  __syncthreads();
+  if (tid == (s_pick < INT32_MAX ? s_pick : s_last)) {
+    a.tokens[slot] = (int)~(uint32_t)s_sorted[tid];
+    if (a.logprob) a.logprob[row] = (float)log(w / z);
+  }
+}
+
 constexpr int SAMPLE_WHOLE = 32768;
 // parts of a row; 0: it has none
 inline int sample_parts(int vocab, int dtype) {
@@ -912,7 +1022,11 @@ inline int sample_parts(int vocab, int dtype) {
 template <int DT>
 hipError_t sample_launch(SampleArgs a, hipStream_t st) {
   a.parts = sample_parts(a.vocab, DT);
-  if (!a.parts) {
+  if (a.vocab <= 64) {
+    HS_LAUNCH((k_sample_few<DT, 64>), dim3((uint32_t)a.rows), dim3(64), 0, st, a);
+  } else if (a.vocab <= 256) {
+    HS_LAUNCH((k_sample_few<DT, 256>), dim3((uint32_t)a.rows), dim3(256), 0, st, a);
+  } else if (!a.parts) {
     HS_LAUNCH((k_sample_draw<DT, true>), dim3((uint32_t)a.rows), dim3(SD_THREADS), 0, st, a);
   } else {
     HS_LAUNCH((k_sample_parts<DT>), dim3((uint32_t)(a.rows * a.parts)), dim3(SP_THREADS), 0, st, a);

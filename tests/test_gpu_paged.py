@@ -214,6 +214,17 @@ def test_shared_beginnings(dtype, hd, kv, group, n, groups, alone):
     attend_case(hs, dtype, hd, kv, group, lengths, table, total, block, starts, shared, seed=n)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("n,groups,kv,group", [(74, 1, 1, 7), (40, 1, 2, 16), (90, 2, 1, 5), (140, 70, 1, 2),
+                                               (200, 130, 1, 1)])
+def test_large_groups(dtype, hd, n, groups, kv, group):
+    """Tiles of 256 columns that rows lie across, and of 128; more groups than a wave has lanes."""
+    import paper_2603_12707_amd as hs
+    lengths, table, starts, shared, total = grouped(n, groups, [320, 1088, 64], [1, 40, 5, 0], 64, n)
+    attend_case(hs, dtype, hd, kv, group, lengths, table, total, 64, starts, shared, layers=1, seed=n)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("shared", [[1], [15], [16], [17], [100], [0], [128], [129, 0, 7]])
 def test_shared_beginnings_that_end_anywhere(dtype, shared):
@@ -286,6 +297,8 @@ def test_what_lies_past_the_lengths_is_not_looked_at(dtype):
 @pytest.mark.parametrize("loud", [30.0, 1000.0])
 def test_loud_scores(dtype, loud):
     import paper_2603_12707_amd as hs
+    lengths, table, starts, shared, total = grouped(60, 1, [200], [1, 70], 16, 7)
+    attend_case(hs, dtype, 128, 1, 4, lengths, table, total, 16, starts, shared, loud=loud)
     lengths, table, starts, shared, total = grouped(20, 2, [200], [1, 70], 16, 7)
     attend_case(hs, dtype, 64, 2, 4, lengths, table, total, 16, starts, shared, loud=loud)
 
@@ -304,6 +317,9 @@ def test_scale_and_bounds(dtype):
     lengths, table, starts, shared, total = grouped(8, 2, [96], [50, 120], 16, 9)
     attend_case(hs, dtype, 64, 2, 2, lengths, table, total, 16, starts, shared, scale=-0.3)
     attend_case(hs, dtype, 64, 2, 2, lengths, table, total, 16, starts, shared, scale=0.0)
+    l2, t2, s2, h2, n2 = grouped(50, 1, [96], [50, 120], 16, 9)
+    for scale in (-0.3, 0.0):
+        attend_case(hs, dtype, 64, 1, 6, l2, t2, n2, 16, s2, h2, scale=scale)
     # lengths past max_len are cut
     attend_case(hs, dtype, 64, 2, 2, lengths, table, total, 16, starts, shared, max_len=140, max_shared=96)
 

@@ -39,8 +39,9 @@ def params(rows, g, greedy=False):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
-@pytest.mark.parametrize("rows,vocab", [(1, 1), (3, 2), (4, 63), (4, 64), (4, 65), (9, 997), (5, 4096), (5, 8191),
-                                        (5, 8192), (5, 8193), (4, 16384), (6, 16385), (8, 32000), (7, 152064),
+@pytest.mark.parametrize("rows,vocab", [(1, 1), (3, 2), (4, 63), (4, 64), (4, 65), (4, 256), (4, 257), (9, 997), (4, 1024),
+                                        (4, 1025), (5, 4096), (5, 8191),
+                                        (5, 8192), (5, 8193), (4, 16384), (6, 16385), (8, 32000), (3, 32768), (3, 32769), (7, 152064),
                                         (3, 200001)])
 def test_draws_of_every_size(dtype, rows, vocab):
     import paper_2603_12707_amd as hs
@@ -70,7 +71,7 @@ def test_flat_and_peaked_rows(dtype, spread):
     check(hs, x, torch.rand(24, generator=g))
 
 
-@pytest.mark.parametrize("vocab", [40, 5000, 70000])
+@pytest.mark.parametrize("vocab", [40, 250, 1000, 5000, 70000])
 def test_equal_logits_come_by_index(vocab):
     """Ties everywhere, also at each of the borders and the draw: weights that are powers of two, sums that are exact."""
     import paper_2603_12707_amd as hs
@@ -93,7 +94,7 @@ def test_equal_logits_come_by_index(vocab):
             check(hs, y[[0, 1, 3]], uu[:3], top_k=torch.tensor([32, 16, 8]), top_p=torch.tensor([0.5, 0.25, 0.125]))
 
 
-@pytest.mark.parametrize("vocab", [6, 9001, 70001])
+@pytest.mark.parametrize("vocab", [6, 200, 1001, 9001, 70001])
 def test_rows_without_a_distribution_and_banned_words(vocab):
     import paper_2603_12707_amd as hs
     g = gen(1)
@@ -120,10 +121,11 @@ def test_rows_without_a_distribution_and_banned_words(vocab):
         check(hs, x, u, *args)
 
 
-def test_parameters_at_their_ends():
+@pytest.mark.parametrize("vocab", [50, 900, 3000, 50000])
+def test_parameters_at_their_ends(vocab):
     import paper_2603_12707_amd as hs
     g = gen(5)
-    n, vocab = 18, 3000
+    n = 18
     x = torch.randn(n, vocab, generator=g) * 2
     t, k = torch.full((n,), 0.8), torch.zeros(n, dtype=torch.int64)
     p, m = torch.ones(n), torch.zeros(n)
@@ -135,6 +137,32 @@ def test_parameters_at_their_ends():
     u[15], u[16], u[17] = 1.0, -0.5, math.nan
     check(hs, x, u, t, k, p, m)
     check(hs, x, u, None, k, p, m)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [20000, 90000])
+def test_rows_drawn_from_by_themselves(dtype, vocab):
+    """Rows that the bins say little about: flat ones, thousands of equal logits, borders far below the largest."""
+    import paper_2603_12707_amd as hs
+    g = gen(vocab)
+    x = torch.randn(16, vocab, generator=g)
+    x[:4] *= 1e-3
+    x[4:6] = torch.randint(0, 3, (2, vocab), generator=g).float()
+    x[6:8] *= 0.05
+    x[8:12] *= 200.0
+    x[12:14] = -80.0 + x[12:14]
+    x[12:14, 7] = 0.0
+    x[14:] = torch.arange(vocab) * -(2.0 ** -12)
+    t = torch.tensor([1.0, 0.5, 3e4, 2.0] * 4)
+    u = torch.rand(16, generator=g)
+    k = torch.tensor([vocab - 3, 1000, 0, 17] * 4)
+    p, m = torch.tensor([0.9, 1.0, 0.5, 0.999] * 4), torch.tensor([0.0, 1e-30, 0.3, 0.0] * 4)
+    y = x.to(R.DT[dtype])
+    check(hs, y, u)
+    check(hs, y, u, t, top_k=k)
+    check(hs, y, u, t, top_p=p)
+    check(hs, y, u, t, min_p=m)
+    check(hs, y, u, t, k, p, m)
 
 
 def test_draws_follow_the_distribution():
