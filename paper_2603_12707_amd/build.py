@@ -9,12 +9,12 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhs.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("hs_api.cpp", "hs_gemm.hip", "hs_attn.hip", "hs_misc.hip", "hs_paged.hip", "hs_sample.hip",
-                                               "hs_handoff.cpp")]
+SOURCES = [os.path.join(CSRC, f) for f in ("hs_api.cpp", "hs_gemm.hip", "hs_attn.hip", "hs_misc.hip", "hs_handoff.cpp")]
 DEPS = SOURCES + [os.path.join(CSRC, "hs_internal.h"), os.path.join(CSRC, "hs_device.h"),
                   os.path.join(CSRC, "hs_gemm_epi.h"), os.path.join(CSRC, "hs_gemm_dma.h"),
                   os.path.join(CSRC, "hs_gemm_plan.h"),
                   os.path.join(CSRC, "hs_kvq.h"), os.path.join(CSRC, "hs_logprobs.h"),
+                  os.path.join(CSRC, "hs_paged.h"), os.path.join(CSRC, "hs_sample.h"),
                   os.path.join(ROOT, "include", "hs.h")]
 
 FLAGS = [

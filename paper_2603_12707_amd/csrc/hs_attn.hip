@@ -6,6 +6,7 @@
 // 2 * L * n_kv * d_h * s_ctx elements per request (Eq. 1, §4.1).  Work is
 // split along the positions so that short batches still fill the GPU.
 #include "hs_device.h"
+#include "hs_paged.h"
 
 #include <cfloat>
 

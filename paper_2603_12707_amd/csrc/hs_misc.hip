@@ -1,9 +1,11 @@
 // hs_misc.hip — embedding gather, prefill input rows, greedy selection and
 // length bookkeeping kernels of the decode engine (gfx950); the 4-bit cache's
-// kernels and the token log probabilities come in by their headers.
+// kernels, the token log probabilities and the token draws come in by their
+// headers.
 #include "hs_device.h"
 #include "hs_kvq.h"
 #include "hs_logprobs.h"
+#include "hs_sample.h"
 
 namespace hs {
 namespace {

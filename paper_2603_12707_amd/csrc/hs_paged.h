@@ -1,6 +1,8 @@
-// hs_paged.hip — a paged KV cache in the model's own type (gfx950): new rows
+// hs_paged.h — a paged KV cache in the model's own type (gfx950): new rows
 // normalised, turned and stored, and attention over it where rows of a group
-// share their first positions.
+// share their first positions.  Included by hs_attn.hip.
+#pragma once
+
 #include "hs_device.h"
 
 #include <algorithm>

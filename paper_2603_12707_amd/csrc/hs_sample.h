@@ -1,5 +1,6 @@
-// hs_sample.hip — a token drawn for each row of logits from a given uniform
-// number, after temperature, top-k, top-p and min-p (gfx950).
+// hs_sample.h — a token drawn for each row of logits from a given uniform
+// number, after temperature, top-k, top-p and min-p (gfx950).  Included by
+// hs_misc.hip.
 //
 // In falling order of the logits (the lowest index first among equals) every
 // one of the three leaves a beginning of the row, and the draw is a walk down
@@ -13,6 +14,8 @@
 // left is sorted.  A work group draws from a row, which it reads three or four times
 // (L2 holds it).  The bins of long rows are summed by a launch before, in parts that
 // stay in registers, on one grid.
+#pragma once
+
 #include "hs_device.h"
 
 #include <algorithm>
