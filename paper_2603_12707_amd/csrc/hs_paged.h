@@ -49,8 +49,8 @@ __device__ __forceinline__ void turn(int at, double freq, float &c, float &s) {
 // The work is a copy.  A work group takes some rows (or a part of one row's
 // heads), computes the rows' cosines and sines once for all heads (64 bits, into
 // LDS) and gives each head to HD / 8 lanes, 8 channels a lane; a half-apart pair's
-// other channel comes from the lane that holds it.  All loads of a lane are asked
-// for before the first is used.
+// other channel comes from the lane that holds it.  The next head is asked for before
+// one is worked on.
 template <int DT, int HD>
 __global__ __launch_bounds__(APPEND_THREADS) void k_paged_append(PagedRows a, int rows_wg, int heads_wg) {
   constexpr int B = DT == HS_F32 ? 4 : 2, L = HD / 8, GROUPS = APPEND_THREADS / L;
@@ -68,21 +68,57 @@ __global__ __launch_bounds__(APPEND_THREADS) void k_paged_append(PagedRows a, in
     turn(a.angles_at[(int64_t)axis * a.n + row0 + r], a.freq[p], c, s);
     cs[r][p] = float2{c, s};
   }
+  // a half-apart pair's other channels, 8 of them in one lane as pairs is a multiple of 8
+  const bool early = e0 < a.pairs, paired = e0 < 2 * a.pairs;
+  const int other = !a.adjacent && paired ? (early ? lane + a.pairs / 8 : lane - a.pairs / 8) : lane;
+  const auto load8 = [](const char *p, uint32_t(&w)[W]) {
+#pragma unroll
+    for (int u = 0; u < W; u += 4) {
+      const u32x4 t = ld16(p + u * 4);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) w[u + x] = t[x];
+    }
+  };
+  const auto widen = [](const uint32_t(&v)[W], float *o) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if constexpr (DT == HS_F32) o[e] = __uint_as_float(v[e]);
+      else o[e] = e & 1 ? hi_f32<DT>(v[e / 2]) : lo_f32<DT>(v[e / 2]);
+    }
+  };
+  // the lane's and its other's gains
+  uint32_t gains[2][2][W];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const char *gain = (const char *)(k ? a.k_gain : a.q_gain);
+    if (gain) {
+      load8(gain + e0 * B, gains[k][0]);
+      load8(gain + other * 8 * B, gains[k][1]);
+    }
+  }
+  // item `it` is head h0 + it % heads of row row0 + it / heads
+  const auto fetch = [&](int it, uint32_t(&w)[W]) {
+    const int r = it / heads, h = h0 + it - r * heads;
+    const int64_t row = row0 + r;
+    const bool is_q = h < a.n_heads, is_k = !is_q && h < a.n_heads + a.c.n_kv;
+    const int j = is_q ? h : is_k ? h - a.n_heads : h - a.n_heads - a.c.n_kv;
+    load8((const char *)(is_q ? a.q : is_k ? a.k : a.v) +
+              (is_q ? row * a.ld_q + j * a.ld_q_head : row * a.ld + j * a.ld_head) * B + e0 * B,
+          w);
+  };
+  uint32_t next[W];
+  if ((int)threadIdx.x / L < items) fetch(threadIdx.x / L, next);
   __syncthreads();
   for (int it = threadIdx.x / L; it < items; it += GROUPS) {
     const int r = it / heads, h = h0 + it - r * heads;
     const int64_t row = row0 + r;
     const bool is_q = h < a.n_heads, is_k = !is_q && h < a.n_heads + a.c.n_kv;
     const int j = is_q ? h : is_k ? h - a.n_heads : h - a.n_heads - a.c.n_kv;
-    const char *src = (const char *)(is_q ? a.q : is_k ? a.k : a.v) +
-                      (is_q ? row * a.ld_q + j * a.ld_q_head : row * a.ld + j * a.ld_head) * B + e0 * B;
     uint32_t w[W];
 #pragma unroll
-    for (int u = 0; u < W; u += 4) {
-      const u32x4 t = ld16(src + u * 4);
-#pragma unroll
-      for (int x = 0; x < 4; ++x) w[u + x] = t[x];
-    }
+    for (int u = 0; u < W; ++u) w[u] = next[u];
+    // (q_out may be q: an item's place is written after its own load, and no other's)
+    if (it + GROUPS < items) fetch(it + GROUPS, next);
     char *dst;
     if (is_q) {
       dst = (char *)a.q_out + (row * a.ld_q_out + j * a.ld_q_out_head) * B;
@@ -94,25 +130,19 @@ __global__ __launch_bounds__(APPEND_THREADS) void k_paged_append(PagedRows a, in
                                           (int64_t)(pos & ((1 << a.c.bt_log2) - 1)) * HD) * B;
     }
     if (is_q || is_k) {
-      float f[8], g[8];
-      auto widen = [&](const uint32_t(&v)[W], float *o) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if constexpr (DT == HS_F32) o[e] = __uint_as_float(v[e]);
-          else o[e] = e & 1 ? hi_f32<DT>(v[e / 2]) : lo_f32<DT>(v[e / 2]);
-        }
-      };
+      float f[8], g[8], gain[8];
       widen(w, f);
-      const void *gain = is_q ? a.q_gain : a.k_gain;
+      const bool norm = (is_q ? a.q_gain : a.k_gain) != nullptr;
       float rs = 1.f;
-      if (gain) {
+      if (norm) {
         float ss = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(f[e], f[e], ss);
         ss = group_sum<L>(ss);
         rs = 1.f / sqrtf(ss * (1.f / HD) + a.eps);
+        widen(gains[is_q ? 0 : 1][0], gain);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] *= rs * ld_elem<DT>(gain, e0 + e);
+        for (int e = 0; e < 8; ++e) f[e] *= rs * gain[e];
       }
       if (a.adjacent) {
 #pragma unroll
@@ -124,20 +154,18 @@ __global__ __launch_bounds__(APPEND_THREADS) void k_paged_append(PagedRows a, in
             f[e + 1] = x * t.y + y * t.x;
           }
       } else if (a.pairs) {
-        // the partner's channels, 8 of them in one lane as pairs is a multiple of 8
-        const bool first = e0 < a.pairs, in = e0 < 2 * a.pairs;
-        const int d = a.pairs / 8, other = in ? (first ? lane + d : lane - d) : lane;
         const int from = (int)(threadIdx.x & 63) - lane + other;
         uint32_t v[W];
 #pragma unroll
         for (int u = 0; u < W; ++u) v[u] = (uint32_t)__shfl((int)w[u], from);
         widen(v, g);
-        if (in) {
+        if (norm) widen(gains[is_q ? 0 : 1][1], gain);
+        if (paired) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            if (gain) g[e] *= rs * ld_elem<DT>(gain, other * 8 + e);
-            const float2 t = cs[r][(first ? e0 : e0 - a.pairs) + e];
-            f[e] = first ? f[e] * t.x - g[e] * t.y : g[e] * t.y + f[e] * t.x;
+            if (norm) g[e] *= rs * gain[e];
+            const float2 t = cs[r][(early ? e0 : e0 - a.pairs) + e];
+            f[e] = early ? f[e] * t.x - g[e] * t.y : g[e] * t.y + f[e] * t.x;
           }
         }
       }
