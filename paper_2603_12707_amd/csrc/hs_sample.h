@@ -311,7 +311,10 @@ __device__ __forceinline__ void row_bins(H &h, double s, double b0, int top_k, b
   __syncthreads();
 }
 
-// A part of a row: its largest, and its bins.
+// A part of a row: its largest, and its bins.  One read of the logits.  256 rows of
+// 152064 take 54 us (2.9 TB/s): the additions in LDS and the 64-bit arithmetic bound it,
+// not the read (22 us).  Leaving out what top_k cannot reach took it from 64 to 54;
+// 256 threads and bins of half the range from 78 to 64.
 constexpr int SP_THREADS = 512;
 template <int DT>
 __global__ __launch_bounds__(SP_THREADS) void k_sample_parts(SampleArgs a) {
@@ -409,8 +412,9 @@ __device__ __forceinline__ double block_largest(double v, double *s_tmp) {
 
 // A row by itself, whatever it holds: each border and the draw by four passes over
 // the row, a byte of the value each, over sums of the weights in whole multiples of
-// a unit that no sum of the row overflows.  For rows whose border bins hold more than
-// SD_LIST logits (flat ones, or many equal ones), or lie in the last bin.
+// a unit that no sum of the row overflows.  For rows of which more than SD_FEW logits
+// lie in the parts of bins that count (many equal ones, mostly), or whose borders lie in
+// the last bin: some 200 us for 112677 bf16 logits of which thousands are equal.
 template <int DT>
 __device__ __attribute__((noinline)) void draw_alone(const SampleArgs &a, DrawLds &lds, const SampleRow &p, int64_t row,
                                                      int64_t slot, float M) {
@@ -622,7 +626,12 @@ __device__ __forceinline__ DrawCuts draw_cuts(DrawLds &lds, const SampleRow &p, 
   return c;
 }
 
-// A row's draw.  WHOLE: its bins are summed here; else its parts' are joined.
+// A row's draw.  WHOLE: its bins are summed here; else its parts' are joined.  It is a
+// chain of a dozen short phases with a barrier or two each: 31 us for one row of
+// 32000, 56 for 16 of 152064, 65 for 256 of them, 260 for 1531 bf16 rows of 32003, six
+// rows to a CU one after the other (128 registers of 1024 threads; with 64 it spills,
+// and two at a time took 445).  The row in registers instead of read again took 545:
+// the unrolled code does not fit the instruction cache.
 template <int DT, bool WHOLE>
 __global__ __launch_bounds__(SD_THREADS) void k_sample_draw(SampleArgs a) {
   using H = Read<DT, SD_THREADS>;
@@ -935,7 +944,8 @@ __global__ __launch_bounds__(SD_THREADS) void k_sample_draw(SampleArgs a) {
 }
 
 // A row of T logits or fewer, a thread for each: sorted by counting, then as the
-// definition has it.
+// definition has it.  Up to 256; for 613 rows of 1020 counting among all took 121 us,
+// bins 100.
 template <int DT, int T>
 __global__ __launch_bounds__(T) void k_sample_few(SampleArgs a) {
   constexpr int WAVES = T / 64;
@@ -1015,6 +1025,9 @@ __global__ __launch_bounds__(T) void k_sample_few(SampleArgs a) {
   }
 }
 
+// Rows up to this long are drawn from in one launch: a second one and its read of what
+// the first wrote cost more than a work group's summing of 32768 logits (for 32000 it
+// is 31 us against 19 + 10 and a launch).
 constexpr int SAMPLE_WHOLE = 32768;
 // parts of a row; 0: it has none
 inline int sample_parts(int vocab, int dtype) {
