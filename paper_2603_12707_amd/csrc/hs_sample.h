@@ -85,8 +85,9 @@ constexpr double SM_EQUAL = 0x1p-44;
 constexpr int SM_BINS = 1024;
 constexpr double SM_FINE = 16.0;
 // A weight relative to its bin's upper end, in (e^-1/16, 1], as a whole multiple of
-// 2^-49: a part's 2^14 of them sum in 63 bits, in any order to the same.
-constexpr double SM_ONE = 8.0;  // the number whose last place is 2^-49
+// 2^-48: a part's (or short row's) 2^15 of them at most sum in 64 bits, in any order to
+// the same.
+constexpr double SM_ONE = 16.0;  // the number whose last place is 2^-48
 __device__ __forceinline__ uint64_t bin_weight(double xs, double b) {
 #pragma clang fp contract(off)  // xs is the rounded product that b comes from
   const double r = (xs - (b + 1.0)) * (1.0 / SM_FINE);  // -1/16 .. 0
@@ -666,7 +667,7 @@ __global__ __launch_bounds__(SD_THREADS) void k_sample_draw(SampleArgs a) {
   const bool cut_k = p.top_k < V;
 
   // the row's bins, one of each thread
-  const auto bin_scale = [](int b) { return exp(-(double)b / SM_FINE) * 0x1p-49; };
+  const auto bin_scale = [](int b) { return exp(-(double)b / SM_FINE) * 0x1p-48; };
   const double scale = bin_scale(tid);
   double w = 0.0, total, before;
   int count = 0;
@@ -707,7 +708,7 @@ __global__ __launch_bounds__(SD_THREADS) void k_sample_draw(SampleArgs a) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           w += (double)near_w[u] * scale;
-          if (far_w[u]) far += (double)far_w[u] * (exp(-(tid + off[u]) / SM_FINE) * 0x1p-49);
+          if (far_w[u]) far += (double)far_w[u] * (exp(-(tid + off[u]) / SM_FINE) * 0x1p-48);
           count += (int)near_n[u];
           far_count += (int)far_n[u];
         }
@@ -855,7 +856,7 @@ __global__ __launch_bounds__(SD_THREADS) void k_sample_draw(SampleArgs a) {
   if (bm2 < 0) bm2 = SD_THREADS;
   cut = draw_cuts(lds, p, bin, total, V, bm2);
   lds.need[tid] = cut.need;
-  // (2^14 weights of a part sum in 63 bits)
+  // (a part of a bin may hold more of a long row's than sum in 64 bits)
   if (__syncthreads_or(cut.past || count > 1 << 14)) {
     draw_alone<DT>(a, lds, p, row, slot, M);
     return;

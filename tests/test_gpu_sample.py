@@ -140,6 +140,20 @@ def test_parameters_at_their_ends(vocab):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [32768, 65536, 98304])
+def test_whole_parts_of_equal_logits_far_from_zero(dtype, vocab):
+    """As many weights of one as a work group sums: x / T so large that a bin is less than a rounding."""
+    import paper_2603_12707_amd as hs
+    x = torch.full((4, vocab), 3e38)
+    x[1] = -3e38
+    x[2, 1::2] = 2.9e38
+    x[3, 5:] = -math.inf
+    u, t = torch.tensor([0.75, 0.3125, 0.5, 0.9]), torch.full((4,), 1e-3)
+    check(hs, x.to(R.DT[dtype]), u, t)
+    check(hs, x.to(R.DT[dtype]), u, t, top_k=torch.tensor([vocab // 2, 16, 0, 3]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("vocab", [20000, 90000])
 def test_rows_drawn_from_by_themselves(dtype, vocab):
     """Rows that the bins say little about: flat ones, thousands of equal logits, borders far below the largest."""
