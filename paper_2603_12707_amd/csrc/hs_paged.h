@@ -920,10 +920,11 @@ hipError_t attn_launch(const PagedAttn &a, hipStream_t st) {
 template <int DT, int HD>
 hipError_t append_launch(const PagedRows &a, hipStream_t st) {
   const int heads = a.n_heads + 2 * a.c.n_kv, at_once = APPEND_THREADS / (HD / 8);
-  // one row's heads over several work groups while those are few, then several rows a work group
-  const int64_t spread = (int64_t)a.n * ((heads + at_once - 1) / at_once);
-  const int heads_wg = spread <= 1024 ? std::min(heads, at_once) : heads;
-  const int rows_wg = spread <= 1024 ? 1 : APPEND_ROWS;
+  // heads to a work group: as many as it holds at once, more where 2048 work groups have
+  // more; they are some of a row's, or those of up to APPEND_ROWS rows
+  const int64_t want = std::max<int64_t>(at_once, (int64_t)a.n * heads / 2048);
+  const int rows_wg = (int)std::min<int64_t>(std::max<int64_t>(want / heads, 1), APPEND_ROWS);
+  const int heads_wg = want >= heads ? heads : (int)std::min<int64_t>((want + at_once - 1) / at_once * at_once, heads);
   const int parts = (heads + heads_wg - 1) / heads_wg;
   const int64_t groups = ((int64_t)a.n + rows_wg - 1) / rows_wg * parts;
   HS_LAUNCH((k_paged_append<DT, HD>), dim3((uint32_t)groups), dim3(APPEND_THREADS), 0, st, a, rows_wg, heads_wg);

@@ -117,6 +117,13 @@ def test_many_rows_in_large_blocks():
     rows_case(hs, "bf16", 128, 4, 28, 5003, block=1024, axes=3, norm=True)
 
 
+def test_many_heads_of_some_rows():
+    """A row's heads over several work groups, several passes each."""
+    import paper_2603_12707_amd as hs
+    rows_case(hs, "f32", 64, 32, 256, 300, block=64, axes=2, norm=True)
+    rows_case(hs, "bf16", 128, 32, 512, 61, block=64, axes=1, norm=True, in_place=True)
+
+
 def test_angles_default_to_positions():
     import paper_2603_12707_amd as hs
     n, hd = 9, 64
