@@ -188,6 +188,22 @@ __global__ __launch_bounds__(APPEND_THREADS) void k_paged_append(PagedRows a, in
 // ---------------------------------------------------------------------------
 constexpr int PG_WAVES = 4;
 constexpr int PG_STRIPE = PG_WAVES * 32;  // positions that a work group takes at a time
+// 16-bit parts in which a weight enters the second product: 22 bits of it in f16, 24 in
+// bf16.  (With two parts of bf16, 16 bits, outputs were rounded to another number than
+// an fp32 form's often enough to differ by 2.8e-4 in norm for large groups, 8e-5 now.
+// The third part costs those 14 % and others 2 to 3 %.)
+template <int DT>
+constexpr int PG_PARTS = DT == HS_BF16 ? 3 : 2;
+// two weights in parts
+template <int DT>
+__device__ __forceinline__ void weight_parts(float p0, float p1, uint32_t (&w)[PG_PARTS<DT>]) {
+#pragma unroll
+  for (int i = 0; i < PG_PARTS<DT>; ++i) {
+    w[i] = pack2<DT>(p0, p1);
+    p0 -= lo_f32<DT>(w[i]);
+    p1 -= hi_f32<DT>(w[i]);
+  }
+}
 
 __device__ __forceinline__ int paged_most(const PagedRef &c) {
   return (int)min((int64_t)c.table_ld << c.bt_log2, (int64_t)INT32_MAX);
@@ -291,8 +307,7 @@ __device__ __forceinline__ PagedUnit paged_unit(const PagedAttn &a, int unit, in
 // V^T P^T, takes them.  Its k slots of lane group g are positions 4 g .. 4 g + 3 of
 // both tiles of a stripe; its rows are channels: a lane loads VE = HD / 16
 // consecutive channels of those positions, and row m of tile dt is channel VE m +
-// dt.  P enters as two parts of the type, hi + lo: 22 bits of it in f16, 16 in bf16,
-// whose rounding (2^-17) is 1/256 of the output's.  fp32 runs on the fp32 products.
+// dt.  P enters in parts of the type (PG_PARTS).  fp32 runs on the fp32 products.
 //
 // Loads go through buffer descriptors made for a tile of 16 positions, which
 // end where the positions do: what lies past them reads as zeros.
@@ -428,7 +443,7 @@ __device__ __forceinline__ void attn_columns(const PagedAttn &a, uint32_t block,
           }
         }
     }
-    uint32_t ph[CT][4], pl[CT][4];
+    uint32_t ps[CT][PG_PARTS<DT>][4];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
       float top = -INFINITY;
@@ -459,9 +474,10 @@ __device__ __forceinline__ void attn_columns(const PagedAttn &a, uint32_t block,
       if constexpr (DT != HS_F32) {
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          const float p0 = s[ct][x >> 1][2 * (x & 1)], p1 = s[ct][x >> 1][2 * (x & 1) + 1];
-          ph[ct][x] = pack2<DT>(p0, p1);
-          pl[ct][x] = pack2<DT>(p0 - lo_f32<DT>(ph[ct][x]), p1 - hi_f32<DT>(ph[ct][x]));
+          uint32_t w[PG_PARTS<DT>];
+          weight_parts<DT>(s[ct][x >> 1][2 * (x & 1)], s[ct][x >> 1][2 * (x & 1) + 1], w);
+#pragma unroll
+          for (int i = 0; i < PG_PARTS<DT>; ++i) ps[ct][i][x] = w[i];
         }
       }
     }
@@ -487,10 +503,10 @@ __device__ __forceinline__ void attn_columns(const PagedAttn &a, uint32_t block,
           av[2 * u + 1] = __builtin_amdgcn_perm(b.v[u][3][dt / 2], b.v[u][2][dt / 2], sel);
         }
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-          o[ct][dt] = mma<DT>(av, u32x4{ph[ct][0], ph[ct][1], ph[ct][2], ph[ct][3]}, o[ct][dt]);
-          o[ct][dt] = mma<DT>(av, u32x4{pl[ct][0], pl[ct][1], pl[ct][2], pl[ct][3]}, o[ct][dt]);
-        }
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int i = 0; i < PG_PARTS<DT>; ++i)
+            o[ct][dt] = mma<DT>(av, u32x4{ps[ct][i][0], ps[ct][i][1], ps[ct][i][2], ps[ct][i][3]}, o[ct][dt]);
       }
     }
   };
@@ -567,7 +583,7 @@ __device__ __forceinline__ void attn_columns(const PagedAttn &a, uint32_t block,
 // column c, and these are its k slots of the second product, O^T += V^T P^T, with
 // the rows of V taken in the same order.  Output row m of tile dt is channel VE m +
 // dt: a lane reads VE = HD / 32 consecutive channels of eight positions.  P enters
-// as hi + lo, as in attn_columns.  16-byte chunk j of K's row p lies at chunk j ^ p, so
+// in parts, as in attn_columns.  16-byte chunk j of K's row p lies at chunk j ^ p, so
 // that the 32 rows that a product reads spread over the banks.
 //
 // 256 rows of 28 heads over 32768 positions: 219 us, 550 TFLOP/s by the definition's
@@ -711,7 +727,7 @@ __device__ __forceinline__ void shared_columns(const PagedAttn &a, uint32_t bloc
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[u][i] -= up;
     }
-    u32x4 ph, pl;
+    u32x4 ps[PG_PARTS<DT>];
     const auto parts = [&](int x) {  // of 16 positions
       float sum = 0.f;
 #pragma unroll
@@ -719,15 +735,19 @@ __device__ __forceinline__ void shared_columns(const PagedAttn &a, uint32_t bloc
         const float p0 = __builtin_amdgcn_exp2f(s[x / 2][8 * (x & 1) + 2 * y]);
         const float p1 = __builtin_amdgcn_exp2f(s[x / 2][8 * (x & 1) + 2 * y + 1]);
         sum += p0 + p1;
-        ph[y] = pack2<DT>(p0, p1);
-        pl[y] = pack2<DT>(p0 - lo_f32<DT>(ph[y]), p1 - hi_f32<DT>(ph[y]));
+        uint32_t w[PG_PARTS<DT>];
+        weight_parts<DT>(p0, p1, w);
+#pragma unroll
+        for (int i = 0; i < PG_PARTS<DT>; ++i) ps[i][y] = w[i];
       }
       l += sum;
     };
     parts(0);
 #pragma unroll
     for (int x = 0; x < 2 * NU; ++x) {
-      const u32x4 hi_x = ph, lo_x = pl;
+      u32x4 px[PG_PARTS<DT>];
+#pragma unroll
+      for (int i = 0; i < PG_PARTS<DT>; ++i) px[i] = ps[i];
       const unsigned char *vp = vt + (16 * x + 4 * h) * ROW + c * (VE * 2);
       uint32_t v[8][VE / 2];
 #pragma unroll
@@ -750,13 +770,13 @@ __device__ __forceinline__ void shared_columns(const PagedAttn &a, uint32_t bloc
         for (int y = 0; y < 4; ++y) av[dt][y] = __builtin_amdgcn_perm(v[2 * y + 1][dt / 2], v[2 * y][dt / 2], sel);
       }
 #pragma unroll
-      for (int dt = 0; dt < VE; ++dt) o[dt] = mma32<DT>(av[dt], hi_x, o[dt]);
+      for (int k = 0; k < PG_PARTS<DT>; ++k)
 #pragma unroll
-      for (int dt = 0; dt < VE; ++dt) o[dt] = mma32<DT>(av[dt], lo_x, o[dt]);
+        for (int dt = 0; dt < VE; ++dt) o[dt] = mma32<DT>(av[dt], px[k], o[dt]);
       // the vector unit works on the next weights while the matrix cores multiply: a
       // product, then what fits behind it
 #pragma unroll
-      for (int i = 0; i < 2 * VE; ++i) {
+      for (int i = 0; i < PG_PARTS<DT> * VE; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
         __builtin_amdgcn_sched_group_barrier(0x2, 6, 0);
         __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);

@@ -452,3 +452,36 @@ def test_a_step_of_answers_to_one_prompt():
         out = cache.attention(0, q, pos + 1, group_starts=starts, shared=shared, max_len=128, max_shared=96)
         want, off = R.attention(q.cpu(), blocks.cpu(), table, 0, (pos + 1).cpu(), torch.arange(n))
         close(out, want, off, "bf16")
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("own,heads", [(True, 1), (False, 1), (False, 2), (False, 4)])
+def test_weights_of_24_bits(hd, own, heads):
+    """Of weights 1, 1 and w, times -(w's first 8 bits), -(its next 8) and 1, what is left is w's last bits.  Row and
+    channel i: w = e^-q_i, with little in common with any sum of two bf16 numbers."""
+    import paper_2603_12707_amd as hs
+    bf = torch.bfloat16
+    q = torch.cat([torch.arange(128, 256) / 2.0 ** e for e in (8, 9, 10, 11)]).to(bf)  # each of 8 bits
+    w = torch.exp(-q.double())
+    one = w.to(bf).double()
+    two = (w - one).to(bf).double()
+    left = w - one - two
+    pick = left.abs().argsort(descending=True)[:64]
+    q, w, one, two, left = (t[pick] for t in (q, w, one, two, left))
+    assert float(left.abs().min()) > 1.2e-6
+    blocks = torch.zeros(1, 1, 2, 1, 16, hd, dtype=bf)
+    blocks[0, 0, 0, 0, 2, 0] = -1.0
+    blocks[0, 0, 1, 0, 0, :64], blocks[0, 0, 1, 0, 1, :64], blocks[0, 0, 1, 0, 2, :64] = (-one).to(bf), (-two).to(bf), 1.0
+    queries = torch.zeros(64, heads, hd, dtype=bf)
+    queries[:, :, 0] = q[:, None]
+    cache = hs.PagedCache(blocks.cuda(), torch.zeros(1, 1, dtype=torch.int64, device="cuda"))
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    kw = {} if own else dict(group_starts=i32(0, 64), shared=i32(3))
+    got = cache.attention(0, queries.cuda(), i32(*[3] * 64), seqs=i32(*[0] * 64), scale=1.0, max_len=16, **kw)
+    got = torch.diagonal(got.double().cpu()[:, :, :64], dim1=0, dim2=2).T  # [row][head], channel = row
+    want = (left / (2 + w))[:, None].expand(-1, heads)
+    # the score in base 2 (at most 1.44) is off by 2^-23 of itself, the exponential by 2^-23, a third part by 2^-25 and
+    # nine sums of at most 1 by 2^-24 each
+    off = (1.0 * 2.0 ** -23 + 2.0 ** -23 + 2.0 ** -25 + 9 * 2.0 ** -24) / 2.0
+    bound = off + R.half_step(want, "bf16")
+    assert ((got - want).abs() <= bound).all(), float(((got - want).abs() / bound).max())
