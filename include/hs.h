@@ -513,7 +513,9 @@ int hs_paged_append(const hs_paged_cache *cache, int32_t layer, int32_t n, int32
  * lengths and the shared positions and shape the launch; positions from max_len on
  * are not attended, and of shared[g] more than max_shared is not taken as shared.
  * Scores and sums are fp32, and have to be finite; weights enter the second product
- * with 22 bits for HS_F16, 24 for HS_BF16 and HS_F32; values have to be finite.
+ * with 24 bits for HS_BF16 and HS_F32, for HS_F16 with 22, or to 2^-26 of the largest
+ * weight among the 32 or 64 positions that are summed at once, where that is more;
+ * values have to be finite.
  * q, out, ld_q and ld_out are aligned as in hs_paged_append.  workspace: device
  * memory of hs_paged_attention_workspace bytes (which may be 0: then it may be
  * NULL), 16-byte aligned; nothing in it is kept from call to call.  Calls that may

@@ -441,7 +441,7 @@ struct PagedAttn {
   int64_t pre_units;
   int n_pre, n_own;
   float *part_o;   // [n][n_heads][n_own + n_pre][head_dim]
-  float *part_ml;  // [n][n_heads][n_own + n_pre][2]: base-2 maximum (-inf: no position), sum
+  float *part_ml;  // [n][n_heads][n_own + n_pre][2]: base-2 score that weights are relative to (-inf: no position), sum
 };
 constexpr int PAGED_MAX_SPLITS = 64;
 void paged_plan(int dtype, int64_t n, int n_heads, int n_kv, int max_len, int n_groups, int max_shared, PagedAttn *a);

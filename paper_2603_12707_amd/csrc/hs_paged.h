@@ -194,6 +194,26 @@ constexpr int PG_STRIPE = PG_WAVES * 32;  // positions that a work group takes a
 // The third part costs those 14 % and others 2 to 3 %.)
 template <int DT>
 constexpr int PG_PARTS = DT == HS_BF16 ? 3 : 2;
+// Weights are 2^(score - m).  o / l does not depend on m, which moves only where a
+// wave's tile has a score that passes it by more than PG_UP, and then to PG_TO below that
+// column's largest.  The weights of fp32 and bf16 may fall as low as they like.  Those of
+// f16 end at 2^-24, so m moves down too, where a column's largest is less than PG_LOW
+// above it: o and l are fp32 and hold what came before.  So a weight is off by 2^-34 of the
+// largest up to its tile, and by 2^-26 of the largest in its tile, at most.  (With m at
+// the largest of all, thousands of equal positions 2^-25 below one vanished;
+// following them costs 3 % of large groups and 4 % of drafts.)  m stays within PG_DOWN of where it was highest, so that o is finite; scores that far
+// down weigh nothing.
+template <int DT>
+constexpr float PG_UP = DT == HS_F16 ? 15.f : 8.f;
+template <int DT>
+constexpr float PG_TO = DT == HS_F16 ? 9.f : 0.f;
+constexpr float PG_LOW = 1.f, PG_DOWN = 48.f;
+// f16: where m moves to for a tile whose largest score is top, `over` of it
+__device__ __forceinline__ float moved(float m, float top, float over, float highest) {
+  if (!(over > PG_UP<HS_F16> || over < PG_LOW) || top == -INFINITY) return m;
+  const float mn = fmaxf(top - PG_TO<HS_F16>, highest - PG_DOWN);
+  return top - mn > PG_UP<HS_F16> ? top : mn;  // (scores so large that the difference is rounded)
+}
 // two weights in parts
 template <int DT>
 __device__ __forceinline__ void weight_parts(float p0, float p1, uint32_t (&w)[PG_PARTS<DT>]) {
@@ -411,11 +431,11 @@ __device__ __forceinline__ void attn_columns(const PagedAttn &a, uint32_t block,
   };
 
   const float c2 = a.scale * 1.4426950408889634f;
-  float m[CT], l[CT];
+  float m[CT], l[CT], highest[CT];  // (the highest m: f16)
   f32x4 o[CT][VE];
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
-    m[ct] = -INFINITY;
+    m[ct] = highest[ct] = -INFINITY;
     l[ct] = 0.f;
 #pragma unroll
     for (int dt = 0; dt < VE; ++dt) o[ct][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -451,12 +471,21 @@ __device__ __forceinline__ void attn_columns(const PagedAttn &a, uint32_t block,
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = fmaxf(top, s[ct][u][i]);
-      // m, the same for the four lanes of a column, is raised only where a score
-      // passes it by more than 2^8: o / l does not depend on it
-      if (__ballot(top > m[ct] + 8.f)) {
+      // m is the same for the four lanes of a column
+      bool move = __ballot(top - m[ct] > PG_UP<DT>);
+      if constexpr (DT == HS_F16) {
+        uint64_t low = __ballot(top - m[ct] < PG_LOW);
+        low &= low >> 32;
+        move |= (low & low >> 16 & 0xFFFF) != 0;
+      }
+      if (move) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float mn = fmaxf(m[ct], top);
+        float mn = fmaxf(m[ct], top);
+        if constexpr (DT == HS_F16) {
+          mn = moved(m[ct], top, top - m[ct], highest[ct]);
+          highest[ct] = fmaxf(highest[ct], mn);
+        }
         const float corr = m[ct] == mn ? 1.f : __builtin_amdgcn_exp2f(m[ct] - mn);
         l[ct] *= corr;
 #pragma unroll
@@ -675,7 +704,7 @@ __device__ __forceinline__ void shared_columns(const PagedAttn &a, uint32_t bloc
       for (int w = 0; w < 4; ++w) q[k][w] = c2 == 0.f ? 0u : q[k][w] ^ 0x80008000u;
     c2 = c2 == 0.f ? 1.f : -c2;
   }
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, l = 0.f, highest = -INFINITY;
   f32x16 o[VE];
 #pragma unroll
   for (int dt = 0; dt < VE; ++dt)
@@ -703,8 +732,7 @@ __device__ __forceinline__ void shared_columns(const PagedAttn &a, uint32_t bloc
         for (int i = 0; i < 16; ++i)
           if (8 * (i / 4 & 1) + 4 * h + i % 4 >= s_rows[buf][2 * (u0 + u) + i / 8]) s[u][i] = -INFINITY;
     }
-    // scores less m, which is raised only where one passes it by more than 2^8 (or there
-    // is none yet): o / l does not depend on it
+    // scores less m
     const float ref = m == -INFINITY ? 0.f : m;
     float top = -INFINITY;
 #pragma unroll
@@ -714,9 +742,19 @@ __device__ __forceinline__ void shared_columns(const PagedAttn &a, uint32_t bloc
         s[u][i] = __builtin_fmaf(s[u][i], c2, -ref);
         top = fmaxf(top, s[u][i]);
       }
-    if (__ballot(top > 8.f || m == -INFINITY)) {
+    bool move = __ballot(top > PG_UP<DT> || m == -INFINITY);
+    if constexpr (DT == HS_F16) {
+      const uint64_t low = __ballot(top < PG_LOW);
+      move |= (uint32_t)(low & low >> 32) != 0;
+    }
+    if (move) {
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float mn = fmaxf(m, ref + top), up = mn == -INFINITY ? 0.f : mn - ref;
+      float mn = fmaxf(m, ref + top);
+      if constexpr (DT == HS_F16) {
+        mn = moved(m, ref + top, m == -INFINITY ? INFINITY : top, highest);
+        highest = fmaxf(highest, mn);
+      }
+      const float up = mn == -INFINITY ? 0.f : mn - ref;
       const float corr = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);
       l *= corr;
 #pragma unroll
@@ -725,7 +763,11 @@ __device__ __forceinline__ void shared_columns(const PagedAttn &a, uint32_t bloc
 #pragma unroll
       for (int u = 0; u < NU; ++u)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[u][i] -= up;
+        for (int i = 0; i < 16; ++i) {
+          s[u][i] -= up;
+          // (of scores so large that their sum with m is rounded; NaN stays)
+          if constexpr (DT == HS_F16) s[u][i] = s[u][i] > PG_UP<DT> ? PG_UP<DT> : s[u][i];
+        }
     }
     u32x4 ps[PG_PARTS<DT>];
     const auto parts = [&](int x) {  // of 16 positions

@@ -485,3 +485,92 @@ def test_weights_of_24_bits(hd, own, heads):
     off = (1.0 * 2.0 ** -23 + 2.0 ** -23 + 2.0 ** -25 + 9 * 2.0 ** -24) / 2.0
     bound = off + R.half_step(want, "bf16")
     assert ((got - want).abs() <= bound).all(), float(((got - want).abs() / bound).max())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("at", [0, 4100, 8000])
+@pytest.mark.parametrize("nats", [11.0, 13.5, 15.5, 17.5, 19.0])
+@pytest.mark.parametrize("n,group", [(1, 1), (5, 4), (40, 2), (90, 4)])
+def test_a_position_far_above_all_others(dtype, at, nats, n, group):
+    """Its value is 0, as of positions that take the weight which nothing else wants: what comes out is the others', some
+    2^-16 to 2^-28 of it each, of rows by themselves and of groups in tiles of every width."""
+    import paper_2603_12707_amd as hs
+    length, hd, dt = 8001, 64, R.DT[dtype]
+    width = -(-length // 256)
+    blocks = torch.zeros(width, 1, 2, 1, 256, hd, dtype=dt)
+    blocks[at // 256, 0, 0, 0, at % 256, 0] = nats
+    blocks[:, 0, 1, 0] = (1.0 + torch.arange(hd) / hd).to(dt)
+    blocks[at // 256, 0, 1, 0, at % 256] = 0.0
+    table = torch.randperm(width, generator=gen(2))[None]
+    placed = torch.empty_like(blocks)
+    placed[table[0]] = blocks
+    q = torch.zeros(n, group, hd, dtype=dt)
+    q[:, :, 0] = 1.0
+    own = torch.zeros(n, dtype=torch.int32)
+    lengths = torch.full((n,), length, dtype=torch.int32)
+    want, off = R.attention(q[:1, :1], placed, table, 0, lengths[:1], own[:1], scale=1.0)  # every row and head alike
+    cache = hs.PagedCache(placed.cuda(), table.cuda())
+    for shared in (0, 8000, length) if n > 1 else (0,):
+        kw = {}
+        if shared:
+            kw = dict(group_starts=torch.tensor([0, n], dtype=torch.int32).cuda(), max_shared=shared,
+                      shared=torch.tensor([shared], dtype=torch.int32).cuda())
+        got = cache.attention(0, q.cuda(), lengths.cuda(), seqs=own.cuda(), scale=1.0, **kw)
+        close(got, want.expand(n, group, -1), off.expand(n, group, -1), dtype)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("order", ["falling", "rising", "steps"])
+def test_scores_that_fall_and_rise_along_a_row(hd, order):
+    """f16 weights over 60 bits and more, in either order, so that no one scale holds them all."""
+    import paper_2603_12707_amd as hs
+    length, g = 3000, gen(hd)
+    table = torch.randperm(12, generator=g)[None]
+    score = {"falling": torch.linspace(45, 0, 3072), "rising": torch.linspace(0, 45, 3072),
+             "steps": torch.tensor([0.0, 14.0, 3.0, 44.0, 20.0, 0.0]).repeat_interleave(512)}[order]
+    k = torch.zeros(12, 256, hd)
+    k[..., 0] = score.reshape(12, 256)
+    v = torch.randn(12, 256, hd, generator=g)
+    blocks = torch.zeros(12, 1, 2, 1, 256, hd, dtype=torch.float16)
+    blocks[table[0], 0, 0, 0], blocks[table[0], 0, 1, 0] = k.half(), v.half()
+    for n, group in ((3, 1), (33, 2), (49, 4)):
+        q = torch.zeros(n, group, hd)
+        q[..., 0] = torch.linspace(-1, 1, n * group).reshape(n, group)
+        q[..., 1:] = torch.randn(n, group, hd - 1, generator=g)
+        kw = dict(seqs=torch.zeros(n, dtype=torch.int32), scale=1.0, layers=1, blocks=blocks.cuda(), q=q.half())
+        lengths = torch.randint(1, length, (n,), generator=g, dtype=torch.int32)
+        attend_case(hs, "f16", hd, 1, group, lengths, table, 12, 256, **kw)
+        lengths = torch.full((n,), length, dtype=torch.int32)
+        attend_case(hs, "f16", hd, 1, group, lengths, table, 12, 256, torch.tensor([0, n], dtype=torch.int32),
+                    torch.tensor([2900], dtype=torch.int32), **kw)
+
+
+@pytest.mark.parametrize("loud", [30.0, 300.0])
+def test_loud_scores_in_half_precision(loud):
+    import paper_2603_12707_amd as hs
+    for n, groups, kv, hd in ((60, 1, 1, 128), (20, 2, 2, 64)):
+        lengths, table, starts, shared, total = grouped(n, groups, [200], [1, 70], 16, 7)
+        attend_case(hs, "f16", hd, kv, 4, lengths, table, total, 16, starts, shared, loud=loud)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("n,group", [(6, 2), (50, 2), (50, 5)])
+def test_nan_and_immense_queries_are_their_own(dtype, n, group):
+    """A NaN query gives NaN; scores of 10^9, whose differences to a maximum are rounded, give finite outputs, and other
+    rows are as without them."""
+    import paper_2603_12707_amd as hs
+    lengths, table, starts, shared, total = grouped(n, 1, [320], [20, 90], 16, 8)
+    blocks = R.blocks(total, 1, 1, 16, 64, dtype, 4)
+    cache = hs.PagedCache(blocks, table.cuda())
+    q = torch.randn(n, group, 64, generator=gen(2)).to(R.DT[dtype])
+    call = lambda q, **kw: cache.attention(0, q.cuda(), lengths.cuda(), scale=1000.0, **kw)  # noqa: E731
+    kw = dict(group_starts=starts.cuda(), shared=shared.cuda())
+    q[3] = 60000.0 * torch.sign(q[3])
+    first = [call(q), call(q, **kw)]
+    q[2, 1, 3] = math.nan
+    for got, before in zip((call(q), call(q, **kw)), first):
+        assert bool(torch.isfinite(before).all())
+        assert bool(torch.isnan(got[2, 1]).all())
+        rest = torch.ones(n, group, dtype=torch.bool)
+        rest[2, 1] = False
+        assert torch.equal(got[rest.cuda()], before[rest.cuda()])
