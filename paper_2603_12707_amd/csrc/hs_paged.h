@@ -200,9 +200,9 @@ constexpr int PG_PARTS = DT == HS_BF16 ? 3 : 2;
 // f16 end at 2^-24, so m moves down too, where a column's largest is less than PG_LOW
 // above it: o and l are fp32 and hold what came before.  So a weight is off by 2^-34 of the
 // largest up to its tile, and by 2^-26 of the largest in its tile, at most.  (With m at
-// the largest of all, thousands of equal positions 2^-25 below one vanished;
-// following them costs 3 % of large groups and 4 % of drafts.)  m stays within PG_DOWN of where it was highest, so that o is finite; scores that far
-// down weigh nothing.
+// the largest of all, thousands of equal positions 2^-25 below one vanished; following
+// them costs 3 % of large groups and 4 % of drafts.)  m stays within PG_DOWN of where it
+// was highest, so that o is finite; scores that far down weigh nothing.
 template <int DT>
 constexpr float PG_UP = DT == HS_F16 ? 15.f : 8.f;
 template <int DT>
