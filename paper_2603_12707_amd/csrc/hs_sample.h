@@ -56,14 +56,15 @@ __device__ __forceinline__ SampleRow sample_row(const SampleArgs &a, int64_t at)
   r.top_p = a.top_p ? a.top_p[at] : 1.f;
   r.min_p = a.min_p ? a.min_p[at] : 0.f;
   const int k = a.top_k ? a.top_k[at] : 0;
-  r.top_k = k <= 0 || k > a.vocab ? a.vocab : k;
+  // (no weight reaches a min_p above 1: the first alone stays, whatever equals it)
+  r.top_k = r.min_p > 1.f ? 1 : k <= 0 || k > a.vocab ? a.vocab : k;
   r.bad = !(t >= 0.f) || t == INFINITY || r.top_p != r.top_p || r.min_p != r.min_p || u != u;
   r.greedy = t == 0.f;
   r.inv_t = 1.0 / (double)t;
   r.u = u < 0.f ? 0.0 : u >= 1.f ? 1.0 - 0x1p-24 : (double)u;
   return r;
 }
-// the least float that min_p leaves, M at most
+// the least float that min_p leaves, M at most (of a min_p above 1 top_k leaves the first)
 __device__ __forceinline__ float min_p_floor(const SampleRow &p, float M) {
   const double least = fmin((double)M + log((double)p.min_p) / p.inv_t, (double)M);
   float f = (float)fmax(least, -(double)FLT_MAX);

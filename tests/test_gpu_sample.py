@@ -247,3 +247,21 @@ def test_no_rows():
     import paper_2603_12707_amd as hs
     t, lp = hs.sample_tokens(torch.empty(0, 100, device="cuda"), torch.empty(0, device="cuda"))
     assert t.shape == lp.shape == (0,)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [40, 250, 1000, 5000, 70000])
+def test_a_min_p_above_one_leaves_the_first(vocab, dtype):
+    """Among equal largest logits too: of weights of 1 none reaches it."""
+    import paper_2603_12707_amd as hs
+    x = torch.randint(0, 3, (6, vocab), generator=gen(vocab)).float()
+    x[1] = 0.0
+    x[2, 3:] = -math.inf
+    x[3] = 2.0
+    x[3, : vocab // 2] = 1.0
+    m = torch.tensor([1.5, 1.0 + 2.0 ** -23, math.inf, 7.0, 1.0, 1.0 - 2.0 ** -24])
+    k, p, t = torch.tensor([0, vocab // 2, 0, 5, 0, 0]), torch.tensor([1.0, 0.5, 1.0, 1.0, 1.0, 1.0]), torch.full((6,), 0.5)
+    for u in (0.0, 0.5, 1.0 - 2.0 ** -24):
+        uu = torch.full((6,), u)
+        check(hs, x.to(R.DT[dtype]), uu, min_p=m)
+        check(hs, x.to(R.DT[dtype]), uu, t, k, p, m)
