@@ -809,13 +809,14 @@ __global__ __launch_bounds__(SD_THREADS) void k_sample_draw(SampleArgs a) {
       take(key_float((uint32_t)(k >> 32)), (uint32_t)k);
     }
   };
-  // the part of a bin that a logit lies in, -1: in none that is needed
+  // the part of a bin that a logit lies in, -1: in none that is needed.  (xs - b of an xs
+  // just below zero is rounded to 1: that lies in its bin's first part)
   const auto part = [&](float v, double &xs, double &b) {
     xs = (double)v * s;
     b = floor(xs);
     const double d = b0 - b;
     const int at = d < SM_BINS - 1 ? lds.slot[(int)d] : -1;
-    return at < 0 ? -1 : at * SD_SUB + SD_SUB - 1 - (int)((xs - b) * SD_SUB);
+    return at < 0 ? -1 : at * SD_SUB + SD_SUB - 1 - min((int)((xs - b) * SD_SUB), SD_SUB - 1);
   };
   each([&](float v, uint32_t low) {
     double xs, b;

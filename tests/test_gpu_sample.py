@@ -265,3 +265,26 @@ def test_a_min_p_above_one_leaves_the_first(vocab, dtype):
         uu = torch.full((6,), u)
         check(hs, x.to(R.DT[dtype]), uu, min_p=m)
         check(hs, x.to(R.DT[dtype]), uu, t, k, p, m)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [40, 300, 1000, 5000, 40000])
+def test_logits_just_below_zero(vocab, dtype):
+    """x / T nearer to zero than a rounding of one, from below: at the end of a range of values that begins at -1/16."""
+    import paper_2603_12707_amd as hs
+    g = gen(vocab)
+    x = -torch.rand(6, vocab, generator=g) - 0.5
+    x[0] *= 1e-20
+    x[1] *= 1e-30
+    x[1, vocab // 2 :] = -1.5
+    x[3, ::3] = -1e-25
+    x[4, 7] = 0.05
+    x[4, 8:20] *= 1e-22
+    x[5] = torch.where(torch.arange(vocab) % 2 == 0, -1e-19, 0.1)
+    t = torch.tensor([1.0, 1.0, 1e20, 0.7, 1.0, 1.0])
+    p = torch.tensor([0.5, 0.9, 0.3, 0.2, 0.6, 0.75])
+    for u in (0.0, 0.4, 0.9):
+        uu = torch.full((6,), u)
+        check(hs, x.to(R.DT[dtype]), uu, t)
+        check(hs, x.to(R.DT[dtype]), uu, t, top_p=p)
+        check(hs, x.to(R.DT[dtype]), uu, t, top_k=torch.tensor([17, 30, 1, 12, 9, 33]))
