@@ -581,8 +581,9 @@ int hs_decode_step_logprobs(hs_model *m, hs_kv *kv, const int32_t *tokens_in, in
  * (NULL: 0): device int32 [rows].  Logits of -inf are never drawn.  A row of logits
  * that holds a NaN or +inf, or nothing but -inf, or whose temperature is negative
  * or infinite, or with a NaN among its parameters, has token -1 and logprob NaN.
- * Weights and their sums are held in 64 bits, and results are the same from call to
- * call.  workspace: device memory of hs_sample_tokens_workspace bytes under the rules
+ * Weights and their sums are held in 64 bits or more (in rows whose borders lie among
+ * thousands of near logits or 63 below the largest, as multiples of 2^-63 of the
+ * largest weight), and results are the same from call to call.  workspace: device memory of hs_sample_tokens_workspace bytes under the rules
  * of hs_paged_attention's. */
 int hs_sample_tokens_workspace(int64_t rows, int32_t vocab, uint64_t *bytes);
 int hs_sample_tokens(int32_t dtype, const void *logits, int64_t rows, int32_t vocab, int64_t ld, const float *u,

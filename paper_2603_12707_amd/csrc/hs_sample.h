@@ -377,7 +377,8 @@ struct DrawLds {
   float run_lo[SD_RUNS], run_hi[SD_RUNS];
   int bk, bp0, bp1, bt0, bt1, n, n_few, pick, last;
   uint32_t digit;
-  uint64_t above_u, number, ties;
+  double above;
+  uint64_t number, ties;
 };
 
 // sums over the threads before this one and up to it
@@ -412,11 +413,28 @@ __device__ __forceinline__ double block_largest(double v, double *s_tmp) {
   return v;
 }
 
+// A sum of weights that are whole multiples of 2^-63, in any order the same: up to 2^30
+// of them fit, their upper and lower 32 bits apart.
+struct Mass {
+  unsigned long long hi, lo;
+  __device__ __forceinline__ void add(uint64_t w) {
+    hi += w >> 32;
+    lo += w & 0xFFFFFFFFu;
+  }
+  __device__ __forceinline__ void add(const Mass &m) {
+    hi += m.hi;
+    lo += m.lo;
+  }
+  __device__ __forceinline__ double value() const { return (double)hi * 0x1p32 + (double)lo; }
+};
+
 // A row by itself, whatever it holds: each border and the draw by four passes over
 // the row, a byte of the value each, over sums of the weights in whole multiples of
-// a unit that no sum of the row overflows.  For rows of which more than SD_FEW logits
-// lie in the parts of bins that count (many equal ones, mostly), or whose borders lie in
-// the last bin: some 200 us for 112677 bf16 logits of which thousands are equal.
+// 2^-63 of the largest.  (Multiples of a unit that the row's sum takes in 64 bits, 2^-44 of
+// 200000 logits, are a tenth faster and lose many small weights under a large one.)  For rows of which more
+// than SD_FEW logits lie in the parts of bins that count (many equal ones, mostly), or whose
+// borders lie in the last bin: some 200 us for 112677 bf16 logits of which thousands are
+// equal.
 template <int DT>
 __device__ __attribute__((noinline)) void draw_alone(const SampleArgs &a, DrawLds &lds, const SampleRow &p, int64_t row,
                                                      int64_t slot, float M) {
@@ -424,47 +442,52 @@ __device__ __attribute__((noinline)) void draw_alone(const SampleArgs &a, DrawLd
   const int V = a.vocab, tid = threadIdx.x;
   const H h{(const char *)a.logits + row * a.ld * H::B, V};
   const char *x = h.x;
-  const int bits = 62 - (32 - __clz(V));  // V * 2^bits stays below 2^62
-  const double unit = (double)(1ull << bits), least = (double)M;
-  const auto weight = [&](float v) { return (uint64_t)rint(exp(((double)v - least) * p.inv_t) * unit); };
+  const double least = (double)M;
+  const auto weight = [&](float v) { return (uint64_t)rint(exp(((double)v - least) * p.inv_t) * 0x1p63); };
   const auto each = [&](auto f) {
     h.chunks([&](const float *v, int) {
       for (int e = 0; e < H::CE; ++e)
         if (v[e] > -INFINITY) f(v[e]);  // (-inf stands for what is past the row's end, and is never drawn)
     });
   };
+  unsigned long long *const his = lds.bins.mass, *const los = lds.bins.mass + 256;
   // a number and a weight of every thread, summed
-  const auto sum = [&](unsigned long long &n, unsigned long long &m) {
+  const auto sum = [&](unsigned long long &n, Mass m) {
+    unsigned long long *all = lds.bins.mass;
     __syncthreads();
-    if (tid == 0) lds.bins.mass[0] = lds.bins.mass[1] = 0;
+    if (tid < 3) all[tid] = 0;
     __syncthreads();
-    atomicAdd(&lds.bins.mass[0], n);
-    atomicAdd(&lds.bins.mass[1], m);
+    atomicAdd(&all[0], n);
+    atomicAdd(&all[1], m.hi);
+    atomicAdd(&all[2], m.lo);
     __syncthreads();
-    n = lds.bins.mass[0];
-    m = lds.bins.mass[1];
+    n = all[0];
+    return Mass{all[1], all[2]}.value();
   };
   // the value at which `cross` (of the number and the weight up to it) becomes true
   // first; all above it, and its ties
   uint32_t edge = 0;
-  uint64_t above = 0, number = 0, ties = 0;
+  double above = 0.0;
+  uint64_t number = 0, ties = 0;
   const auto find = [&](auto cross, bool by_weight) {
     edge = 0;
-    above = number = 0;
+    number = 0;
+    Mass over{0, 0};  // (thread 0)
     for (int shift = 24; shift >= 0; shift -= 8) {
       __syncthreads();
       if (tid < 256) {
-        lds.bins.mass[tid] = 0;
+        his[tid] = los[tid] = 0;
         lds.bins.count[tid] = 0;
       }
       __syncthreads();
       // (a run of equal digits, of which there are many, is added at once)
       uint32_t digit = 0, n = 0;
-      unsigned long long m = 0;
+      Mass m{0, 0};
       const auto put = [&] {
         if (!n) return;
         atomicAdd(&lds.bins.count[digit], n);
-        atomicAdd(&lds.bins.mass[digit], m);
+        atomicAdd(&his[digit], m.hi);
+        atomicAdd(&los[digit], m.lo);
       };
       each([&](float v) {
         const uint32_t k = value_key(v);
@@ -473,79 +496,85 @@ __device__ __attribute__((noinline)) void draw_alone(const SampleArgs &a, DrawLd
           put();
           digit = k >> shift & 255;
           n = 0;
-          m = 0;
+          m = Mass{0, 0};
         }
         ++n;
-        m += weight(v);
+        m.add(weight(v));
       });
       put();
       __syncthreads();
       if (tid == 0) {
-        uint64_t m = above, n = number;
+        Mass up = over, last_up = over;
+        uint64_t n = number, last_n = n;
         int d = 255, last = -1;
-        uint64_t lm = m, ln = n;
         for (; d >= 0; --d) {
           const uint64_t c = lds.bins.count[d];
           if (!c) continue;
-          if (!by_weight || lds.bins.mass[d]) last = d, lm = m, ln = n;
-          if (cross(n + c, m + lds.bins.mass[d])) break;
+          const Mass of{his[d], los[d]};
+          if (!by_weight || of.hi || of.lo) last = d, last_up = up, last_n = n;
+          Mass to = up;
+          to.add(of);
+          if (cross(n + c, to.value())) break;
           n += c;
-          m += lds.bins.mass[d];
+          up = to;
         }
-        if (d < 0) d = last, m = lm, n = ln;  // (rounding: the last that counts)
+        if (d < 0) d = last, up = last_up, n = last_n;  // (rounding: the last that counts)
+        over = up;
         lds.digit = (uint32_t)d;
-        lds.above_u = m;
+        lds.above = up.value();
         lds.number = n;
         lds.ties = lds.bins.count[d];
       }
       __syncthreads();
       edge |= lds.digit << shift;
-      above = lds.above_u;
+      above = lds.above;
       number = lds.number;
       ties = lds.ties;
     }
   };
-  unsigned long long kept = 0, total = 0;  // of the row's beginning
+  unsigned long long kept = 0;  // of the row's beginning
+  Mass row_mass{0, 0};
   each([&](float v) {
     ++kept;
-    total += weight(v);
+    row_mass.add(weight(v));
   });
-  sum(kept, total);
+  double total = sum(kept, row_mass);
   if ((uint64_t)p.top_k < kept) {
-    find([&](uint64_t n, uint64_t) { return n >= (uint64_t)p.top_k; }, false);
+    find([&](uint64_t n, double) { return n >= (uint64_t)p.top_k; }, false);
     kept = p.top_k;
-    total = above + (kept - number) * weight(key_float(edge));
+    total = above + (double)(kept - number) * (double)weight(key_float(edge));
   }
   if (p.top_p < 1.f) {
-    const double want = fmax((double)p.top_p * (double)total * (1 - SM_EQUAL), 0.5);
+    const double want = fmax((double)p.top_p * total * (1 - SM_EQUAL), 0.5);
     const uint64_t most = kept;
-    find([&](uint64_t, uint64_t m) { return (double)m >= want; }, true);
-    const uint64_t w = weight(key_float(edge));
-    const double n = ceil((want - (double)above) / (double)w);
+    find([&](uint64_t, double m) { return m >= want; }, true);
+    const double w = (double)weight(key_float(edge));
+    const double n = ceil((want - above) / w);
     ties = min(n >= (double)ties ? ties : n > 1.0 ? (uint64_t)n : 1ull, most - number);
-    total = above + ties * w;
+    total = above + (double)ties * w;
     kept = number + ties;
   }
   if (p.min_p > 0.f) {
     // how many reach it, and their weight
     const float least_x = min_p_floor(p, M);
-    unsigned long long n = 0, m = 0;
+    unsigned long long n = 0;
+    Mass m{0, 0};
     each([&](float v) {
       if (v >= least_x) {
         ++n;
-        m += weight(v);
+        m.add(weight(v));
       }
     });
-    sum(n, m);
+    const double reach = sum(n, m);
     if (n < kept) {
       kept = n;
-      total = m;
+      total = reach;
     }
   }
-  const double want = (p.u + SM_EQUAL) * (double)total;
-  find([&](uint64_t, uint64_t m) { return (double)m > want; }, true);
-  const uint64_t w = weight(key_float(edge));
-  const double nth = floor((want - (double)above) / (double)w);
+  const double want = (p.u + SM_EQUAL) * total;
+  find([&](uint64_t, double m) { return m > want; }, true);
+  const double w = (double)weight(key_float(edge));
+  const double nth = floor((want - above) / w);
   ties = min(ties, kept - number);
   int64_t left = nth >= (double)ties ? (int64_t)ties - 1 : nth > 0.0 ? (int64_t)nth : 0;
   // the left-th index that holds it
@@ -564,7 +593,7 @@ __device__ __attribute__((noinline)) void draw_alone(const SampleArgs &a, DrawLd
     if (left < all) {
       if (is && before + (int)__popcll(in & ((1ull << (tid & 63)) - 1)) == left) {
         a.tokens[slot] = i;
-        if (a.logprob) a.logprob[row] = (float)log((double)w / (double)total);
+        if (a.logprob) a.logprob[row] = (float)(((double)key_float(edge) - least) * p.inv_t - log(total * 0x1p-63));
       }
       return;
     }

@@ -288,3 +288,27 @@ def test_logits_just_below_zero(vocab, dtype):
         check(hs, x.to(R.DT[dtype]), uu, t)
         check(hs, x.to(R.DT[dtype]), uu, t, top_p=p)
         check(hs, x.to(R.DT[dtype]), uu, t, top_k=torch.tensor([17, 30, 1, 12, 9, 33]))
+
+
+@pytest.mark.parametrize("vocab", [20000, 32768, 100000, 600000])
+def test_many_small_weights_of_rows_drawn_from_by_themselves(vocab):
+    """Each below 2^-44 of the first one's, as log probabilities show them together; a min_p below them all leaves them
+    in, and its border lies past the bins."""
+    import paper_2603_12707_amd as hs
+    x = torch.full((6, vocab), -32.5)
+    x[1] = -35.0
+    x[2, : vocab // 2] = -30.7
+    x[3] = torch.linspace(-28, -38, vocab)
+    x[4] = -42.0
+    x[5] = -31.0 - torch.arange(vocab).float() / vocab
+    x[:, 11] = 0.0
+    m = torch.full((6,), 1e-30)
+    for u in (0.0, 0.5, 1.0 - 2.0 ** -24):
+        uu = torch.full((6,), u)
+        for k in (None, torch.tensor([vocab // 2, vocab - 5, 0, vocab // 3, 0, 20])):
+            got, lp = hs.sample_tokens(x.cuda(), uu.cuda(), top_k=None if k is None else k.int().cuda(), min_p=m.cuda())
+            want, ref = R.draw(x, uu, top_k=k, min_p=m)
+            assert torch.equal(got.cpu(), want)
+            # the 64-bit form adds up to vocab numbers to a sum between 1 and 2, one after the other, off by 2^-53 each
+            # at most (most of them the same way: the small ones are equal); the log probability is rounded once
+            assert ((lp.double().cpu() - ref).abs() <= ref.abs() * 2.0 ** -24 + vocab * 2.0 ** -53).all()
