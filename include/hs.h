@@ -469,9 +469,9 @@ typedef struct hs_rope {
   int32_t n_pairs, n_axes, adjacent;
 } hs_rope;
 
-/* New rows of one layer, n of them (n * (n_heads + 2 n_kv_heads) below 2^28): keys
- * normalised (k_gain not NULL: x / sqrt(mean x^2 + eps) * k_gain over the head's
- * channels), turned (rope not NULL) and stored, values stored as they are, and
+/* New rows of one layer, n of them (below 2^26, and n * (n_heads + 2 n_kv_heads)
+ * below 2^28): keys normalised (k_gain not NULL: x / sqrt(mean x^2 + eps) * k_gain
+ * over the head's channels), turned (rope not NULL) and stored, values stored as they are, and
  * with n_heads > 0 queries normalised (q_gain) and turned alike into q_out.  Angles
  * are taken in 64 bits, the rest in fp32, rounded once.  Element (row r, head j,
  * channel c) of k is k[r * ld + j * ld_head + c] (v alike), of q q[r * ld_q + j *

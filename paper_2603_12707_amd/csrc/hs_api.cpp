@@ -1682,8 +1682,9 @@ int hs_paged_append(const hs_paged_cache *cache, int32_t layer, int32_t n, int32
   if (((uintptr_t)k | (uintptr_t)v) % 16 || (n_heads && ((uintptr_t)q | (uintptr_t)q_out) % 16) ||
       ((uintptr_t)q_gain | (uintptr_t)k_gain) % 16)
     return fail(HS_E_INVALID, "%s: rows and gains must be 16-byte aligned", fn);
-  // (a launch takes less than 2^32 threads: 8 or 16 to a head)
-  if ((int64_t)n * (n_heads + 2 * cache->n_kv_heads) >= 1 << 28) return fail(HS_E_INVALID, "%s: too many rows", fn);
+  // (a launch takes less than 2^32 threads: 256 to at most 4 rows, 8 or 16 to a head)
+  if (n >= 1 << 26 || (int64_t)n * (n_heads + 2 * cache->n_kv_heads) >= 1 << 28)
+    return fail(HS_E_INVALID, "%s: too many rows", fn);
   rc = kvq_strides(fn, cache->dtype, n, ld, ld_head, cache->n_kv_heads, cache->head_dim);
   if (!rc && n_heads) rc = kvq_strides(fn, cache->dtype, n, ld_q, ld_q_head, n_heads, cache->head_dim);
   if (!rc && n_heads) rc = kvq_strides(fn, cache->dtype, n, ld_q_out, ld_q_out_head, n_heads, cache->head_dim);

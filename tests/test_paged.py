@@ -174,3 +174,10 @@ def test_the_binding_refuses():
     for bad in (x[0], x.T, x.int()):
         with pytest.raises(ValueError):
             hs.sample_tokens(bad, u)
+
+
+@pytest.mark.parametrize("kv,heads", [(1, 0), (1, 1), (1, 2)])
+def test_more_rows_than_a_launch_takes_are_refused(kv, heads):
+    """Of few heads: a work group takes four rows at most, however few they hold."""
+    rows = dict(heads=heads, ld=2 * 64, ld_q=2 * 64, ld_qo=2 * 64)
+    assert append(cache(n_kv_heads=kv), n=1 << 26, **rows) == H.HS_E_INVALID
