@@ -181,3 +181,20 @@ def test_more_rows_than_a_launch_takes_are_refused(kv, heads):
     """Of few heads: a work group takes four rows at most, however few they hold."""
     rows = dict(heads=heads, ld=2 * 64, ld_q=2 * 64, ld_qo=2 * 64)
     assert append(cache(n_kv_heads=kv), n=1 << 26, **rows) == H.HS_E_INVALID
+
+
+def test_sample_workspaces_of_every_length():
+    """Rows up to 32768 logits need none, longer ones some; a call says so before it writes anything."""
+    need = ctypes.c_uint64()
+    for vocab in (1, 64, 257, 32000, 32768):
+        assert hs.lib().hs_sample_tokens_workspace(5, vocab, ctypes.byref(need)) == H.HS_OK
+        assert need.value == 0
+    last = 0
+    for vocab in (32769, 65536, 152064, 200001):
+        assert hs.lib().hs_sample_tokens_workspace(3, vocab, ctypes.byref(need)) == H.HS_OK
+        assert need.value >= max(1, last) and need.value % 3 == 0
+        last = need.value
+        for dtype in (H.HS_F32, H.HS_F16, H.HS_BF16):
+            long = dict(dtype=dtype, rows=3, vocab=vocab, ld=vocab)
+            assert sample(ws_bytes=need.value - 1, **long) == H.HS_E_BUFFER
+            assert sample(ws=None, **long) == H.HS_E_BUFFER
