@@ -103,7 +103,10 @@ __device__ __forceinline__ uint64_t bin_weight(double xs, double b) {
   return __builtin_bit_cast(uint64_t, e + SM_ONE) - __builtin_bit_cast(uint64_t, SM_ONE);
 }
 // The same in the last bin, where all lies 63 below the part's largest: its whole
-// sum is 2^14 e^-63 of that one's weight, and fp32 does for it.
+// sum is 2^15 e^-63 of that one's weight at most, 2^-75, and fp32 does for it: its
+// exponential is off by 2^-15 of itself (the argument, up to 200, is rounded to 2^-17 and its
+// product with log2 e to 2^-16), 2^-90 of the part, where bounds are 1e-12 wide.  (Where a
+// border lies among these the row is drawn from by itself.)
 __device__ __forceinline__ uint64_t tail_weight(double xs, double b) {
 #pragma clang fp contract(off)
   const float e = __expf((float)fmax((xs - (b + 1.0)) * (1.0 / SM_FINE), -200.0));
