@@ -501,11 +501,12 @@ int hs_paged_append(const hs_paged_cache *cache, int32_t layer, int32_t n, int32
  * one sequence: rows of lengths L + 1, L + 2, ... are its next tokens, each of
  * which sees those before it.
  *
- * Groups.  With n_groups > 0 (at most n), rows group_starts[g] .. group_starts[g +
- * 1] - 1 (device int32 [n_groups + 1], not falling, within 0..n) are group g and have
- * their first shared[g] positions (device int32) in common: those are read through
- * the table row of the group's first row, once for all its rows.  Rows before
- * group_starts[0] or from group_starts[n_groups] on are in no group.  A row whose
+ * Groups.  With n_groups > 0 (at most n, and at most 65536, among which each work
+ * group looks its own up), rows group_starts[g] .. group_starts[g + 1] - 1 (device
+ * int32 [n_groups + 1], not falling, within 0..n) are group g and have their first
+ * shared[g] positions (device int32) in common: those are read through the table row
+ * of the group's first row, once for all its rows.  Rows before group_starts[0] or
+ * from group_starts[n_groups] on are in no group.  A row whose
  * length is less than shared[g] attends over its length of them.  The arrays may
  * change between replays of a captured call.
  *

@@ -1732,6 +1732,8 @@ int hs_paged_attention_workspace(const hs_paged_cache *cache, int32_t n, int32_t
     return fail(HS_E_INVALID, "%s: negative row count, or max_len not in 1..2^30", fn);
   if (n_groups < 0 || n_groups > n || max_shared < 0 || max_shared > max_len)
     return fail(HS_E_INVALID, "%s: n_groups is not in 0..n, or max_shared not in 0..max_len", fn);
+  // (every work group looks its own up among them)
+  if (n_groups > 65536) return fail(HS_E_INVALID, "%s: more than 65536 groups", fn);
   if (n_heads <= 0 || n_heads % cache->n_kv_heads || n_heads / cache->n_kv_heads > 16)
     return fail(HS_E_INVALID, "%s: n_heads %d is not 1..16 times n_kv_heads %d", fn, n_heads, cache->n_kv_heads);
   // (a launch takes less than 2^32 threads: 256 to a row, KV head and split)

@@ -198,3 +198,16 @@ def test_sample_workspaces_of_every_length():
             long = dict(dtype=dtype, rows=3, vocab=vocab, ld=vocab)
             assert sample(ws_bytes=need.value - 1, **long) == H.HS_E_BUFFER
             assert sample(ws=None, **long) == H.HS_E_BUFFER
+
+
+def test_more_groups_than_a_work_group_looks_through_are_refused():
+    """Their time grows with their square: 16384 groups of one row and 8 KV heads take 23 ms, 4 million would take minutes."""
+    need = ctypes.c_uint64()
+    c = cache()
+    size = lambda n, groups: hs.lib().hs_paged_attention_workspace(  # noqa: E731
+        ctypes.byref(c), n, 2, 96, groups, 32, ctypes.byref(need))
+    assert size(65537, 65537) == H.HS_E_INVALID
+    assert size(1 << 20, 1 << 20) == H.HS_E_INVALID
+    assert size(1 << 20, 65536) == H.HS_OK
+    assert attend(c, n=1 << 20, heads=2, ld_q=128, ld_out=128, groups=1 << 20, starts=AT, shared=AT,
+                  max_shared=32) == H.HS_E_INVALID
