@@ -513,6 +513,8 @@ int hs_paged_append(const hs_paged_cache *cache, int32_t layer, int32_t n, int32
  * max_len and max_shared (host, max_len 1..2^30, max_shared 0..max_len) bound the
  * lengths and the shared positions and shape the launch; positions from max_len on
  * are not attended, and of shared[g] more than max_shared is not taken as shared.
+ * Rows' own positions are split over work groups as if max_len - max_shared were the
+ * most: where few rows have more of their own, a lower max_shared is faster.
  * Scores and sums are fp32, and have to be finite; weights enter the second product
  * with 24 bits for HS_BF16 and HS_F32, for HS_F16 with 22, or to 2^-26 of the largest
  * weight among the 32 or 64 positions that are summed at once, where that is more;

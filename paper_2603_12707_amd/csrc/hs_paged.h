@@ -332,7 +332,7 @@ __device__ __forceinline__ PagedUnit paged_unit(const PagedAttn &a, int unit, in
 // Loads go through buffer descriptors made for a tile of 16 positions, which
 // end where the positions do: what lies past them reads as zeros.
 //
-// 256 rows of 1 to 2048 positions and 4 KV heads take 113 us, 4.7 TB/s: memory, with two
+// 256 rows of 1 to 2048 positions and 4 KV heads take 114 us, 4.7 TB/s: memory, with two
 // work groups to a CU (registers) and rows of uneven length.  Short rows are a chain of
 // loads (group, length, block number, first tiles): 23 us for 32 rows of 32 heads and
 // some 200 positions.
@@ -615,13 +615,14 @@ __device__ __forceinline__ void attn_columns(const PagedAttn &a, uint32_t block,
 // in parts, as in attn_columns.  16-byte chunk j of K's row p lies at chunk j ^ p, so
 // that the 32 rows that a product reads spread over the banks.
 //
-// 256 rows of 28 heads over 32768 positions: 219 us, 550 TFLOP/s by the definition's
-// operations, 820 with the second part of P.  A wave's tile is 1536 cycles of products
-// and about as many of vector instructions, and two waves to a SIMD overlap them in
-// part: of some 5300 cycles a tile the copies' issue takes 1000 to 1700 with four waves.
-// Eight waves copy half as much a column (242 to 231 us), columns that rows lie across
-// fill the tiles (219).  Tiles of 32 positions, three under way: 267; K, V and weights
-// through registers alone, a wave to itself: 304.
+// 256 rows of 28 heads over 32768 positions in bf16: 271 us, 440 TFLOP/s by the
+// definition's operations, 890 with the parts of P.  A wave's tile is 2048 cycles of
+// products and more than that of vector instructions, and two waves to a SIMD overlap
+// them in part: the matrix cores are busy 48 % of the time, the vector units 53 %.
+// With P in two parts (1536 cycles of products) it was 219: eight waves copy half as much a
+// column as four (242 to 231 us), columns that rows lie across fill the tiles (219).  Tiles of
+// 32 positions, three under way: 267; K, V and weights through registers alone, a wave to
+// itself: 304.
 // Few columns (HALVES 2: 64 at most) are two waves' each; the other two take the same
 // columns over the other half of each tile, and the halves are joined in LDS.
 template <int HD>

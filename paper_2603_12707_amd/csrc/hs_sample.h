@@ -663,8 +663,8 @@ __device__ __forceinline__ DrawCuts draw_cuts(DrawLds &lds, const SampleRow &p, 
 // A row's draw.  WHOLE: its bins are summed here; else its parts' are joined.  It is a
 // chain of a dozen short phases with a barrier or two each: 31 us for one row of
 // 32000, 56 for 16 of 152064, 65 for 256 of them, 260 for 1531 bf16 rows of 32003, six
-// rows to a CU one after the other (128 registers of 1024 threads; with 64 it spills,
-// and two at a time took 445).  The row in registers instead of read again took 545:
+// rows to a CU one after the other (88 KB of LDS and 128 registers of 1024 threads; with
+// 64 registers it spills, and two at a time took 445).  The row in registers instead of read again took 545:
 // the unrolled code does not fit the instruction cache.
 template <int DT, bool WHOLE>
 __global__ __launch_bounds__(SD_THREADS) void k_sample_draw(SampleArgs a) {
@@ -1060,9 +1060,12 @@ __global__ __launch_bounds__(T) void k_sample_few(SampleArgs a) {
   }
 }
 
-// Rows up to this long are drawn from in one launch: a second one and its read of what
-// the first wrote cost more than a work group's summing of 32768 logits (for 32000 it
-// is 31 us against 19 + 10 and a launch).
+// Rows up to this long are drawn from in one launch: for a few of them a second one and
+// its read of what the first wrote cost more than a work group's summing of 32768 logits
+// (one row of 32000 is 31 us against 19 + 10 and a launch).  For many it is the other way
+// round: 1531 bf16 rows of 32003 take 264 us, and took 175 with their bins in a launch of
+// their own and draws by 512 threads in 62 KB of LDS, two to a CU.  The rule does not
+// look at how many rows there are.
 constexpr int SAMPLE_WHOLE = 32768;
 // parts of a row; 0: it has none
 inline int sample_parts(int vocab, int dtype) {

@@ -786,7 +786,8 @@ class PagedCache:
         """Attention of q ([n][n_heads][head_dim]) over the first lengths (int32 [n]) positions of sequences seqs.
         Rows group_starts[g] .. group_starts[g + 1] - 1 (int32 [groups + 1], not falling) have their first shared[g]
         (int32 [groups]) positions in common, which are read once, through the first row's sequence.  max_len bounds
-        the lengths (None: what the table holds), max_shared the shared positions (None: max_len); scale None:
+        the lengths (None: what the table holds), max_shared the shared positions (None: max_len; near what is shared it
+        is faster, as rows' own positions are split by max_len - max_shared); scale None:
         head_dim ** -0.5.  A workspace (attention_workspace) may be kept from call to call; calls on several streams
         do not share one."""
         import torch
