@@ -524,14 +524,14 @@ def test_a_position_far_above_all_others(dtype, at, nats, n, group):
 def test_scores_that_fall_and_rise_along_a_row(hd, order):
     """f16 weights over 60 bits and more, in either order, so that no one scale holds them all."""
     import paper_2603_12707_amd as hs
-    length, g = 3000, gen(hd)
-    table = torch.randperm(12, generator=g)[None]
-    score = {"falling": torch.linspace(45, 0, 3072), "rising": torch.linspace(0, 45, 3072),
-             "steps": torch.tensor([0.0, 14.0, 3.0, 44.0, 20.0, 0.0]).repeat_interleave(512)}[order]
-    k = torch.zeros(12, 256, hd)
-    k[..., 0] = score.reshape(12, 256)
-    v = torch.randn(12, 256, hd, generator=g)
-    blocks = torch.zeros(12, 1, 2, 1, 256, hd, dtype=torch.float16)
+    length, g = 3300, gen(hd)
+    table = torch.randperm(13, generator=g)[None]
+    score = {"falling": torch.linspace(45, 0, 3328), "rising": torch.linspace(0, 45, 3328),
+             "steps": torch.tensor([0.0, 14.0, 3.0, 44.0, 20.0, 0.0]).repeat_interleave(555)[:3328]}[order]
+    k = torch.zeros(13, 256, hd)
+    k[..., 0] = score.reshape(13, 256)
+    v = torch.randn(13, 256, hd, generator=g)
+    blocks = torch.zeros(13, 1, 2, 1, 256, hd, dtype=torch.float16)
     blocks[table[0], 0, 0, 0], blocks[table[0], 0, 1, 0] = k.half(), v.half()
     for n, group in ((3, 1), (33, 2), (49, 4)):
         q = torch.zeros(n, group, hd)
@@ -539,10 +539,10 @@ def test_scores_that_fall_and_rise_along_a_row(hd, order):
         q[..., 1:] = torch.randn(n, group, hd - 1, generator=g)
         kw = dict(seqs=torch.zeros(n, dtype=torch.int32), scale=1.0, layers=1, blocks=blocks.cuda(), q=q.half())
         lengths = torch.randint(1, length, (n,), generator=g, dtype=torch.int32)
-        attend_case(hs, "f16", hd, 1, group, lengths, table, 12, 256, **kw)
+        attend_case(hs, "f16", hd, 1, group, lengths, table, 13, 256, **kw)
         lengths = torch.full((n,), length, dtype=torch.int32)
-        attend_case(hs, "f16", hd, 1, group, lengths, table, 12, 256, torch.tensor([0, n], dtype=torch.int32),
-                    torch.tensor([2900], dtype=torch.int32), **kw)
+        attend_case(hs, "f16", hd, 1, group, lengths, table, 13, 256, torch.tensor([0, n], dtype=torch.int32),
+                    torch.tensor([3200], dtype=torch.int32), **kw)
 
 
 @pytest.mark.parametrize("loud", [30.0, 300.0])
